@@ -112,6 +112,7 @@ def load_library():
             lib.comba_profile_select.restype = I
             lib.comba_status_string.argtypes = [I]
             lib.comba_status_string.restype = ctypes.c_char_p
+            layer.bind(lib)
             _lib = lib
     return _lib
 
@@ -625,3 +626,9 @@ def comba_chunk(q, k, v, g, beta, d, h0=None, *, beta_tilde=None, cu_seqlens=Non
     if _CHUNK_FN is None:
         _CHUNK_FN = _autograd_function()
     return _CHUNK_FN.apply(q, k, v, g, beta, d, h0, beta_tilde, cu_seqlens, cu_seqlens_host)
+
+
+from . import layer  # noqa: E402  (after the helpers that it takes from here)
+from .layer import *  # noqa: E402,F401,F403
+
+__all__ += layer.__all__

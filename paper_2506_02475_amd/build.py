@@ -11,6 +11,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcomba.so")
 SOURCES = [os.path.join(CSRC, "comba_kernels.hip"), os.path.join(CSRC, "comba_recurrent.hip"),
            os.path.join(CSRC, "comba_prologue.hip"), os.path.join(CSRC, "comba_noalloc.hip"),
+           os.path.join(CSRC, "comba_conv.hip"), os.path.join(CSRC, "comba_select.hip"),
+           os.path.join(CSRC, "comba_group_norm.hip"), os.path.join(CSRC, "comba_layer_api.cpp"),
            os.path.join(CSRC, "comba_api.cpp")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -1,0 +1,408 @@
+// Short causal depthwise convolution with a history (the K - 1 inputs before a
+// sequence's first token), bias and SiLU, its backward, and its single-token form:
+//
+//   u_t = bias + sum_j w_j xt_{t+j},   y_t = act(u_t),   xt = [h0; x].
+//
+// Streaming kernels, bound by bytes: a thread holds C consecutive channels and
+// walks a run of tokens with the K - 1 previous rows in registers, so a row is
+// read once but for the runs' first K - 1 rows.
+#include "comba_layer_device.hpp"
+#include "comba_layer_launch.h"
+
+namespace comba {
+
+constexpr int CONV_PF = 4;        // rows loaded ahead, together
+constexpr int CONV_BRUN = 32;     // tokens per run of the backward
+constexpr int CONV_BWAVES = 4;    // runs of a workgroup of the backward
+
+// The non-empty sequence s = [sa, se) that holds token t (0 <= t < Ttot), inside
+// the tokens whatever the offsets hold.
+__device__ __forceinline__ void seq_of_token(const int32_t* __restrict__ cu, int N, int Tseq, int Ttot,
+                                             int t, int& s, int& sa, int& se) {
+  if (!cu) {
+    s = t / Tseq;
+    sa = s * Tseq;
+    se = sa + Tseq;
+    return;
+  }
+  int lo = 0, hi = N - 1;  // the last s with cu[s] <= t
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (cu[mid] <= t) lo = mid; else hi = mid - 1;
+  }
+  s = lo;
+  sa = min(max(cu[lo], 0), t);
+  se = min(max(cu[lo + 1], t + 1), Ttot);
+}
+
+// Channels of a piece, of which nv exist (a piece past D reads the last one's place).
+struct ConvPiece {
+  int c, nv;
+};
+template <int C>
+__device__ __forceinline__ ConvPiece conv_piece(int p, int D) {
+  const int c = min(p * C, max(0, D - 1) / C * C);
+  return {c, min(C, D - c)};
+}
+
+template <int K, int C>
+__device__ __forceinline__ void load_taps(const float* __restrict__ w, int c, int nv, float (&wt)[K][C]) {
+#pragma unroll
+  for (int i = 0; i < C; ++i)
+#pragma unroll
+    for (int j = 0; j < K; ++j) wt[j][i] = w[(long)(c + min(i, nv - 1)) * K + j];
+}
+
+// Row `pos` of sequence s (negative: its history) as floats.
+template <typename Tin, int K, int C, bool VEC>
+__device__ __forceinline__ void load_ext(const ConvArgs& a, int s, int sa, int pos, int c, int nv,
+                                         float (&v)[C]) {
+  Piece<Tin, C, VEC> p;
+  if (pos >= 0) {
+    p.load(static_cast<const Tin*>(a.x) + (long)(sa + pos) * a.x_row + c, nv);
+  } else if (a.h0) {
+    p.load(static_cast<const Tin*>(a.h0) + ((long)s * (K - 1) + (K - 1) + pos) * a.D + c, nv);
+  } else {
+    p.zero();
+  }
+#pragma unroll
+  for (int i = 0; i < C; ++i) v[i] = p.get(i);
+}
+
+template <typename Tin, int K, int C, bool VEC>
+__global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a) {
+  const int pieces = (a.D + C - 1) / C, nruns = (a.Ttot + a.run - 1) / a.run;
+  const long e = (long)blockIdx.x * 256 + threadIdx.x;
+  const long r = e / pieces;
+  const auto [c, nv] = conv_piece<C>(e % pieces, a.D);
+  if (r >= nruns) {  // the final histories
+    const long k = r - nruns;
+    if (!a.ht || k >= (long)a.N * (K - 1)) return;
+    const int s = k / (K - 1), j = k % (K - 1);
+    int sa, se;
+    seq_range(a.cu_seqlens, s, a.Tseq, a.Ttot, sa, se);
+    float v[C];
+    load_ext<Tin, K, C, VEC>(a, s, sa, se - sa - (K - 1) + j, c, nv, v);
+    store_piece<Tin, C, VEC>(static_cast<Tin*>(a.ht) + k * a.D + c, v, nv);
+    return;
+  }
+  const int t0 = r * a.run, t1 = min(t0 + a.run, a.Ttot);
+  float wt[K][C], b[C], xw[K - 1][C];
+  load_taps<K, C>(a.w, c, nv, wt);
+#pragma unroll
+  for (int i = 0; i < C; ++i) b[i] = a.bias ? a.bias[c + min(i, nv - 1)] : 0.f;
+  const Tin* x = static_cast<const Tin*>(a.x) + c;
+  Tin* y = static_cast<Tin*>(a.y) + c;
+  int s, sa, se;
+  seq_of_token(a.cu_seqlens, a.N, a.Tseq, a.Ttot, t0, s, sa, se);
+#pragma unroll
+  for (int m = 0; m < K - 1; ++m) load_ext<Tin, K, C, VEC>(a, s, sa, t0 - sa - (K - 1) + m, c, nv, xw[m]);
+  Piece<Tin, C, VEC> xr[CONV_PF];
+#pragma unroll
+  for (int k = 0; k < CONV_PF; ++k) xr[k].load(x + (long)min(t0 + k, t1 - 1) * a.x_row, nv);
+  for (int tb = t0; tb < t1; tb += CONV_PF) {
+    Piece<Tin, C, VEC> xn[CONV_PF];
+#pragma unroll
+    for (int k = 0; k < CONV_PF; ++k) xn[k].load(x + (long)min(tb + CONV_PF + k, t1 - 1) * a.x_row, nv);
+#pragma unroll
+    for (int k = 0; k < CONV_PF; ++k) {
+      const int t = tb + k;
+      if (t < t1) {
+        if (t >= se) {  // the next sequence starts with its own history
+          seq_of_token(a.cu_seqlens, a.N, a.Tseq, a.Ttot, t, s, sa, se);
+#pragma unroll
+          for (int m = 0; m < K - 1; ++m) load_ext<Tin, K, C, VEC>(a, s, sa, m - (K - 1), c, nv, xw[m]);
+        }
+        float o[C];
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+          const float xv = xr[k].get(i);
+          float u = b[i];
+#pragma unroll
+          for (int m = 0; m < K - 1; ++m) u = fmaf(wt[m][i], xw[m][i], u);
+          u = fmaf(wt[K - 1][i], xv, u);
+          o[i] = a.silu ? u * sigmoid_acc(u) : u;
+#pragma unroll
+          for (int m = 0; m < K - 2; ++m) xw[m][i] = xw[m + 1][i];
+          xw[K - 2][i] = xv;
+        }
+        store_piece<Tin, C, VEC>(y + (long)t * a.D, o, nv);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < CONV_PF; ++k) xr[k] = xn[k];
+  }
+}
+
+// One token per row; the state's rows move up by one.
+template <typename Tin, int K, int C, bool VEC>
+__global__ __launch_bounds__(256) void k_conv_step(ConvArgs a) {
+  const int pieces = (a.D + C - 1) / C;
+  const long e = (long)blockIdx.x * 256 + threadIdx.x;
+  const long row = e / pieces;
+  if (row >= a.N) return;
+  const auto [c, nv] = conv_piece<C>(e % pieces, a.D);
+  const int slot = a.slots ? a.slots[row] : (int)row;
+  Tin* y = static_cast<Tin*>(a.y) + row * a.D + c;
+  float o[C];
+  if (slot < 0 || slot >= a.num_slots) {  // padding
+#pragma unroll
+    for (int i = 0; i < C; ++i) o[i] = 0.f;
+    store_piece<Tin, C, VEC>(y, o, nv);
+    return;
+  }
+  float wt[K][C], v[K][C];
+  load_taps<K, C>(a.w, c, nv, wt);
+  Tin* st = static_cast<Tin*>(a.state) + (long)slot * (K - 1) * a.D + c;
+  Piece<Tin, C, VEC> p[K];
+#pragma unroll
+  for (int j = 0; j < K - 1; ++j) p[j].load(st + (long)j * a.D, nv);
+  p[K - 1].load(static_cast<const Tin*>(a.x) + row * a.x_row + c, nv);
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    float u = a.bias ? a.bias[c + min(i, nv - 1)] : 0.f;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      v[j][i] = p[j].get(i);
+      u = fmaf(wt[j][i], v[j][i], u);
+    }
+    o[i] = a.silu ? u * sigmoid_acc(u) : u;
+  }
+  store_piece<Tin, C, VEC>(y, o, nv);
+#pragma unroll
+  for (int j = 0; j < K - 1; ++j) store_piece<Tin, C, VEC>(st + (long)j * a.D, v[j + 1], nv);
+}
+
+// Backward.  du_t = dy_t act'(u_t) adds w_j du_t to row t - (K - 1) + j of the
+// extended input; a run forms du for its own tokens and the K - 1 after them,
+// and keeps the K rows still open in registers.  Rows before a sequence's first
+// token are its history's; dht adds to the last K - 1 extended rows.  A run's dw
+// and dbias are summed over the workgroup's runs in LDS.
+template <typename Tin, int K, int C, bool VEC>
+__global__ __launch_bounds__(64 * CONV_BWAVES) void k_conv_bwd(ConvArgs a) {
+  __shared__ float part[CONV_BWAVES][K + 1][C][64];
+  const int pieces = (a.D + C - 1) / C, pgs = (pieces + 63) / 64;
+  const int pg = blockIdx.x % pgs, rb = blockIdx.x / pgs;
+  const int lane = lane_id(), w = wave_id_s();
+  const int piece = pg * 64 + lane;
+  const ConvPiece cp = conv_piece<C>(piece, a.D);
+  const int c = cp.c, nl = cp.nv, nv = piece < pieces ? nl : 0;  // channels loaded, stored
+  const int run = rb * CONV_BWAVES + w, t0 = run * CONV_BRUN, t1 = min(t0 + CONV_BRUN, a.Ttot);
+  float dw[K][C], db[C];
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    db[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < K; ++j) dw[j][i] = 0.f;
+  }
+  if (t0 < a.Ttot) {
+    float wt[K][C], b[C], xw[K - 1][C], acc[K][C];
+    load_taps<K, C>(a.w, c, nl, wt);
+#pragma unroll
+    for (int i = 0; i < C; ++i) b[i] = a.bias ? a.bias[c + min(i, nl - 1)] : 0.f;
+    int s, sa, se;
+    seq_of_token(a.cu_seqlens, a.N, a.Tseq, a.Ttot, t0, s, sa, se);
+    auto enter = [&](int t) {  // the window before token t of sequence s
+#pragma unroll
+      for (int m = 0; m < K - 1; ++m) load_ext<Tin, K, C, VEC>(a, s, sa, t - sa - (K - 1) + m, c, nl, xw[m]);
+#pragma unroll
+      for (int m = 0; m < K; ++m)
+#pragma unroll
+        for (int i = 0; i < C; ++i) acc[m][i] = 0.f;
+    };
+    // row r of the tokens (before sa: history) is complete
+    auto put = [&](int r, const float (&v)[C]) {
+      const int ext = r - sa + (K - 1), tail = ext - (se - sa);  // tail >= 0: row of ht
+      const bool tok = r >= sa;
+      if (tok ? (r < t0 || r >= t1) : (!a.dh0 || sa < t0 || sa >= t1)) return;
+      float o[C];
+#pragma unroll
+      for (int i = 0; i < C; ++i) o[i] = v[i];
+      if (a.dht && tail >= 0) {
+        Piece<Tin, C, VEC> p;
+        p.load(static_cast<const Tin*>(a.dht) + ((long)s * (K - 1) + tail) * a.D + c, nl);
+#pragma unroll
+        for (int i = 0; i < C; ++i) o[i] += p.get(i);
+      }
+      Tin* at = tok ? static_cast<Tin*>(a.dx) + (long)r * a.D + c
+                    : static_cast<Tin*>(a.dh0) + ((long)s * (K - 1) + ext) * a.D + c;
+      store_piece<Tin, C, VEC>(at, o, nv);
+    };
+    enter(t0);
+    const Tin *x = static_cast<const Tin*>(a.x) + c, *dy = static_cast<const Tin*>(a.dy) + c;
+    const int tstop = min(t1 + K - 1, a.Ttot);
+    bool done = false;
+    for (int tb = t0; tb < tstop && !done; tb += CONV_PF) {
+      Piece<Tin, C, VEC> xb[CONV_PF], gb[CONV_PF];
+#pragma unroll
+      for (int k = 0; k < CONV_PF; ++k) {
+        const long row = min(tb + k, tstop - 1);
+        xb[k].load(x + row * a.x_row, nl);
+        gb[k].load(dy + row * a.D, nl);
+      }
+#pragma unroll
+      for (int k = 0; k < CONV_PF; ++k) {
+        const int t = tb + k;
+        if (t >= tstop || done) continue;
+        if (t >= se) {
+#pragma unroll
+          for (int m = 0; m < K - 1; ++m) put(t - (K - 1) + m, acc[m]);
+          if (t >= t1) {
+            done = true;
+            continue;
+          }
+          seq_of_token(a.cu_seqlens, a.N, a.Tseq, a.Ttot, t, s, sa, se);
+          enter(t);
+        }
+        const bool mine = t < t1;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+          const float xv = xb[k].get(i);
+          float u = b[i];
+#pragma unroll
+          for (int m = 0; m < K - 1; ++m) u = fmaf(wt[m][i], xw[m][i], u);
+          u = fmaf(wt[K - 1][i], xv, u);
+          float du = gb[k].get(i);
+          if (a.silu) {
+            const float sg = sigmoid_acc(u);
+            du *= sg * fmaf(u, 1.f - sg, 1.f);
+          }
+#pragma unroll
+          for (int j = 0; j < K; ++j) acc[j][i] = fmaf(wt[j][i], du, acc[j][i]);
+          if (mine) {
+#pragma unroll
+            for (int j = 0; j < K - 1; ++j) dw[j][i] = fmaf(du, xw[j][i], dw[j][i]);
+            dw[K - 1][i] = fmaf(du, xv, dw[K - 1][i]);
+            db[i] += du;
+          }
+#pragma unroll
+          for (int m = 0; m < K - 2; ++m) xw[m][i] = xw[m + 1][i];
+          xw[K - 2][i] = xv;
+        }
+        put(t - (K - 1), acc[0]);
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+#pragma unroll
+          for (int m = 0; m < K - 1; ++m) acc[m][i] = acc[m + 1][i];
+          acc[K - 1][i] = 0.f;
+        }
+      }
+    }
+    if (!done) {  // the tokens end here, or the walk stopped inside a sequence past t1
+#pragma unroll
+      for (int m = 0; m < K - 1; ++m) put(tstop - (K - 1) + m, acc[m]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+#pragma unroll
+    for (int j = 0; j < K; ++j) part[w][j][i][lane] = dw[j][i];
+    part[w][K][i][lane] = db[i];
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < (K + 1) * 64 * C; e += 64 * CONV_BWAVES) {
+    const int j = e / (64 * C), ch = e % (64 * C), l = ch / C, i = ch % C;
+    float v = part[0][j][i][l];
+#pragma unroll
+    for (int m = 1; m < CONV_BWAVES; ++m) v += part[m][j][i][l];
+    const int cc = pg * 64 * C + ch;
+    if (cc < a.D) a.part[((long)rb * (K + 1) + j) * a.D + cc] = v;
+  }
+}
+
+// dw and dbias: the workgroups' partial sums in order, split over 16 groups of
+// threads that are added in order; and the histories' gradients of empty sequences.
+constexpr int CONV_DCOLS = 16, CONV_DGROUPS = 16;
+template <typename Tin, int K>
+__global__ __launch_bounds__(256) void k_conv_dw(ConvArgs a) {
+  __shared__ float part[CONV_DGROUPS][CONV_DCOLS];
+  const long n = (long)(K + 1) * a.D;
+  const int nb = (n + CONV_DCOLS - 1) / CONV_DCOLS;
+  if ((int)blockIdx.x >= nb) {  // one block per sequence
+    const int s = blockIdx.x - nb;
+    int sa, se;
+    seq_range(a.cu_seqlens, s, a.Tseq, a.Ttot, sa, se);
+    if (se > sa) return;
+    for (int e = threadIdx.x; e < (K - 1) * a.D; e += 256) {
+      const long at = (long)s * (K - 1) * a.D + e;
+      static_cast<Tin*>(a.dh0)[at] = a.dht ? static_cast<const Tin*>(a.dht)[at] : Tin(0);
+    }
+    return;
+  }
+  const int col = threadIdx.x % CONV_DCOLS, grp = threadIdx.x / CONV_DCOLS;
+  const long e = (long)blockIdx.x * CONV_DCOLS + col;
+  float s = 0.f;
+  if (e < n)
+    for (int r = grp; r < a.nruns; r += CONV_DGROUPS) s += a.part[r * n + e];
+  part[grp][col] = s;
+  __syncthreads();
+  if (grp == 0 && e < n) {
+    for (int i = 1; i < CONV_DGROUPS; ++i) s += part[i][col];
+    const int j = e / a.D;
+    const long c = e % a.D;
+    if (j < K) a.dw[c * K + j] = s;
+    else if (a.dbias) a.dbias[c] = s;
+  }
+}
+
+static bool conv_vec(const ConvArgs& a, int C) {
+  const long m = C * (a.bf16 ? 2 : 4);
+  auto ok = [&](const void* p) { return !p || (uintptr_t)p % m == 0; };
+  return a.D % C == 0 && a.x_row % C == 0 && ok(a.x) && ok(a.h0) && ok(a.y) && ok(a.ht) && ok(a.state) &&
+         ok(a.dy) && ok(a.dht) && ok(a.dx) && ok(a.dh0);
+}
+
+int conv_bwd_runs(const ConvArgs& a) {
+  const int runs = (a.Ttot + CONV_BRUN - 1) / CONV_BRUN;
+  return (runs + CONV_BWAVES - 1) / CONV_BWAVES;
+}
+
+template <typename Tin, int K>
+static hipError_t run_conv_fwd(const ConvArgs& a0) {
+  constexpr int C = 16 / (int)sizeof(Tin);
+  ConvArgs a = a0;
+  const long pieces = (a.D + C - 1) / C;
+  a.run = 32;
+  const long items = ((long)(a.Ttot + a.run - 1) / a.run + (a.ht ? (long)a.N * (K - 1) : 0)) * pieces;
+  const long grid = (items + 255) / 256;
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  if (grid == 0) return hipSuccess;
+  if (conv_vec(a, C)) k_conv_fwd<Tin, K, C, true><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  else k_conv_fwd<Tin, K, C, false><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  return hipGetLastError();
+}
+template <typename Tin, int K>
+static hipError_t run_conv_step(const ConvArgs& a) {
+  constexpr int C = 16 / (int)sizeof(Tin);
+  const long grid = ((long)a.N * ((a.D + C - 1) / C) + 255) / 256;
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  if (conv_vec(a, C)) k_conv_step<Tin, K, C, true><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  else k_conv_step<Tin, K, C, false><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  return hipGetLastError();
+}
+template <typename Tin, int K>
+static hipError_t run_conv_bwd(const ConvArgs& a0) {
+  constexpr int C = 4;
+  ConvArgs a = a0;
+  a.nruns = conv_bwd_runs(a);
+  const long pgs = ((a.D + C - 1) / C + 63) / 64, grid = pgs * a.nruns;
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  if (grid > 0) {
+    if (conv_vec(a, C)) k_conv_bwd<Tin, K, C, true><<<(unsigned)grid, 64 * CONV_BWAVES, 0, a.stream>>>(a);
+    else k_conv_bwd<Tin, K, C, false><<<(unsigned)grid, 64 * CONV_BWAVES, 0, a.stream>>>(a);
+  }
+  const long nb = ((long)(K + 1) * a.D + CONV_DCOLS - 1) / CONV_DCOLS + (a.dh0 ? a.N : 0);
+  k_conv_dw<Tin, K><<<(unsigned)nb, 256, 0, a.stream>>>(a);
+  return hipGetLastError();
+}
+
+#define CONV_DISPATCH(fn, a)                                             \
+  ((a).K == 2   ? ((a).bf16 ? fn<bf16_t, 2>(a) : fn<float, 2>(a))        \
+   : (a).K == 3 ? ((a).bf16 ? fn<bf16_t, 3>(a) : fn<float, 3>(a))        \
+   : (a).K == 4 ? ((a).bf16 ? fn<bf16_t, 4>(a) : fn<float, 4>(a)) : hipErrorInvalidValue)
+
+hipError_t launch_conv_fwd(const ConvArgs& a) { return CONV_DISPATCH(run_conv_fwd, a); }
+hipError_t launch_conv_step(const ConvArgs& a) { return a.N == 0 ? hipSuccess : CONV_DISPATCH(run_conv_step, a); }
+hipError_t launch_conv_bwd(const ConvArgs& a) { return CONV_DISPATCH(run_conv_bwd, a); }
+
+}  // namespace comba

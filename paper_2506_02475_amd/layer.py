@@ -1,0 +1,553 @@
+"""The layer's operators around and beside the token mixer (include/comba_layer.h):
+the short causal convolution with its history, the selective state space scan and
+the group norm per token.
+
+    y, ht = comba_conv_fwd(x, w, bias, h0)              # prompts; comba_conv_step: one token
+    y, ht = comba_select_fwd(u, delta, A, B, C, D, z, delta_bias, h0)   # .._step: one token
+    y = comba_group_norm_fwd(x, groups, weight, bias, z)
+
+and, differentiable (torch.autograd), comba_conv, comba_select, comba_group_norm.
+Activations are bfloat16 or float32 and so are their gradients and outputs;
+parameters, their gradients and the scan's states are float32.  Tensors may be
+column slices of a wider row (a projection's output) where noted; everything
+else is contiguous.  Packed sequences pass ``cu_seqlens`` (and, to have the
+offsets checked, ``cu_seqlens_host``) as in the package's other calls.
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import (COMBA_BF16, COMBA_F32, CombaError, _check, _host_offsets, _ptr, _stream,
+               load_library)
+
+__all__ = ["comba_conv_fwd", "comba_conv_bwd", "comba_conv_step", "comba_conv",
+           "comba_select_fwd", "comba_select_fwd_save", "comba_select_bwd", "comba_select_step",
+           "comba_select", "comba_group_norm_fwd", "comba_group_norm_bwd", "comba_group_norm",
+           "CombaConvShape", "CombaSelectShape", "CombaGroupNormShape"]
+
+ACTIVATIONS = {None: 0, "none": 0, "silu": 1, "sigmoid": 2}
+_I32, _I64, _P = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
+
+
+class CombaConvShape(ctypes.Structure):
+    _fields_ = [("B", _I32), ("T", _I32), ("D", _I32), ("K", _I32), ("num_seqs", _I32),
+                ("cu_seqlens", _P), ("cu_seqlens_host", _P), ("in_dtype", ctypes.c_int),
+                ("activation", ctypes.c_int), ("x_row", _I64)]
+
+
+class CombaSelectShape(ctypes.Structure):
+    _fields_ = [("B", _I32), ("T", _I32), ("D", _I32), ("N", _I32), ("G", _I32),
+                ("num_seqs", _I32), ("cu_seqlens", _P), ("cu_seqlens_host", _P),
+                ("in_dtype", ctypes.c_int), ("delta_softplus", _I32), ("u_row", _I64),
+                ("delta_row", _I64), ("z_row", _I64), ("b_row", _I64), ("c_row", _I64)]
+
+
+class CombaGroupNormShape(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("C", _I32), ("G", _I32), ("x_dtype", ctypes.c_int),
+                ("out_dtype", ctypes.c_int), ("activation", ctypes.c_int), ("eps", ctypes.c_float),
+                ("x_row", _I64), ("z_row", _I64)]
+
+
+def bind(lib):
+    """Declare the C signatures (called by load_library)."""
+    P, Z, I = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
+    conv, sel, norm = (ctypes.POINTER(s) for s in (CombaConvShape, CombaSelectShape,
+                                                   CombaGroupNormShape))
+    for name, args in (("comba_conv_fwd", [conv] + [P] * 7),
+                       ("comba_conv_bwd", [conv] + [P] * 11 + [Z, P]),
+                       ("comba_conv_step", [conv] + [P] * 5 + [_I32, P, P]),
+                       ("comba_select_fwd", [sel] + [P] * 12 + [Z, P]),
+                       ("comba_select_fwd_save", [sel] + [P] * 12 + [Z, P]),
+                       ("comba_select_bwd", [sel] + [P] * 21 + [Z, P]),
+                       ("comba_select_step", [sel] + [P] * 10 + [_I32, P, P]),
+                       ("comba_group_norm_fwd", [norm] + [P] * 6),
+                       ("comba_group_norm_bwd", [norm] + [P] * 10 + [Z, P])):
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = args, I
+    for name, shp in (("comba_conv_workspace_bytes", conv),
+                      ("comba_select_fwd_workspace_bytes", sel),
+                      ("comba_select_bwd_workspace_bytes", sel),
+                      ("comba_group_norm_workspace_bytes", norm)):
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = [shp], Z
+
+
+# ---- argument checks -------------------------------------------------------
+def _code(t, name):
+    import torch
+
+    if not t.is_cuda:
+        raise CombaError("comba: tensors must be on a GPU device")
+    if t.dtype is torch.bfloat16:
+        return COMBA_BF16
+    if t.dtype is torch.float32:
+        return COMBA_F32
+    raise CombaError("comba: %s must be bfloat16 or float32" % name)
+
+
+def _dense(name, t, shape, dtype, dev):
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape) or t.dtype is not dtype or t.get_device() != dev \
+            or not t.is_contiguous():
+        raise CombaError("comba: %s must be a contiguous %s %s on the device"
+                         % (name, str(dtype).replace("torch.", ""), list(shape)))
+
+
+def _row(name, t, lead, shape, dtype, dev):
+    """Elements between token rows of ``t`` (``lead`` leading dimensions of tokens,
+    then a row): a row's elements are contiguous, the rows evenly spaced."""
+    if t is None:
+        return 0
+    if tuple(t.shape) != tuple(shape) or t.dtype is not dtype or t.get_device() != dev:
+        raise CombaError("comba: %s must be %s %s on the device"
+                         % (name, str(dtype).replace("torch.", ""), list(shape)))
+    if t.is_contiguous():
+        return 0
+    st, n = t.stride(), 1
+    for d in range(t.dim() - 1, lead - 1, -1):
+        if shape[d] != 1 and st[d] != n:
+            raise CombaError("comba: a row of %s must be contiguous" % name)
+        n *= shape[d]
+    row, span = None, 1
+    for d in range(lead - 1, -1, -1):
+        if shape[d] == 1:
+            continue
+        if row is None:
+            row = st[d]
+        elif st[d] != row * span:
+            raise CombaError("comba: the rows of %s must be evenly spaced" % name)
+        span *= shape[d]
+    if row is None:
+        return 0
+    if row < n:
+        raise CombaError("comba: the rows of %s overlap" % name)
+    return row
+
+
+def _seqs(B, cu_seqlens, cu_seqlens_host, dev):
+    """(sequences, device pointer, host offsets) of a call."""
+    if cu_seqlens is None:
+        if cu_seqlens_host is not None:
+            raise CombaError("comba: cu_seqlens_host needs cu_seqlens")
+        return B, None, None
+    import torch
+
+    if cu_seqlens.dtype is not torch.int32 or not cu_seqlens.is_contiguous() \
+            or cu_seqlens.get_device() != dev or B != 1:
+        raise CombaError("comba: cu_seqlens must be contiguous int32 on the device, B == 1")
+    N = cu_seqlens.numel() - 1
+    return N, cu_seqlens.data_ptr(), _host_offsets(cu_seqlens_host, N + 1)
+
+
+def _slots(slots, rows, dev):
+    if slots is None:
+        return
+    import torch
+
+    if slots.dtype is not torch.int32 or tuple(slots.shape) != (rows,) \
+            or not slots.is_contiguous() or slots.get_device() != dev:
+        raise CombaError("comba: slots must be contiguous int32 [B] on the device")
+
+
+def _activation(name, allowed):
+    if name not in allowed:
+        raise CombaError("comba: activation must be one of %s" % (allowed,))
+    return ACTIVATIONS[name]
+
+
+def _workspace(fn, shp, given, device):
+    import torch
+
+    nbytes = fn(ctypes.byref(shp))
+    if nbytes == 0:
+        _check(2)
+    if given is not None and given.numel() >= nbytes:
+        return given
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _host_ptr(host):
+    return None if host is None else host.ctypes.data
+
+
+# ---- short causal convolution -------------------------------------------------
+_CONV_ACT = (None, "none", "silu")
+
+
+def _conv_shape(x, w, bias, h0, activation, cu_seqlens, cu_seqlens_host):
+    import torch
+
+    code, dev = _code(x, "x"), x.get_device()
+    if x.dim() != 3 or w.dim() != 2 or w.shape[0] != x.shape[2]:
+        raise CombaError("comba: x must be [B,T,D] and w [D,K]")
+    B, T, D = x.shape
+    K = w.shape[1]
+    _dense("w", w, (D, K), torch.float32, dev)
+    _dense("bias", bias, (D,), torch.float32, dev)
+    N, cu, host = _seqs(B, cu_seqlens, cu_seqlens_host, dev)
+    _dense("h0", h0, (N, K - 1, D), x.dtype, dev)
+    row = _row("x", x, 2, (B, T, D), x.dtype, dev)
+    shp = CombaConvShape(B, T, D, K, N, cu, _host_ptr(host), code,
+                         _activation(activation, _CONV_ACT), row)
+    shp._keep = host
+    return shp, (B, T, D, K, N, dev)
+
+
+def comba_conv_fwd(x, w, bias=None, h0=None, *, activation="silu", cu_seqlens=None,
+                   cu_seqlens_host=None, output_final_state=True, stream=None):
+    """Short causal depthwise convolution.  Returns (y [B,T,D], ht [N,K-1,D] or None).
+
+    x [B,T,D] (may be a column slice); w [D,K] float32, K = 2..4, the newest token
+    under the last tap; bias [D] float32; h0 [N,K-1,D]: each sequence's inputs
+    before its first token, oldest first (None: zeros); ht: those before its next."""
+    import torch
+
+    shp, (B, T, D, K, N, dev) = _conv_shape(x, w, bias, h0, activation, cu_seqlens,
+                                            cu_seqlens_host)
+    y = torch.empty((B, T, D), dtype=x.dtype, device=x.device)
+    ht = torch.empty((N, K - 1, D), dtype=x.dtype, device=x.device) if output_final_state else None
+    _check(load_library().comba_conv_fwd(ctypes.byref(shp), _ptr(x), _ptr(w), _ptr(bias), _ptr(h0),
+                                         _ptr(y), _ptr(ht), _stream(stream, x.device)))
+    return y, ht
+
+
+def comba_conv_bwd(x, w, bias, h0, dy, dht=None, *, activation="silu", cu_seqlens=None,
+                   cu_seqlens_host=None, need_dh0=True, workspace=None, stream=None):
+    """Backward of comba_conv_fwd from dy [B,T,D] (and dht [N,K-1,D]), both in the dtype of
+    x.  Returns dict dx (dtype of x), dw, dbias (float32; None without bias), dh0."""
+    import torch
+
+    lib = load_library()
+    shp, (B, T, D, K, N, dev) = _conv_shape(x, w, bias, h0, activation, cu_seqlens,
+                                            cu_seqlens_host)
+    _dense("dy", dy, (B, T, D), x.dtype, dev)
+    _dense("dht", dht, (N, K - 1, D), x.dtype, dev)
+    out = {"dx": torch.empty((B, T, D), dtype=x.dtype, device=x.device),
+           "dw": torch.empty_like(w),
+           "dbias": None if bias is None else torch.empty_like(bias),
+           "dh0": torch.empty((N, K - 1, D), dtype=x.dtype, device=x.device) if need_dh0 else None}
+    ws = _workspace(lib.comba_conv_workspace_bytes, shp, workspace, x.device)
+    _check(lib.comba_conv_bwd(ctypes.byref(shp), _ptr(x), _ptr(w), _ptr(bias), _ptr(h0), _ptr(dy),
+                              _ptr(dht), _ptr(out["dx"]), _ptr(out["dw"]), _ptr(out["dbias"]),
+                              _ptr(out["dh0"]), _ptr(ws), ws.numel(), _stream(stream, x.device)))
+    return out
+
+
+def comba_conv_step(x, w, bias, state, *, slots=None, activation="silu", stream=None):
+    """One token per row: returns y [B,D]; ``state`` [S,K-1,D] is updated in place.
+
+    x [B,D] (may be a column slice).  Row b uses slot slots[b] (int32 on the device; a
+    slot outside [0, S) marks padding: y zero, no state touched), or slot b."""
+    import torch
+
+    code, dev = _code(x, "x"), x.get_device()
+    if x.dim() != 2 or w.dim() != 2 or w.shape[0] != x.shape[1] or state.dim() != 3:
+        raise CombaError("comba: x must be [B,D], w [D,K] and state [S,K-1,D]")
+    B, D = x.shape
+    K = w.shape[1]
+    _dense("w", w, (D, K), torch.float32, dev)
+    _dense("bias", bias, (D,), torch.float32, dev)
+    _dense("state", state, (state.shape[0], K - 1, D), x.dtype, dev)
+    _slots(slots, B, dev)
+    shp = CombaConvShape(B, 1, D, K, B, None, None, code, _activation(activation, _CONV_ACT),
+                         _row("x", x, 1, (B, D), x.dtype, dev))
+    y = torch.empty((B, D), dtype=x.dtype, device=x.device)
+    _check(load_library().comba_conv_step(ctypes.byref(shp), _ptr(x), _ptr(w), _ptr(bias),
+                                          _ptr(state), _ptr(slots), state.shape[0], _ptr(y),
+                                          _stream(stream, x.device)))
+    return y
+
+
+# ---- selective state space scan --------------------------------------------------
+def _select_shape(lead, u, delta, A, B, C, D, z, delta_bias, delta_softplus, N, cu, host):
+    import torch
+
+    code, dev, dt = _code(u, "u"), u.get_device(), u.dtype
+    f32 = torch.float32
+    shape = tuple(u.shape)
+    width = shape[-1]
+    if A.dim() != 2 or A.shape[0] != width:
+        raise CombaError("comba: A must be [D,N]")
+    n = A.shape[1]
+    if B.dim() not in (lead + 1, lead + 2):
+        raise CombaError("comba: B and C must be [..,G,N] or [..,N]")
+    bshape = shape[:-1] + ((B.shape[lead],) if B.dim() == lead + 2 else ()) + (n,)
+    G = B.shape[lead] if B.dim() == lead + 2 else 1
+    _dense("A", A, (width, n), f32, dev)
+    _dense("D", D, (width,), f32, dev)
+    _dense("delta_bias", delta_bias, (width,), f32, dev)
+    rows = [_row(name, t, lead, s, dt, dev)
+            for name, t, s in (("u", u, shape), ("delta", delta, shape), ("z", z, shape),
+                               ("B", B, bshape), ("C", C, bshape))]
+    batch, T = (shape[0], 1) if lead == 1 else shape[:2]
+    shp = CombaSelectShape(batch, T, width, n, G, N, cu, _host_ptr(host), code,
+                           1 if delta_softplus else 0, *rows)
+    shp._keep = host
+    return shp, n, bshape
+
+
+def _select(save, u, delta, A, B, C, D, z, delta_bias, h0, delta_softplus, cu_seqlens,
+            cu_seqlens_host, output_final_state, workspace, stream):
+    import torch
+
+    lib = load_library()
+    _code(u, "u")
+    if u.dim() != 3:
+        raise CombaError("comba: u must be [B,T,D]")
+    S, cu, host = _seqs(u.shape[0], cu_seqlens, cu_seqlens_host, u.get_device())
+    shp, n, _ = _select_shape(2, u, delta, A, B, C, D, z, delta_bias, delta_softplus, S, cu, host)
+    width = u.shape[2]
+    _dense("h0", h0, (S, width, n), torch.float32, u.get_device())
+    y = torch.empty(u.shape, dtype=u.dtype, device=u.device)
+    ht = torch.empty((S, width, n), dtype=torch.float32, device=u.device) \
+        if output_final_state else None
+    size = lib.comba_select_bwd_workspace_bytes if save else lib.comba_select_fwd_workspace_bytes
+    ws = _workspace(size, shp, workspace, u.device)
+    fn = lib.comba_select_fwd_save if save else lib.comba_select_fwd
+    _check(fn(ctypes.byref(shp), _ptr(u), _ptr(delta), _ptr(A), _ptr(B), _ptr(C), _ptr(D), _ptr(z),
+              _ptr(delta_bias), _ptr(h0), _ptr(y), _ptr(ht), _ptr(ws), ws.numel(),
+              _stream(stream, u.device)))
+    return y, ht, ws
+
+
+def comba_select_fwd(u, delta, A, B, C, D=None, z=None, delta_bias=None, h0=None, *,
+                     delta_softplus=True, cu_seqlens=None, cu_seqlens_host=None,
+                     output_final_state=True, workspace=None, stream=None):
+    """Selective state space scan.  Returns (y [B,T,D], ht [S,D,N] float32 or None).
+
+    With dt = softplus(delta + delta_bias) per channel and token,
+    h_t = exp(dt A) h_{t-1} + dt u_t B_t,  y_t = (<C_t, h_t> + D u_t) silu(z_t).
+    u, delta, z [B,T,D]; B, C [B,T,G,N] or [B,T,N] (G groups of channels), all of one dtype
+    and each possibly a column slice; A [D,N], D, delta_bias [D], h0 [S,D,N] float32.
+    D, z, delta_bias and h0 may be None.  N: 8, 16 or 32."""
+    y, ht, _ = _select(False, u, delta, A, B, C, D, z, delta_bias, h0, delta_softplus, cu_seqlens,
+                       cu_seqlens_host, output_final_state, workspace, stream)
+    return y, ht
+
+
+def comba_select_fwd_save(u, delta, A, B, C, D=None, z=None, delta_bias=None, h0=None, *,
+                          delta_softplus=True, cu_seqlens=None, cu_seqlens_host=None,
+                          output_final_state=True, workspace=None, stream=None):
+    """comba_select_fwd that also keeps the states its backward needs.  Returns (y, ht,
+    workspace); pass the same inputs and ``workspace`` to comba_select_bwd."""
+    return _select(True, u, delta, A, B, C, D, z, delta_bias, h0, delta_softplus, cu_seqlens,
+                   cu_seqlens_host, output_final_state, workspace, stream)
+
+
+def comba_select_bwd(u, delta, A, B, C, D, z, delta_bias, h0, dy, dht=None, *, workspace,
+                     delta_softplus=True, cu_seqlens=None, cu_seqlens_host=None, need_dh0=True,
+                     stream=None):
+    """Backward of comba_select_fwd_save from dy [B,T,D] (dtype of u) and dht [S,D,N] float32.
+    Returns dict du, ddelta, dz, dB, dC (dtype of u), dA, dD, ddelta_bias, dh0 (float32); the
+    entries of absent inputs are None."""
+    import torch
+
+    lib = load_library()
+    _code(u, "u")
+    if u.dim() != 3:
+        raise CombaError("comba: u must be [B,T,D]")
+    dev, f32 = u.get_device(), torch.float32
+    S, cu, host = _seqs(u.shape[0], cu_seqlens, cu_seqlens_host, dev)
+    shp, n, bshape = _select_shape(2, u, delta, A, B, C, D, z, delta_bias, delta_softplus, S, cu,
+                                   host)
+    width = u.shape[2]
+    _dense("h0", h0, (S, width, n), f32, dev)
+    _dense("dht", dht, (S, width, n), f32, dev)
+    _dense("dy", dy, u.shape, u.dtype, dev)
+
+    def like(shape, dtype, given=True):
+        return torch.empty(shape, dtype=dtype, device=u.device) if given else None
+
+    out = {"du": like(u.shape, u.dtype), "ddelta": like(u.shape, u.dtype),
+           "dA": like(A.shape, f32), "dB": like(bshape, u.dtype), "dC": like(bshape, u.dtype),
+           "dD": like((width,), f32, D is not None), "dz": like(u.shape, u.dtype, z is not None),
+           "ddelta_bias": like((width,), f32, delta_bias is not None),
+           "dh0": like((S, width, n), f32, need_dh0)}
+    if workspace is None or workspace.numel() < lib.comba_select_bwd_workspace_bytes(
+            ctypes.byref(shp)):
+        raise CombaError("comba: comba_select_bwd needs the workspace filled by "
+                         "comba_select_fwd_save")
+    _check(lib.comba_select_bwd(
+        ctypes.byref(shp), _ptr(u), _ptr(delta), _ptr(A), _ptr(B), _ptr(C), _ptr(D), _ptr(z),
+        _ptr(delta_bias), _ptr(h0), _ptr(dy), _ptr(dht), _ptr(out["du"]), _ptr(out["ddelta"]),
+        _ptr(out["dA"]), _ptr(out["dB"]), _ptr(out["dC"]), _ptr(out["dD"]), _ptr(out["dz"]),
+        _ptr(out["ddelta_bias"]), _ptr(out["dh0"]), _ptr(workspace), workspace.numel(),
+        _stream(stream, u.device)))
+    return out
+
+
+def comba_select_step(u, delta, A, B, C, D, z, delta_bias, state, *, slots=None,
+                      delta_softplus=True, stream=None):
+    """One token per row: returns y [B,D]; ``state`` [S,D,N] float32 is updated in place.
+    u, delta, z [B,D]; B, C [B,G,N] or [B,N]; slots as in comba_conv_step."""
+    import torch
+
+    if u.dim() != 2 or state.dim() != 3:
+        raise CombaError("comba: u must be [B,D] and state [S,D,N]")
+    rows = u.shape[0]
+    shp, n, _ = _select_shape(1, u, delta, A, B, C, D, z, delta_bias, delta_softplus, rows, None,
+                              None)
+    dev = u.get_device()
+    _dense("state", state, (state.shape[0], u.shape[1], n), torch.float32, dev)
+    _slots(slots, rows, dev)
+    y = torch.empty(u.shape, dtype=u.dtype, device=u.device)
+    _check(load_library().comba_select_step(
+        ctypes.byref(shp), _ptr(u), _ptr(delta), _ptr(A), _ptr(B), _ptr(C), _ptr(D), _ptr(z),
+        _ptr(delta_bias), _ptr(state), _ptr(slots), state.shape[0], _ptr(y),
+        _stream(stream, u.device)))
+    return y
+
+
+# ---- group norm per token -------------------------------------------------------
+_NORM_ACT = (None, "none", "silu", "sigmoid")
+
+
+def _norm_shape(x, groups, weight, bias, z, activation, eps, out):
+    import torch
+
+    xc, dev = _code(x, "x"), x.get_device()
+    if x.dim() < 1 or groups < 1 or x.shape[-1] < 1 or x.shape[-1] % groups:
+        raise CombaError("comba: x must be [..,C] with C a multiple of groups")
+    if out is not torch.bfloat16 and out is not torch.float32:
+        raise CombaError("comba: out_dtype must be bfloat16 or float32")
+    if out is not x.dtype and x.dtype is not torch.float32:
+        raise CombaError("comba: x must be float32 or have the output's dtype")
+    C = x.shape[-1]
+    _dense("weight", weight, (C,), torch.float32, dev)
+    _dense("bias", bias, (C,), torch.float32, dev)
+    lead = x.dim() - 1
+    xr = _row("x", x, lead, x.shape, x.dtype, dev)
+    zr = _row("z", z, lead, x.shape, out, dev)
+    rows = x.numel() // C
+    return CombaGroupNormShape(rows, C, groups, xc,
+                               COMBA_BF16 if out is torch.bfloat16 else COMBA_F32,
+                               _activation(activation, _NORM_ACT), eps, xr, zr)
+
+
+def comba_group_norm_fwd(x, groups, weight=None, bias=None, z=None, *, activation="silu",
+                         eps=1e-5, out_dtype=None, stream=None):
+    """Group norm of every token over the channels of each of ``groups`` groups, then
+    y = act(n), or with the gate z: y = n act(z).
+
+    x [..,C] and z may be column slices; weight, bias [C] float32 or None.  y has
+    ``out_dtype`` (default: the dtype of z, else of x); x is float32 or of that dtype."""
+    import torch
+
+    out = out_dtype or (x.dtype if z is None else z.dtype)
+    shp = _norm_shape(x, groups, weight, bias, z, activation, eps, out)
+    y = torch.empty(x.shape, dtype=out, device=x.device)
+    _check(load_library().comba_group_norm_fwd(ctypes.byref(shp), _ptr(x), _ptr(weight),
+                                               _ptr(bias), _ptr(z), _ptr(y),
+                                               _stream(stream, x.device)))
+    return y
+
+
+def comba_group_norm_bwd(x, groups, weight, bias, z, dy, *, activation="silu", eps=1e-5,
+                         workspace=None, stream=None):
+    """Backward of comba_group_norm_fwd from dy (the forward's output dtype).  Returns dict dx
+    (dtype of x), dz (dtype of dy, None without z), dweight, dbias (float32, None where absent)."""
+    import torch
+
+    lib = load_library()
+    shp = _norm_shape(x, groups, weight, bias, z, activation, eps, dy.dtype)
+    _dense("dy", dy, x.shape, dy.dtype, x.get_device())
+    out = {"dx": torch.empty(x.shape, dtype=x.dtype, device=x.device),
+           "dz": None if z is None else torch.empty(x.shape, dtype=dy.dtype, device=x.device),
+           "dweight": None if weight is None else torch.empty_like(weight),
+           "dbias": None if bias is None else torch.empty_like(bias)}
+    ws = _workspace(lib.comba_group_norm_workspace_bytes, shp, workspace, x.device)
+    _check(lib.comba_group_norm_bwd(ctypes.byref(shp), _ptr(x), _ptr(weight), _ptr(bias), _ptr(z),
+                                    _ptr(dy), _ptr(out["dx"]), _ptr(out["dz"]),
+                                    _ptr(out["dweight"]), _ptr(out["dbias"]), _ptr(ws), ws.numel(),
+                                    _stream(stream, x.device)))
+    return out
+
+
+# ---- torch.autograd ---------------------------------------------------------------
+_FNS = {}
+
+
+def _functions():
+    if _FNS:
+        return _FNS
+    import torch
+
+    def needed(ctx, grads):
+        return tuple(g if n else None for g, n in zip(grads, ctx.needs_input_grad))
+
+    class Conv(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, bias, h0, kw):
+            ctx.set_materialize_grads(False)
+            ctx.save_for_backward(x, w, bias, h0)
+            ctx.kw = kw
+            return comba_conv_fwd(x, w, bias, h0, **kw)
+
+        @staticmethod
+        def backward(ctx, dy, dht):
+            x, w, bias, h0 = ctx.saved_tensors
+            dy = torch.zeros_like(x, memory_format=torch.contiguous_format) if dy is None \
+                else dy.contiguous()
+            gr = comba_conv_bwd(x, w, bias, h0, dy, None if dht is None else dht.contiguous(),
+                                need_dh0=h0 is not None and ctx.needs_input_grad[3], **ctx.kw)
+            return needed(ctx, (gr["dx"], gr["dw"], gr["dbias"], gr["dh0"], None))
+
+    class Select(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, u, delta, A, B, C, D, z, bias, h0, kw):
+            ctx.set_materialize_grads(False)
+            y, ht, ws = comba_select_fwd_save(u, delta, A, B, C, D, z, bias, h0, **kw)
+            ctx.save_for_backward(u, delta, A, B, C, D, z, bias, h0, ws)
+            ctx.kw = kw
+            return y, ht
+
+        @staticmethod
+        def backward(ctx, dy, dht):
+            u, delta, A, B, C, D, z, bias, h0, ws = ctx.saved_tensors
+            dy = torch.zeros_like(u, memory_format=torch.contiguous_format) if dy is None \
+                else dy.contiguous()
+            gr = comba_select_bwd(u, delta, A, B, C, D, z, bias, h0, dy,
+                                  None if dht is None else dht.contiguous(), workspace=ws,
+                                  need_dh0=h0 is not None and ctx.needs_input_grad[8], **ctx.kw)
+            names = ("du", "ddelta", "dA", "dB", "dC", "dD", "dz", "ddelta_bias", "dh0")
+            return needed(ctx, tuple(gr[n] for n in names) + (None,))
+
+    class GroupNorm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, z, groups, kw, out_dtype):
+            ctx.save_for_backward(x, weight, bias, z)
+            ctx.groups, ctx.kw = groups, kw
+            return comba_group_norm_fwd(x, groups, weight, bias, z, out_dtype=out_dtype, **kw)
+
+        @staticmethod
+        def backward(ctx, dy):
+            x, weight, bias, z = ctx.saved_tensors
+            gr = comba_group_norm_bwd(x, ctx.groups, weight, bias, z, dy.contiguous(), **ctx.kw)
+            return needed(ctx, (gr["dx"], gr["dweight"], gr["dbias"], gr["dz"], None, None, None))
+
+    _FNS.update(conv=Conv, select=Select, norm=GroupNorm)
+    return _FNS
+
+
+def comba_conv(x, w, bias=None, h0=None, *, activation="silu", cu_seqlens=None,
+               cu_seqlens_host=None):
+    """Differentiable comba_conv_fwd: (y, ht); gradients flow to x, w, bias and h0."""
+    kw = dict(activation=activation, cu_seqlens=cu_seqlens, cu_seqlens_host=cu_seqlens_host)
+    return _functions()["conv"].apply(x, w, bias, h0, kw)
+
+
+def comba_select(u, delta, A, B, C, D=None, z=None, delta_bias=None, h0=None, *,
+                 delta_softplus=True, cu_seqlens=None, cu_seqlens_host=None):
+    """Differentiable comba_select_fwd: (y, ht); gradients flow to every tensor.  Each call
+    keeps its workspace until the backward has run."""
+    kw = dict(delta_softplus=delta_softplus, cu_seqlens=cu_seqlens,
+              cu_seqlens_host=cu_seqlens_host)
+    return _functions()["select"].apply(u, delta, A, B, C, D, z, delta_bias, h0, kw)
+
+
+def comba_group_norm(x, groups, weight=None, bias=None, z=None, *, activation="silu", eps=1e-5,
+                     out_dtype=None):
+    """Differentiable comba_group_norm_fwd: gradients flow to x, weight, bias and z."""
+    kw = dict(activation=activation, eps=eps)
+    return _functions()["norm"].apply(x, weight, bias, z, groups, kw, out_dtype)
