@@ -52,10 +52,13 @@ comba_status check_rows(const Shape* s, Rows* r) {
   return COMBA_OK;
 }
 
+// Rows of up to 4M values: the byte offsets inside a tile of 64 rows stay below 2^31.
+constexpr int64_t kMaxRow = (int64_t)1 << 22;
+
 // The elements between rows of a named input: given, or contiguous.
 bool row_stride(int64_t given, int64_t width, long* row) {
   *row = given == 0 ? width : given;
-  return *row >= width && *row < ((int64_t)1 << 40);
+  return *row >= width && *row <= kMaxRow;
 }
 
 // ---- convolution -------------------------------------------------------------
@@ -63,7 +66,7 @@ comba_status conv_args(const comba_conv_shape* s, comba::ConvArgs* a) {
   if (!s) return COMBA_ERR_NULL;
   if (!dtype_ok(s->in_dtype)) return COMBA_ERR_DTYPE;
   if (s->activation != COMBA_ACT_NONE && s->activation != COMBA_ACT_SILU) return COMBA_ERR_SHAPE;
-  if (s->K < 2 || s->K > 4 || s->D <= 0 || s->D > (1 << 24)) return COMBA_ERR_SHAPE;
+  if (s->K < 2 || s->K > 4 || s->D <= 0 || s->D > kMaxRow) return COMBA_ERR_SHAPE;
   Rows r{};
   const comba_status st = check_rows(s, &r);
   if (st != COMBA_OK) return st;
@@ -111,7 +114,7 @@ comba_status select_args(const comba_select_shape* s, comba::SelectArgs* a) {
   if (!s) return COMBA_ERR_NULL;
   if (!dtype_ok(s->in_dtype)) return COMBA_ERR_DTYPE;
   if (s->N != 8 && s->N != 16 && s->N != 32) return COMBA_ERR_SHAPE;
-  if (s->D <= 0 || s->D > (1 << 24) || s->G <= 0 || s->D % s->G) return COMBA_ERR_SHAPE;
+  if (s->D <= 0 || s->D > kMaxRow || s->G <= 0 || s->D % s->G) return COMBA_ERR_SHAPE;
   Rows r{};
   const comba_status st = check_rows(s, &r);
   if (st != COMBA_OK) return st;
@@ -185,7 +188,7 @@ comba_status group_norm_args(const comba_group_norm_shape* s, comba::GroupNormAr
   if (s->activation != COMBA_ACT_NONE && s->activation != COMBA_ACT_SILU &&
       s->activation != COMBA_ACT_SIGMOID)
     return COMBA_ERR_SHAPE;
-  if (s->rows < 0 || s->rows > INT32_MAX || s->C <= 0 || s->C > (1 << 24) || s->G <= 0 || s->C % s->G)
+  if (s->rows < 0 || s->rows > INT32_MAX || s->C <= 0 || s->C > kMaxRow || s->G <= 0 || s->C % s->G)
     return COMBA_ERR_SHAPE;
   if (!(s->eps >= 0.f)) return COMBA_ERR_SHAPE;
   *a = comba::GroupNormArgs{};

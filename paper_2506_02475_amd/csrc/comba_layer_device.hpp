@@ -14,6 +14,17 @@ __device__ __forceinline__ uint32_t bf16_bits(float x) {
 }
 __device__ __forceinline__ void store_elem(bf16_t* p, float x) { *p = (bf16_t)bf16_bits(x); }
 
+// A byte offset past every buffer below, and a raw buffer over `rows` rows from
+// row0 on.  Loads past it give zeros and stores past it are dropped, so tails of
+// tokens and channels need no branch and no second address.  (The record count is
+// clipped below BUF_OOB: callers keep the offsets they use below it.)
+constexpr unsigned BUF_OOB = 0x80000000u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const void* p, long row0, long row_bytes, long rows) {
+  const long n = rows * row_bytes;
+  return clip_rsrc(const_cast<char*>(static_cast<const char*>(p)) + row0 * row_bytes,
+                   n < (long)BUF_OOB ? (unsigned)n : BUF_OOB - 1);
+}
+
 // C consecutive channels as loaded.  VEC: one load of C * sizeof(T) bytes (the
 // address is a multiple of that); else element by element, of which nv >= 1
 // exist (the others repeat the last one).
@@ -50,6 +61,44 @@ struct Piece {
         const uint32_t lo = p[min(2 * i, nv - 1)];
         const uint32_t hi = 2 * i + 1 < C ? p[min(2 * i + 1, nv - 1)] : 0;
         r[i] = lo | (hi << 16);
+      }
+    }
+  }
+  // The same from a raw buffer at byte off; what lies past the buffer reads as
+  // zeros, and so do channels from nv on (VEC: a lane without channels has an
+  // offset past every buffer).
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, unsigned off, int nv) {
+    if constexpr (VEC) {
+      if constexpr (BYTES == 2) {
+        r[0] = __builtin_amdgcn_raw_buffer_load_b16(rs, off, 0, 0);
+      } else if constexpr (BYTES == 4) {
+        r[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0);
+      } else if constexpr (BYTES == 8) {
+        const auto u = __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0);
+        r[0] = u[0];
+        r[1] = u[1];
+      } else {
+#pragma unroll
+        for (int i = 0; i < NW / 4; ++i) {
+          const auto u = __builtin_amdgcn_raw_buffer_load_b128(rs, off + 16 * i, 0, 0);
+          r[4 * i] = u[0];
+          r[4 * i + 1] = u[1];
+          r[4 * i + 2] = u[2];
+          r[4 * i + 3] = u[3];
+        }
+      }
+    } else {
+      auto at = [&](int i) { return i < nv ? off + i * (unsigned)sizeof(T) : BUF_OOB; };
+      if constexpr (is_f32<T>::value) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, at(i), 0, 0);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+          const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, at(2 * i), 0, 0);
+          const uint32_t hi = 2 * i + 1 < C ? (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, at(2 * i + 1), 0, 0) : 0;
+          r[i] = lo | (hi << 16);
+        }
       }
     }
   }
@@ -100,36 +149,63 @@ __device__ __forceinline__ void store_piece(T* p, const float (&v)[C], int nv) {
   }
 }
 
+// Stores the first nv of C channels at byte off of a raw buffer (see Piece::load).
+template <typename T, int C, bool VEC>
+__device__ __forceinline__ void store_piece(__amdgpu_buffer_rsrc_t rs, unsigned off, const float (&v)[C], int nv) {
+  if constexpr (!VEC) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const unsigned at = i < nv ? off + i * (unsigned)sizeof(T) : BUF_OOB;
+      if constexpr (is_f32<T>::value) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[i]), rs, at, 0, 0);
+      else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)bf16_bits(v[i]), rs, at, 0, 0);
+    }
+  } else {
+    typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+    typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+    constexpr int NW = (C * (int)sizeof(T) + 3) / 4;
+    uint32_t u[NW];
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      if constexpr (is_f32<T>::value) u[i] = __float_as_uint(v[i]);
+      else if constexpr (C == 1) u[i] = bf16_bits(v[0]);
+      else u[i] = bf16_bits(v[2 * i]) | (bf16_bits(v[2 * i + 1]) << 16);
+    }
+    if constexpr (C * sizeof(T) == 2) {
+      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)u[0], rs, off, 0, 0);
+    } else if constexpr (NW == 1) {
+      __builtin_amdgcn_raw_buffer_store_b32(u[0], rs, off, 0, 0);
+    } else if constexpr (NW == 2) {
+      __builtin_amdgcn_raw_buffer_store_b64((u32x2_t{u[0], u[1]}), rs, off, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NW / 4; ++i)
+        __builtin_amdgcn_raw_buffer_store_b128((u32x4_t{u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]}), rs,
+                                               off + 16 * i, 0, 0);
+    }
+  }
+}
+
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
-// e^x: the hardware's 2^y with the rounding error of y = x log2(e) put back
-// (y's absolute error is a relative one of the result: 5e-7 at |x| = 8 without).
-__device__ __forceinline__ float exp_acc(float x) {
-  const float y = x * LOG2E;
-  const float e = __builtin_amdgcn_exp2f(y);
-  // infinite y (x = -inf, or past the range): nothing to put back
-  const float r = fabsf(y) < 1e30f ? fmaf(x, LOG2E, -y) * LN2 : 0.f;
-  return fmaf(e, r, e);
-}
-// Logistic function (hardware reciprocal, about 1 ulp; 1 + e^-x >= 1).
+// Logistic function (hardware 2^x and reciprocal, each within about an ulp; 1 +
+// e^-x >= 1; x = -inf gives 0, +inf 1, NaN stays NaN).
 __device__ __forceinline__ float sigmoid_acc(float x) {
-  return __builtin_amdgcn_rcpf(1.f + exp_acc(-x));
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-LOG2E * x));
 }
 // log(1 + e^x) = max(x, 0) + log1p(e), e = e^-|x| in (0, 1], with
-// log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3: the odd series to s^13, whose
-// remainder is below 2e-8 of the value.  (log(1 + e) itself would lose the low
-// bits of a small e, and steps of 0.001 are ordinary here.)
+// log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3.  2 artanh(s) / s is a
+// polynomial of degree 4 in s^2, fitted at Chebyshev points of [0, 1/9]
+// (relative error 4e-9).  (log(1 + e) itself would lose the low bits of a
+// small e, and steps of 0.001 are ordinary here.)
 __device__ __forceinline__ float softplus_acc(float x) {
-  const float e = exp_acc(-fabsf(x));
+  const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(x));
   const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;
-  float p = 1.f / 13.f;
-  p = fmaf(p, q, 1.f / 11.f);
-  p = fmaf(p, q, 1.f / 9.f);
-  p = fmaf(p, q, 1.f / 7.f);
-  p = fmaf(p, q, 1.f / 5.f);
-  p = fmaf(p, q, 1.f / 3.f);
-  p = fmaf(p, q, 1.f);
-  return fmaf(2.f * s, p, x > 0.f ? x : 0.f);
+  float p = 0.28174657f;
+  p = fmaf(p, q, 0.27961419f);
+  p = fmaf(p, q, 0.40024854f);
+  p = fmaf(p, q, 0.66666316f);
+  p = fmaf(p, q, 2.0000000f);
+  return fmaf(s, p, __builtin_elementwise_maximum(x, 0.f));  // (a NaN stays one)
 }
 
 // Tokens [a, b) of sequence s, inside [0, Ttot] whatever the offsets hold.

@@ -66,7 +66,7 @@ struct SelectArgs {
   hipStream_t stream;
 };
 // Channels of one workgroup of the backward, and its blocks per group.
-constexpr int select_block_channels(int N) { return N == 8 ? 64 : 1024 / N; }
+constexpr int select_block_channels(int N) { return 512 / N; }
 hipError_t launch_select_fwd(const SelectArgs& a);
 hipError_t launch_select_bwd(const SelectArgs& a);
 hipError_t launch_select_step(const SelectArgs& a);

@@ -6,18 +6,20 @@
 // matrix units: the work is one exponential and four vector operations per
 // (channel, state, token), and these, not the bytes, bound every long call.
 //
-// Layout of a wave: CW channels x N states.  A lane holds CPL channels x 4
-// states (lane group ng = lane / CG takes states 4 ng .. 4 ng + 3, lane cg = lane
+// Layout of a wave: CW channels x N states.  A lane holds CPL = 2 channels x 4
+// states (four channels of decays and states spilled: 2,440 us instead of 410 at
+// 4 x 4,096 tokens, 4,096 channels, 16 states) (lane group ng = lane / CG takes states 4 ng .. 4 ng + 3, lane cg = lane
 // % CG takes channels CPL cg ..), so that sums over states are three in-lane
 // adds and log2(N / 4) lane exchanges for CPL channels at once, and sums over
 // channels (the gradients of B and C) start with in-lane adds as well.
 //
 // Time: a workgroup's W waves take consecutive chunks of L tokens of a tile.  A
 // wave forms its chunk's decays once and keeps them in registers, with the
-// chunk's state from a zero start; the chunks' (product of decays, state) pairs
-// are combined through LDS, and a second pass, now from the true state, reuses
-// the decays.  The second pass costs three operations more per value than a
-// walk token by token, but leaves W times as many waves.
+// chunk's state and outputs from a zero start; the chunks' (product of decays,
+// state) pairs are combined through LDS, each state by the thread that owns it,
+// and a second pass adds what the true state gives, with the kept decays.  The
+// second pass costs two operations more per value than a walk token by token,
+// but leaves W times as many waves.
 #include "comba_layer_device.hpp"
 #include "comba_layer_launch.h"
 
@@ -28,7 +30,8 @@ struct SelTile {
   static constexpr int LN = N / 4;     // lane groups over the states
   static constexpr int CG = 64 / LN;   // lanes over the channels
   static constexpr int CW = CG * CPL;  // channels of a wave
-  static constexpr int LNB = LN == 2 ? 1 : LN == 4 ? 2 : 3;  // log2
+  static constexpr int NE = CW * N;    // states of a wave, 4 CPL per lane
+  static constexpr int LOW = LN == 2 ? 5 : LN == 4 ? 4 : 3;  // lowest lane bit of the state group
   static_assert(LN == 2 || LN == 4 || LN == 8, "states per channel");
 };
 
@@ -60,84 +63,112 @@ __device__ __forceinline__ void lds_put(float* p, const float (&v)[C]) {
   }
 }
 
-// B or C rows of a chunk as loaded: lane l takes NB consecutive states of one token.
-template <typename Tin, int N, int L>
-struct StateRows {
-  static constexpr int NB = L * N / 64;
-  static_assert(NB >= 1 && N % NB == 0, "a lane's states lie in one token");
-  float v[NB];
-  __device__ __forceinline__ static int token() { return lane_id() * NB / N; }
-  __device__ __forceinline__ static int state() { return lane_id() * NB % N; }
-  __device__ __forceinline__ void load(const Tin* p) {
-#pragma unroll
-    for (int e = 0; e < NB; ++e) v[e] = to_f(p[e]);
-  }
+// What a workgroup works on: a sequence and a block of CW channels of one
+// group.  Two neighbouring blocks, which share the 128-byte lines of their
+// rows, go to workgroups eight apart and so to the same XCD.
+struct SelBlock {
+  int seq, blk, g;     // sequence, block (of all groups), group
+  int c0, cend;        // channels [c0, cend)
+  int tok0, len;       // the sequence's tokens
 };
+template <int CW>
+__device__ __forceinline__ SelBlock sel_block(const SelectArgs& a) {
+  const int Dg = a.D / a.G, nblk = (Dg + CW - 1) / CW, nb = a.G * nblk;
+  int b = blockIdx.x;
+  if ((b | 15) < (int)gridDim.x) b = (b & ~15) | ((b & 7) << 1) | ((b >> 3) & 1);
+  SelBlock s;
+  s.seq = b / nb;
+  s.blk = b - s.seq * nb;
+  s.g = s.blk / nblk;
+  s.c0 = s.g * Dg + (s.blk - s.g * nblk) * CW;
+  s.cend = min(s.c0 + CW, (s.g + 1) * Dg);
+  int t1;
+  seq_range(a.cu_seqlens, s.seq, a.Tseq, a.Ttot, s.tok0, t1);
+  s.len = t1 - s.tok0;
+  return s;
+}
 
-template <typename Tin, int N, int CPL, int L, int W, bool VEC>
+// The state that thread `slot` of the exchange owns, as (channel in the block,
+// state): slot = (i * 64 + lane) * 4 + j is the lane's channel i, state j.
+template <int N, int CPL>
+__device__ __forceinline__ void sel_slot(int slot, int& ch, int& n) {
+  using S = SelTile<N, CPL>;
+  const int i = slot / 256, l = (slot >> 2) & 63, j = slot & 3;
+  ch = (l % S::CG) * CPL + i;
+  n = (l / S::CG) * 4 + j;
+}
+
+template <typename Tin, int N, int CPL, int L, int W, bool VEC, bool Z>
 __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
   using S = SelTile<N, CPL>;
-  constexpr int LN = S::LN, CG = S::CG, CW = S::CW, TL = L / LN, TILE = L * W;
-  static_assert(L % LN == 0, "tokens per lane");
-  using SR = StateRows<Tin, N, L>;
+  constexpr int LN = S::LN, CG = S::CG, CW = S::CW, NE = S::NE, TL = L / LN, TILE = L * W;
+  constexpr int NB = L * N / 64;        // states of a B or C row that a lane loads
+  constexpr int EPT = NE / (64 * W);    // states of the exchange that a thread owns
+  constexpr unsigned EB = sizeof(Tin);
+  static_assert(L % LN == 0 && N % NB == 0 && NE % (64 * W) == 0, "tile");
   struct WaveLds {
     float dt[L][CW], xu[L][CW], B[L][N], C[L][N];
   };
   __shared__ __align__(16) WaveLds lds[W];
-  __shared__ float4 ex[W - 1][2][CPL][64];  // a chunk's decay product and its state from zero
-  __shared__ float4 hb[CPL][64];            // the state at the tile's start
+  // per chunk: its decay product, and its state from zero, which the owner
+  // replaces by the state at its start
+  __shared__ __align__(16) float ex[W][2][NE];
 
+  const SelBlock sb = sel_block<CW>(a);
   const int lane = lane_id(), w = wave_id_s(), ng = lane / CG, cg = lane % CG;
-  const int Dg = a.D / a.G, nblk = (Dg + CW - 1) / CW, nb = a.G * nblk;
-  const int seq = blockIdx.x / nb, blk = blockIdx.x % nb, g = blk / nblk;
-  const int cl = g * Dg + (blk % nblk) * CW + cg * CPL;  // first channel of the lane
-  const int nv = max(0, min(CPL, (g + 1) * Dg - cl));    // how many of them exist
-  const int cs = nv > 0 ? cl : g * Dg, ns = max(nv, 1);   // a place that may be read
-  int tok0, tok1;
-  seq_range(a.cu_seqlens, seq, a.Tseq, a.Ttot, tok0, tok1);
-  const int len = tok1 - tok0;
+  const int cl = sb.c0 + cg * CPL, nv = max(0, min(CPL, sb.cend - cl));  // the lane's channels
+  const int len = sb.len;
   WaveLds& my = lds[w];
 
   float A2[CPL][4], h[CPL][4], bias[CPL], skip[CPL];
 #pragma unroll
   for (int i = 0; i < CPL; ++i) {
-    const int c = min(cs + i, cs + ns - 1);
+    const int c = i < nv ? cl + i : sb.c0;
     bias[i] = a.bias ? a.bias[c] : 0.f;
     skip[i] = a.Dskip ? a.Dskip[c] : 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      A2[i][j] = i < nv ? a.A[(long)c * N + ng * 4 + j] * LOG2E : 0.f;
-      h[i][j] = a.h0 ? a.h0[((long)seq * a.D + c) * N + ng * 4 + j] : 0.f;
-    }
+    for (int j = 0; j < 4; ++j) A2[i][j] = i < nv ? a.A[(long)c * N + ng * 4 + j] * LOG2E : 0.f;
   }
-  if (w == W - 1) {
+  float H[EPT];  // the owned states at the tile's start
 #pragma unroll
-    for (int i = 0; i < CPL; ++i) hb[i][lane] = make_float4(h[i][0], h[i][1], h[i][2], h[i][3]);
+  for (int e = 0; e < EPT; ++e) {
+    int ch, n;
+    sel_slot<N, CPL>(threadIdx.x + e * 64 * W, ch, n);
+    H[e] = a.h0 && sb.c0 + ch < sb.cend ? a.h0[((long)sb.seq * a.D + sb.c0 + ch) * N + n] : 0.f;
   }
 
+  // byte offsets of the lane's pieces in a tile's rows
+  const unsigned tok = w * L + ng, cb = nv > 0 ? (unsigned)cl * EB : BUF_OOB;
+  const unsigned ub = a.u_row * EB, db = a.delta_row * EB, zb = a.z_row * EB, yb = a.D * EB;
+  const unsigned uo = tok * ub + cb, dof = tok * db + cb, zo = Z ? tok * zb + cb : 0, yo = tok * yb + cb;
+  const int bt = lane * NB / N, bs = lane * NB % N;  // the lane's part of the chunk's B, C
+  const unsigned bo = (w * L + bt) * (unsigned)(a.b_row * EB) + (sb.g * N + bs) * EB;
+  const unsigned co = (w * L + bt) * (unsigned)(a.c_row * EB) + (sb.g * N + bs) * EB;
   Piece<Tin, CPL, VEC> pu[TL], pd[TL], pz[TL];
-  SR pb, pc;
-  const Tin *u = static_cast<const Tin*>(a.u), *delta = static_cast<const Tin*>(a.delta),
-            *z = static_cast<const Tin*>(a.z), *Bm = static_cast<const Tin*>(a.Bm),
-            *Cm = static_cast<const Tin*>(a.Cm);
-  // a chunk's rows; past the end the last row, whose values staging drops
-  auto load = [&](int t0) {
+  Piece<Tin, NB, VEC> pb, pc;
+  auto load = [&](int base) {
+    const long row = sb.tok0 + base;
+    const int rows = len - base;
+    const auto ru = rows_rsrc(a.u, row, ub, rows), rd = rows_rsrc(a.delta, row, db, rows);
+    const auto rb = rows_rsrc(a.Bm, row, a.b_row * EB, rows), rc = rows_rsrc(a.Cm, row, a.c_row * EB, rows);
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
-      const long row = tok0 + min(t0 + ng + LN * k, len - 1);
-      pu[k].load(u + row * a.u_row + cs, ns);
-      pd[k].load(delta + row * a.delta_row + cs, ns);
-      if (z) pz[k].load(z + row * a.z_row + cs, ns);
+      pu[k].load(ru, uo + k * LN * ub, nv);
+      pd[k].load(rd, dof + k * LN * db, nv);
     }
-    const long row = tok0 + min(t0 + SR::token(), len - 1);
-    pb.load(Bm + row * a.b_row + g * N + SR::state());
-    pc.load(Cm + row * a.c_row + g * N + SR::state());
+    if constexpr (Z) {
+      const auto rz = rows_rsrc(a.z, row, zb, rows);
+#pragma unroll
+      for (int k = 0; k < TL; ++k) pz[k].load(rz, zo + k * LN * zb, nv);
+    }
+    pb.load(rb, bo, NB);
+    pc.load(rc, co, NB);
   };
-  if (len > 0) load(w * L);
+  if (len > 0) load(0);
   for (int base = 0; base < len; base += TILE) {
     const int t0 = base + w * L;
-    // stage the chunk: dt and dt u per (token, channel), B and C in fp32; zeros
-    // past the end, which leave the state as it is
+    // stage the chunk: dt and dt u per (token, channel), B and C in fp32; past
+    // the end dt = 0 and zeros as loaded leave the state as it is
     Piece<Tin, CPL, VEC> cu_[TL], cz[TL];
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
@@ -145,32 +176,35 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
       const bool ok = t0 + tl < len;
       float dt[CPL], xu[CPL];
 #pragma unroll
+      for (int i = 0; i < CPL; ++i) dt[i] = pd[k].get(i) + bias[i];
+      if (a.softplus) {
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) dt[i] = softplus_acc(dt[i]);
+      }
+#pragma unroll
       for (int i = 0; i < CPL; ++i) {
-        const float raw = pd[k].get(i) + bias[i];
-        const float d = a.softplus ? softplus_acc(raw) : raw;
-        const bool on = ok && i < nv;
-        dt[i] = on ? d : 0.f;
-        xu[i] = on ? d * pu[k].get(i) : 0.f;
+        dt[i] = ok ? dt[i] : 0.f;
+        xu[i] = dt[i] * pu[k].get(i);
       }
       lds_put<CPL>(&my.dt[tl][cg * CPL], dt);
       lds_put<CPL>(&my.xu[tl][cg * CPL], xu);
       cu_[k] = pu[k];
-      cz[k] = pz[k];
+      if constexpr (Z) cz[k] = pz[k];
     }
     {
-      const int tl = SR::token();
-      const bool ok = t0 + tl < len;
+      float v[NB];
 #pragma unroll
-      for (int e = 0; e < SR::NB; ++e) {
-        my.B[tl][SR::state() + e] = ok ? pb.v[e] : 0.f;
-        my.C[tl][SR::state() + e] = ok ? pc.v[e] : 0.f;
-      }
+      for (int e = 0; e < NB; ++e) v[e] = pb.get(e);
+      lds_put<NB>(&my.B[bt][bs], v);
+#pragma unroll
+      for (int e = 0; e < NB; ++e) v[e] = pc.get(e);
+      lds_put<NB>(&my.C[bt][bs], v);
     }
     __builtin_amdgcn_wave_barrier();
-    if (base + TILE < len) load(t0 + TILE);
+    if (base + TILE < len) load(base + TILE);
 
-    // first pass: decays, the chunk's state from zero
-    float dec[L][CPL][4], sdt[CPL];
+    // first pass: decays, the chunk's state from zero and its part of the outputs
+    float dec[L][CPL][4], yp[L * CPL], sdt[CPL];
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
       sdt[i] = 0.f;
@@ -180,106 +214,98 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
 #pragma unroll
     for (int t = 0; t < L; ++t) {
       __builtin_amdgcn_sched_barrier(0);
-      float dt[CPL], xu[CPL], Bv[4];
+      float dt[CPL], xu[CPL], Bv[4], Cv[4];
       lds_get<CPL>(&my.dt[t][cg * CPL], dt);
       lds_get<CPL>(&my.xu[t][cg * CPL], xu);
       lds_get<4>(&my.B[t][ng * 4], Bv);
+      lds_get<4>(&my.C[t][ng * 4], Cv);
 #pragma unroll
       for (int i = 0; i < CPL; ++i) {
         sdt[i] += dt[i];
+        float s = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           dec[t][i][j] = __builtin_amdgcn_exp2f(dt[i] * A2[i][j]);
-          h[i][j] = fmaf(dec[t][i][j], h[i][j], xu[i] * Bv[j]);
+          h[i][j] = t == 0 ? xu[i] * Bv[j] : fmaf(dec[t][i][j], h[i][j], xu[i] * Bv[j]);
+          s = j == 0 ? Cv[0] * h[i][0] : fmaf(Cv[j], h[i][j], s);
         }
+        yp[t * CPL + i] = s;
       }
     }
-    if (w < W - 1) {
-#pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        ex[w][0][i][lane] = make_float4(
-            __builtin_amdgcn_exp2f(sdt[i] * A2[i][0]), __builtin_amdgcn_exp2f(sdt[i] * A2[i][1]),
-            __builtin_amdgcn_exp2f(sdt[i] * A2[i][2]), __builtin_amdgcn_exp2f(sdt[i] * A2[i][3]));
-        ex[w][1][i][lane] = make_float4(h[i][0], h[i][1], h[i][2], h[i][3]);
-      }
-    }
-    __syncthreads();
-    // the true state at the chunk's start: the tile's, through the chunks before
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
-      const float4 f = hb[i][lane];
-      h[i][0] = f.x;
-      h[i][1] = f.y;
-      h[i][2] = f.z;
-      h[i][3] = f.w;
-    }
-    for (int m = 0; m < w; ++m) {
+      float p[4];
 #pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        const float4 p = ex[m][0][i][lane], f = ex[m][1][i][lane];
-        h[i][0] = fmaf(p.x, h[i][0], f.x);
-        h[i][1] = fmaf(p.y, h[i][1], f.y);
-        h[i][2] = fmaf(p.z, h[i][2], f.z);
-        h[i][3] = fmaf(p.w, h[i][3], f.w);
+      for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(sdt[i] * A2[i][j]);
+      lds_put<4>(&ex[w][0][(i * 64 + lane) * 4], p);
+      lds_put<4>(&ex[w][1][(i * 64 + lane) * 4], h[i]);
+    }
+    __syncthreads();
+    // the states at the chunks' starts, each state by its owner
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      const int s = threadIdx.x + e * 64 * W;
+      float p[W], f[W];
+#pragma unroll
+      for (int m = 0; m < W; ++m) {
+        p[m] = ex[m][0][s];
+        f[m] = ex[m][1][s];
+      }
+#pragma unroll
+      for (int m = 0; m < W; ++m) {
+        ex[m][1][s] = H[e];
+        H[e] = fmaf(p[m], H[e], f[m]);
       }
     }
     __syncthreads();
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) lds_get<4>(&ex[w][1][(i * 64 + lane) * 4], h[i]);
     if (a.ck && t0 % SELECT_CK == 0 && t0 < len) {
-      float* ck = a.ck + ((long)(tok0 / SELECT_CK + seq + t0 / SELECT_CK) * a.D + cl) * N + ng * 4;
+      float* ck = a.ck + ((long)(sb.tok0 / SELECT_CK + sb.seq + t0 / SELECT_CK) * a.D + cl) * N + ng * 4;
 #pragma unroll
       for (int i = 0; i < CPL; ++i)
         if (i < nv) *reinterpret_cast<float4*>(ck + i * N) = make_float4(h[i][0], h[i][1], h[i][2], h[i][3]);
     }
-    // second pass: the states, and their sums with C, LN tokens at a time: lane
-    // group ng ends with token ng's, whose u and z it holds
+    // second pass: what that state adds, decayed, to the outputs
+#pragma unroll
+    for (int t = 0; t < L; ++t) {
+      __builtin_amdgcn_sched_barrier(0);
+      float Cv[4];
+      lds_get<4>(&my.C[t][ng * 4], Cv);
+#pragma unroll
+      for (int i = 0; i < CPL; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          h[i][j] *= dec[t][i][j];
+          yp[t * CPL + i] = fmaf(Cv[j], h[i][j], yp[t * CPL + i]);
+        }
+    }
+    // sums over the lane groups, LN tokens at a time: lane group ng ends with
+    // token ng's, whose u and z it holds
+    const auto ry = rows_rsrc(a.y, sb.tok0 + base, yb, len - base);
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
-      float yp[LN * CPL];
+      float* yk = yp + k * LN * CPL;
+      spread_sum<LN * CPL, 5, S::LOW>(yk);
+      float y[CPL];
 #pragma unroll
-      for (int e = 0; e < LN; ++e) {
-        const int t = k * LN + e;
-        __builtin_amdgcn_sched_barrier(0);
-        float xu[CPL], Bv[4], Cv[4];
-        lds_get<CPL>(&my.xu[t][cg * CPL], xu);
-        lds_get<4>(&my.B[t][ng * 4], Bv);
-        lds_get<4>(&my.C[t][ng * 4], Cv);
-#pragma unroll
-        for (int i = 0; i < CPL; ++i) {
-          float s = 0.f;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            h[i][j] = fmaf(dec[t][i][j], h[i][j], xu[i] * Bv[j]);
-            s = j == 0 ? Cv[0] * h[i][0] : fmaf(Cv[j], h[i][j], s);
-          }
-          yp[e * CPL + i] = s;
+      for (int i = 0; i < CPL; ++i) {
+        y[i] = fmaf(skip[i], cu_[k].get(i), yk[i]);
+        if constexpr (Z) {
+          const float zv = cz[k].get(i);
+          y[i] *= zv * sigmoid_acc(zv);
         }
       }
-      spread_sum<LN * CPL, 5, 6 - S::LNB>(yp);
-      const int t = t0 + ng + LN * k;
-      if (t < len) {
-        float y[CPL];
-#pragma unroll
-        for (int i = 0; i < CPL; ++i) {
-          y[i] = fmaf(skip[i], cu_[k].get(i), yp[i]);
-          if (z) {
-            const float zv = cz[k].get(i);
-            y[i] *= zv * sigmoid_acc(zv);
-          }
-        }
-        store_piece<Tin, CPL, VEC>(static_cast<Tin*>(a.y) + (long)(tok0 + t) * a.D + cl, y, nv);
-      }
-    }
-    if (w == W - 1) {
-#pragma unroll
-      for (int i = 0; i < CPL; ++i) hb[i][lane] = make_float4(h[i][0], h[i][1], h[i][2], h[i][3]);
+      store_piece<Tin, CPL, VEC>(ry, yo + k * LN * yb, y, nv);
     }
   }
-  if (a.ht && w == W - 1) {
+  if (a.ht) {
 #pragma unroll
-    for (int i = 0; i < CPL; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (i < nv) a.ht[((long)seq * a.D + cl + i) * N + ng * 4 + j] = h[i][j];
+    for (int e = 0; e < EPT; ++e) {
+      int ch, n;
+      sel_slot<N, CPL>(threadIdx.x + e * 64 * W, ch, n);
+      if (sb.c0 + ch < sb.cend) a.ht[((long)sb.seq * a.D + sb.c0 + ch) * N + n] = H[e];
+    }
   }
 }
 
@@ -294,141 +320,148 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
 // its state from zero and its gradient from zero, one exchange gives both true
 // ends, and a second pass forms the states (kept in registers) and then the
 // gradients.  dB and dC of the workgroup's channels go to a partial sum.
-template <typename Tin, int N, bool VEC>
+template <typename Tin, int N, int CPL, bool VEC, bool Z>
 __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
-  constexpr int CPL = select_block_channels(N) * N / 256, L = 4, W = 8;
+  constexpr int L = 4, W = 8;
   using S = SelTile<N, CPL>;
-  constexpr int LN = S::LN, CG = S::CG, CW = S::CW, TL = (L + LN - 1) / LN, TILE = L * W;
-  constexpr int VL = CPL / LN > 0 ? CPL / LN : 1;  // channels of a lane after a sum over the states
-  static_assert(TILE == SELECT_CK, "a tile starts at a kept state");
+  constexpr int LN = S::LN, CG = S::CG, CW = S::CW, NE = S::NE, TL = (L + LN - 1) / LN, TILE = L * W;
+  constexpr int NB = L * N / 64 > 0 ? L * N / 64 : 1, EPT = NE / (64 * W);
+  constexpr unsigned EB = sizeof(Tin);
+  static_assert(TILE == SELECT_CK && NE % (64 * W) == 0, "a tile starts at a kept state");
   struct WaveLds {
     float dt[L][CW], xu[L][CW], gy[L][CW], yp[L][CW], B[L][N], C[L][N];
+    float u[L][CW], slope[L][CW], dz[L][CW], odt[L][CW];  // of a lane's own tokens
   };
   __shared__ __align__(16) WaveLds lds[W];
-  __shared__ float4 ex[W][3][CPL][64];  // a chunk's decay product, state and gradient from zero
-  __shared__ float4 gb[CPL][64];        // gradient of the state that leaves the tile, decayed
+  // per chunk: its decay product, and its state and gradient from zero, which
+  // the owner replaces by the state at its start and the gradient at its end
+  __shared__ __align__(16) float ex[W][3][NE];
 
+  const SelBlock sb = sel_block<CW>(a);
   const int lane = lane_id(), w = wave_id_s(), ng = lane / CG, cg = lane % CG;
-  const int Dg = a.D / a.G, nblk = (Dg + CW - 1) / CW, nb = a.G * nblk;
-  const int seq = blockIdx.x / nb, blk = blockIdx.x % nb, g = blk / nblk;
-  const int cl = g * Dg + (blk % nblk) * CW + cg * CPL;
-  const int nv = max(0, min(CPL, (g + 1) * Dg - cl));
-  const int cs = nv > 0 ? cl : g * Dg, ns = max(nv, 1);
-  int tok0, tok1;
-  seq_range(a.cu_seqlens, seq, a.Tseq, a.Ttot, tok0, tok1);
-  const int len = tok1 - tok0;
+  const int cl = sb.c0 + cg * CPL, nv = max(0, min(CPL, sb.cend - cl));
+  const int len = sb.len, ntiles = (len + TILE - 1) / TILE;
   WaveLds& my = lds[w];
 
-  float A2[CPL][4], dA[CPL][4], bias[CPL], skip[CPL], dD[CPL], db[CPL];
+  float A2[CPL][4], dA[CPL][4], bias[CPL], skip[CPL], dD[CPL], dbias[CPL];
 #pragma unroll
   for (int i = 0; i < CPL; ++i) {
-    const int c = min(cs + i, cs + ns - 1);
+    const int c = i < nv ? cl + i : sb.c0;
     bias[i] = a.bias ? a.bias[c] : 0.f;
     skip[i] = a.Dskip ? a.Dskip[c] : 0.f;
-    dD[i] = db[i] = 0.f;
+    dD[i] = dbias[i] = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       A2[i][j] = i < nv ? a.A[(long)c * N + ng * 4 + j] * LOG2E : 0.f;
       dA[i][j] = 0.f;
     }
   }
-  if (w == 0) {
+  // owned states: the decayed gradient that enters the tile from the tokens
+  // after it, and the kept state at the tile's start
+  float Gc[EPT], hk[EPT];
+  long own[EPT];  // place in a [D, N] state, negative: none
 #pragma unroll
-    for (int i = 0; i < CPL; ++i) {
-      float f[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        f[j] = a.dht && i < nv ? a.dht[((long)seq * a.D + cl + i) * N + ng * 4 + j] : 0.f;
-      gb[i][lane] = make_float4(f[0], f[1], f[2], f[3]);
-    }
+  for (int e = 0; e < EPT; ++e) {
+    int ch, n;
+    sel_slot<N, CPL>(threadIdx.x + e * 64 * W, ch, n);
+    own[e] = sb.c0 + ch < sb.cend ? (long)(sb.c0 + ch) * N + n : -1;
+    Gc[e] = a.dht && own[e] >= 0 ? a.dht[(long)sb.seq * a.D * N + own[e]] : 0.f;
   }
-  const Tin *u = static_cast<const Tin*>(a.u), *delta = static_cast<const Tin*>(a.delta),
-            *z = static_cast<const Tin*>(a.z), *dy = static_cast<const Tin*>(a.dy);
-  const Tin *Bm = static_cast<const Tin*>(a.Bm), *Cm = static_cast<const Tin*>(a.Cm);
-  const int ntiles = (len + TILE - 1) / TILE;
 
+  const unsigned tok = w * L + min(ng, L - 1);
+  const unsigned cb = nv > 0 && ng < L ? (unsigned)cl * EB : BUF_OOB;
+  const unsigned ub = a.u_row * EB, db = a.delta_row * EB, zb = a.z_row * EB, yb = a.D * EB;
+  const unsigned uo = tok * ub + cb, dof = tok * db + cb, zo = Z ? tok * zb + cb : 0, yo = tok * yb + cb;
+  const int bt = lane * NB / N, bs = lane * NB % N;
+  const bool bok = bt < L;
+  const unsigned bo = bok ? (w * L + bt) * (unsigned)(a.b_row * EB) + (sb.g * N + bs) * EB : BUF_OOB;
+  const unsigned co = bok ? (w * L + bt) * (unsigned)(a.c_row * EB) + (sb.g * N + bs) * EB : BUF_OOB;
   Piece<Tin, CPL, VEC> pu[TL], pd[TL], pz[TL], py[TL];
-  constexpr int SN = L * N / 64 > 0 ? L * N / 64 : 1;  // states per lane of the chunk's B, C rows
-  const int stok = min(lane * SN / N, L - 1), sst = lane * SN % N;
-  float pb[SN], pc[SN];
-  float4 pk[CPL];  // the kept state at the tile's start
+  Piece<Tin, NB, VEC> pb, pc;
   auto load = [&](int tile) {
-    const int t0 = tile * TILE + w * L;
+    const long row = sb.tok0 + tile * TILE;
+    const int rows = len - tile * TILE;
+    const auto ru = rows_rsrc(a.u, row, ub, rows), rd = rows_rsrc(a.delta, row, db, rows);
+    const auto rb = rows_rsrc(a.Bm, row, a.b_row * EB, rows), rc = rows_rsrc(a.Cm, row, a.c_row * EB, rows);
+    const auto ry = rows_rsrc(a.dy, row, yb, rows);
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
-      const long row = tok0 + min(t0 + min(ng + LN * k, L - 1), len - 1);
-      pu[k].load(u + row * a.u_row + cs, ns);
-      pd[k].load(delta + row * a.delta_row + cs, ns);
-      if (z) pz[k].load(z + row * a.z_row + cs, ns);
-      py[k].load(dy + row * a.D + cs, ns);
+      pu[k].load(ru, uo + k * LN * ub, nv);
+      pd[k].load(rd, dof + k * LN * db, nv);
+      py[k].load(ry, yo + k * LN * yb, nv);
     }
-    const long row = tok0 + min(t0 + stok, len - 1);
+    if constexpr (Z) {
+      const auto rz = rows_rsrc(a.z, row, zb, rows);
 #pragma unroll
-    for (int e = 0; e < SN; ++e) {
-      pb[e] = to_f(Bm[row * a.b_row + g * N + sst + e]);
-      pc[e] = to_f(Cm[row * a.c_row + g * N + sst + e]);
+      for (int k = 0; k < TL; ++k) pz[k].load(rz, zo + k * LN * zb, nv);
     }
-    const float* ck = a.ck + ((long)(tok0 / SELECT_CK + seq + tile) * a.D + cs) * N + ng * 4;
+    pb.load(rb, bo, NB);
+    pc.load(rc, co, NB);
+    const float* ck = a.ck + (long)(sb.tok0 / SELECT_CK + sb.seq + tile) * a.D * N;
 #pragma unroll
-    for (int i = 0; i < CPL; ++i) pk[i] = *reinterpret_cast<const float4*>(ck + min(i, ns - 1) * N);
+    for (int e = 0; e < EPT; ++e) hk[e] = ck[max(own[e], (long)sb.c0 * N)];
   };
   if (ntiles > 0) load(ntiles - 1);
   for (int tile = ntiles - 1; tile >= 0; --tile) {
-    const int t0 = tile * TILE + w * L;
-    float h[CPL][4], G[CPL][4];
-    float4 hk[CPL];
-    // per own token: raw u, dt and gy stay in registers; slope = d dt / d raw,
-    // and for z: silu(z), silu'(z) dy
-    float ou[TL][CPL], oslope[TL][CPL], odz[TL][CPL], odt[TL][CPL], ogy[TL][CPL];
+    const int base = tile * TILE, t0 = base + w * L;
+    float h[CPL][4], G[CPL][4], hs0[EPT];
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
       const int tl = ng + LN * k;
       const bool ok = tl < L && t0 + tl < len;
-      float xu[CPL];
+      float dt[CPL], xu[CPL], gy[CPL], uv[CPL], sl[CPL], dz[CPL];
 #pragma unroll
       for (int i = 0; i < CPL; ++i) {
-        const bool on = ok && i < nv;
-        const float raw = pd[k].get(i) + bias[i];
-        odt[k][i] = on ? (a.softplus ? softplus_acc(raw) : raw) : 0.f;
-        oslope[k][i] = a.softplus ? sigmoid_acc(raw) : 1.f;
-        ou[k][i] = on ? pu[k].get(i) : 0.f;
-        xu[i] = odt[k][i] * ou[k][i];
-        float dyv = on ? py[k].get(i) : 0.f;
-        odz[k][i] = 0.f;
-        if (z) {
-          const float zv = on ? pz[k].get(i) : 0.f, sg = sigmoid_acc(zv);
-          odz[k][i] = dyv * sg * fmaf(zv, 1.f - sg, 1.f);
-          dyv *= zv * sg;
+        dt[i] = pd[k].get(i) + bias[i];
+        sl[i] = 1.f;
+        uv[i] = pu[k].get(i);
+        gy[i] = py[k].get(i);
+      }
+      if (a.softplus) {
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+          sl[i] = sigmoid_acc(dt[i]);
+          dt[i] = softplus_acc(dt[i]);
         }
-        ogy[k][i] = dyv;
+      }
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) {
+        dt[i] = ok ? dt[i] : 0.f;
+        xu[i] = dt[i] * uv[i];
+        if constexpr (Z) {
+          const float zv = pz[k].get(i), sg = sigmoid_acc(zv);
+          dz[i] = gy[i] * sg * fmaf(zv, 1.f - sg, 1.f);
+          gy[i] *= zv * sg;
+        }
       }
       if (tl < L) {
-        lds_put<CPL>(&my.dt[tl][cg * CPL], odt[k]);
+        lds_put<CPL>(&my.dt[tl][cg * CPL], dt);
         lds_put<CPL>(&my.xu[tl][cg * CPL], xu);
-        lds_put<CPL>(&my.gy[tl][cg * CPL], ogy[k]);
+        lds_put<CPL>(&my.gy[tl][cg * CPL], gy);
+        lds_put<CPL>(&my.u[tl][cg * CPL], uv);
+        lds_put<CPL>(&my.odt[tl][cg * CPL], dt);
+        lds_put<CPL>(&my.slope[tl][cg * CPL], sl);
+        if constexpr (Z) lds_put<CPL>(&my.dz[tl][cg * CPL], dz);
       }
     }
-    if (lane * SN < L * N) {
-      const bool ok = t0 + stok < len;
+    if (bok) {
+      float v[NB];
 #pragma unroll
-      for (int e = 0; e < SN; ++e) {
-        my.B[stok][sst + e] = ok ? pb[e] : 0.f;
-        my.C[stok][sst + e] = ok ? pc[e] : 0.f;
-      }
+      for (int e = 0; e < NB; ++e) v[e] = pb.get(e);
+      lds_put<NB>(&my.B[bt][bs], v);
+#pragma unroll
+      for (int e = 0; e < NB; ++e) v[e] = pc.get(e);
+      lds_put<NB>(&my.C[bt][bs], v);
     }
 #pragma unroll
-    for (int i = 0; i < CPL; ++i) hk[i] = pk[i];
+    for (int e = 0; e < EPT; ++e) hs0[e] = hk[e];
     __builtin_amdgcn_wave_barrier();
     if (tile > 0) load(tile - 1);
 
     // the chunk from zero, forward then backward
     float dec[L][CPL][4], sdt[CPL];
 #pragma unroll
-    for (int i = 0; i < CPL; ++i) {
-      sdt[i] = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) h[i][j] = G[i][j] = 0.f;
-    }
+    for (int i = 0; i < CPL; ++i) sdt[i] = 0.f;
 #pragma unroll
     for (int t = 0; t < L; ++t) {
       __builtin_amdgcn_sched_barrier(0);
@@ -442,7 +475,7 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           dec[t][i][j] = __builtin_amdgcn_exp2f(dt[i] * A2[i][j]);
-          h[i][j] = fmaf(dec[t][i][j], h[i][j], xu[i] * Bv[j]);
+          h[i][j] = t == 0 ? xu[i] * Bv[j] : fmaf(dec[t][i][j], h[i][j], xu[i] * Bv[j]);
         }
       }
     }
@@ -455,204 +488,192 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
 #pragma unroll
       for (int i = 0; i < CPL; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) G[i][j] = dec[t][i][j] * fmaf(Cv[j], gy[i], G[i][j]);
+        for (int j = 0; j < 4; ++j)
+          G[i][j] = dec[t][i][j] * (t == L - 1 ? Cv[j] * gy[i] : fmaf(Cv[j], gy[i], G[i][j]));
     }
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
-      ex[w][0][i][lane] = make_float4(
-          __builtin_amdgcn_exp2f(sdt[i] * A2[i][0]), __builtin_amdgcn_exp2f(sdt[i] * A2[i][1]),
-          __builtin_amdgcn_exp2f(sdt[i] * A2[i][2]), __builtin_amdgcn_exp2f(sdt[i] * A2[i][3]));
-      ex[w][1][i][lane] = make_float4(h[i][0], h[i][1], h[i][2], h[i][3]);
-      ex[w][2][i][lane] = make_float4(G[i][0], G[i][1], G[i][2], G[i][3]);
+      float p[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(sdt[i] * A2[i][j]);
+      lds_put<4>(&ex[w][0][(i * 64 + lane) * 4], p);
+      lds_put<4>(&ex[w][1][(i * 64 + lane) * 4], h[i]);
+      lds_put<4>(&ex[w][2][(i * 64 + lane) * 4], G[i]);
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < CPL; ++i) {
-      const float4 f = gb[i][lane];
-      G[i][0] = f.x;
-      G[i][1] = f.y;
-      G[i][2] = f.z;
-      G[i][3] = f.w;
-      h[i][0] = hk[i].x;
-      h[i][1] = hk[i].y;
-      h[i][2] = hk[i].z;
-      h[i][3] = hk[i].w;
-    }
-    for (int m = 0; m < w; ++m) {
+    for (int e = 0; e < EPT; ++e) {
+      const int s = threadIdx.x + e * 64 * W;
+      float p[W], f[W], q[W], c = hs0[e];
 #pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        const float4 p = ex[m][0][i][lane], f = ex[m][1][i][lane];
-        h[i][0] = fmaf(p.x, h[i][0], f.x);
-        h[i][1] = fmaf(p.y, h[i][1], f.y);
-        h[i][2] = fmaf(p.z, h[i][2], f.z);
-        h[i][3] = fmaf(p.w, h[i][3], f.w);
+      for (int m = 0; m < W; ++m) {
+        p[m] = ex[m][0][s];
+        f[m] = ex[m][1][s];
+        q[m] = ex[m][2][s];
       }
-    }
-    for (int m = W - 1; m > w; --m) {
 #pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        const float4 p = ex[m][0][i][lane], f = ex[m][2][i][lane];
-        G[i][0] = fmaf(p.x, G[i][0], f.x);
-        G[i][1] = fmaf(p.y, G[i][1], f.y);
-        G[i][2] = fmaf(p.z, G[i][2], f.z);
-        G[i][3] = fmaf(p.w, G[i][3], f.w);
+      for (int m = 0; m < W; ++m) {
+        ex[m][1][s] = c;
+        c = fmaf(p[m], c, f[m]);
+      }
+#pragma unroll
+      for (int m = W - 1; m >= 0; --m) {
+        ex[m][2][s] = Gc[e];
+        Gc[e] = fmaf(p[m], Gc[e], q[m]);
       }
     }
     __syncthreads();
     // second pass: the states (hs[t] enters token t)
     float hs[L + 1][CPL][4];
 #pragma unroll
-    for (int i = 0; i < CPL; ++i)
+    for (int i = 0; i < CPL; ++i) {
+      lds_get<4>(&ex[w][1][(i * 64 + lane) * 4], hs[0][i]);
+      lds_get<4>(&ex[w][2][(i * 64 + lane) * 4], G[i]);
+    }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) hs[0][i][j] = h[i][j];
+    for (int t2 = 0; t2 < L; t2 += 2) {
+      float s[2 * CPL];
 #pragma unroll
-    for (int t = 0; t < L; ++t) {
-      __builtin_amdgcn_sched_barrier(0);
-      float xu[CPL], Bv[4], Cv[4], s[CPL];
-      lds_get<CPL>(&my.xu[t][cg * CPL], xu);
-      lds_get<4>(&my.B[t][ng * 4], Bv);
-      lds_get<4>(&my.C[t][ng * 4], Cv);
+      for (int tt = 0; tt < 2; ++tt) {
+        __builtin_amdgcn_sched_barrier(0);
+        const int t = t2 + tt;
+        float xu[CPL], Bv[4], Cv[4];
+        lds_get<CPL>(&my.xu[t][cg * CPL], xu);
+        lds_get<4>(&my.B[t][ng * 4], Bv);
+        if constexpr (Z) lds_get<4>(&my.C[t][ng * 4], Cv);
 #pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        s[i] = 0.f;
+        for (int i = 0; i < CPL; ++i) {
+          float v = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          hs[t + 1][i][j] = fmaf(dec[t][i][j], hs[t][i][j], xu[i] * Bv[j]);
-          s[i] = fmaf(Cv[j], hs[t + 1][i][j], s[i]);
+          for (int j = 0; j < 4; ++j) {
+            hs[t + 1][i][j] = fmaf(dec[t][i][j], hs[t][i][j], xu[i] * Bv[j]);
+            if constexpr (Z) v = j == 0 ? Cv[0] * hs[t + 1][i][0] : fmaf(Cv[j], hs[t + 1][i][j], v);
+          }
+          s[tt * CPL + i] = v;
         }
       }
-      if (z) {  // the ungated output, for dz
-        spread_sum<CPL, 5, 6 - S::LNB>(s);
+      if constexpr (Z) {  // the ungated output, for dz
+        constexpr int VL = 2 * CPL / LN > 0 ? 2 * CPL / LN : 1;
+        spread_sum<2 * CPL, 5, S::LOW>(s);
+        const int v = LN >= 2 * CPL ? ng / (LN / (2 * CPL) > 0 ? LN / (2 * CPL) : 1) : ng * VL;
         float o[VL];
 #pragma unroll
         for (int i = 0; i < VL; ++i) o[i] = s[i];
-        const int at = cg * CPL + (LN >= CPL ? ng / (LN / CPL) : ng * VL);
-        lds_put<VL>(&my.yp[t][at], o);
+        lds_put<VL>(&my.yp[t2 + v / CPL][cg * CPL + v % CPL], o);
       }
     }
     // second pass: the gradients
+    const auto rbc = rows_rsrc(a.bcp, (long)sb.blk * a.Ttot + sb.tok0 + base, 2 * N * 4, len - base);
 #pragma unroll
-    for (int t = L - 1; t >= 0; --t) {
-      __builtin_amdgcn_sched_barrier(0);
-      float dt[CPL], xu[CPL], gy[CPL], Bv[4], Cv[4], bc[8], sb[CPL], sa[CPL];
-      lds_get<CPL>(&my.dt[t][cg * CPL], dt);
-      lds_get<CPL>(&my.xu[t][cg * CPL], xu);
-      lds_get<CPL>(&my.gy[t][cg * CPL], gy);
-      lds_get<4>(&my.B[t][ng * 4], Bv);
-      lds_get<4>(&my.C[t][ng * 4], Cv);
+    for (int t2 = L - 2; t2 >= 0; t2 -= 2) {
+      float bc[16];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) bc[j] = 0.f;
+      for (int tt = 1; tt >= 0; --tt) {
+        __builtin_amdgcn_sched_barrier(0);
+        const int t = t2 + tt;
+        float dt[CPL], xu[CPL], gy[CPL], Bv[4], Cv[4], sm[2 * CPL];
+        lds_get<CPL>(&my.dt[t][cg * CPL], dt);
+        lds_get<CPL>(&my.xu[t][cg * CPL], xu);
+        lds_get<CPL>(&my.gy[t][cg * CPL], gy);
+        lds_get<4>(&my.B[t][ng * 4], Bv);
+        lds_get<4>(&my.C[t][ng * 4], Cv);
 #pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        sb[i] = sa[i] = 0.f;
+        for (int i = 0; i < CPL; ++i) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float dh = fmaf(Cv[j], gy[i], G[i][j]);
-          G[i][j] = dec[t][i][j] * dh;
-          const float p = G[i][j] * hs[t][i][j];
-          sb[i] = fmaf(dh, Bv[j], sb[i]);
-          sa[i] = fmaf(A2[i][j], p, sa[i]);
-          dA[i][j] = fmaf(dt[i], p, dA[i][j]);
-          bc[j] = fmaf(dh, xu[i], bc[j]);
-          bc[4 + j] = fmaf(gy[i], hs[t + 1][i][j], bc[4 + j]);
+          for (int j = 0; j < 4; ++j) {
+            const float dh = fmaf(Cv[j], gy[i], G[i][j]);
+            G[i][j] = dec[t][i][j] * dh;
+            const float p = G[i][j] * hs[t][i][j];
+            sm[i] = j == 0 ? dh * Bv[0] : fmaf(dh, Bv[j], sm[i]);
+            sm[CPL + i] = j == 0 ? A2[i][0] * p : fmaf(A2[i][j], p, sm[CPL + i]);
+            dA[i][j] = fmaf(dt[i], p, dA[i][j]);
+            bc[tt * 8 + j] = i == 0 ? dh * xu[0] : fmaf(dh, xu[i], bc[tt * 8 + j]);
+            bc[tt * 8 + 4 + j] = i == 0 ? gy[0] * hs[t + 1][0][j] : fmaf(gy[i], hs[t + 1][i][j], bc[tt * 8 + 4 + j]);
+          }
         }
-      }
-      // over the states: <B, dh> and <A, p> replace the token's xu and dt
-      spread_sum<CPL, 5, 6 - S::LNB>(sb);
-      spread_sum<CPL, 5, 6 - S::LNB>(sa);
-      float ob[VL], oa[VL];
+        // over the states: <B, dh> and <A, p> replace the token's xu and dt
+        constexpr int VL = 2 * CPL / LN > 0 ? 2 * CPL / LN : 1;
+        spread_sum<2 * CPL, 5, S::LOW>(sm);
+        const int v = LN >= 2 * CPL ? ng / (LN / (2 * CPL) > 0 ? LN / (2 * CPL) : 1) : ng * VL;
+        float o[VL];
 #pragma unroll
-      for (int i = 0; i < VL; ++i) {
-        ob[i] = sb[i];
-        oa[i] = sa[i];
+        for (int i = 0; i < VL; ++i) o[i] = sm[i];
+        __builtin_amdgcn_wave_barrier();
+        lds_put<VL>(v < CPL ? &my.xu[t][cg * CPL + v] : &my.dt[t][cg * CPL + v - CPL], o);
       }
-      const int at = cg * CPL + (LN >= CPL ? ng / (LN / CPL) : ng * VL);
-      __builtin_amdgcn_wave_barrier();
-      lds_put<VL>(&my.xu[t][at], ob);
-      lds_put<VL>(&my.dt[t][at], oa);
-      // over the channels: lane cg's top three bits say which of the 8 values it holds
-      spread_sum<8, 5 - S::LNB, 0>(bc);
-      constexpr int REST = CG / 8;  // lanes with the same value
-      if (cg % REST == 0 && t0 + t < len) {
-        const int v = cg / REST;
-        a.bcp[((long)blk * a.Ttot + tok0 + t0 + t) * (2 * N) + (v >> 2) * N + ng * 4 + (v & 3)] = bc[0];
-      }
-    }
-    if (w == 0) {
+      // over the channels, two tokens' 16 values; dB and dC of a token side by side
+      constexpr int VB = 16 / CG > 0 ? 16 / CG : 1, REST = CG / 16 > 0 ? CG / 16 : 1;
+      spread_sum<16, S::LOW - 1, 0>(bc);
+      const int v = CG >= 16 ? cg / REST : cg * VB;
+      const unsigned at = ((w * L + t2 + (v >> 3)) * 2 * N + ((v >> 2) & 1) * N + ng * 4 + (v & 3)) * 4;
 #pragma unroll
-      for (int i = 0; i < CPL; ++i) gb[i][lane] = make_float4(G[i][0], G[i][1], G[i][2], G[i][3]);
+      for (int i = 0; i < VB; ++i)
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(bc[i]), rbc, cg % REST ? BUF_OOB : at + 4 * i, 0, 0);
     }
     __builtin_amdgcn_wave_barrier();
     // the own tokens' gradients
+    const auto rdu = rows_rsrc(a.du, sb.tok0 + base, yb, len - base);
+    const auto rdd = rows_rsrc(a.ddelta, sb.tok0 + base, yb, len - base);
+    const auto rdz = rows_rsrc(a.dz, sb.tok0 + base, yb, Z ? len - base : 0);
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
-      const int tl = ng + LN * k, t = t0 + tl;
-      if (tl < L && t < len) {
-        float sb[CPL], sa[CPL], yp[CPL], du[CPL], dd[CPL], dz[CPL];
-        lds_get<CPL>(&my.xu[tl][cg * CPL], sb);
-        lds_get<CPL>(&my.dt[tl][cg * CPL], sa);
-        if (z) lds_get<CPL>(&my.yp[tl][cg * CPL], yp);
-#pragma unroll
-        for (int i = 0; i < CPL; ++i) {
-          du[i] = fmaf(odt[k][i], sb[i], skip[i] * ogy[k][i]);
-          dd[i] = fmaf(ou[k][i], sb[i], LN2 * sa[i]) * oslope[k][i];
-          dD[i] = fmaf(ogy[k][i], ou[k][i], dD[i]);
-          db[i] += dd[i];
-          dz[i] = z ? odz[k][i] * fmaf(skip[i], ou[k][i], yp[i]) : 0.f;
-        }
-        const long at = (long)(tok0 + t) * a.D + cl;
-        store_piece<Tin, CPL, VEC>(static_cast<Tin*>(a.du) + at, du, nv);
-        store_piece<Tin, CPL, VEC>(static_cast<Tin*>(a.ddelta) + at, dd, nv);
-        if (z) store_piece<Tin, CPL, VEC>(static_cast<Tin*>(a.dz) + at, dz, nv);
+      const int tl = min(ng + LN * k, L - 1);
+      const bool ok = ng + LN * k < L && t0 + tl < len;
+      float sbv[CPL], sa[CPL], yp[CPL], du[CPL], dd[CPL], dz[CPL], uv[CPL], sl[CPL], gy[CPL], dt[CPL];
+      lds_get<CPL>(&my.odt[tl][cg * CPL], dt);
+      lds_get<CPL>(&my.xu[tl][cg * CPL], sbv);
+      lds_get<CPL>(&my.dt[tl][cg * CPL], sa);
+      lds_get<CPL>(&my.u[tl][cg * CPL], uv);
+      lds_get<CPL>(&my.gy[tl][cg * CPL], gy);
+      lds_get<CPL>(&my.slope[tl][cg * CPL], sl);
+      if constexpr (Z) {
+        lds_get<CPL>(&my.yp[tl][cg * CPL], yp);
+        lds_get<CPL>(&my.dz[tl][cg * CPL], dz);
       }
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) {
+        du[i] = fmaf(dt[i], sbv[i], skip[i] * gy[i]);
+        dd[i] = fmaf(uv[i], sbv[i], LN2 * sa[i]) * sl[i];
+        dD[i] = fmaf(gy[i], uv[i], dD[i]);
+        dbias[i] += ok ? dd[i] : 0.f;
+        if constexpr (Z) dz[i] *= fmaf(skip[i], uv[i], yp[i]);
+      }
+      store_piece<Tin, CPL, VEC>(rdu, yo + k * LN * yb, du, nv);
+      store_piece<Tin, CPL, VEC>(rdd, yo + k * LN * yb, dd, nv);
+      if constexpr (Z) store_piece<Tin, CPL, VEC>(rdz, yo + k * LN * yb, dz, nv);
     }
   }
   // the sequence's parameter gradients: the waves' sums in order, dD and dbias
   // also over the lane groups, which held different tokens
   __syncthreads();
-  float4* part = &ex[0][0][0][0];  // [W][CPL][64] dA, then [W][2][CPL][64] floats
-  float* pd2 = reinterpret_cast<float*>(part + W * CPL * 64);
+  float* red = &ex[0][1][0];  // [W][2][CPL][64], in the chunks' second parts
+  static_assert(2 * CPL * 64 <= NE, "room for the sums");
 #pragma unroll
   for (int i = 0; i < CPL; ++i) {
-    part[(w * CPL + i) * 64 + lane] = make_float4(dA[i][0], dA[i][1], dA[i][2], dA[i][3]);
-    pd2[((w * 2 + 0) * CPL + i) * 64 + lane] = dD[i];
-    pd2[((w * 2 + 1) * CPL + i) * 64 + lane] = db[i];
+    lds_put<4>(&ex[w][0][(i * 64 + lane) * 4], dA[i]);
+    red[w * 3 * NE + (0 * CPL + i) * 64 + lane] = dD[i];
+    red[w * 3 * NE + (1 * CPL + i) * 64 + lane] = dbias[i];
   }
   __syncthreads();
-  if (w == 0) {
 #pragma unroll
-    for (int i = 0; i < CPL; ++i) {
-      float4 s = part[i * 64 + lane];
-      for (int m = 1; m < W; ++m) {
-        const float4 v = part[(m * CPL + i) * 64 + lane];
-        s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
-      }
-      if (i < nv) {
-        float* p = a.dap + ((long)seq * a.D + cl + i) * (N + 2);
-        p[ng * 4] = s.x;
-        p[ng * 4 + 1] = s.y;
-        p[ng * 4 + 2] = s.z;
-        p[ng * 4 + 3] = s.w;
-        if (ng == 0) {
-          float sd = 0.f, sb = 0.f;
-          for (int m = 0; m < W; ++m)
-            for (int e = 0; e < LN; ++e) {
-              sd += pd2[((m * 2 + 0) * CPL + i) * 64 + e * CG + cg];
-              sb += pd2[((m * 2 + 1) * CPL + i) * 64 + e * CG + cg];
-            }
-          p[N] = sd;
-          p[N + 1] = sb;
-        }
-        if (a.dh0) {
-          const float4 f = gb[i][lane];
-          float* q = a.dh0 + ((long)seq * a.D + cl + i) * N + ng * 4;
-          q[0] = f.x;
-          q[1] = f.y;
-          q[2] = f.z;
-          q[3] = f.w;
-        }
-      }
+  for (int e = 0; e < EPT; ++e) {
+    const int s = threadIdx.x + e * 64 * W;
+    float v = ex[0][0][s];
+#pragma unroll
+    for (int m = 1; m < W; ++m) v += ex[m][0][s];
+    if (own[e] >= 0) {
+      const int c = own[e] / N, n = own[e] % N;
+      a.dap[((long)sb.seq * a.D + c) * (N + 2) + n] = v;
+      if (a.dh0) a.dh0[(long)sb.seq * a.D * N + own[e]] = Gc[e];
     }
+  }
+  const int ch = threadIdx.x % CW, which = threadIdx.x / CW;
+  if (which < 2 && sb.c0 + ch < sb.cend) {
+    float v = 0.f;
+    for (int m = 0; m < W; ++m)
+      for (int e = 0; e < min(LN, L); ++e)
+        v += red[m * 3 * NE + (which * CPL + ch % CPL) * 64 + e * CG + ch / CPL];
+    a.dap[((long)sb.seq * a.D + sb.c0 + ch) * (N + 2) + N + which] = v;
   }
 }
 
@@ -736,35 +757,44 @@ __global__ __launch_bounds__(256) void k_select_step(SelectArgs a) {
   }
 }
 
-// Whether every row piece of C channels may be loaded at once.
-static bool rows_vec(const SelectArgs& a, int C, bool bwd) {
-  const long eb = a.bf16 ? 2 : 4, m = C * eb;
-  auto ok = [&](const void* p, long row) { return !p || ((uintptr_t)p % m == 0 && row % C == 0); };
-  bool v = (a.D / a.G) % C == 0 && ok(a.u, a.u_row) && ok(a.delta, a.delta_row) && ok(a.z, a.z_row);
-  if (!bwd) return v && ok(a.y, a.D);
-  return v && ok(a.dy, a.D) && ok(a.du, a.D) && ok(a.ddelta, a.D) && ok(a.dz, a.D);
+// Whether every piece of C channels, and of nb states of a B or C row, may be
+// loaded and stored at once.
+static bool rows_vec(const SelectArgs& a, int C, int nb, bool bwd) {
+  const long eb = a.bf16 ? 2 : 4;
+  auto ok = [&](const void* p, long row, long n) { return !p || ((uintptr_t)p % (n * eb) == 0 && row % n == 0); };
+  const bool v = (a.D / a.G) % C == 0 && ok(a.u, a.u_row, C) && ok(a.delta, a.delta_row, C) &&
+                 ok(a.z, a.z_row, C) && ok(a.Bm, a.b_row, nb) && ok(a.Cm, a.c_row, nb);
+  if (!bwd) return v && ok(a.y, a.D, C);
+  return v && ok(a.dy, a.D, C) && ok(a.du, a.D, C) && ok(a.ddelta, a.D, C) && ok(a.dz, a.D, C);
 }
 
 template <typename Tin, int N>
 static hipError_t run_fwd(const SelectArgs& a) {
-  constexpr int CPL = 4, L = 8, W = 8, CW = SelTile<N, CPL>::CW;
+  constexpr int CPL = 2, L = 8, W = 8, CW = SelTile<N, CPL>::CW;
   const int Dg = a.D / a.G;
   const long grid = (long)a.S * a.G * ((Dg + CW - 1) / CW);
   if (grid > INT32_MAX) return hipErrorInvalidValue;
-  if (rows_vec(a, CPL, false))
-    k_select_fwd<Tin, N, CPL, L, W, true><<<(unsigned)grid, 64 * W, 0, a.stream>>>(a);
-  else
-    k_select_fwd<Tin, N, CPL, L, W, false><<<(unsigned)grid, 64 * W, 0, a.stream>>>(a);
+  const bool vec = rows_vec(a, CPL, L * N / 64, false);
+  const dim3 g((unsigned)grid), b(64 * W);
+  if (vec && a.z) k_select_fwd<Tin, N, CPL, L, W, true, true><<<g, b, 0, a.stream>>>(a);
+  else if (vec) k_select_fwd<Tin, N, CPL, L, W, true, false><<<g, b, 0, a.stream>>>(a);
+  else if (a.z) k_select_fwd<Tin, N, CPL, L, W, false, true><<<g, b, 0, a.stream>>>(a);
+  else k_select_fwd<Tin, N, CPL, L, W, false, false><<<g, b, 0, a.stream>>>(a);
   return hipGetLastError();
 }
 
 template <typename Tin, int N>
 static hipError_t run_bwd(const SelectArgs& a) {
+  constexpr int CPL = select_block_channels(N) * N / 256;
   const long grid = (long)a.S * a.G * a.nblk;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   if (grid > 0) {
-    if (rows_vec(a, select_block_channels(N) * N / 256, true)) k_select_bwd<Tin, N, true><<<(unsigned)grid, 512, 0, a.stream>>>(a);
-    else k_select_bwd<Tin, N, false><<<(unsigned)grid, 512, 0, a.stream>>>(a);
+    const bool vec = rows_vec(a, CPL, N >= 16 ? N / 16 : 1, true);
+    const dim3 g((unsigned)grid), b(512);
+    if (vec && a.z) k_select_bwd<Tin, N, CPL, true, true><<<g, b, 0, a.stream>>>(a);
+    else if (vec) k_select_bwd<Tin, N, CPL, true, false><<<g, b, 0, a.stream>>>(a);
+    else if (a.z) k_select_bwd<Tin, N, CPL, false, true><<<g, b, 0, a.stream>>>(a);
+    else k_select_bwd<Tin, N, CPL, false, false><<<g, b, 0, a.stream>>>(a);
   }
   const long nbc = (long)a.Ttot * a.G * 2 * N, np = (long)a.D * (N + 2);
   if (nbc > 0) k_select_dbc<Tin><<<(unsigned)((nbc + 255) / 256), 256, 0, a.stream>>>(a);
