@@ -13,17 +13,27 @@ __device__ __forceinline__ uint32_t bf16_bits(float x) {
   return __builtin_bit_cast(uint16_t, (__bf16)x);
 }
 __device__ __forceinline__ void store_elem(bf16_t* p, float x) { *p = (bf16_t)bf16_bits(x); }
-
-// A byte offset past every buffer below, and a raw buffer over `rows` rows from
-// row0 on.  Loads past it give zeros and stores past it are dropped, so tails of
-// tokens and channels need no branch and no second address.  (The record count is
-// clipped below BUF_OOB: callers keep the offsets they use below it.)
-constexpr unsigned BUF_OOB = 0x80000000u;
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const void* p, long row0, long row_bytes, long rows) {
-  const long n = rows * row_bytes;
-  return clip_rsrc(const_cast<char*>(static_cast<const char*>(p)) + row0 * row_bytes,
-                   n < (long)BUF_OOB ? (unsigned)n : BUF_OOB - 1);
+// Two at once (one v_cvt_pk_bf16_f32), the first in the low half.
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
 }
+
+// A byte offset past every buffer below, and raw buffers over a few rows of a
+// tensor.  Loads past a buffer give zeros and stores past it are dropped, so tails
+// of tokens and channels need no branch and no second address.
+constexpr unsigned BUF_OOB = 0x80000000u;
+struct RowsAt {  // walks a tensor's rows in steps
+  const char* p;
+  unsigned rb;  // bytes between rows; a step's rows span less than BUF_OOB
+  __device__ __forceinline__ RowsAt(const void* t, long row0, long row_bytes)
+      : p(static_cast<const char*>(t) + row0 * row_bytes), rb((unsigned)row_bytes) {}
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows(int n) const {
+    return clip_rsrc(const_cast<char*>(p), (unsigned)n * rb);
+  }
+  __device__ __forceinline__ void step(int n) { p += (long)n * (int)rb; }
+};
 
 // C consecutive channels as loaded.  VEC: one load of C * sizeof(T) bytes (the
 // address is a multiple of that); else element by element, of which nv >= 1
@@ -135,7 +145,7 @@ __device__ __forceinline__ void store_piece(T* p, const float (&v)[C], int nv) {
     } else {
       uint32_t u[C / 2];
 #pragma unroll
-      for (int i = 0; i < C / 2; ++i) u[i] = bf16_bits(v[2 * i]) | (bf16_bits(v[2 * i + 1]) << 16);
+      for (int i = 0; i < C / 2; ++i) u[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
       if constexpr (C == 2) {
         *reinterpret_cast<uint32_t*>(p) = u[0];
       } else if constexpr (C == 4) {
@@ -168,7 +178,7 @@ __device__ __forceinline__ void store_piece(__amdgpu_buffer_rsrc_t rs, unsigned 
     for (int i = 0; i < NW; ++i) {
       if constexpr (is_f32<T>::value) u[i] = __float_as_uint(v[i]);
       else if constexpr (C == 1) u[i] = bf16_bits(v[0]);
-      else u[i] = bf16_bits(v[2 * i]) | (bf16_bits(v[2 * i + 1]) << 16);
+      else u[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
     }
     if constexpr (C * sizeof(T) == 2) {
       __builtin_amdgcn_raw_buffer_store_b16((uint16_t)u[0], rs, off, 0, 0);

@@ -146,23 +146,28 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
   const unsigned co = (w * L + bt) * (unsigned)(a.c_row * EB) + (sb.g * N + bs) * EB;
   Piece<Tin, CPL, VEC> pu[TL], pd[TL], pz[TL];
   Piece<Tin, NB, VEC> pb, pc;
+  RowsAt tu(a.u, sb.tok0, ub), td(a.delta, sb.tok0, db), tz(a.z, sb.tok0, zb), ty(a.y, sb.tok0, yb);
+  RowsAt tb(a.Bm, sb.tok0, a.b_row * EB), tc(a.Cm, sb.tok0, a.c_row * EB);
   auto load = [&](int base) {
-    const long row = sb.tok0 + base;
-    const int rows = len - base;
-    const auto ru = rows_rsrc(a.u, row, ub, rows), rd = rows_rsrc(a.delta, row, db, rows);
-    const auto rb = rows_rsrc(a.Bm, row, a.b_row * EB, rows), rc = rows_rsrc(a.Cm, row, a.c_row * EB, rows);
+    const int rows = min(len - base, TILE);
+    const auto ru = tu.rows(rows), rd = td.rows(rows), rb = tb.rows(rows), rc = tc.rows(rows);
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
       pu[k].load(ru, uo + k * LN * ub, nv);
       pd[k].load(rd, dof + k * LN * db, nv);
     }
     if constexpr (Z) {
-      const auto rz = rows_rsrc(a.z, row, zb, rows);
+      const auto rz = tz.rows(rows);
 #pragma unroll
       for (int k = 0; k < TL; ++k) pz[k].load(rz, zo + k * LN * zb, nv);
     }
     pb.load(rb, bo, NB);
     pc.load(rc, co, NB);
+    tu.step(TILE);
+    td.step(TILE);
+    if constexpr (Z) tz.step(TILE);
+    tb.step(TILE);
+    tc.step(TILE);
   };
   if (len > 0) load(0);
   for (int base = 0; base < len; base += TILE) {
@@ -229,6 +234,7 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
           h[i][j] = t == 0 ? xu[i] * Bv[j] : fmaf(dec[t][i][j], h[i][j], xu[i] * Bv[j]);
           s = j == 0 ? Cv[0] * h[i][0] : fmaf(Cv[j], h[i][j], s);
         }
+        asm("" : "+v"(s));  // formed here: deferred, every token's states would stay in registers
         yp[t * CPL + i] = s;
       }
     }
@@ -282,7 +288,8 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
     }
     // sums over the lane groups, LN tokens at a time: lane group ng ends with
     // token ng's, whose u and z it holds
-    const auto ry = rows_rsrc(a.y, sb.tok0 + base, yb, len - base);
+    const auto ry = ty.rows(min(len - base, TILE));
+    ty.step(TILE);
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
       float* yk = yp + k * LN * CPL;
@@ -359,12 +366,12 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
   // owned states: the decayed gradient that enters the tile from the tokens
   // after it, and the kept state at the tile's start
   float Gc[EPT], hk[EPT];
-  long own[EPT];  // place in a [D, N] state, negative: none
+  int own[EPT];  // place in a [D, N] state, negative: none
 #pragma unroll
   for (int e = 0; e < EPT; ++e) {
     int ch, n;
     sel_slot<N, CPL>(threadIdx.x + e * 64 * W, ch, n);
-    own[e] = sb.c0 + ch < sb.cend ? (long)(sb.c0 + ch) * N + n : -1;
+    own[e] = sb.c0 + ch < sb.cend ? (sb.c0 + ch) * N + n : -1;
     Gc[e] = a.dht && own[e] >= 0 ? a.dht[(long)sb.seq * a.D * N + own[e]] : 0.f;
   }
 
@@ -378,12 +385,16 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
   const unsigned co = bok ? (w * L + bt) * (unsigned)(a.c_row * EB) + (sb.g * N + bs) * EB : BUF_OOB;
   Piece<Tin, CPL, VEC> pu[TL], pd[TL], pz[TL], py[TL];
   Piece<Tin, NB, VEC> pb, pc;
+  const long last = sb.tok0 + (long)max(ntiles - 1, 0) * TILE;  // the walk's first tile
+  RowsAt tu(a.u, last, ub), td(a.delta, last, db), tz(a.z, last, zb), ty(a.dy, last, yb);
+  RowsAt tb(a.Bm, last, a.b_row * EB), tc(a.Cm, last, a.c_row * EB);
+  RowsAt tdu(a.du, last, yb), tdd(a.ddelta, last, yb), tdz(a.dz, last, yb);
+  RowsAt tbc(a.bcp, (long)sb.blk * a.Ttot + last, 2 * N * 4);
+  const float* ck = a.ck + (long)(sb.tok0 / SELECT_CK + sb.seq + max(ntiles - 1, 0)) * a.D * N;
   auto load = [&](int tile) {
-    const long row = sb.tok0 + tile * TILE;
-    const int rows = len - tile * TILE;
-    const auto ru = rows_rsrc(a.u, row, ub, rows), rd = rows_rsrc(a.delta, row, db, rows);
-    const auto rb = rows_rsrc(a.Bm, row, a.b_row * EB, rows), rc = rows_rsrc(a.Cm, row, a.c_row * EB, rows);
-    const auto ry = rows_rsrc(a.dy, row, yb, rows);
+    const int rows = min(len - tile * TILE, TILE);
+    const auto ru = tu.rows(rows), rd = td.rows(rows), rb = tb.rows(rows), rc = tc.rows(rows);
+    const auto ry = ty.rows(rows);
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
       pu[k].load(ru, uo + k * LN * ub, nv);
@@ -391,15 +402,21 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
       py[k].load(ry, yo + k * LN * yb, nv);
     }
     if constexpr (Z) {
-      const auto rz = rows_rsrc(a.z, row, zb, rows);
+      const auto rz = tz.rows(rows);
 #pragma unroll
       for (int k = 0; k < TL; ++k) pz[k].load(rz, zo + k * LN * zb, nv);
     }
     pb.load(rb, bo, NB);
     pc.load(rc, co, NB);
-    const float* ck = a.ck + (long)(sb.tok0 / SELECT_CK + sb.seq + tile) * a.D * N;
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) hk[e] = ck[max(own[e], (long)sb.c0 * N)];
+    for (int e = 0; e < EPT; ++e) hk[e] = ck[max(own[e], sb.c0 * N)];
+    tu.step(-TILE);
+    td.step(-TILE);
+    if constexpr (Z) tz.step(-TILE);
+    ty.step(-TILE);
+    tb.step(-TILE);
+    tc.step(-TILE);
+    ck -= (long)a.D * N;
   };
   if (ntiles > 0) load(ntiles - 1);
   for (int tile = ntiles - 1; tile >= 0; --tile) {
@@ -563,7 +580,8 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
       }
     }
     // second pass: the gradients
-    const auto rbc = rows_rsrc(a.bcp, (long)sb.blk * a.Ttot + sb.tok0 + base, 2 * N * 4, len - base);
+    const int rows = min(len - base, TILE);
+    const auto rbc = tbc.rows(rows);
 #pragma unroll
     for (int t2 = L - 2; t2 >= 0; t2 -= 2) {
       float bc[16];
@@ -612,9 +630,11 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
     }
     __builtin_amdgcn_wave_barrier();
     // the own tokens' gradients
-    const auto rdu = rows_rsrc(a.du, sb.tok0 + base, yb, len - base);
-    const auto rdd = rows_rsrc(a.ddelta, sb.tok0 + base, yb, len - base);
-    const auto rdz = rows_rsrc(a.dz, sb.tok0 + base, yb, Z ? len - base : 0);
+    const auto rdu = tdu.rows(rows), rdd = tdd.rows(rows), rdz = tdz.rows(Z ? rows : 0);
+    tbc.step(-TILE);
+    tdu.step(-TILE);
+    tdd.step(-TILE);
+    if constexpr (Z) tdz.step(-TILE);
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
       const int tl = min(ng + LN * k, L - 1);
