@@ -88,10 +88,63 @@ size_t conv_ws_bytes(const comba::ConvArgs& a) {
 
 // ---- selective scan -----------------------------------------------------------
 struct SelectLayout {
-  size_t ck, bcp, dap, total;
+  size_t ck, bcp, dap, segF, segdt, total;
 };
 
-SelectLayout select_layout(const comba::SelectArgs& a, bool save) {
+constexpr int kTile = 64;  // a segment's length is a multiple of it
+
+// Cuts rows into segments when their workgroups, one per CU, leave CUs idle or
+// wait for a long row: the main kernel then runs over segments side by side,
+// after a first pass over all but one segment of each row that is cut (`pre` of
+// the main kernel's time per token).  Packed rows of up to a CU's share of all
+// tokens stay whole.  Takes the number with the least time, counted in tokens
+// walked one after the other (`launch`: the first pass's launch and the
+// segments' starts).  Measured, whole rows / segments, us: 16 states, one row of
+// 8,192 tokens, 2,048 channels: forward 387 / 167, backward 1,022 / 361; 1,000
+// tokens: forward 54 / 31; 4 rows of 4,096, which fill the CUs: 219 whole, 297 to
+// 321 cut.
+void select_segments(comba::SelectArgs* a, bool bwd) {
+  a->segs = 1;
+  a->seglen = a->segmin = 1 << 30;
+  if (a->longest < 2 * kTile || a->S == 0) return;  // short, or not known
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess ||
+      hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
+    return;
+  const double pre = bwd ? 0.25 : 0.6, launch = bwd ? 64 : 128;
+  const double blocks = (double)a->G * a->nblk, share = (double)a->Ttot * blocks / cus;
+  auto rounds = [&](double rows) { return (double)(((int64_t)(rows * blocks) + cus - 1) / cus); };
+  const double longest = (double)a->longest;
+  if (a->cu_host && longest <= share) return;
+  double best = a->cu_host ? longest : rounds(a->S) * longest;
+  for (int p = 2; p <= 32; p *= 2) {
+    const int64_t len = (a->longest + (int64_t)p * kTile - 1) / ((int64_t)p * kTile) * kTile;
+    if (len * (p - 1) >= a->longest) break;
+    double t = launch;
+    if (!a->cu_host) {
+      t += (rounds((double)a->S * p) + pre * rounds((double)a->S * (p - 1))) * (double)len;
+    } else {
+      int64_t first = 0;  // tokens of the first pass
+      for (int i = 0; i < a->S; ++i) {
+        const int64_t n = a->cu_host[i + 1] - a->cu_host[i];
+        if ((double)n > share) first += (n - 1) / len * len;
+      }
+      const double f = (double)first * blocks / cus;
+      t += ((double)len > share ? (double)len : share) + pre * ((double)len > f ? (double)len : f);
+    }
+    if (t < best && (int64_t)a->S * p * a->G * a->nblk <= INT32_MAX) {
+      best = t;
+      a->segs = p;
+      a->seglen = (int)len;
+      a->segmin = a->cu_host ? (int)share : 0;
+    }
+  }
+}
+
+// Workspace of a forward, or (save) of a saving forward and its backward, whose
+// segments are chosen apart.
+SelectLayout select_layout(const comba::SelectArgs& a0, bool save) {
+  comba::SelectArgs a = a0;
   SelectLayout L{};
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -99,13 +152,20 @@ SelectLayout select_layout(const comba::SelectArgs& a, bool save) {
     off += round_up(bytes);
     return at;
   };
+  select_segments(&a, false);
+  size_t segs = a.segs;
   if (save) {
+    select_segments(&a, true);
     // states: a sequence's start at tok0 / SELECT_CK + its number, which leaves
     // room for a partial interval per sequence
     L.ck = take(((size_t)a.Ttot / comba::SELECT_CK + a.S + 1) * a.D * a.N * sizeof(float));
     L.bcp = take((size_t)a.G * a.nblk * a.Ttot * 2 * a.N * sizeof(float));
-    L.dap = take((size_t)a.S * a.D * (a.N + 2) * sizeof(float));
+    L.dap = take((size_t)a.S * a.segs * a.D * (a.N + 2) * sizeof(float));
+    if ((size_t)a.segs > segs) segs = a.segs;
   }
+  const size_t rows = segs > 1 ? (size_t)a.S * segs * a.D : 0;
+  L.segF = take(rows * a.N * sizeof(float));
+  L.segdt = take(rows * sizeof(float));
   L.total = off + kAlign;
   return L;
 }
@@ -128,6 +188,7 @@ comba_status select_args(const comba_select_shape* s, comba::SelectArgs* a) {
   a->Tseq = r.Tseq;
   a->Ttot = r.Ttot;
   a->longest = r.longest;
+  a->cu_host = s->cu_seqlens ? s->cu_seqlens_host : nullptr;
   a->cu_seqlens = s->cu_seqlens;
   const int bc = comba::select_block_channels(s->N);
   a->nblk = (s->D / s->G + bc - 1) / bc;
@@ -175,7 +236,11 @@ comba_status select_fwd(bool save, const comba_select_shape* shape, const void* 
   if (ws_bytes < L.total) return COMBA_ERR_WORKSPACE;
   a.y = y;
   a.ht = ht;
-  if (save) a.ck = reinterpret_cast<float*>(static_cast<char*>(ws) + L.ck);
+  char* base = static_cast<char*>(ws);
+  if (save) a.ck = reinterpret_cast<float*>(base + L.ck);
+  select_segments(&a, false);
+  a.segF = reinterpret_cast<float*>(base + L.segF);
+  a.segdt = reinterpret_cast<float*>(base + L.segdt);
   a.stream = static_cast<hipStream_t>(stream);
   return done(comba::launch_select_fwd(a));
 }
@@ -353,6 +418,9 @@ comba_status comba_select_bwd(const comba_select_shape* shape, const void* u, co
   a.ck = reinterpret_cast<float*>(base + L.ck);
   a.bcp = reinterpret_cast<float*>(base + L.bcp);
   a.dap = reinterpret_cast<float*>(base + L.dap);
+  select_segments(&a, true);
+  a.segF = reinterpret_cast<float*>(base + L.segF);
+  a.segdt = reinterpret_cast<float*>(base + L.segdt);
   a.dy = dy;
   a.dht = dht;
   a.du = du;

@@ -44,6 +44,7 @@ struct SelectArgs {
   bool bf16, softplus, vec;  // vec: whole groups of channels in one load (set by the launchers)
   int D, N, G, S, Tseq, Ttot;  // S sequences
   const int32_t* cu_seqlens;
+  const int32_t* cu_host;  // the host's copy, or NULL (host code only)
   long longest;  // tokens of the longest sequence (packed without host offsets: 0)
   long u_row, delta_row, z_row, b_row, c_row;
   const void *u, *delta, *Bm, *Cm, *z;
@@ -61,8 +62,13 @@ struct SelectArgs {
   void *du, *ddelta, *dz, *dB, *dC;
   float *dA, *dD, *dbias, *dh0;
   int nblk;      // channel blocks per group
+  // rows of more than `segmin` tokens cut into up to `segs` segments of `seglen`
+  // tokens: each segment's end from zero and the sum of its steps
+  int segs, seglen, segmin;
+  float* segF;   // [sequence][segment][D][N]
+  float* segdt;  // [sequence][segment][D]
   float* bcp;    // [channel block][token][2 N] partial dB, dC of one block's channels
-  float* dap;    // [sequence][D][N + 2] partial dA, dD, dbias
+  float* dap;    // [sequence][segment][D][N + 2] partial dA, dD, dbias
   hipStream_t stream;
 };
 // Channels of one workgroup of the backward, and its blocks per group.

@@ -63,13 +63,15 @@ __device__ __forceinline__ void lds_put(float* p, const float (&v)[C]) {
   }
 }
 
-// What a workgroup works on: a sequence and a block of CW channels of one
-// group.  Two neighbouring blocks, which share the 128-byte lines of their
+// What a workgroup works on: a segment of a sequence and a block of CW channels
+// of one group.  Two neighbouring blocks, which share the 128-byte lines of their
 // rows, go to workgroups eight apart and so to the same XCD.
 struct SelBlock {
-  int seq, blk, g;     // sequence, block (of all groups), group
-  int c0, cend;        // channels [c0, cend)
-  int tok0, len;       // the sequence's tokens
+  int seq, seg, blk, g;  // sequence, its segment, channel block (of all groups), group
+  int c0, cend;          // channels [c0, cend)
+  int tok0, len;         // the sequence's tokens
+  int t0, t1;            // the segment's tokens, counted in the sequence
+  int nseg;              // the sequence's segments (at least one)
 };
 template <int CW>
 __device__ __forceinline__ SelBlock sel_block(const SelectArgs& a) {
@@ -77,14 +79,20 @@ __device__ __forceinline__ SelBlock sel_block(const SelectArgs& a) {
   int b = blockIdx.x;
   if ((b | 15) < (int)gridDim.x) b = (b & ~15) | ((b & 7) << 1) | ((b >> 3) & 1);
   SelBlock s;
-  s.seq = b / nb;
-  s.blk = b - s.seq * nb;
+  const int r = b / nb;
+  s.blk = b - r * nb;
+  s.seq = r / a.segs;
+  s.seg = r - s.seq * a.segs;
   s.g = s.blk / nblk;
   s.c0 = s.g * Dg + (s.blk - s.g * nblk) * CW;
   s.cend = min(s.c0 + CW, (s.g + 1) * Dg);
   int t1;
   seq_range(a.cu_seqlens, s.seq, a.Tseq, a.Ttot, s.tok0, t1);
   s.len = t1 - s.tok0;
+  const bool cut = s.len > a.segmin;
+  s.nseg = cut ? min((s.len + a.seglen - 1) / a.seglen, a.segs) : 1;
+  s.t0 = cut ? min(s.len, s.seg * a.seglen) : (s.seg > 0 ? s.len : 0);
+  s.t1 = cut ? min(s.len, s.t0 + a.seglen) : s.len;
   return s;
 }
 
@@ -96,6 +104,196 @@ __device__ __forceinline__ void sel_slot(int slot, int& ch, int& n) {
   const int i = slot / 256, l = (slot >> 2) & 63, j = slot & 3;
   ch = (l % S::CG) * CPL + i;
   n = (l / S::CG) * 4 + j;
+}
+
+// A segment's end from a zero start, for rows cut into segments: its final state
+// (REV: the decayed gradient of the state that enters it) and, per channel, the
+// sum of its steps, whose exponential is the segment's decay product.
+template <typename Tin, int N, int CPL, bool VEC, bool REV>
+__global__ __launch_bounds__(512) void k_select_seg(SelectArgs a) {
+  constexpr int L = 8, W = 8;
+  using S = SelTile<N, CPL>;
+  constexpr int LN = S::LN, CG = S::CG, CW = S::CW, NE = S::NE, TL = L / LN, TILE = L * W;
+  constexpr int NB = L * N / 64, EPT = NE / (64 * W);
+  constexpr unsigned EB = sizeof(Tin);
+  static_assert(L % LN == 0 && N % NB == 0 && NE % (64 * W) == 0, "tile");
+  struct WaveLds {
+    float dt[L][CW], x[L][CW], R[L][N];  // x R: dt u B, or gy C
+  };
+  __shared__ __align__(16) WaveLds lds[W];
+  __shared__ __align__(16) float ex[W][2][NE];
+
+  const SelBlock sb = sel_block<CW>(a);
+  // the last segment's end is nobody's start (REV: the first one's)
+  if (sb.t0 >= sb.t1 || sb.seg == (REV ? 0 : sb.nseg - 1)) return;
+  const int lane = lane_id(), w = wave_id_s(), ng = lane / CG, cg = lane % CG;
+  const int cl = sb.c0 + cg * CPL, nv = max(0, min(CPL, sb.cend - cl));
+  WaveLds& my = lds[w];
+  const bool gate = REV && a.z;
+
+  float A2[CPL][4], bias[CPL], total[CPL];
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    const int c = i < nv ? cl + i : sb.c0;
+    bias[i] = a.bias ? a.bias[c] : 0.f;
+    total[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) A2[i][j] = i < nv ? a.A[(long)c * N + ng * 4 + j] * LOG2E : 0.f;
+  }
+  float H[EPT];
+#pragma unroll
+  for (int e = 0; e < EPT; ++e) H[e] = 0.f;
+
+  const unsigned tok = w * L + ng, cb = nv > 0 ? (unsigned)cl * EB : BUF_OOB;
+  const long xrow = REV ? a.D : a.u_row, rrow = REV ? a.c_row : a.b_row;
+  const unsigned xb = xrow * EB, db = a.delta_row * EB, zb = a.z_row * EB;
+  const unsigned xo = tok * xb + cb, dof = tok * db + cb, zo = tok * zb + cb;
+  const int bt = lane * NB / N, bs = lane * NB % N;
+  const unsigned ro = (w * L + bt) * (unsigned)(rrow * EB) + (sb.g * N + bs) * EB;
+  const int tiles = (sb.t1 - sb.t0 + TILE - 1) / TILE, dir = REV ? -TILE : TILE;
+  const long row0 = sb.tok0 + sb.t0 + (REV ? (long)(tiles - 1) * TILE : 0);
+  RowsAt tx(REV ? a.dy : a.u, row0, xb), td(a.delta, row0, db), tz(a.z, row0, zb);
+  RowsAt tr(REV ? a.Cm : a.Bm, row0, rrow * EB);
+  Piece<Tin, CPL, VEC> px[TL], pd[TL], pz[TL];
+  Piece<Tin, NB, VEC> pr;
+  auto load = [&](int tile) {  // in the order of the walk
+    const int rows = min(sb.t1 - sb.t0 - (REV ? tiles - 1 - tile : tile) * TILE, TILE);
+    const auto rx = tx.rows(rows), rd = td.rows(rows), rr = tr.rows(rows);
+#pragma unroll
+    for (int k = 0; k < TL; ++k) {
+      px[k].load(rx, xo + k * LN * xb, nv);
+      pd[k].load(rd, dof + k * LN * db, nv);
+    }
+    if (gate) {
+      const auto rz = tz.rows(rows);
+#pragma unroll
+      for (int k = 0; k < TL; ++k) pz[k].load(rz, zo + k * LN * zb, nv);
+    }
+    pr.load(rr, ro, NB);
+    tx.step(dir);
+    td.step(dir);
+    if (gate) tz.step(dir);
+    tr.step(dir);
+  };
+  load(0);
+  for (int tile = 0; tile < tiles; ++tile) {
+    const int t0 = sb.t0 + (REV ? tiles - 1 - tile : tile) * TILE + w * L;
+#pragma unroll
+    for (int k = 0; k < TL; ++k) {
+      const int tl = ng + LN * k;
+      const bool ok = t0 + tl < sb.t1;
+      float dt[CPL], x[CPL];
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) {
+        dt[i] = pd[k].get(i) + bias[i];
+        x[i] = px[k].get(i);
+      }
+      if (a.softplus) {
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) dt[i] = softplus_acc(dt[i]);
+      }
+      if (gate) {
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+          const float zv = pz[k].get(i);
+          x[i] *= zv * sigmoid_acc(zv);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) {
+        dt[i] = ok ? dt[i] : 0.f;
+        if constexpr (!REV) x[i] *= dt[i];
+        total[i] += dt[i];
+      }
+      lds_put<CPL>(&my.dt[tl][cg * CPL], dt);
+      lds_put<CPL>(&my.x[tl][cg * CPL], x);
+    }
+    {
+      float v[NB];
+#pragma unroll
+      for (int e = 0; e < NB; ++e) v[e] = pr.get(e);
+      lds_put<NB>(&my.R[bt][bs], v);
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (tile + 1 < tiles) load(tile + 1);
+    float h[CPL][4], sdt[CPL];
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      sdt[i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) h[i][j] = 0.f;
+    }
+#pragma unroll
+    for (int tt = 0; tt < L; ++tt) {
+      const int t = REV ? L - 1 - tt : tt;
+      float dt[CPL], x[CPL], Rv[4];
+      lds_get<CPL>(&my.dt[t][cg * CPL], dt);
+      lds_get<CPL>(&my.x[t][cg * CPL], x);
+      lds_get<4>(&my.R[t][ng * 4], Rv);
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) {
+        sdt[i] += dt[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float d = __builtin_amdgcn_exp2f(dt[i] * A2[i][j]);
+          if constexpr (REV) h[i][j] = d * fmaf(x[i], Rv[j], h[i][j]);
+          else h[i][j] = fmaf(d, h[i][j], x[i] * Rv[j]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      float p[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(sdt[i] * A2[i][j]);
+      lds_put<4>(&ex[w][0][(i * 64 + lane) * 4], p);
+      lds_put<4>(&ex[w][1][(i * 64 + lane) * 4], h[i]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      const int s = threadIdx.x + e * 64 * W;
+#pragma unroll
+      for (int mm = 0; mm < W; ++mm) {
+        const int m = REV ? W - 1 - mm : mm;
+        H[e] = fmaf(ex[m][0][s], H[e], ex[m][1][s]);
+      }
+    }
+    __syncthreads();
+  }
+  const long at = (long)(sb.seq * a.segs + sb.seg) * a.D;
+#pragma unroll
+  for (int e = 0; e < EPT; ++e) {
+    int ch, n;
+    sel_slot<N, CPL>(threadIdx.x + e * 64 * W, ch, n);
+    if (sb.c0 + ch < sb.cend) a.segF[(at + sb.c0 + ch) * N + n] = H[e];
+  }
+  // the steps' sum: over the lane groups and waves, which held different tokens
+  float* red = &ex[0][0][0];
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) red[(w * CPL + i) * 64 + lane] = total[i];
+  __syncthreads();
+  const int ch = threadIdx.x;
+  if (ch < CW && sb.c0 + ch < sb.cend) {
+    float v = 0.f;
+    for (int m = 0; m < W; ++m)
+      for (int e = 0; e < LN; ++e) v += red[(m * CPL + ch % CPL) * 64 + e * CG + ch / CPL];
+    a.segdt[at + sb.c0 + ch] = v;
+  }
+}
+
+// The state (REV: its gradient) that enters a segment: the sequence's, through
+// the segments before (after) it.
+template <int N, bool REV>
+__device__ __forceinline__ float seg_enter(const SelectArgs& a, const SelBlock& sb, int c, int n, float h) {
+  const float A2 = a.A[(long)c * N + n] * LOG2E;
+  const int m = REV ? sb.nseg - 1 - sb.seg : sb.seg;
+#pragma unroll 4
+  for (int k = 0; k < m; ++k) {
+    const long at = (long)(sb.seq * a.segs + (REV ? sb.nseg - 1 - k : k)) * a.D + c;
+    h = fmaf(__builtin_amdgcn_exp2f(A2 * a.segdt[at]), h, a.segF[at * N + n]);
+  }
+  return h;
 }
 
 template <typename Tin, int N, int CPL, int L, int W, bool VEC, bool Z>
@@ -117,7 +315,8 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
   const SelBlock sb = sel_block<CW>(a);
   const int lane = lane_id(), w = wave_id_s(), ng = lane / CG, cg = lane % CG;
   const int cl = sb.c0 + cg * CPL, nv = max(0, min(CPL, sb.cend - cl));  // the lane's channels
-  const int len = sb.len;
+  const int len = sb.t1;  // the segment's end
+  if (sb.seg > 0 && sb.t0 >= len) return;
   WaveLds& my = lds[w];
 
   float A2[CPL][4], h[CPL][4], bias[CPL], skip[CPL];
@@ -134,7 +333,9 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
   for (int e = 0; e < EPT; ++e) {
     int ch, n;
     sel_slot<N, CPL>(threadIdx.x + e * 64 * W, ch, n);
-    H[e] = a.h0 && sb.c0 + ch < sb.cend ? a.h0[((long)sb.seq * a.D + sb.c0 + ch) * N + n] : 0.f;
+    const bool on = sb.c0 + ch < sb.cend;
+    H[e] = a.h0 && on ? a.h0[((long)sb.seq * a.D + sb.c0 + ch) * N + n] : 0.f;
+    if (sb.seg > 0 && on) H[e] = seg_enter<N, false>(a, sb, sb.c0 + ch, n, H[e]);
   }
 
   // byte offsets of the lane's pieces in a tile's rows
@@ -146,8 +347,9 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
   const unsigned co = (w * L + bt) * (unsigned)(a.c_row * EB) + (sb.g * N + bs) * EB;
   Piece<Tin, CPL, VEC> pu[TL], pd[TL], pz[TL];
   Piece<Tin, NB, VEC> pb, pc;
-  RowsAt tu(a.u, sb.tok0, ub), td(a.delta, sb.tok0, db), tz(a.z, sb.tok0, zb), ty(a.y, sb.tok0, yb);
-  RowsAt tb(a.Bm, sb.tok0, a.b_row * EB), tc(a.Cm, sb.tok0, a.c_row * EB);
+  const long row0 = sb.tok0 + sb.t0;
+  RowsAt tu(a.u, row0, ub), td(a.delta, row0, db), tz(a.z, row0, zb), ty(a.y, row0, yb);
+  RowsAt tb(a.Bm, row0, a.b_row * EB), tc(a.Cm, row0, a.c_row * EB);
   auto load = [&](int base) {
     const int rows = min(len - base, TILE);
     const auto ru = tu.rows(rows), rd = td.rows(rows), rb = tb.rows(rows), rc = tc.rows(rows);
@@ -169,8 +371,8 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
     tb.step(TILE);
     tc.step(TILE);
   };
-  if (len > 0) load(0);
-  for (int base = 0; base < len; base += TILE) {
+  if (sb.t0 < len) load(sb.t0);
+  for (int base = sb.t0; base < len; base += TILE) {
     const int t0 = base + w * L;
     // stage the chunk: dt and dt u per (token, channel), B and C in fp32; past
     // the end dt = 0 and zeros as loaded leave the state as it is
@@ -306,7 +508,7 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
       store_piece<Tin, CPL, VEC>(ry, yo + k * LN * yb, y, nv);
     }
   }
-  if (a.ht) {
+  if (a.ht && sb.seg == sb.nseg - 1) {
 #pragma unroll
     for (int e = 0; e < EPT; ++e) {
       int ch, n;
@@ -347,7 +549,8 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
   const SelBlock sb = sel_block<CW>(a);
   const int lane = lane_id(), w = wave_id_s(), ng = lane / CG, cg = lane % CG;
   const int cl = sb.c0 + cg * CPL, nv = max(0, min(CPL, sb.cend - cl));
-  const int len = sb.len, ntiles = (len + TILE - 1) / TILE;
+  const int len = sb.t1, tile0 = sb.t0 / TILE;  // the segment's tiles: none past the sequence's end
+  const int ntiles = sb.t0 < len ? (len + TILE - 1) / TILE : tile0;
   WaveLds& my = lds[w];
 
   float A2[CPL][4], dA[CPL][4], bias[CPL], skip[CPL], dD[CPL], dbias[CPL];
@@ -373,6 +576,7 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
     sel_slot<N, CPL>(threadIdx.x + e * 64 * W, ch, n);
     own[e] = sb.c0 + ch < sb.cend ? (sb.c0 + ch) * N + n : -1;
     Gc[e] = a.dht && own[e] >= 0 ? a.dht[(long)sb.seq * a.D * N + own[e]] : 0.f;
+    if (sb.seg < sb.nseg - 1 && own[e] >= 0) Gc[e] = seg_enter<N, true>(a, sb, sb.c0 + ch, n, Gc[e]);
   }
 
   const unsigned tok = w * L + min(ng, L - 1);
@@ -418,8 +622,8 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
     tc.step(-TILE);
     ck -= (long)a.D * N;
   };
-  if (ntiles > 0) load(ntiles - 1);
-  for (int tile = ntiles - 1; tile >= 0; --tile) {
+  if (ntiles > tile0) load(ntiles - 1);
+  for (int tile = ntiles - 1; tile >= tile0; --tile) {
     const int base = tile * TILE, t0 = base + w * L;
     float h[CPL][4], G[CPL][4], hs0[EPT];
 #pragma unroll
@@ -473,7 +677,7 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
 #pragma unroll
     for (int e = 0; e < EPT; ++e) hs0[e] = hk[e];
     __builtin_amdgcn_wave_barrier();
-    if (tile > 0) load(tile - 1);
+    if (tile > tile0) load(tile - 1);
 
     // the chunk from zero, forward then backward
     float dec[L][CPL][4], sdt[CPL];
@@ -683,8 +887,8 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
     for (int m = 1; m < W; ++m) v += ex[m][0][s];
     if (own[e] >= 0) {
       const int c = own[e] / N, n = own[e] % N;
-      a.dap[((long)sb.seq * a.D + c) * (N + 2) + n] = v;
-      if (a.dh0) a.dh0[(long)sb.seq * a.D * N + own[e]] = Gc[e];
+      a.dap[((long)(sb.seq * a.segs + sb.seg) * a.D + c) * (N + 2) + n] = v;
+      if (a.dh0 && sb.seg == 0) a.dh0[(long)sb.seq * a.D * N + own[e]] = Gc[e];
     }
   }
   const int ch = threadIdx.x % CW, which = threadIdx.x / CW;
@@ -693,7 +897,7 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
     for (int m = 0; m < W; ++m)
       for (int e = 0; e < min(LN, L); ++e)
         v += red[m * 3 * NE + (which * CPL + ch % CPL) * 64 + e * CG + ch / CPL];
-    a.dap[((long)sb.seq * a.D + sb.c0 + ch) * (N + 2) + N + which] = v;
+    a.dap[((long)(sb.seq * a.segs + sb.seg) * a.D + sb.c0 + ch) * (N + 2) + N + which] = v;
   }
 }
 
@@ -715,14 +919,14 @@ __global__ __launch_bounds__(256) void k_select_dbc(SelectArgs a) {
   store_elem(out + (t * a.G + g) * a.N + (s < a.N ? s : s - a.N), sum);
 }
 
-// dA, dD and dbias: the sequences' partial sums in order.
+// dA, dD and dbias: the segments' partial sums in order.
 __global__ __launch_bounds__(256) void k_select_dparam(SelectArgs a) {
   const int N2 = a.N + 2;
   const long n = (long)a.D * N2;
   const long e = (long)blockIdx.x * 256 + threadIdx.x;
   if (e >= n) return;
   float sum = 0.f;
-  for (int s = 0; s < a.S; ++s) sum += a.dap[s * n + e];
+  for (int s = 0; s < a.S * a.segs; ++s) sum += a.dap[s * n + e];
   const int k = e % N2;
   const long c = e / N2;
   if (k < a.N) a.dA[c * a.N + k] = sum;
@@ -788,33 +992,40 @@ static bool rows_vec(const SelectArgs& a, int C, int nb, bool bwd) {
   return v && ok(a.dy, a.D, C) && ok(a.du, a.D, C) && ok(a.ddelta, a.D, C) && ok(a.dz, a.D, C);
 }
 
+constexpr int SEL_CPL = 2;  // channels of a lane
+
+template <typename Tin, int N, bool REV>
+static void run_seg(const SelectArgs& a, unsigned grid) {
+  if (a.segs <= 1) return;
+  if (rows_vec(a, SEL_CPL, N / 8, REV)) k_select_seg<Tin, N, SEL_CPL, true, REV><<<grid, 512, 0, a.stream>>>(a);
+  else k_select_seg<Tin, N, SEL_CPL, false, REV><<<grid, 512, 0, a.stream>>>(a);
+}
+
 template <typename Tin, int N>
 static hipError_t run_fwd(const SelectArgs& a) {
-  constexpr int CPL = 2, L = 8, W = 8, CW = SelTile<N, CPL>::CW;
-  const int Dg = a.D / a.G;
-  const long grid = (long)a.S * a.G * ((Dg + CW - 1) / CW);
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  constexpr int CPL = SEL_CPL, L = 8, W = 8;
+  static_assert(SelTile<N, CPL>::CW == select_block_channels(N), "one block of channels throughout");
+  const unsigned grid = (unsigned)a.S * a.segs * a.G * a.nblk;
+  run_seg<Tin, N, false>(a, grid);
   const bool vec = rows_vec(a, CPL, L * N / 64, false);
-  const dim3 g((unsigned)grid), b(64 * W);
-  if (vec && a.z) k_select_fwd<Tin, N, CPL, L, W, true, true><<<g, b, 0, a.stream>>>(a);
-  else if (vec) k_select_fwd<Tin, N, CPL, L, W, true, false><<<g, b, 0, a.stream>>>(a);
-  else if (a.z) k_select_fwd<Tin, N, CPL, L, W, false, true><<<g, b, 0, a.stream>>>(a);
-  else k_select_fwd<Tin, N, CPL, L, W, false, false><<<g, b, 0, a.stream>>>(a);
+  if (vec && a.z) k_select_fwd<Tin, N, CPL, L, W, true, true><<<grid, 64 * W, 0, a.stream>>>(a);
+  else if (vec) k_select_fwd<Tin, N, CPL, L, W, true, false><<<grid, 64 * W, 0, a.stream>>>(a);
+  else if (a.z) k_select_fwd<Tin, N, CPL, L, W, false, true><<<grid, 64 * W, 0, a.stream>>>(a);
+  else k_select_fwd<Tin, N, CPL, L, W, false, false><<<grid, 64 * W, 0, a.stream>>>(a);
   return hipGetLastError();
 }
 
 template <typename Tin, int N>
 static hipError_t run_bwd(const SelectArgs& a) {
-  constexpr int CPL = select_block_channels(N) * N / 256;
-  const long grid = (long)a.S * a.G * a.nblk;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  constexpr int CPL = SEL_CPL;
+  const unsigned grid = (unsigned)a.S * a.segs * a.G * a.nblk;
   if (grid > 0) {
+    run_seg<Tin, N, true>(a, grid);
     const bool vec = rows_vec(a, CPL, N >= 16 ? N / 16 : 1, true);
-    const dim3 g((unsigned)grid), b(512);
-    if (vec && a.z) k_select_bwd<Tin, N, CPL, true, true><<<g, b, 0, a.stream>>>(a);
-    else if (vec) k_select_bwd<Tin, N, CPL, true, false><<<g, b, 0, a.stream>>>(a);
-    else if (a.z) k_select_bwd<Tin, N, CPL, false, true><<<g, b, 0, a.stream>>>(a);
-    else k_select_bwd<Tin, N, CPL, false, false><<<g, b, 0, a.stream>>>(a);
+    if (vec && a.z) k_select_bwd<Tin, N, CPL, true, true><<<grid, 512, 0, a.stream>>>(a);
+    else if (vec) k_select_bwd<Tin, N, CPL, true, false><<<grid, 512, 0, a.stream>>>(a);
+    else if (a.z) k_select_bwd<Tin, N, CPL, false, true><<<grid, 512, 0, a.stream>>>(a);
+    else k_select_bwd<Tin, N, CPL, false, false><<<grid, 512, 0, a.stream>>>(a);
   }
   const long nbc = (long)a.Ttot * a.G * 2 * N, np = (long)a.D * (N + 2);
   if (nbc > 0) k_select_dbc<Tin><<<(unsigned)((nbc + 255) / 256), 256, 0, a.stream>>>(a);

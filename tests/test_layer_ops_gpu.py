@@ -586,3 +586,19 @@ def test_another_stream_and_a_graph():
         got = [t.clone() for t in (out, cs, ss)]
         for a, c in zip(got, eager(k + 1)):
             assert torch.equal(a, c), k
+
+
+SEGMENTED = [
+    ("one_row", dict(B=1, T=1500, D=40, N=16, dht=True)),
+    ("one_row_f32", dict(B=1, T=2311, D=12, N=8, dtype="f32", dht=True)),
+    ("two_rows_n32", dict(B=2, T=900, D=20, N=32, z=False, dht=True)),
+    ("no_states", dict(B=1, T=700, D=33, N=16, h0=False, off=1)),
+    ("packed", dict(D=24, N=16, lens=[1100, 1, 0, 64, 700, 129], host=True, dht=True)),
+]
+
+
+@pytest.mark.parametrize("name,kw", SEGMENTED, ids=[c[0] for c in SEGMENTED])
+def test_select_rows_cut_into_segments(name, kw):
+    """Few long rows: their segments run side by side."""
+    _log("select segments " + name)
+    _check_select("seg_" + name, kw)
