@@ -16,6 +16,7 @@ offsets checked, ``cu_seqlens_host``) as in the package's other calls.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 from . import (COMBA_BF16, COMBA_F32, CombaError, _check, _host_offsets, _ptr, _stream,
                load_library)
@@ -48,50 +49,59 @@ class CombaGroupNormShape(ctypes.Structure):
                 ("x_row", _I64), ("z_row", _I64)]
 
 
+# A call packs its shape struct with these (a third of the cost of a ctypes
+# Structure: at one token per call the binding, not the kernel, bounds the rate).
+_CONV = struct.Struct("@iiiiiPPiiq")
+_SELECT = struct.Struct("@iiiiiiPPiiqqqqq")
+_NORM = struct.Struct("@qiiiiifqq")
+assert _CONV.size == ctypes.sizeof(CombaConvShape)
+assert _SELECT.size == ctypes.sizeof(CombaSelectShape)
+assert _NORM.size == ctypes.sizeof(CombaGroupNormShape)
+
+
 def bind(lib):
-    """Declare the C signatures (called by load_library)."""
+    """Declare the C signatures (called by load_library); the shape structs pass as bytes."""
     P, Z, I = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
-    conv, sel, norm = (ctypes.POINTER(s) for s in (CombaConvShape, CombaSelectShape,
-                                                   CombaGroupNormShape))
-    for name, args in (("comba_conv_fwd", [conv] + [P] * 7),
-                       ("comba_conv_bwd", [conv] + [P] * 11 + [Z, P]),
-                       ("comba_conv_step", [conv] + [P] * 5 + [_I32, P, P]),
-                       ("comba_select_fwd", [sel] + [P] * 12 + [Z, P]),
-                       ("comba_select_fwd_save", [sel] + [P] * 12 + [Z, P]),
-                       ("comba_select_bwd", [sel] + [P] * 21 + [Z, P]),
-                       ("comba_select_step", [sel] + [P] * 10 + [_I32, P, P]),
-                       ("comba_group_norm_fwd", [norm] + [P] * 6),
-                       ("comba_group_norm_bwd", [norm] + [P] * 10 + [Z, P])):
+    for name, args in (("comba_conv_fwd", [P] * 8),
+                       ("comba_conv_bwd", [P] * 12 + [Z, P]),
+                       ("comba_conv_step", [P] * 6 + [_I32, P, P]),
+                       ("comba_select_fwd", [P] * 13 + [Z, P]),
+                       ("comba_select_fwd_save", [P] * 13 + [Z, P]),
+                       ("comba_select_bwd", [P] * 22 + [Z, P]),
+                       ("comba_select_step", [P] * 11 + [_I32, P, P]),
+                       ("comba_group_norm_fwd", [P] * 7),
+                       ("comba_group_norm_bwd", [P] * 11 + [Z, P])):
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, I
-    for name, shp in (("comba_conv_workspace_bytes", conv),
-                      ("comba_select_fwd_workspace_bytes", sel),
-                      ("comba_select_bwd_workspace_bytes", sel),
-                      ("comba_group_norm_workspace_bytes", norm)):
+    for name in ("comba_conv_workspace_bytes", "comba_select_fwd_workspace_bytes",
+                 "comba_select_bwd_workspace_bytes", "comba_group_norm_workspace_bytes"):
         fn = getattr(lib, name)
-        fn.argtypes, fn.restype = [shp], Z
+        fn.argtypes, fn.restype = [P], Z
 
 
 # ---- argument checks -------------------------------------------------------
 def _code(t, name):
     import torch
 
-    if not t.is_cuda:
+    if t.get_device() < 0:
         raise CombaError("comba: tensors must be on a GPU device")
-    if t.dtype is torch.bfloat16:
+    dt = t.dtype
+    if dt is torch.bfloat16:
         return COMBA_BF16
-    if t.dtype is torch.float32:
+    if dt is torch.float32:
         return COMBA_F32
     raise CombaError("comba: %s must be bfloat16 or float32" % name)
 
 
 def _dense(name, t, shape, dtype, dev):
+    """The pointer of a contiguous tensor of this shape (None: absent)."""
     if t is None:
-        return
-    if tuple(t.shape) != tuple(shape) or t.dtype is not dtype or t.get_device() != dev \
+        return None
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev \
             or not t.is_contiguous():
         raise CombaError("comba: %s must be a contiguous %s %s on the device"
                          % (name, str(dtype).replace("torch.", ""), list(shape)))
+    return t.data_ptr()
 
 
 def _row(name, t, lead, shape, dtype, dev):
@@ -99,7 +109,7 @@ def _row(name, t, lead, shape, dtype, dev):
     then a row): a row's elements are contiguous, the rows evenly spaced."""
     if t is None:
         return 0
-    if tuple(t.shape) != tuple(shape) or t.dtype is not dtype or t.get_device() != dev:
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
         raise CombaError("comba: %s must be %s %s on the device"
                          % (name, str(dtype).replace("torch.", ""), list(shape)))
     if t.is_contiguous():
@@ -130,7 +140,7 @@ def _seqs(B, cu_seqlens, cu_seqlens_host, dev):
     if cu_seqlens is None:
         if cu_seqlens_host is not None:
             raise CombaError("comba: cu_seqlens_host needs cu_seqlens")
-        return B, None, None
+        return B, 0, None
     import torch
 
     if cu_seqlens.dtype is not torch.int32 or not cu_seqlens.is_contiguous() \
@@ -142,12 +152,13 @@ def _seqs(B, cu_seqlens, cu_seqlens_host, dev):
 
 def _slots(slots, rows, dev):
     if slots is None:
-        return
+        return None
     import torch
 
-    if slots.dtype is not torch.int32 or tuple(slots.shape) != (rows,) \
+    if slots.dtype is not torch.int32 or slots.shape != (rows,) \
             or not slots.is_contiguous() or slots.get_device() != dev:
         raise CombaError("comba: slots must be contiguous int32 [B] on the device")
+    return slots.data_ptr()
 
 
 def _activation(name, allowed):
@@ -159,7 +170,7 @@ def _activation(name, allowed):
 def _workspace(fn, shp, given, device):
     import torch
 
-    nbytes = fn(ctypes.byref(shp))
+    nbytes = fn(shp)
     if nbytes == 0:
         _check(2)
     if given is not None and given.numel() >= nbytes:
@@ -168,7 +179,12 @@ def _workspace(fn, shp, given, device):
 
 
 def _host_ptr(host):
-    return None if host is None else host.ctypes.data
+    return 0 if host is None else host.ctypes.data
+
+
+def _run(status):
+    if status:
+        _check(status)
 
 
 # ---- short causal convolution -------------------------------------------------
@@ -181,17 +197,17 @@ def _conv_shape(x, w, bias, h0, activation, cu_seqlens, cu_seqlens_host):
     code, dev = _code(x, "x"), x.get_device()
     if x.dim() != 3 or w.dim() != 2 or w.shape[0] != x.shape[2]:
         raise CombaError("comba: x must be [B,T,D] and w [D,K]")
-    B, T, D = x.shape
+    shape = x.shape
+    B, T, D = shape
     K = w.shape[1]
-    _dense("w", w, (D, K), torch.float32, dev)
-    _dense("bias", bias, (D,), torch.float32, dev)
     N, cu, host = _seqs(B, cu_seqlens, cu_seqlens_host, dev)
-    _dense("h0", h0, (N, K - 1, D), x.dtype, dev)
-    row = _row("x", x, 2, (B, T, D), x.dtype, dev)
-    shp = CombaConvShape(B, T, D, K, N, cu, _host_ptr(host), code,
-                         _activation(activation, _CONV_ACT), row)
-    shp._keep = host
-    return shp, (B, T, D, K, N, dev)
+    row = _row("x", x, 2, shape, x.dtype, dev)
+    shp = _CONV.pack(B, T, D, K, N, cu, _host_ptr(host), code, _activation(activation, _CONV_ACT),
+                     row)
+    ptrs = (x.data_ptr(), _dense("w", w, (D, K), torch.float32, dev),
+            _dense("bias", bias, (D,), torch.float32, dev),
+            _dense("h0", h0, (N, K - 1, D), x.dtype, dev))
+    return shp, host, ptrs, (N, K - 1, D), dev
 
 
 def comba_conv_fwd(x, w, bias=None, h0=None, *, activation="silu", cu_seqlens=None,
@@ -201,14 +217,12 @@ def comba_conv_fwd(x, w, bias=None, h0=None, *, activation="silu", cu_seqlens=No
     x [B,T,D] (may be a column slice); w [D,K] float32, K = 2..4, the newest token
     under the last tap; bias [D] float32; h0 [N,K-1,D]: each sequence's inputs
     before its first token, oldest first (None: zeros); ht: those before its next."""
-    import torch
-
-    shp, (B, T, D, K, N, dev) = _conv_shape(x, w, bias, h0, activation, cu_seqlens,
-                                            cu_seqlens_host)
-    y = torch.empty((B, T, D), dtype=x.dtype, device=x.device)
-    ht = torch.empty((N, K - 1, D), dtype=x.dtype, device=x.device) if output_final_state else None
-    _check(load_library().comba_conv_fwd(ctypes.byref(shp), _ptr(x), _ptr(w), _ptr(bias), _ptr(h0),
-                                         _ptr(y), _ptr(ht), _stream(stream, x.device)))
+    shp, _host, ptrs, state, dev = _conv_shape(x, w, bias, h0, activation, cu_seqlens,
+                                               cu_seqlens_host)
+    y = x.new_empty(x.shape)
+    ht = x.new_empty(state) if output_final_state else None
+    _run(load_library().comba_conv_fwd(shp, *ptrs, y.data_ptr(), _ptr(ht),
+                                       _stream(stream, x.device)))
     return y, ht
 
 
@@ -219,18 +233,16 @@ def comba_conv_bwd(x, w, bias, h0, dy, dht=None, *, activation="silu", cu_seqlen
     import torch
 
     lib = load_library()
-    shp, (B, T, D, K, N, dev) = _conv_shape(x, w, bias, h0, activation, cu_seqlens,
-                                            cu_seqlens_host)
-    _dense("dy", dy, (B, T, D), x.dtype, dev)
-    _dense("dht", dht, (N, K - 1, D), x.dtype, dev)
-    out = {"dx": torch.empty((B, T, D), dtype=x.dtype, device=x.device),
-           "dw": torch.empty_like(w),
+    shp, _host, ptrs, state, dev = _conv_shape(x, w, bias, h0, activation, cu_seqlens,
+                                               cu_seqlens_host)
+    grads = (_dense("dy", dy, x.shape, x.dtype, dev), _dense("dht", dht, state, x.dtype, dev))
+    out = {"dx": x.new_empty(x.shape), "dw": torch.empty_like(w),
            "dbias": None if bias is None else torch.empty_like(bias),
-           "dh0": torch.empty((N, K - 1, D), dtype=x.dtype, device=x.device) if need_dh0 else None}
+           "dh0": x.new_empty(state) if need_dh0 else None}
     ws = _workspace(lib.comba_conv_workspace_bytes, shp, workspace, x.device)
-    _check(lib.comba_conv_bwd(ctypes.byref(shp), _ptr(x), _ptr(w), _ptr(bias), _ptr(h0), _ptr(dy),
-                              _ptr(dht), _ptr(out["dx"]), _ptr(out["dw"]), _ptr(out["dbias"]),
-                              _ptr(out["dh0"]), _ptr(ws), ws.numel(), _stream(stream, x.device)))
+    _run(lib.comba_conv_bwd(shp, *ptrs, *grads, _ptr(out["dx"]), _ptr(out["dw"]),
+                            _ptr(out["dbias"]), _ptr(out["dh0"]), _ptr(ws), ws.numel(),
+                            _stream(stream, x.device)))
     return out
 
 
@@ -241,21 +253,19 @@ def comba_conv_step(x, w, bias, state, *, slots=None, activation="silu", stream=
     slot outside [0, S) marks padding: y zero, no state touched), or slot b."""
     import torch
 
-    code, dev = _code(x, "x"), x.get_device()
-    if x.dim() != 2 or w.dim() != 2 or w.shape[0] != x.shape[1] or state.dim() != 3:
+    code, dev, shape, taps, pool = _code(x, "x"), x.get_device(), x.shape, w.shape, state.shape
+    if len(shape) != 2 or len(taps) != 2 or taps[0] != shape[1] or len(pool) != 3:
         raise CombaError("comba: x must be [B,D], w [D,K] and state [S,K-1,D]")
-    B, D = x.shape
-    K = w.shape[1]
-    _dense("w", w, (D, K), torch.float32, dev)
-    _dense("bias", bias, (D,), torch.float32, dev)
-    _dense("state", state, (state.shape[0], K - 1, D), x.dtype, dev)
-    _slots(slots, B, dev)
-    shp = CombaConvShape(B, 1, D, K, B, None, None, code, _activation(activation, _CONV_ACT),
-                         _row("x", x, 1, (B, D), x.dtype, dev))
-    y = torch.empty((B, D), dtype=x.dtype, device=x.device)
-    _check(load_library().comba_conv_step(ctypes.byref(shp), _ptr(x), _ptr(w), _ptr(bias),
-                                          _ptr(state), _ptr(slots), state.shape[0], _ptr(y),
-                                          _stream(stream, x.device)))
+    B, D = shape
+    K, dt = taps[1], x.dtype
+    shp = _CONV.pack(B, 1, D, K, B, 0, 0, code, _activation(activation, _CONV_ACT),
+                     _row("x", x, 1, shape, dt, dev))
+    y = x.new_empty(shape)
+    _run(load_library().comba_conv_step(
+        shp, x.data_ptr(), _dense("w", w, taps, torch.float32, dev),
+        _dense("bias", bias, (D,), torch.float32, dev),
+        _dense("state", state, (pool[0], K - 1, D), dt, dev), _slots(slots, B, dev), pool[0],
+        y.data_ptr(), _stream(stream, x.device)))
     return y
 
 
@@ -265,26 +275,32 @@ def _select_shape(lead, u, delta, A, B, C, D, z, delta_bias, delta_softplus, N, 
 
     code, dev, dt = _code(u, "u"), u.get_device(), u.dtype
     f32 = torch.float32
-    shape = tuple(u.shape)
+    shape, ashape, bshape = u.shape, A.shape, B.shape
     width = shape[-1]
-    if A.dim() != 2 or A.shape[0] != width:
+    if len(ashape) != 2 or ashape[0] != width:
         raise CombaError("comba: A must be [D,N]")
-    n = A.shape[1]
-    if B.dim() not in (lead + 1, lead + 2):
+    n = ashape[1]
+    if len(bshape) == lead + 2:
+        G = bshape[lead]
+        want = shape[:-1] + (G, n)
+    elif len(bshape) == lead + 1:
+        G = 1
+        want = shape[:-1] + (n,)
+    else:
         raise CombaError("comba: B and C must be [..,G,N] or [..,N]")
-    bshape = shape[:-1] + ((B.shape[lead],) if B.dim() == lead + 2 else ()) + (n,)
-    G = B.shape[lead] if B.dim() == lead + 2 else 1
-    _dense("A", A, (width, n), f32, dev)
-    _dense("D", D, (width,), f32, dev)
-    _dense("delta_bias", delta_bias, (width,), f32, dev)
-    rows = [_row(name, t, lead, s, dt, dev)
-            for name, t, s in (("u", u, shape), ("delta", delta, shape), ("z", z, shape),
-                               ("B", B, bshape), ("C", C, bshape))]
-    batch, T = (shape[0], 1) if lead == 1 else shape[:2]
-    shp = CombaSelectShape(batch, T, width, n, G, N, cu, _host_ptr(host), code,
-                           1 if delta_softplus else 0, *rows)
-    shp._keep = host
-    return shp, n, bshape
+    if lead == 1:
+        batch, T = shape[0], 1
+    else:
+        batch, T = shape[0], shape[1]
+    shp = _SELECT.pack(batch, T, width, n, G, N, cu, _host_ptr(host), code,
+                       1 if delta_softplus else 0, _row("u", u, lead, shape, dt, dev),
+                       _row("delta", delta, lead, shape, dt, dev),
+                       _row("z", z, lead, shape, dt, dev), _row("B", B, lead, want, dt, dev),
+                       _row("C", C, lead, want, dt, dev))
+    ptrs = (u.data_ptr(), delta.data_ptr(), _dense("A", A, ashape, f32, dev), B.data_ptr(),
+            C.data_ptr(), _dense("D", D, (width,), f32, dev), None if z is None else z.data_ptr(),
+            _dense("delta_bias", delta_bias, (width,), f32, dev))
+    return shp, ptrs, n, want
 
 
 def _select(save, u, delta, A, B, C, D, z, delta_bias, h0, delta_softplus, cu_seqlens,
@@ -296,18 +312,17 @@ def _select(save, u, delta, A, B, C, D, z, delta_bias, h0, delta_softplus, cu_se
     if u.dim() != 3:
         raise CombaError("comba: u must be [B,T,D]")
     S, cu, host = _seqs(u.shape[0], cu_seqlens, cu_seqlens_host, u.get_device())
-    shp, n, _ = _select_shape(2, u, delta, A, B, C, D, z, delta_bias, delta_softplus, S, cu, host)
-    width = u.shape[2]
-    _dense("h0", h0, (S, width, n), torch.float32, u.get_device())
-    y = torch.empty(u.shape, dtype=u.dtype, device=u.device)
-    ht = torch.empty((S, width, n), dtype=torch.float32, device=u.device) \
-        if output_final_state else None
+    shp, ptrs, n, _ = _select_shape(2, u, delta, A, B, C, D, z, delta_bias, delta_softplus, S, cu,
+                                    host)
+    state = (S, u.shape[2], n)
+    h0p = _dense("h0", h0, state, torch.float32, u.get_device())
+    y = u.new_empty(u.shape)
+    ht = A.new_empty(state) if output_final_state else None
     size = lib.comba_select_bwd_workspace_bytes if save else lib.comba_select_fwd_workspace_bytes
     ws = _workspace(size, shp, workspace, u.device)
     fn = lib.comba_select_fwd_save if save else lib.comba_select_fwd
-    _check(fn(ctypes.byref(shp), _ptr(u), _ptr(delta), _ptr(A), _ptr(B), _ptr(C), _ptr(D), _ptr(z),
-              _ptr(delta_bias), _ptr(h0), _ptr(y), _ptr(ht), _ptr(ws), ws.numel(),
-              _stream(stream, u.device)))
+    _run(fn(shp, *ptrs, h0p, y.data_ptr(), _ptr(ht), ws.data_ptr(), ws.numel(),
+            _stream(stream, u.device)))
     return y, ht, ws
 
 
@@ -349,31 +364,24 @@ def comba_select_bwd(u, delta, A, B, C, D, z, delta_bias, h0, dy, dht=None, *, w
         raise CombaError("comba: u must be [B,T,D]")
     dev, f32 = u.get_device(), torch.float32
     S, cu, host = _seqs(u.shape[0], cu_seqlens, cu_seqlens_host, dev)
-    shp, n, bshape = _select_shape(2, u, delta, A, B, C, D, z, delta_bias, delta_softplus, S, cu,
-                                   host)
-    width = u.shape[2]
-    _dense("h0", h0, (S, width, n), f32, dev)
-    _dense("dht", dht, (S, width, n), f32, dev)
-    _dense("dy", dy, u.shape, u.dtype, dev)
-
-    def like(shape, dtype, given=True):
-        return torch.empty(shape, dtype=dtype, device=u.device) if given else None
-
-    out = {"du": like(u.shape, u.dtype), "ddelta": like(u.shape, u.dtype),
-           "dA": like(A.shape, f32), "dB": like(bshape, u.dtype), "dC": like(bshape, u.dtype),
-           "dD": like((width,), f32, D is not None), "dz": like(u.shape, u.dtype, z is not None),
-           "ddelta_bias": like((width,), f32, delta_bias is not None),
-           "dh0": like((S, width, n), f32, need_dh0)}
-    if workspace is None or workspace.numel() < lib.comba_select_bwd_workspace_bytes(
-            ctypes.byref(shp)):
+    shp, ptrs, n, bshape = _select_shape(2, u, delta, A, B, C, D, z, delta_bias, delta_softplus, S,
+                                         cu, host)
+    state = (S, u.shape[2], n)
+    given = (_dense("h0", h0, state, f32, dev), _dense("dy", dy, u.shape, u.dtype, dev),
+             _dense("dht", dht, state, f32, dev))
+    out = {"du": u.new_empty(u.shape), "ddelta": u.new_empty(u.shape),
+           "dA": A.new_empty(A.shape), "dB": u.new_empty(bshape), "dC": u.new_empty(bshape),
+           "dD": None if D is None else A.new_empty(D.shape),
+           "dz": None if z is None else u.new_empty(u.shape),
+           "ddelta_bias": None if delta_bias is None else A.new_empty(delta_bias.shape),
+           "dh0": A.new_empty(state) if need_dh0 else None}
+    if workspace is None or workspace.numel() < lib.comba_select_bwd_workspace_bytes(shp):
         raise CombaError("comba: comba_select_bwd needs the workspace filled by "
                          "comba_select_fwd_save")
-    _check(lib.comba_select_bwd(
-        ctypes.byref(shp), _ptr(u), _ptr(delta), _ptr(A), _ptr(B), _ptr(C), _ptr(D), _ptr(z),
-        _ptr(delta_bias), _ptr(h0), _ptr(dy), _ptr(dht), _ptr(out["du"]), _ptr(out["ddelta"]),
-        _ptr(out["dA"]), _ptr(out["dB"]), _ptr(out["dC"]), _ptr(out["dD"]), _ptr(out["dz"]),
-        _ptr(out["ddelta_bias"]), _ptr(out["dh0"]), _ptr(workspace), workspace.numel(),
-        _stream(stream, u.device)))
+    _run(lib.comba_select_bwd(
+        shp, *ptrs, *given, *(_ptr(out[k]) for k in ("du", "ddelta", "dA", "dB", "dC", "dD", "dz",
+                                                     "ddelta_bias", "dh0")),
+        workspace.data_ptr(), workspace.numel(), _stream(stream, u.device)))
     return out
 
 
@@ -383,19 +391,17 @@ def comba_select_step(u, delta, A, B, C, D, z, delta_bias, state, *, slots=None,
     u, delta, z [B,D]; B, C [B,G,N] or [B,N]; slots as in comba_conv_step."""
     import torch
 
-    if u.dim() != 2 or state.dim() != 3:
+    shape, pool = u.shape, state.shape
+    if len(shape) != 2 or len(pool) != 3:
         raise CombaError("comba: u must be [B,D] and state [S,D,N]")
-    rows = u.shape[0]
-    shp, n, _ = _select_shape(1, u, delta, A, B, C, D, z, delta_bias, delta_softplus, rows, None,
-                              None)
+    rows = shape[0]
+    shp, ptrs, n, _ = _select_shape(1, u, delta, A, B, C, D, z, delta_bias, delta_softplus, rows,
+                                    0, None)
     dev = u.get_device()
-    _dense("state", state, (state.shape[0], u.shape[1], n), torch.float32, dev)
-    _slots(slots, rows, dev)
-    y = torch.empty(u.shape, dtype=u.dtype, device=u.device)
-    _check(load_library().comba_select_step(
-        ctypes.byref(shp), _ptr(u), _ptr(delta), _ptr(A), _ptr(B), _ptr(C), _ptr(D), _ptr(z),
-        _ptr(delta_bias), _ptr(state), _ptr(slots), state.shape[0], _ptr(y),
-        _stream(stream, u.device)))
+    y = u.new_empty(shape)
+    _run(load_library().comba_select_step(
+        shp, *ptrs, _dense("state", state, (pool[0], shape[1], n), torch.float32, dev),
+        _slots(slots, rows, dev), pool[0], y.data_ptr(), _stream(stream, u.device)))
     return y
 
 
@@ -406,23 +412,22 @@ _NORM_ACT = (None, "none", "silu", "sigmoid")
 def _norm_shape(x, groups, weight, bias, z, activation, eps, out):
     import torch
 
-    xc, dev = _code(x, "x"), x.get_device()
-    if x.dim() < 1 or groups < 1 or x.shape[-1] < 1 or x.shape[-1] % groups:
+    xc, dev, dt, f32, shape = _code(x, "x"), x.get_device(), x.dtype, torch.float32, x.shape
+    lead = len(shape) - 1
+    if lead < 0 or groups < 1 or shape[-1] < 1 or shape[-1] % groups:
         raise CombaError("comba: x must be [..,C] with C a multiple of groups")
-    if out is not torch.bfloat16 and out is not torch.float32:
+    if out is not torch.bfloat16 and out is not f32:
         raise CombaError("comba: out_dtype must be bfloat16 or float32")
-    if out is not x.dtype and x.dtype is not torch.float32:
+    if out is not dt and dt is not f32:
         raise CombaError("comba: x must be float32 or have the output's dtype")
-    C = x.shape[-1]
-    _dense("weight", weight, (C,), torch.float32, dev)
-    _dense("bias", bias, (C,), torch.float32, dev)
-    lead = x.dim() - 1
-    xr = _row("x", x, lead, x.shape, x.dtype, dev)
-    zr = _row("z", z, lead, x.shape, out, dev)
-    rows = x.numel() // C
-    return CombaGroupNormShape(rows, C, groups, xc,
-                               COMBA_BF16 if out is torch.bfloat16 else COMBA_F32,
-                               _activation(activation, _NORM_ACT), eps, xr, zr)
+    C = shape[-1]
+    shp = _NORM.pack(x.numel() // C, C, groups, xc,
+                     COMBA_BF16 if out is torch.bfloat16 else COMBA_F32,
+                     _activation(activation, _NORM_ACT), eps, _row("x", x, lead, shape, dt, dev),
+                     _row("z", z, lead, shape, out, dev))
+    ptrs = (x.data_ptr(), _dense("weight", weight, (C,), f32, dev),
+            _dense("bias", bias, (C,), f32, dev), None if z is None else z.data_ptr())
+    return shp, ptrs
 
 
 def comba_group_norm_fwd(x, groups, weight=None, bias=None, z=None, *, activation="silu",
@@ -432,14 +437,10 @@ def comba_group_norm_fwd(x, groups, weight=None, bias=None, z=None, *, activatio
 
     x [..,C] and z may be column slices; weight, bias [C] float32 or None.  y has
     ``out_dtype`` (default: the dtype of z, else of x); x is float32 or of that dtype."""
-    import torch
-
     out = out_dtype or (x.dtype if z is None else z.dtype)
-    shp = _norm_shape(x, groups, weight, bias, z, activation, eps, out)
-    y = torch.empty(x.shape, dtype=out, device=x.device)
-    _check(load_library().comba_group_norm_fwd(ctypes.byref(shp), _ptr(x), _ptr(weight),
-                                               _ptr(bias), _ptr(z), _ptr(y),
-                                               _stream(stream, x.device)))
+    shp, ptrs = _norm_shape(x, groups, weight, bias, z, activation, eps, out)
+    y = x.new_empty(x.shape, dtype=out)
+    _run(load_library().comba_group_norm_fwd(shp, *ptrs, y.data_ptr(), _stream(stream, x.device)))
     return y
 
 
@@ -447,20 +448,16 @@ def comba_group_norm_bwd(x, groups, weight, bias, z, dy, *, activation="silu", e
                          workspace=None, stream=None):
     """Backward of comba_group_norm_fwd from dy (the forward's output dtype).  Returns dict dx
     (dtype of x), dz (dtype of dy, None without z), dweight, dbias (float32, None where absent)."""
-    import torch
-
     lib = load_library()
-    shp = _norm_shape(x, groups, weight, bias, z, activation, eps, dy.dtype)
-    _dense("dy", dy, x.shape, dy.dtype, x.get_device())
-    out = {"dx": torch.empty(x.shape, dtype=x.dtype, device=x.device),
-           "dz": None if z is None else torch.empty(x.shape, dtype=dy.dtype, device=x.device),
-           "dweight": None if weight is None else torch.empty_like(weight),
-           "dbias": None if bias is None else torch.empty_like(bias)}
+    shp, ptrs = _norm_shape(x, groups, weight, bias, z, activation, eps, dy.dtype)
+    dyp = _dense("dy", dy, x.shape, dy.dtype, x.get_device())
+    out = {"dx": x.new_empty(x.shape), "dz": None if z is None else dy.new_empty(x.shape),
+           "dweight": None if weight is None else weight.new_empty(weight.shape),
+           "dbias": None if bias is None else bias.new_empty(bias.shape)}
     ws = _workspace(lib.comba_group_norm_workspace_bytes, shp, workspace, x.device)
-    _check(lib.comba_group_norm_bwd(ctypes.byref(shp), _ptr(x), _ptr(weight), _ptr(bias), _ptr(z),
-                                    _ptr(dy), _ptr(out["dx"]), _ptr(out["dz"]),
-                                    _ptr(out["dweight"]), _ptr(out["dbias"]), _ptr(ws), ws.numel(),
-                                    _stream(stream, x.device)))
+    _run(lib.comba_group_norm_bwd(shp, *ptrs, dyp, _ptr(out["dx"]), _ptr(out["dz"]),
+                                  _ptr(out["dweight"]), _ptr(out["dbias"]), ws.data_ptr(),
+                                  ws.numel(), _stream(stream, x.device)))
     return out
 
 
