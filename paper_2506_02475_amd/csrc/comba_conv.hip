@@ -12,8 +12,16 @@
 namespace comba {
 
 constexpr int CONV_PF = 4;        // rows loaded ahead, together
-constexpr int CONV_BRUN = 32;     // tokens per run of the backward
 constexpr int CONV_BWAVES = 4;    // runs of a workgroup of the backward
+
+// Tokens per run: 32, or 16 or 8 where 32 would leave less than three waves a
+// SIMD (a run reads K - 1 rows more than its own; the backward forms as many du
+// more).  us by run 8 / 16 / 32 / 64, bf16: forward 16,384 tokens x 4,096 channels
+// 84 / 68 / 59 / 64; 18,384 x 2,048: 41 / 34 / 39 / 36; 1,000 x 2,048: 12 / 12 / 18 / 29.
+static int conv_run(const ConvArgs& a, int C) {
+  const long items = (long)a.Ttot * ((a.D + C - 1) / C);
+  return items >= 32L * 192 * 1024 ? 32 : items >= 16L * 64 * 1024 ? 16 : 8;
+}
 
 // The non-empty sequence s = [sa, se) that holds token t (0 <= t < Ttot), inside
 // the tokens whatever the offsets hold.
@@ -134,43 +142,58 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a) {
   }
 }
 
-// One token per row; the state's rows move up by one.
-template <typename Tin, int K, int C, bool VEC>
+// One token per row; the state's rows move up by one.  A thread takes its
+// channels of R rows, so that the taps, twice a row's bytes, are read once.
+template <typename Tin, int K, int C, bool VEC, int R>
 __global__ __launch_bounds__(256) void k_conv_step(ConvArgs a) {
   const int pieces = (a.D + C - 1) / C;
   const long e = (long)blockIdx.x * 256 + threadIdx.x;
-  const long row = e / pieces;
-  if (row >= a.N) return;
+  const long row0 = e / pieces * R;
+  if (row0 >= a.N) return;
   const auto [c, nv] = conv_piece<C>(e % pieces, a.D);
-  const int slot = a.slots ? a.slots[row] : (int)row;
-  Tin* y = static_cast<Tin*>(a.y) + row * a.D + c;
-  float o[C];
-  if (slot < 0 || slot >= a.num_slots) {  // padding
+  int slot[R];
 #pragma unroll
-    for (int i = 0; i < C; ++i) o[i] = 0.f;
-    store_piece<Tin, C, VEC>(y, o, nv);
-    return;
+  for (int r = 0; r < R; ++r) {
+    const long row = min(row0 + r, (long)a.N - 1);
+    slot[r] = a.slots ? a.slots[row] : (int)row;
   }
-  float wt[K][C], v[K][C];
-  load_taps<K, C>(a.w, c, nv, wt);
-  Tin* st = static_cast<Tin*>(a.state) + (long)slot * (K - 1) * a.D + c;
-  Piece<Tin, C, VEC> p[K];
+  Piece<Tin, C, VEC> p[R][K];
+  Tin* st[R];
+  bool on[R];
 #pragma unroll
-  for (int j = 0; j < K - 1; ++j) p[j].load(st + (long)j * a.D, nv);
-  p[K - 1].load(static_cast<const Tin*>(a.x) + row * a.x_row + c, nv);
+  for (int r = 0; r < R; ++r) {
+    on[r] = slot[r] >= 0 && slot[r] < a.num_slots;  // else padding
+    st[r] = static_cast<Tin*>(a.state) + (long)(on[r] ? slot[r] : 0) * (K - 1) * a.D + c;
+    if (a.num_slots > 0) {
 #pragma unroll
-  for (int i = 0; i < C; ++i) {
-    float u = a.bias ? a.bias[c + min(i, nv - 1)] : 0.f;
-#pragma unroll
-    for (int j = 0; j < K; ++j) {
-      v[j][i] = p[j].get(i);
-      u = fmaf(wt[j][i], v[j][i], u);
+      for (int j = 0; j < K - 1; ++j) p[r][j].load(st[r] + (long)j * a.D, nv);
     }
-    o[i] = a.silu ? u * sigmoid_acc(u) : u;
+    p[r][K - 1].load(static_cast<const Tin*>(a.x) + min(row0 + r, (long)a.N - 1) * a.x_row + c, nv);
   }
-  store_piece<Tin, C, VEC>(y, o, nv);
+  float wt[K][C], b[C];
+  load_taps<K, C>(a.w, c, nv, wt);
 #pragma unroll
-  for (int j = 0; j < K - 1; ++j) store_piece<Tin, C, VEC>(st + (long)j * a.D, v[j + 1], nv);
+  for (int i = 0; i < C; ++i) b[i] = a.bias ? a.bias[c + min(i, nv - 1)] : 0.f;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (row0 + r >= a.N) break;
+    float o[C], v[K][C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      float u = b[i];
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        v[j][i] = p[r][j].get(i);
+        u = fmaf(wt[j][i], v[j][i], u);
+      }
+      o[i] = on[r] ? (a.silu ? u * sigmoid_acc(u) : u) : 0.f;
+    }
+    store_piece<Tin, C, VEC>(static_cast<Tin*>(a.y) + (row0 + r) * a.D + c, o, nv);
+    if (on[r]) {
+#pragma unroll
+      for (int j = 0; j < K - 1; ++j) store_piece<Tin, C, VEC>(st[r] + (long)j * a.D, v[j + 1], nv);
+    }
+  }
 }
 
 // Backward.  du_t = dy_t act'(u_t) adds w_j du_t to row t - (K - 1) + j of the
@@ -187,7 +210,7 @@ __global__ __launch_bounds__(64 * CONV_BWAVES) void k_conv_bwd(ConvArgs a) {
   const int piece = pg * 64 + lane;
   const ConvPiece cp = conv_piece<C>(piece, a.D);
   const int c = cp.c, nl = cp.nv, nv = piece < pieces ? nl : 0;  // channels loaded, stored
-  const int run = rb * CONV_BWAVES + w, t0 = run * CONV_BRUN, t1 = min(t0 + CONV_BRUN, a.Ttot);
+  const int t0 = (rb * CONV_BWAVES + w) * a.run, t1 = min(t0 + a.run, a.Ttot);
   float dw[K][C], db[C];
 #pragma unroll
   for (int i = 0; i < C; ++i) {
@@ -352,9 +375,10 @@ static bool conv_vec(const ConvArgs& a, int C) {
          ok(a.dy) && ok(a.dht) && ok(a.dx) && ok(a.dh0);
 }
 
+constexpr int CONV_BC = 4;  // channels of a thread of the backward
 int conv_bwd_runs(const ConvArgs& a) {
-  const int runs = (a.Ttot + CONV_BRUN - 1) / CONV_BRUN;
-  return (runs + CONV_BWAVES - 1) / CONV_BWAVES;
+  const int tokens = conv_run(a, CONV_BC) * CONV_BWAVES;
+  return (a.Ttot + tokens - 1) / tokens;
 }
 
 template <typename Tin, int K>
@@ -362,7 +386,7 @@ static hipError_t run_conv_fwd(const ConvArgs& a0) {
   constexpr int C = 16 / (int)sizeof(Tin);
   ConvArgs a = a0;
   const long pieces = (a.D + C - 1) / C;
-  a.run = 32;
+  a.run = conv_run(a, C);
   const long items = ((long)(a.Ttot + a.run - 1) / a.run + (a.ht ? (long)a.N * (K - 1) : 0)) * pieces;
   const long grid = (items + 255) / 256;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
@@ -371,19 +395,26 @@ static hipError_t run_conv_fwd(const ConvArgs& a0) {
   else k_conv_fwd<Tin, K, C, false><<<(unsigned)grid, 256, 0, a.stream>>>(a);
   return hipGetLastError();
 }
-template <typename Tin, int K>
-static hipError_t run_conv_step(const ConvArgs& a) {
-  constexpr int C = 16 / (int)sizeof(Tin);
-  const long grid = ((long)a.N * ((a.D + C - 1) / C) + 255) / 256;
+template <typename Tin, int K, int R>
+static hipError_t conv_step_rows(const ConvArgs& a) {
+  constexpr int C = 8 / (int)sizeof(Tin);
+  const long grid = ((long)((a.N + R - 1) / R) * ((a.D + C - 1) / C) + 255) / 256;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
-  if (conv_vec(a, C)) k_conv_step<Tin, K, C, true><<<(unsigned)grid, 256, 0, a.stream>>>(a);
-  else k_conv_step<Tin, K, C, false><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  if (conv_vec(a, C)) k_conv_step<Tin, K, C, true, R><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  else k_conv_step<Tin, K, C, false, R><<<(unsigned)grid, 256, 0, a.stream>>>(a);
   return hipGetLastError();
 }
 template <typename Tin, int K>
+static hipError_t run_conv_step(const ConvArgs& a) {
+  // four rows a thread where that leaves two workgroups per CU
+  return (long)a.N * a.D * (int)sizeof(Tin) >= 4L * 512 * 256 * 8 ? conv_step_rows<Tin, K, 4>(a)
+                                                                   : conv_step_rows<Tin, K, 1>(a);
+}
+template <typename Tin, int K>
 static hipError_t run_conv_bwd(const ConvArgs& a0) {
-  constexpr int C = 4;
+  constexpr int C = CONV_BC;
   ConvArgs a = a0;
+  a.run = conv_run(a, C);
   a.nruns = conv_bwd_runs(a);
   const long pgs = ((a.D + C - 1) / C + 63) / 64, grid = pgs * a.nruns;
   if (grid > INT32_MAX) return hipErrorInvalidValue;

@@ -5,11 +5,11 @@
 //   n = (x - mean) rstd w + b,   y = act(n)  |  n act(z).
 //
 // Bound by bytes: every value is read and written once.  A group's channels lie
-// in the registers of a team of 1..64 lanes (a power of two), KV pieces of four
-// per lane, so that mean and variance are two passes over registers.  A team
-// keeps its group and walks rows, with weight and bias (backward: and their
-// gradients' sums) in registers.  Groups of more than 1,024 channels take a
-// workgroup per group and read x again from the caches (k_group_norm_wide_*).
+// in the registers of a team of 1..64 lanes (a power of two) or of a workgroup of
+// 256, KV pieces of four per lane, so that mean and variance are two passes over
+// registers.  A team keeps its group and walks rows, with weight and bias
+// (backward: and their gradients' sums) in registers.  Groups of more than 4,096
+// channels read x again from the caches (k_group_norm_wide).
 #include "comba_layer_device.hpp"
 #include "comba_layer_launch.h"
 
@@ -17,7 +17,7 @@ namespace comba {
 
 constexpr int GN_C = 4;  // channels of a piece
 
-// Sum over the lanes of a team (team: a power of two), the same in every lane.
+// Sum over the lanes of a team (team: a power of two up to 64), the same in every lane.
 __device__ __forceinline__ float team_sum(float x, int team) {
   if (team > 1) x = xsum<0>(x);
   if (team > 2) x = xsum<1>(x);
@@ -48,13 +48,31 @@ __device__ __forceinline__ float act_slope(comba_activation act, float t, float&
   return s * (1.f - s);
 }
 
+// Sum over a workgroup of 256, the same in every thread.
+__device__ __forceinline__ float block_sum(float x, float* lds) {
+  x = team_sum(x, 64);
+  if (lane_id() == 0) lds[wave_id()] = x;
+  __syncthreads();
+  const float s = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+  __syncthreads();
+  return s;
+}
+
+// The same over the team: a wave's lanes, or the workgroup.
+template <bool BLOCK>
+__device__ __forceinline__ float gn_sum(float x, int team, float* lds) {
+  if constexpr (BLOCK) return block_sum(x, lds);
+  return team_sum(x, team);
+}
+
 struct GnTeam {
   int team;    // lanes
   int chunks;  // row chunks: team (group, chunk) takes rows chunk, chunk + chunks, ..
 };
 
-template <typename Tx, typename To, int KV, bool VEC, bool BWD>
+template <typename Tx, typename To, int KV, bool VEC, bool BLOCK, bool BWD>
 __global__ __launch_bounds__(256) void k_group_norm(GroupNormArgs a, GnTeam tm) {
+  __shared__ float lds[4];
   const int m = a.C / a.G, team = tm.team;
   const long id = ((long)blockIdx.x * 256 + threadIdx.x) / team;
   const int l = threadIdx.x & (team - 1);
@@ -102,7 +120,7 @@ __global__ __launch_bounds__(256) void k_group_norm(GroupNormArgs a, GnTeam tm) 
         sum += v[k][i];
       }
     if (r + tm.chunks < a.rows) load(r + tm.chunks);
-    const float mean = team_sum(sum, team) * inv;
+    const float mean = gn_sum<BLOCK>(sum, team, lds) * inv;
 #pragma unroll
     for (int k = 0; k < KV; ++k)
 #pragma unroll
@@ -110,7 +128,7 @@ __global__ __launch_bounds__(256) void k_group_norm(GroupNormArgs a, GnTeam tm) 
         v[k][i] = i < nv[k] ? v[k][i] - mean : 0.f;
         sq = fmaf(v[k][i], v[k][i], sq);
       }
-    const float rstd = rsqrtf(team_sum(sq, team) * inv + a.eps);
+    const float rstd = rsqrtf(gn_sum<BLOCK>(sq, team, lds) * inv + a.eps);
     if constexpr (!BWD) {
 #pragma unroll
       for (int k = 0; k < KV; ++k) {
@@ -143,8 +161,8 @@ __global__ __launch_bounds__(256) void k_group_norm(GroupNormArgs a, GnTeam tm) 
         }
         if (z) store_piece<To, GN_C, VEC>(static_cast<To*>(a.dz) + r * a.C + c[k], dz, nv[k]);
       }
-      s1 = team_sum(s1, team) * inv;
-      s2 = team_sum(s2, team) * inv;
+      s1 = gn_sum<BLOCK>(s1, team, lds) * inv;
+      s2 = gn_sum<BLOCK>(s2, team, lds) * inv;
 #pragma unroll
       for (int k = 0; k < KV; ++k) {
         float dx[GN_C];
@@ -166,17 +184,7 @@ __global__ __launch_bounds__(256) void k_group_norm(GroupNormArgs a, GnTeam tm) 
   }
 }
 
-// Sum over a workgroup of 256, the same in every thread.
-__device__ __forceinline__ float block_sum(float x, float* lds) {
-  x = team_sum(x, 64);
-  if (lane_id() == 0) lds[wave_id()] = x;
-  __syncthreads();
-  const float s = (lds[0] + lds[1]) + (lds[2] + lds[3]);
-  __syncthreads();
-  return s;
-}
-
-// Groups too wide for a wave's registers: a workgroup per (group, chunk of rows).
+// Groups too wide for registers: a workgroup per (group, chunk of rows).
 template <typename Tx, typename To, bool BWD>
 __global__ __launch_bounds__(256) void k_group_norm_wide(GroupNormArgs a, GnTeam tm) {
   __shared__ float lds[4];
@@ -242,35 +250,41 @@ __global__ __launch_bounds__(256) void k_group_norm_wide(GroupNormArgs a, GnTeam
   }
 }
 
-// dweight and dbias: the chunks' partial sums in order, split over 16 groups of
-// threads that are added in order.
-constexpr int GN_COLS = 16, GN_GROUPS = 16;
-__global__ __launch_bounds__(256) void k_group_norm_dw(GroupNormArgs a) {
-  __shared__ float part[GN_GROUPS][GN_COLS];
-  const int col = threadIdx.x % GN_COLS, grp = threadIdx.x / GN_COLS;
-  const long n = 2L * a.C, e = (long)blockIdx.x * GN_COLS + col;
+// dweight and dbias: the chunks' partial sums, each of 16 waves every 16th in
+// order, then the waves in order.
+constexpr int GN_WAVES = 16;
+__global__ __launch_bounds__(64 * GN_WAVES) void k_group_norm_dw(GroupNormArgs a) {
+  __shared__ float part[GN_WAVES][64];
+  const int lane = lane_id(), w = wave_id_s();
+  const long n = 2L * a.C, e = (long)blockIdx.x * 64 + lane;
   float s = 0.f;
-  if (e < n)
-    for (int r = grp; r < a.blocks; r += GN_GROUPS) s += a.part[r * n + e];
-  part[grp][col] = s;
+  if (e < n) {
+#pragma unroll 8
+    for (int r = w; r < a.blocks; r += GN_WAVES) s += a.part[r * n + e];
+  }
+  part[w][lane] = s;
   __syncthreads();
-  if (grp == 0 && e < n) {
-    for (int i = 1; i < GN_GROUPS; ++i) s += part[i][col];
+  if (w == 0 && e < n) {
+    for (int i = 1; i < GN_WAVES; ++i) s += part[i][lane];
     if (e < a.C) { if (a.dw) a.dw[e] = s; }
     else if (a.db) a.db[e - a.C] = s;
   }
 }
 
-// The team of a group of m channels, and how many teams walk the rows.
+// The team of a group of m channels, and how many teams walk the rows: 1,024 lanes
+// per CU (bf16, 16,384 x 4,096 channels, groups of 128: 512 / 1,024 / 2,048 lanes
+// forward 102 / 84 / 92 us, backward 149 / 149 / 154).
+constexpr long GN_LANES = 1024;
 static GnTeam gn_team(const GroupNormArgs& a, int& kv) {
   const int m = a.C / a.G, pieces = (m + GN_C - 1) / GN_C;
   GnTeam t{};
   t.team = 1;
   while (t.team < 64 && t.team * 2 < pieces) t.team *= 2;
+  if (pieces > 4 * 64) t.team = 256;
   const int need = (pieces + t.team - 1) / t.team;
   kv = need <= 2 ? 2 : need <= 4 ? 4 : 0;
   const long lanes = (long)a.G * (kv ? t.team : 256);
-  long chunks = 256L * 8 * 4 * 64 / lanes;  // eight workgroups' worth of lanes per CU
+  long chunks = 256L * GN_LANES / lanes;  // lanes per CU
   chunks = chunks < 1 ? 1 : chunks > a.rows ? a.rows : chunks;
   t.chunks = (int)chunks;
   return t;
@@ -296,16 +310,18 @@ static hipError_t run_group_norm(const GroupNormArgs& a0) {
                      ok(a.dz, sizeof(To), a.C);
     const long threads = (long)t.chunks * a.G * (kv ? t.team : 256), grid = (threads + 255) / 256;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-#define GN_LAUNCH(KV)                                                                              \
-  if (vec) k_group_norm<Tx, To, KV, true, BWD><<<(unsigned)grid, 256, 0, a.stream>>>(a, t);        \
-  else k_group_norm<Tx, To, KV, false, BWD><<<(unsigned)grid, 256, 0, a.stream>>>(a, t);
-    if (kv == 2) { GN_LAUNCH(2) }
-    else if (kv == 4) { GN_LAUNCH(4) }
+#define GN_LAUNCH(KV, BLOCK)                                                                       \
+  if (vec) k_group_norm<Tx, To, KV, true, BLOCK, BWD><<<(unsigned)grid, 256, 0, a.stream>>>(a, t); \
+  else k_group_norm<Tx, To, KV, false, BLOCK, BWD><<<(unsigned)grid, 256, 0, a.stream>>>(a, t);
+    if (kv == 2 && t.team < 256) { GN_LAUNCH(2, false) }
+    else if (kv == 4 && t.team < 256) { GN_LAUNCH(4, false) }
+    else if (kv == 2) { GN_LAUNCH(2, true) }
+    else if (kv == 4) { GN_LAUNCH(4, true) }
     else k_group_norm_wide<Tx, To, BWD><<<(unsigned)grid, 256, 0, a.stream>>>(a, t);
 #undef GN_LAUNCH
   }
   if (BWD && (a.dw || a.db))
-    k_group_norm_dw<<<(unsigned)((2L * a.C + GN_COLS - 1) / GN_COLS), 256, 0, a.stream>>>(a);
+    k_group_norm_dw<<<(unsigned)((2L * a.C + 63) / 64), 64 * GN_WAVES, 0, a.stream>>>(a);
   return hipGetLastError();
 }
 

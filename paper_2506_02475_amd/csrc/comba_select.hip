@@ -935,49 +935,73 @@ __global__ __launch_bounds__(256) void k_select_dparam(SelectArgs a) {
 }
 
 // One token per row: a lane holds 4 states of one channel, consecutive lanes
-// consecutive states, so that a wave reads and writes whole kilobytes of the state.
-template <typename Tin, int N>
+// consecutive states, so that a wave reads and writes whole kilobytes of the
+// state.  A thread takes R rows, all loaded before the first is used.
+template <typename Tin, int N, bool VEC, int R>
 __global__ __launch_bounds__(256) void k_select_step(SelectArgs a) {
   constexpr int LN = N / 4;
-  const int nbx = (a.D * LN + 255) / 256;  // workgroups per row
-  const int row = blockIdx.x / nbx, e = (blockIdx.x - row * nbx) * 256 + threadIdx.x;
+  const int nbx = (a.D * LN + 255) / 256;  // workgroups per R rows
+  const int rb = blockIdx.x / nbx, e = (blockIdx.x - rb * nbx) * 256 + threadIdx.x;
   const int c = e / LN, ng = e % LN;
   const bool on = c < a.D;  // whole lane groups: a channel's lanes agree
-  const int slot = a.slots ? a.slots[row] : row;
-  Tin* y = static_cast<Tin*>(a.y) + (long)row * a.D + c;
-  if (slot < 0 || slot >= a.num_slots) {  // padding
-    if (on && ng == 0) store_elem(y, 0.f);
-    return;
-  }
   const int cc = on ? c : a.D - 1, g = cc / (a.D / a.G);
-  const float uv = to_f(static_cast<const Tin*>(a.u)[row * a.u_row + cc]);
-  float raw = to_f(static_cast<const Tin*>(a.delta)[row * a.delta_row + cc]);
-  if (a.bias) raw += a.bias[cc];
-  const float dt = a.softplus ? softplus_acc(raw) : raw, xu = dt * uv;
-  const Tin* Bp = static_cast<const Tin*>(a.Bm) + row * a.b_row + g * N + ng * 4;
-  const Tin* Cp = static_cast<const Tin*>(a.Cm) + row * a.c_row + g * N + ng * 4;
-  const float* Ap = a.A + (long)cc * N + ng * 4;
-  float* hp = a.state + ((long)slot * a.D + cc) * N + ng * 4;
-  float h[4], s = 0.f;
+  int row[R], slot[R];
+  bool live[R];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    h[j] = fmaf(__builtin_amdgcn_exp2f(dt * (Ap[j] * LOG2E)), hp[j], xu * to_f(Bp[j]));
-    s = fmaf(to_f(Cp[j]), h[j], s);
+  for (int r = 0; r < R; ++r) {
+    row[r] = min(rb * R + r, a.S - 1);
+    slot[r] = a.slots ? a.slots[row[r]] : row[r];
+    live[r] = slot[r] >= 0 && slot[r] < a.num_slots;  // else padding
   }
-  if (on) {
+  // every load unconditional (a load under a branch is waited for on the spot):
+  // padding reads slot 0, or without any slot an A row, and drops it; without z, u
+  const bool any = a.num_slots > 0;
+  const Tin* zp = static_cast<const Tin*>(a.z ? a.z : a.u);
+  const long zrow = a.z ? a.z_row : a.u_row;
+  float A2[4], hv[R][4];
+  Piece<Tin, 4, VEC> pb[R], pc[R];
+  Piece<Tin, 1, true> pu[R], pd[R], pz[R];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) hp[j] = h[j];
+  for (int r = 0; r < R; ++r) {
+    const float* hp = (any ? a.state : a.A) + ((long)(live[r] ? slot[r] : 0) * a.D + cc) * N + ng * 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) hv[r][j] = __builtin_nontemporal_load(hp + j);
+    pu[r].load(static_cast<const Tin*>(a.u) + row[r] * a.u_row + cc, 1);
+    pd[r].load(static_cast<const Tin*>(a.delta) + row[r] * a.delta_row + cc, 1);
+    pz[r].load(zp + row[r] * zrow + cc, 1);
+    pb[r].load(static_cast<const Tin*>(a.Bm) + row[r] * a.b_row + g * N + ng * 4, 4);
+    pc[r].load(static_cast<const Tin*>(a.Cm) + row[r] * a.c_row + g * N + ng * 4, 4);
   }
-  s = xsum<0>(s);
-  if constexpr (LN >= 4) s = xsum<1>(s);
-  if constexpr (LN >= 8) s = xsum<2>(s);
-  if (on && ng == 0) {
-    float v = a.Dskip ? fmaf(a.Dskip[cc], uv, s) : s;
-    if (a.z) {
-      const float zv = to_f(static_cast<const Tin*>(a.z)[row * a.z_row + cc]);
-      v *= zv * sigmoid_acc(zv);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) A2[j] = a.A[(long)cc * N + ng * 4 + j] * LOG2E;
+  const float bias = a.bias ? a.bias[cc] : 0.f, skip = a.Dskip ? a.Dskip[cc] : 0.f;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const float uv = pu[r].get(0), raw = pd[r].get(0) + bias;
+    const float dt = a.softplus ? softplus_acc(raw) : raw, xu = dt * uv;
+    float h[4], s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      h[j] = fmaf(__builtin_amdgcn_exp2f(dt * A2[j]), hv[r][j], xu * pb[r].get(j));
+      s = fmaf(pc[r].get(j), h[j], s);
     }
-    store_elem(y, v);
+    s = xsum<0>(s);
+    if constexpr (LN >= 4) s = xsum<1>(s);
+    if constexpr (LN >= 8) s = xsum<2>(s);
+    const bool mine = on && rb * R + r < a.S;
+    if (mine && live[r]) {
+      float* hp = a.state + ((long)slot[r] * a.D + cc) * N + ng * 4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) __builtin_nontemporal_store(h[j], hp + j);
+    }
+    if (mine && ng == 0) {
+      float v = fmaf(skip, uv, s);
+      if (a.z) {
+        const float zv = pz[r].get(0);
+        v *= zv * sigmoid_acc(zv);
+      }
+      store_elem(static_cast<Tin*>(a.y) + (long)row[r] * a.D + c, live[r] ? v : 0.f);
+    }
   }
 }
 
@@ -1033,12 +1057,20 @@ static hipError_t run_bwd(const SelectArgs& a) {
   return hipGetLastError();
 }
 
+template <typename Tin, int N, int R>
+static hipError_t step_rows(const SelectArgs& a) {
+  const long grid = ((long)a.D * (N / 4) + 255) / 256 * ((a.S + R - 1) / R);
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  const long m = 4 * sizeof(Tin);
+  const bool vec = (uintptr_t)a.Bm % m == 0 && (uintptr_t)a.Cm % m == 0 && a.b_row % 4 == 0 && a.c_row % 4 == 0;
+  if (vec) k_select_step<Tin, N, true, R><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  else k_select_step<Tin, N, false, R><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  return hipGetLastError();
+}
 template <typename Tin, int N>
 static hipError_t run_step(const SelectArgs& a) {
-  const long grid = ((long)a.D * (N / 4) + 255) / 256 * a.S;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  k_select_step<Tin, N><<<(unsigned)grid, 256, 0, a.stream>>>(a);
-  return hipGetLastError();
+  // four rows a thread where that leaves four workgroups per CU
+  return (long)a.S * a.D * (N / 4) >= 4L * 1024 * 256 ? step_rows<Tin, N, 4>(a) : step_rows<Tin, N, 1>(a);
 }
 
 #define SELECT_DISPATCH(fn, a)                                                              \

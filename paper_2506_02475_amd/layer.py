@@ -115,6 +115,8 @@ def _row(name, t, lead, shape, dtype, dev):
     if t.is_contiguous():
         return 0
     st, n = t.stride(), 1
+    if lead == 1 and len(st) == 2 and st[1] == 1 and st[0] >= shape[1]:
+        return st[0]
     for d in range(t.dim() - 1, lead - 1, -1):
         if shape[d] != 1 and st[d] != n:
             raise CombaError("comba: a row of %s must be contiguous" % name)

@@ -353,6 +353,9 @@ NORM = [
     ("bf16_wide", dict(rows=7, C=1501, G=1, gate=True, off=1)),
     ("f32_wide_groups", dict(rows=3, C=5000, G=2, dtype="f32", act="sigmoid")),
     ("bf16_wide_8k", dict(rows=4, C=8192, G=1)),
+    ("bf16_one_group_4096", dict(rows=5, C=4096, G=1, gate=True)),
+    ("f32_two_groups_3000", dict(rows=700, C=6000, G=2, dtype="f32")),
+    ("f32_wide_rows", dict(rows=600, C=4100, G=1, dtype="f32", gate=True)),
     ("bf16_100", dict(rows=50, C=1100, G=11, act="silu")),
     ("no_affine", dict(rows=8, C=256, G=2, affine=False, gate=True)),
     ("one_row", dict(rows=1, C=2048, G=16, xt="f32", gate=True)),
