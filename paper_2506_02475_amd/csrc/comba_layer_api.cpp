@@ -91,8 +91,6 @@ struct SelectLayout {
   size_t ck, bcp, dap, segF, segdt, total;
 };
 
-constexpr int kTile = 64;  // a segment's length is a multiple of it
-
 // Cuts rows into segments when their workgroups, one per CU, leave CUs idle or
 // wait for a long row: the main kernel then runs over segments side by side,
 // after a first pass over all but one segment of each row that is cut (`pre` of
@@ -106,7 +104,8 @@ constexpr int kTile = 64;  // a segment's length is a multiple of it
 void select_segments(comba::SelectArgs* a, bool bwd) {
   a->segs = 1;
   a->seglen = a->segmin = 1 << 30;
-  if (a->longest < 2 * kTile || a->S == 0) return;  // short, or not known
+  const int64_t tile = comba::select_tile(a->N);
+  if (a->longest < 2 * tile || a->S == 0) return;  // short, or not known
   int dev = 0, cus = 0;
   if (hipGetDevice(&dev) != hipSuccess ||
       hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
@@ -118,23 +117,23 @@ void select_segments(comba::SelectArgs* a, bool bwd) {
   if (a->cu_host && longest <= share) return;
   double best = a->cu_host ? longest : rounds(a->S) * longest;
   for (int p = 2; p <= 32; p *= 2) {
-    const int64_t len = (a->longest + (int64_t)p * kTile - 1) / ((int64_t)p * kTile) * kTile;
-    if (len * (p - 1) >= a->longest) break;
+    const int64_t len = (a->longest + p * tile - 1) / (p * tile) * tile, n = (a->longest + len - 1) / len;
+    if (n < 2) break;
     double t = launch;
     if (!a->cu_host) {
-      t += (rounds((double)a->S * p) + pre * rounds((double)a->S * (p - 1))) * (double)len;
+      t += (rounds((double)a->S * n) + pre * rounds((double)a->S * (n - 1))) * (double)len;
     } else {
       int64_t first = 0;  // tokens of the first pass
       for (int i = 0; i < a->S; ++i) {
-        const int64_t n = a->cu_host[i + 1] - a->cu_host[i];
-        if ((double)n > share) first += (n - 1) / len * len;
+        const int64_t tokens = a->cu_host[i + 1] - a->cu_host[i];
+        if ((double)tokens > share) first += (tokens - 1) / len * len;
       }
       const double f = (double)first * blocks / cus;
       t += ((double)len > share ? (double)len : share) + pre * ((double)len > f ? (double)len : f);
     }
-    if (t < best && (int64_t)a->S * p * a->G * a->nblk <= INT32_MAX) {
+    if (t < best && (int64_t)a->S * n * a->G * a->nblk <= INT32_MAX) {
       best = t;
-      a->segs = p;
+      a->segs = (int)n;
       a->seglen = (int)len;
       a->segmin = a->cu_host ? (int)share : 0;
     }
@@ -156,9 +155,9 @@ SelectLayout select_layout(const comba::SelectArgs& a0, bool save) {
   size_t segs = a.segs;
   if (save) {
     select_segments(&a, true);
-    // states: a sequence's start at tok0 / SELECT_CK + its number, which leaves
+    // states: a sequence's start at tok0 / select_ck + its number, which leaves
     // room for a partial interval per sequence
-    L.ck = take(((size_t)a.Ttot / comba::SELECT_CK + a.S + 1) * a.D * a.N * sizeof(float));
+    L.ck = take(((size_t)a.Ttot / comba::select_ck(a.N) + a.S + 1) * a.D * a.N * sizeof(float));
     L.bcp = take((size_t)a.G * a.nblk * a.Ttot * 2 * a.N * sizeof(float));
     L.dap = take((size_t)a.S * a.segs * a.D * (a.N + 2) * sizeof(float));
     if ((size_t)a.segs > segs) segs = a.segs;

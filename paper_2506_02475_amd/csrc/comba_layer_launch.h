@@ -37,8 +37,11 @@ hipError_t launch_conv_fwd(const ConvArgs& a);
 hipError_t launch_conv_bwd(const ConvArgs& a);
 hipError_t launch_conv_step(const ConvArgs& a);
 
-// Tokens between the states that the saving forward keeps for the backward.
-constexpr int SELECT_CK = 32;
+// Tokens between the states that the saving forward keeps for the backward, one
+// tile of the backward (8 states per channel: the LDS of twelve waves would not fit).
+constexpr int select_ck(int N) { return N == 8 ? 32 : 48; }
+// A segment's length is a multiple of every kernel's tile.
+constexpr int select_tile(int N) { return N == 8 ? 64 : 96; }
 
 struct SelectArgs {
   bool bf16, softplus, vec;  // vec: whole groups of channels in one load (set by the launchers)
@@ -51,7 +54,7 @@ struct SelectArgs {
   const float *A, *Dskip, *bias, *h0;
   void* y;
   float* ht;
-  float* ck;  // states at every SELECT_CK-th token of each sequence, or NULL
+  float* ck;  // states at every select_ck(N)-th token of each sequence, or NULL
   // step
   float* state;
   const int32_t* slots;

@@ -25,6 +25,10 @@
 
 namespace comba {
 
+constexpr int SEL_CPL = 2;  // channels of a lane
+// Waves of a forward workgroup: three a SIMD, where the registers suffice.
+constexpr int sel_waves(int N) { return N == 8 ? 8 : 12; }
+
 template <int N, int CPL>
 struct SelTile {
   static constexpr int LN = N / 4;     // lane groups over the states
@@ -110,13 +114,13 @@ __device__ __forceinline__ void sel_slot(int slot, int& ch, int& n) {
 // (REV: the decayed gradient of the state that enters it) and, per channel, the
 // sum of its steps, whose exponential is the segment's decay product.
 template <typename Tin, int N, int CPL, bool VEC, bool REV>
-__global__ __launch_bounds__(512) void k_select_seg(SelectArgs a) {
-  constexpr int L = 8, W = 8;
+__global__ __launch_bounds__(64 * sel_waves(N)) void k_select_seg(SelectArgs a) {
+  constexpr int L = 8, W = sel_waves(N);
   using S = SelTile<N, CPL>;
   constexpr int LN = S::LN, CG = S::CG, CW = S::CW, NE = S::NE, TL = L / LN, TILE = L * W;
-  constexpr int NB = L * N / 64, EPT = NE / (64 * W);
+  constexpr int NB = L * N / 64;
   constexpr unsigned EB = sizeof(Tin);
-  static_assert(L % LN == 0 && N % NB == 0 && NE % (64 * W) == 0, "tile");
+  static_assert(L % LN == 0 && N % NB == 0, "tile");
   struct WaveLds {
     float dt[L][CW], x[L][CW], R[L][N];  // x R: dt u B, or gy C
   };
@@ -140,9 +144,8 @@ __global__ __launch_bounds__(512) void k_select_seg(SelectArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) A2[i][j] = i < nv ? a.A[(long)c * N + ng * 4 + j] * LOG2E : 0.f;
   }
-  float H[EPT];
-#pragma unroll
-  for (int e = 0; e < EPT; ++e) H[e] = 0.f;
+  const int own = threadIdx.x;  // the state that this thread owns, below NE
+  float H = 0.f;
 
   const unsigned tok = w * L + ng, cb = nv > 0 ? (unsigned)cl * EB : BUF_OOB;
   const long xrow = REV ? a.D : a.u_row, rrow = REV ? a.c_row : a.b_row;
@@ -250,24 +253,19 @@ __global__ __launch_bounds__(512) void k_select_seg(SelectArgs a) {
       lds_put<4>(&ex[w][1][(i * 64 + lane) * 4], h[i]);
     }
     __syncthreads();
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      const int s = threadIdx.x + e * 64 * W;
+    if (own < NE) {
 #pragma unroll
       for (int mm = 0; mm < W; ++mm) {
         const int m = REV ? W - 1 - mm : mm;
-        H[e] = fmaf(ex[m][0][s], H[e], ex[m][1][s]);
+        H = fmaf(ex[m][0][own], H, ex[m][1][own]);
       }
     }
     __syncthreads();
   }
   const long at = (long)(sb.seq * a.segs + sb.seg) * a.D;
-#pragma unroll
-  for (int e = 0; e < EPT; ++e) {
-    int ch, n;
-    sel_slot<N, CPL>(threadIdx.x + e * 64 * W, ch, n);
-    if (sb.c0 + ch < sb.cend) a.segF[(at + sb.c0 + ch) * N + n] = H[e];
-  }
+  int oc, on;
+  sel_slot<N, CPL>(own, oc, on);
+  if (own < NE && sb.c0 + oc < sb.cend) a.segF[(at + sb.c0 + oc) * N + on] = H;
   // the steps' sum: over the lane groups and waves, which held different tokens
   float* red = &ex[0][0][0];
 #pragma unroll
@@ -301,9 +299,8 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
   using S = SelTile<N, CPL>;
   constexpr int LN = S::LN, CG = S::CG, CW = S::CW, NE = S::NE, TL = L / LN, TILE = L * W;
   constexpr int NB = L * N / 64;        // states of a B or C row that a lane loads
-  constexpr int EPT = NE / (64 * W);    // states of the exchange that a thread owns
   constexpr unsigned EB = sizeof(Tin);
-  static_assert(L % LN == 0 && N % NB == 0 && NE % (64 * W) == 0, "tile");
+  static_assert(L % LN == 0 && N % NB == 0, "tile");
   struct WaveLds {
     float dt[L][CW], xu[L][CW], B[L][N], C[L][N];
   };
@@ -328,15 +325,14 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) A2[i][j] = i < nv ? a.A[(long)c * N + ng * 4 + j] * LOG2E : 0.f;
   }
-  float H[EPT];  // the owned states at the tile's start
-#pragma unroll
-  for (int e = 0; e < EPT; ++e) {
-    int ch, n;
-    sel_slot<N, CPL>(threadIdx.x + e * 64 * W, ch, n);
-    const bool on = sb.c0 + ch < sb.cend;
-    H[e] = a.h0 && on ? a.h0[((long)sb.seq * a.D + sb.c0 + ch) * N + n] : 0.f;
-    if (sb.seg > 0 && on) H[e] = seg_enter<N, false>(a, sb, sb.c0 + ch, n, H[e]);
-  }
+  // the state that this thread owns, below NE, at the tile's start
+  const int own = threadIdx.x;
+  int oc, on;
+  sel_slot<N, CPL>(own, oc, on);
+  const bool has = own < NE && sb.c0 + oc < sb.cend;
+  const long oat = ((long)sb.seq * a.D + sb.c0 + oc) * N + on;
+  float H = a.h0 && has ? a.h0[oat] : 0.f;
+  if (sb.seg > 0 && has) H = seg_enter<N, false>(a, sb, sb.c0 + oc, on, H);
 
   // byte offsets of the lane's pieces in a tile's rows
   const unsigned tok = w * L + ng, cb = nv > 0 ? (unsigned)cl * EB : BUF_OOB;
@@ -418,6 +414,8 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) h[i][j] = 0.f;
     }
+    const bool live = t0 < len;  // a chunk past the end leaves the state as it is
+    if (live) {
 #pragma unroll
     for (int t = 0; t < L; ++t) {
       __builtin_amdgcn_sched_barrier(0);
@@ -440,6 +438,7 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
         yp[t * CPL + i] = s;
       }
     }
+    }
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
       float p[4];
@@ -450,26 +449,27 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
     }
     __syncthreads();
     // the states at the chunks' starts, each state by its owner
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      const int s = threadIdx.x + e * 64 * W;
+    if (own < NE) {
       float p[W], f[W];
 #pragma unroll
       for (int m = 0; m < W; ++m) {
-        p[m] = ex[m][0][s];
-        f[m] = ex[m][1][s];
+        p[m] = ex[m][0][own];
+        f[m] = ex[m][1][own];
       }
 #pragma unroll
       for (int m = 0; m < W; ++m) {
-        ex[m][1][s] = H[e];
-        H[e] = fmaf(p[m], H[e], f[m]);
+        ex[m][1][own] = H;
+        H = fmaf(p[m], H, f[m]);
       }
     }
     __syncthreads();
+    const auto ry = ty.rows(min(len - base, TILE));
+    ty.step(TILE);
+    if (!live) continue;
 #pragma unroll
     for (int i = 0; i < CPL; ++i) lds_get<4>(&ex[w][1][(i * 64 + lane) * 4], h[i]);
-    if (a.ck && t0 % SELECT_CK == 0 && t0 < len) {
-      float* ck = a.ck + ((long)(sb.tok0 / SELECT_CK + sb.seq + t0 / SELECT_CK) * a.D + cl) * N + ng * 4;
+    if (a.ck && t0 % select_ck(N) == 0) {
+      float* ck = a.ck + ((long)(sb.tok0 / select_ck(N) + sb.seq + t0 / select_ck(N)) * a.D + cl) * N + ng * 4;
 #pragma unroll
       for (int i = 0; i < CPL; ++i)
         if (i < nv) *reinterpret_cast<float4*>(ck + i * N) = make_float4(h[i][0], h[i][1], h[i][2], h[i][3]);
@@ -490,8 +490,6 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
     }
     // sums over the lane groups, LN tokens at a time: lane group ng ends with
     // token ng's, whose u and z it holds
-    const auto ry = ty.rows(min(len - base, TILE));
-    ty.step(TILE);
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
       float* yk = yp + k * LN * CPL;
@@ -508,14 +506,7 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
       store_piece<Tin, CPL, VEC>(ry, yo + k * LN * yb, y, nv);
     }
   }
-  if (a.ht && sb.seg == sb.nseg - 1) {
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      int ch, n;
-      sel_slot<N, CPL>(threadIdx.x + e * 64 * W, ch, n);
-      if (sb.c0 + ch < sb.cend) a.ht[((long)sb.seq * a.D + sb.c0 + ch) * N + n] = H[e];
-    }
-  }
+  if (a.ht && sb.seg == sb.nseg - 1 && has) a.ht[oat] = H;
 }
 
 // Backward.  With gy_t = dy_t silu(z_t) and dh_t the gradient of h_t,
@@ -523,20 +514,20 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
 //   ddt_t = <A, p_t> + u_t <B_t, dh_t>,   dA = sum_t dt_t p_t,   du_t = dt_t <B_t, dh_t> + Dskip gy_t,
 //   dB_t = sum_c dh_t dt_t u_t,           dC_t = sum_c gy_t h_t.
 // A workgroup walks its sequence's tiles from the last to the first.  The
-// states come from the forward's kept ones (one per SELECT_CK = one tile), the
+// states come from the forward's kept ones (one per tile), the
 // gradient through the later tiles is carried.  Inside a tile the chunks run
 // side by side in both directions as in the forward: each wave forms its decays,
 // its state from zero and its gradient from zero, one exchange gives both true
 // ends, and a second pass forms the states (kept in registers) and then the
 // gradients.  dB and dC of the workgroup's channels go to a partial sum.
 template <typename Tin, int N, int CPL, bool VEC, bool Z>
-__global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
-  constexpr int L = 4, W = 8;
+__global__ __launch_bounds__(16 * select_ck(N)) void k_select_bwd(SelectArgs a) {
+  constexpr int L = 4, W = select_ck(N) / L;
   using S = SelTile<N, CPL>;
   constexpr int LN = S::LN, CG = S::CG, CW = S::CW, NE = S::NE, TL = (L + LN - 1) / LN, TILE = L * W;
-  constexpr int NB = L * N / 64 > 0 ? L * N / 64 : 1, EPT = NE / (64 * W);
+  constexpr int NB = L * N / 64 > 0 ? L * N / 64 : 1;
   constexpr unsigned EB = sizeof(Tin);
-  static_assert(TILE == SELECT_CK && NE % (64 * W) == 0, "a tile starts at a kept state");
+  static_assert(64 * W >= NE, "an owner for every state");
   struct WaveLds {
     float dt[L][CW], xu[L][CW], gy[L][CW], yp[L][CW], B[L][N], C[L][N];
     float u[L][CW], slope[L][CW], dz[L][CW], odt[L][CW];  // of a lane's own tokens
@@ -566,18 +557,14 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
       dA[i][j] = 0.f;
     }
   }
-  // owned states: the decayed gradient that enters the tile from the tokens
-  // after it, and the kept state at the tile's start
-  float Gc[EPT], hk[EPT];
-  int own[EPT];  // place in a [D, N] state, negative: none
-#pragma unroll
-  for (int e = 0; e < EPT; ++e) {
-    int ch, n;
-    sel_slot<N, CPL>(threadIdx.x + e * 64 * W, ch, n);
-    own[e] = sb.c0 + ch < sb.cend ? (sb.c0 + ch) * N + n : -1;
-    Gc[e] = a.dht && own[e] >= 0 ? a.dht[(long)sb.seq * a.D * N + own[e]] : 0.f;
-    if (sb.seg < sb.nseg - 1 && own[e] >= 0) Gc[e] = seg_enter<N, true>(a, sb, sb.c0 + ch, n, Gc[e]);
-  }
+  // the state that this thread owns, below NE: the decayed gradient that enters
+  // the tile from the tokens after it, and the kept state at the tile's start
+  int oc, on;
+  sel_slot<N, CPL>(threadIdx.x, oc, on);
+  const bool owner = threadIdx.x < NE, has = owner && sb.c0 + oc < sb.cend;
+  const int own = has ? (sb.c0 + oc) * N + on : sb.c0 * N;  // place in a [D, N] state
+  float Gc = a.dht && has ? a.dht[(long)sb.seq * a.D * N + own] : 0.f, hk;
+  if (sb.seg < sb.nseg - 1 && has) Gc = seg_enter<N, true>(a, sb, sb.c0 + oc, on, Gc);
 
   const unsigned tok = w * L + min(ng, L - 1);
   const unsigned cb = nv > 0 && ng < L ? (unsigned)cl * EB : BUF_OOB;
@@ -594,7 +581,7 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
   RowsAt tb(a.Bm, last, a.b_row * EB), tc(a.Cm, last, a.c_row * EB);
   RowsAt tdu(a.du, last, yb), tdd(a.ddelta, last, yb), tdz(a.dz, last, yb);
   RowsAt tbc(a.bcp, (long)sb.blk * a.Ttot + last, 2 * N * 4);
-  const float* ck = a.ck + (long)(sb.tok0 / SELECT_CK + sb.seq + max(ntiles - 1, 0)) * a.D * N;
+  const float* ck = a.ck + (long)(sb.tok0 / select_ck(N) + sb.seq + max(ntiles - 1, 0)) * a.D * N;
   auto load = [&](int tile) {
     const int rows = min(len - tile * TILE, TILE);
     const auto ru = tu.rows(rows), rd = td.rows(rows), rb = tb.rows(rows), rc = tc.rows(rows);
@@ -612,8 +599,7 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
     }
     pb.load(rb, bo, NB);
     pc.load(rc, co, NB);
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) hk[e] = ck[max(own[e], sb.c0 * N)];
+    hk = ck[own];
     tu.step(-TILE);
     td.step(-TILE);
     if constexpr (Z) tz.step(-TILE);
@@ -625,7 +611,7 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
   if (ntiles > tile0) load(ntiles - 1);
   for (int tile = ntiles - 1; tile >= tile0; --tile) {
     const int base = tile * TILE, t0 = base + w * L;
-    float h[CPL][4], G[CPL][4], hs0[EPT];
+    float h[CPL][4], G[CPL][4];
 #pragma unroll
     for (int k = 0; k < TL; ++k) {
       const int tl = ng + LN * k;
@@ -674,8 +660,7 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
       for (int e = 0; e < NB; ++e) v[e] = pc.get(e);
       lds_put<NB>(&my.C[bt][bs], v);
     }
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) hs0[e] = hk[e];
+    const float hs0 = hk;
     __builtin_amdgcn_wave_barrier();
     if (tile > tile0) load(tile - 1);
 
@@ -722,10 +707,9 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
       lds_put<4>(&ex[w][2][(i * 64 + lane) * 4], G[i]);
     }
     __syncthreads();
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      const int s = threadIdx.x + e * 64 * W;
-      float p[W], f[W], q[W], c = hs0[e];
+    if (owner) {
+      const int s = threadIdx.x;
+      float p[W], f[W], q[W], c = hs0;
 #pragma unroll
       for (int m = 0; m < W; ++m) {
         p[m] = ex[m][0][s];
@@ -739,8 +723,8 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
       }
 #pragma unroll
       for (int m = W - 1; m >= 0; --m) {
-        ex[m][2][s] = Gc[e];
-        Gc[e] = fmaf(p[m], Gc[e], q[m]);
+        ex[m][2][s] = Gc;
+        Gc = fmaf(p[m], Gc, q[m]);
       }
     }
     __syncthreads();
@@ -879,17 +863,13 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
     red[w * 3 * NE + (1 * CPL + i) * 64 + lane] = dbias[i];
   }
   __syncthreads();
+  const long part = (long)(sb.seq * a.segs + sb.seg) * a.D;
+  if (has) {
+    float v = ex[0][0][threadIdx.x];
 #pragma unroll
-  for (int e = 0; e < EPT; ++e) {
-    const int s = threadIdx.x + e * 64 * W;
-    float v = ex[0][0][s];
-#pragma unroll
-    for (int m = 1; m < W; ++m) v += ex[m][0][s];
-    if (own[e] >= 0) {
-      const int c = own[e] / N, n = own[e] % N;
-      a.dap[((long)(sb.seq * a.segs + sb.seg) * a.D + c) * (N + 2) + n] = v;
-      if (a.dh0 && sb.seg == 0) a.dh0[(long)sb.seq * a.D * N + own[e]] = Gc[e];
-    }
+    for (int m = 1; m < W; ++m) v += ex[m][0][threadIdx.x];
+    a.dap[(part + sb.c0 + oc) * (N + 2) + on] = v;
+    if (a.dh0 && sb.seg == 0) a.dh0[(long)sb.seq * a.D * N + own] = Gc;
   }
   const int ch = threadIdx.x % CW, which = threadIdx.x / CW;
   if (which < 2 && sb.c0 + ch < sb.cend) {
@@ -897,7 +877,7 @@ __global__ __launch_bounds__(512) void k_select_bwd(SelectArgs a) {
     for (int m = 0; m < W; ++m)
       for (int e = 0; e < min(LN, L); ++e)
         v += red[m * 3 * NE + (which * CPL + ch % CPL) * 64 + e * CG + ch / CPL];
-    a.dap[((long)(sb.seq * a.segs + sb.seg) * a.D + sb.c0 + ch) * (N + 2) + N + which] = v;
+    a.dap[(part + sb.c0 + ch) * (N + 2) + N + which] = v;
   }
 }
 
@@ -1016,18 +996,16 @@ static bool rows_vec(const SelectArgs& a, int C, int nb, bool bwd) {
   return v && ok(a.dy, a.D, C) && ok(a.du, a.D, C) && ok(a.ddelta, a.D, C) && ok(a.dz, a.D, C);
 }
 
-constexpr int SEL_CPL = 2;  // channels of a lane
-
 template <typename Tin, int N, bool REV>
 static void run_seg(const SelectArgs& a, unsigned grid) {
   if (a.segs <= 1) return;
-  if (rows_vec(a, SEL_CPL, N / 8, REV)) k_select_seg<Tin, N, SEL_CPL, true, REV><<<grid, 512, 0, a.stream>>>(a);
-  else k_select_seg<Tin, N, SEL_CPL, false, REV><<<grid, 512, 0, a.stream>>>(a);
+  if (rows_vec(a, SEL_CPL, N / 8, REV)) k_select_seg<Tin, N, SEL_CPL, true, REV><<<grid, 64 * sel_waves(N), 0, a.stream>>>(a);
+  else k_select_seg<Tin, N, SEL_CPL, false, REV><<<grid, 64 * sel_waves(N), 0, a.stream>>>(a);
 }
 
 template <typename Tin, int N>
 static hipError_t run_fwd(const SelectArgs& a) {
-  constexpr int CPL = SEL_CPL, L = 8, W = 8;
+  constexpr int CPL = SEL_CPL, L = 8, W = sel_waves(N);
   static_assert(SelTile<N, CPL>::CW == select_block_channels(N), "one block of channels throughout");
   const unsigned grid = (unsigned)a.S * a.segs * a.G * a.nblk;
   run_seg<Tin, N, false>(a, grid);
@@ -1046,10 +1024,10 @@ static hipError_t run_bwd(const SelectArgs& a) {
   if (grid > 0) {
     run_seg<Tin, N, true>(a, grid);
     const bool vec = rows_vec(a, CPL, N >= 16 ? N / 16 : 1, true);
-    if (vec && a.z) k_select_bwd<Tin, N, CPL, true, true><<<grid, 512, 0, a.stream>>>(a);
-    else if (vec) k_select_bwd<Tin, N, CPL, true, false><<<grid, 512, 0, a.stream>>>(a);
-    else if (a.z) k_select_bwd<Tin, N, CPL, false, true><<<grid, 512, 0, a.stream>>>(a);
-    else k_select_bwd<Tin, N, CPL, false, false><<<grid, 512, 0, a.stream>>>(a);
+    if (vec && a.z) k_select_bwd<Tin, N, CPL, true, true><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
+    else if (vec) k_select_bwd<Tin, N, CPL, true, false><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
+    else if (a.z) k_select_bwd<Tin, N, CPL, false, true><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
+    else k_select_bwd<Tin, N, CPL, false, false><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
   }
   const long nbc = (long)a.Ttot * a.G * 2 * N, np = (long)a.D * (N + 2);
   if (nbc > 0) k_select_dbc<Tin><<<(unsigned)((nbc + 255) / 256), 256, 0, a.stream>>>(a);
