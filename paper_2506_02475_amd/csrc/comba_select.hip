@@ -67,6 +67,13 @@ __device__ __forceinline__ void lds_put(float* p, const float (&v)[C]) {
   }
 }
 
+// p[c], or 0 without p: loaded without a branch (which would be waited for on the
+// spot) from `any`, which has as many values.
+__device__ __forceinline__ float or_zero(const float* p, const float* any, int c) {
+  const float v = (p ? p : any)[c];
+  return p ? v : 0.f;
+}
+
 // What a workgroup works on: a segment of a sequence and a block of CW channels
 // of one group.  Two neighbouring blocks, which share the 128-byte lines of their
 // rows, go to workgroups eight apart and so to the same XCD.
@@ -87,6 +94,19 @@ __device__ __forceinline__ SelBlock sel_block(const SelectArgs& a) {
   s.blk = b - r * nb;
   s.seq = r / a.segs;
   s.seg = r - s.seq * a.segs;
+  if (a.cu_seqlens && a.S > 1 && a.S <= 64) {
+    // packed: the longest work first (lane l ranks sequence l by its segments'
+    // length), so that no long one starts when the others are done
+    const int l = lane_id();
+    int n = l < a.S ? a.cu_seqlens[l + 1] - a.cu_seqlens[l] : 0;
+    n = n > a.segmin ? min(n, a.seglen) : n;
+    int rank = 0;
+    for (int j = 0; j < a.S; ++j) {
+      const int m = __builtin_amdgcn_readlane(n, j);
+      rank += m > n || (m == n && j < l);
+    }
+    s.seq = __builtin_ctzll(__ballot(l < a.S && rank == s.seq));
+  }
   s.g = s.blk / nblk;
   s.c0 = s.g * Dg + (s.blk - s.g * nblk) * CW;
   s.cend = min(s.c0 + CW, (s.g + 1) * Dg);
@@ -135,18 +155,6 @@ __global__ __launch_bounds__(64 * sel_waves(N)) void k_select_seg(SelectArgs a) 
   WaveLds& my = lds[w];
   const bool gate = REV && a.z;
 
-  float A2[CPL][4], bias[CPL], total[CPL];
-#pragma unroll
-  for (int i = 0; i < CPL; ++i) {
-    const int c = i < nv ? cl + i : sb.c0;
-    bias[i] = a.bias ? a.bias[c] : 0.f;
-    total[i] = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) A2[i][j] = i < nv ? a.A[(long)c * N + ng * 4 + j] * LOG2E : 0.f;
-  }
-  const int own = threadIdx.x;  // the state that this thread owns, below NE
-  float H = 0.f;
-
   const unsigned tok = w * L + ng, cb = nv > 0 ? (unsigned)cl * EB : BUF_OOB;
   const long xrow = REV ? a.D : a.u_row, rrow = REV ? a.c_row : a.b_row;
   const unsigned xb = xrow * EB, db = a.delta_row * EB, zb = a.z_row * EB;
@@ -179,6 +187,21 @@ __global__ __launch_bounds__(64 * sel_waves(N)) void k_select_seg(SelectArgs a) 
     tr.step(dir);
   };
   load(0);
+
+  float A2[CPL][4], bias[CPL], total[CPL];
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    const int c = i < nv ? cl + i : sb.c0;
+    bias[i] = or_zero(a.bias, a.A, c);
+    total[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float v = a.A[(long)c * N + ng * 4 + j];
+      A2[i][j] = i < nv ? v * LOG2E : 0.f;
+    }
+  }
+  const int own = threadIdx.x;  // the state that this thread owns, below NE
+  float H = 0.f;
   for (int tile = 0; tile < tiles; ++tile) {
     const int t0 = sb.t0 + (REV ? tiles - 1 - tile : tile) * TILE + w * L;
 #pragma unroll
@@ -316,24 +339,6 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
   if (sb.seg > 0 && sb.t0 >= len) return;
   WaveLds& my = lds[w];
 
-  float A2[CPL][4], h[CPL][4], bias[CPL], skip[CPL];
-#pragma unroll
-  for (int i = 0; i < CPL; ++i) {
-    const int c = i < nv ? cl + i : sb.c0;
-    bias[i] = a.bias ? a.bias[c] : 0.f;
-    skip[i] = a.Dskip ? a.Dskip[c] : 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) A2[i][j] = i < nv ? a.A[(long)c * N + ng * 4 + j] * LOG2E : 0.f;
-  }
-  // the state that this thread owns, below NE, at the tile's start
-  const int own = threadIdx.x;
-  int oc, on;
-  sel_slot<N, CPL>(own, oc, on);
-  const bool has = own < NE && sb.c0 + oc < sb.cend;
-  const long oat = ((long)sb.seq * a.D + sb.c0 + oc) * N + on;
-  float H = a.h0 && has ? a.h0[oat] : 0.f;
-  if (sb.seg > 0 && has) H = seg_enter<N, false>(a, sb, sb.c0 + oc, on, H);
-
   // byte offsets of the lane's pieces in a tile's rows
   const unsigned tok = w * L + ng, cb = nv > 0 ? (unsigned)cl * EB : BUF_OOB;
   const unsigned ub = a.u_row * EB, db = a.delta_row * EB, zb = a.z_row * EB, yb = a.D * EB;
@@ -368,6 +373,27 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
     tc.step(TILE);
   };
   if (sb.t0 < len) load(sb.t0);
+
+  float A2[CPL][4], h[CPL][4], bias[CPL], skip[CPL];
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    const int c = i < nv ? cl + i : sb.c0;
+    bias[i] = or_zero(a.bias, a.A, c);
+    skip[i] = or_zero(a.Dskip, a.A, c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float v = a.A[(long)c * N + ng * 4 + j];
+      A2[i][j] = i < nv ? v * LOG2E : 0.f;
+    }
+  }
+  // the state that this thread owns, below NE, at the tile's start
+  const int own = threadIdx.x;
+  int oc, on;
+  sel_slot<N, CPL>(own, oc, on);
+  const bool has = own < NE && sb.c0 + oc < sb.cend;
+  const long oat = ((long)sb.seq * a.D + sb.c0 + oc) * N + on;
+  float H = a.h0 && has ? a.h0[oat] : 0.f;
+  if (sb.seg > 0 && has) H = seg_enter<N, false>(a, sb, sb.c0 + oc, on, H);
   for (int base = sb.t0; base < len; base += TILE) {
     const int t0 = base + w * L;
     // stage the chunk: dt and dt u per (token, channel), B and C in fp32; past
@@ -544,27 +570,13 @@ __global__ __launch_bounds__(16 * select_ck(N)) void k_select_bwd(SelectArgs a) 
   const int ntiles = sb.t0 < len ? (len + TILE - 1) / TILE : tile0;
   WaveLds& my = lds[w];
 
-  float A2[CPL][4], dA[CPL][4], bias[CPL], skip[CPL], dD[CPL], dbias[CPL];
-#pragma unroll
-  for (int i = 0; i < CPL; ++i) {
-    const int c = i < nv ? cl + i : sb.c0;
-    bias[i] = a.bias ? a.bias[c] : 0.f;
-    skip[i] = a.Dskip ? a.Dskip[c] : 0.f;
-    dD[i] = dbias[i] = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      A2[i][j] = i < nv ? a.A[(long)c * N + ng * 4 + j] * LOG2E : 0.f;
-      dA[i][j] = 0.f;
-    }
-  }
   // the state that this thread owns, below NE: the decayed gradient that enters
   // the tile from the tokens after it, and the kept state at the tile's start
   int oc, on;
   sel_slot<N, CPL>(threadIdx.x, oc, on);
   const bool owner = threadIdx.x < NE, has = owner && sb.c0 + oc < sb.cend;
   const int own = has ? (sb.c0 + oc) * N + on : sb.c0 * N;  // place in a [D, N] state
-  float Gc = a.dht && has ? a.dht[(long)sb.seq * a.D * N + own] : 0.f, hk;
-  if (sb.seg < sb.nseg - 1 && has) Gc = seg_enter<N, true>(a, sb, sb.c0 + oc, on, Gc);
+  float Gc, hk;
 
   const unsigned tok = w * L + min(ng, L - 1);
   const unsigned cb = nv > 0 && ng < L ? (unsigned)cl * EB : BUF_OOB;
@@ -609,6 +621,23 @@ __global__ __launch_bounds__(16 * select_ck(N)) void k_select_bwd(SelectArgs a) 
     ck -= (long)a.D * N;
   };
   if (ntiles > tile0) load(ntiles - 1);
+
+  float A2[CPL][4], dA[CPL][4], bias[CPL], skip[CPL], dD[CPL], dbias[CPL];
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    const int c = i < nv ? cl + i : sb.c0;
+    bias[i] = or_zero(a.bias, a.A, c);
+    skip[i] = or_zero(a.Dskip, a.A, c);
+    dD[i] = dbias[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float v = a.A[(long)c * N + ng * 4 + j];
+      A2[i][j] = i < nv ? v * LOG2E : 0.f;
+      dA[i][j] = 0.f;
+    }
+  }
+  Gc = a.dht && has ? a.dht[(long)sb.seq * a.D * N + own] : 0.f;
+  if (sb.seg < sb.nseg - 1 && has) Gc = seg_enter<N, true>(a, sb, sb.c0 + oc, on, Gc);
   for (int tile = ntiles - 1; tile >= tile0; --tile) {
     const int base = tile * TILE, t0 = base + w * L;
     float h[CPL][4], G[CPL][4];
@@ -881,22 +910,31 @@ __global__ __launch_bounds__(16 * select_ck(N)) void k_select_bwd(SelectArgs a) 
   }
 }
 
-// dB, dC of every (token, group, state): the channel blocks' partial sums in order.
+// dB, dC of every (token, group, state): the channel blocks' partial sums in
+// order, four values a thread.
 template <typename Tin>
 __global__ __launch_bounds__(256) void k_select_dbc(SelectArgs a) {
   const int N2 = 2 * a.N;
   const long n = (long)a.Ttot * a.G * N2;
-  const long e = (long)blockIdx.x * 256 + threadIdx.x;
+  const long e = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
   if (e >= n) return;
   const int s = e % N2;
   const long tg = e / N2;
   const int g = tg / a.Ttot;
   const long t = tg % a.Ttot;
-  const float* p = a.bcp + ((long)g * a.nblk * a.Ttot + t) * N2 + s;
-  float sum = 0.f;
-  for (int b = 0; b < a.nblk; ++b) sum += p[(long)b * a.Ttot * N2];
-  Tin* out = static_cast<Tin*>(s < a.N ? a.dB : a.dC);
-  store_elem(out + (t * a.G + g) * a.N + (s < a.N ? s : s - a.N), sum);
+  const float4* p = reinterpret_cast<const float4*>(a.bcp + ((long)g * a.nblk * a.Ttot + t) * N2 + s);
+  const long row = (long)a.Ttot * N2 / 4;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int b = 0; b < a.nblk; ++b) {
+    const float4 f = p[b * row];
+    v = make_float4(v.x + f.x, v.y + f.y, v.z + f.z, v.w + f.w);
+  }
+  Tin* out = static_cast<Tin*>(s < a.N ? a.dB : a.dC) + (t * a.G + g) * a.N + (s < a.N ? s : s - a.N);
+  store_elem(out, v.x);
+  store_elem(out + 1, v.y);
+  store_elem(out + 2, v.z);
+  store_elem(out + 3, v.w);
 }
 
 // dA, dD and dbias: the segments' partial sums in order.
@@ -1029,7 +1067,7 @@ static hipError_t run_bwd(const SelectArgs& a) {
     else if (a.z) k_select_bwd<Tin, N, CPL, false, true><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
     else k_select_bwd<Tin, N, CPL, false, false><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
   }
-  const long nbc = (long)a.Ttot * a.G * 2 * N, np = (long)a.D * (N + 2);
+  const long nbc = (long)a.Ttot * a.G * 2 * N / 4, np = (long)a.D * (N + 2);
   if (nbc > 0) k_select_dbc<Tin><<<(unsigned)((nbc + 255) / 256), 256, 0, a.stream>>>(a);
   k_select_dparam<<<(unsigned)((np + 255) / 256), 256, 0, a.stream>>>(a);
   return hipGetLastError();
