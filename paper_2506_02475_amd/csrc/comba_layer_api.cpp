@@ -52,7 +52,7 @@ comba_status check_rows(const Shape* s, Rows* r) {
   return COMBA_OK;
 }
 
-// Rows of up to 4M values: the byte offsets inside a tile of 64 rows stay below 2^31.
+// Rows of up to 4M values: the byte offsets inside a tile of 96 rows stay below 2^31.
 constexpr int64_t kMaxRow = (int64_t)1 << 22;
 
 // The elements between rows of a named input: given, or contiguous.

@@ -18,8 +18,7 @@ from __future__ import annotations
 import ctypes
 import struct
 
-from . import (COMBA_BF16, COMBA_F32, CombaError, _check, _host_offsets, _ptr, _stream,
-               load_library)
+from . import (COMBA_BF16, COMBA_F32, CombaError, _check, _host_offsets, _ptr, load_library)
 
 __all__ = ["comba_conv_fwd", "comba_conv_bwd", "comba_conv_step", "comba_conv",
            "comba_select_fwd", "comba_select_fwd_save", "comba_select_bwd", "comba_select_step",
@@ -189,6 +188,22 @@ def _run(status):
         _check(status)
 
 
+def _on(stream, dev, *made):
+    """The stream handle of a call.  Tensors that the call makes on another stream than
+    torch's current one are marked as used there, so that their memory is not given away
+    while the kernels still run."""
+    import torch
+
+    here = torch._C._cuda_getCurrentRawStream(dev)
+    if stream is None or stream == here:
+        return here
+    ext = torch.cuda.ExternalStream(stream, device=dev)
+    for t in made:
+        if t is not None:
+            t.record_stream(ext)
+    return stream
+
+
 # ---- short causal convolution -------------------------------------------------
 _CONV_ACT = (None, "none", "silu")
 
@@ -224,7 +239,7 @@ def comba_conv_fwd(x, w, bias=None, h0=None, *, activation="silu", cu_seqlens=No
     y = x.new_empty(x.shape)
     ht = x.new_empty(state) if output_final_state else None
     _run(load_library().comba_conv_fwd(shp, *ptrs, y.data_ptr(), _ptr(ht),
-                                       _stream(stream, x.device)))
+                                       _on(stream, dev, y, ht)))
     return y, ht
 
 
@@ -244,7 +259,7 @@ def comba_conv_bwd(x, w, bias, h0, dy, dht=None, *, activation="silu", cu_seqlen
     ws = _workspace(lib.comba_conv_workspace_bytes, shp, workspace, x.device)
     _run(lib.comba_conv_bwd(shp, *ptrs, *grads, _ptr(out["dx"]), _ptr(out["dw"]),
                             _ptr(out["dbias"]), _ptr(out["dh0"]), _ptr(ws), ws.numel(),
-                            _stream(stream, x.device)))
+                            _on(stream, dev, ws, *out.values())))
     return out
 
 
@@ -267,7 +282,7 @@ def comba_conv_step(x, w, bias, state, *, slots=None, activation="silu", stream=
         shp, x.data_ptr(), _dense("w", w, taps, torch.float32, dev),
         _dense("bias", bias, (D,), torch.float32, dev),
         _dense("state", state, (pool[0], K - 1, D), dt, dev), _slots(slots, B, dev), pool[0],
-        y.data_ptr(), _stream(stream, x.device)))
+        y.data_ptr(), _on(stream, dev, y)))
     return y
 
 
@@ -324,7 +339,7 @@ def _select(save, u, delta, A, B, C, D, z, delta_bias, h0, delta_softplus, cu_se
     ws = _workspace(size, shp, workspace, u.device)
     fn = lib.comba_select_fwd_save if save else lib.comba_select_fwd
     _run(fn(shp, *ptrs, h0p, y.data_ptr(), _ptr(ht), ws.data_ptr(), ws.numel(),
-            _stream(stream, u.device)))
+            _on(stream, u.get_device(), y, ht, ws)))
     return y, ht, ws
 
 
@@ -383,7 +398,7 @@ def comba_select_bwd(u, delta, A, B, C, D, z, delta_bias, h0, dy, dht=None, *, w
     _run(lib.comba_select_bwd(
         shp, *ptrs, *given, *(_ptr(out[k]) for k in ("du", "ddelta", "dA", "dB", "dC", "dD", "dz",
                                                      "ddelta_bias", "dh0")),
-        workspace.data_ptr(), workspace.numel(), _stream(stream, u.device)))
+        workspace.data_ptr(), workspace.numel(), _on(stream, dev, *out.values())))
     return out
 
 
@@ -403,7 +418,7 @@ def comba_select_step(u, delta, A, B, C, D, z, delta_bias, state, *, slots=None,
     y = u.new_empty(shape)
     _run(load_library().comba_select_step(
         shp, *ptrs, _dense("state", state, (pool[0], shape[1], n), torch.float32, dev),
-        _slots(slots, rows, dev), pool[0], y.data_ptr(), _stream(stream, u.device)))
+        _slots(slots, rows, dev), pool[0], y.data_ptr(), _on(stream, dev, y)))
     return y
 
 
@@ -442,7 +457,8 @@ def comba_group_norm_fwd(x, groups, weight=None, bias=None, z=None, *, activatio
     out = out_dtype or (x.dtype if z is None else z.dtype)
     shp, ptrs = _norm_shape(x, groups, weight, bias, z, activation, eps, out)
     y = x.new_empty(x.shape, dtype=out)
-    _run(load_library().comba_group_norm_fwd(shp, *ptrs, y.data_ptr(), _stream(stream, x.device)))
+    _run(load_library().comba_group_norm_fwd(shp, *ptrs, y.data_ptr(),
+                                             _on(stream, x.get_device(), y)))
     return y
 
 
@@ -459,7 +475,7 @@ def comba_group_norm_bwd(x, groups, weight, bias, z, dy, *, activation="silu", e
     ws = _workspace(lib.comba_group_norm_workspace_bytes, shp, workspace, x.device)
     _run(lib.comba_group_norm_bwd(shp, *ptrs, dyp, _ptr(out["dx"]), _ptr(out["dz"]),
                                   _ptr(out["dweight"]), _ptr(out["dbias"]), ws.data_ptr(),
-                                  ws.numel(), _stream(stream, x.device)))
+                                  ws.numel(), _on(stream, x.get_device(), ws, *out.values())))
     return out
 
 

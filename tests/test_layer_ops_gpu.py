@@ -605,3 +605,68 @@ def test_select_rows_cut_into_segments(name, kw):
     """Few long rows: their segments run side by side."""
     _log("select segments " + name)
     _check_select("seg_" + name, kw)
+
+
+def test_a_stream_given_by_handle():
+    """Every call on a stream that is not torch's current one, its temporary memory reused by the
+    current stream right after: the results are those of the current stream."""
+    import torch
+
+    import paper_2506_02475_amd as comba
+
+    _log("stream handle")
+    host, dev, _, _, ddy, _, _, call, _ = _select_case("handle", B=2, T=400, D=96, N=16)
+    c, d, _, ccall, _ = _conv_case("handle", B=2, T=300, D=64, K=4)
+    _, ndev, _, ndy, act, _, _ = _norm_case("handle", rows=300, C=256, G=2, gate=True)
+
+    def calls(s):
+        y, ht, ws = comba.comba_select_fwd_save(*dev, stream=s, **call)
+        out = [y, ht]
+        gr = comba.comba_select_bwd(*dev, ddy, workspace=ws, stream=s, **call)
+        out += [gr[k] for k in sorted(gr)]
+        out += list(comba.comba_select_fwd(*dev, stream=s, **call))
+        out += list(comba.comba_conv_fwd(d["x"], d["w"], d["b"], d["h0"], stream=s, **ccall))
+        gr = comba.comba_conv_bwd(d["x"], d["w"], d["b"], d["h0"], d["dy"], stream=s, **ccall)
+        out += [gr[k] for k in sorted(gr)]
+        out.append(comba.comba_group_norm_fwd(*ndev, activation=act, stream=s))
+        gr = comba.comba_group_norm_bwd(*ndev, ndy, activation=act, stream=s)
+        out += [gr[k] for k in sorted(gr)]
+        del ws
+        for _ in range(8):  # the current stream takes what was freed
+            torch.full((1 << 20,), float("nan"), device="cuda")
+        return out
+
+    want = calls(None)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = calls(side.cuda_stream)
+    torch.cuda.synchronize()
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert torch.equal(a, b), i
+
+
+def test_values_before_a_nan_are_untouched():
+    """A NaN reaches its own channel's later outputs, not the earlier ones of its chunk, tile or
+    segment; its gradients not the later tokens'."""
+    import torch
+
+    import paper_2506_02475_amd as comba
+
+    _log("before a NaN")
+    host, dev, _, _, ddy, _, _, call, _ = _select_case("causal", B=1, T=700, D=40, N=16)
+    y0, _, ws = comba.comba_select_fwd_save(*dev, **call)
+    g0 = comba.comba_select_bwd(*dev, ddy, workspace=ws, **call)
+    for t in (0, 5, 333, 699):
+        u = dev[0].clone()
+        u[0, t, 7] = float("nan")
+        y, _, _ = comba.comba_select_fwd_save(u, *dev[1:], **call)
+        assert torch.equal(y[0, :t], y0[0, :t]) and torch.isnan(y[0, t:, 7]).all()
+        other = [c for c in range(40) if c != 7]
+        assert torch.equal(y[0][:, other], y0[0][:, other])
+        dy = ddy.clone()
+        dy[0, t, 7] = float("nan")
+        g = comba.comba_select_bwd(*dev, dy, workspace=ws, **call)
+        for n in ("du", "ddelta"):
+            assert torch.equal(g[n][0, t + 1:], g0[n][0, t + 1:]), (t, n)
+            assert torch.isnan(g[n][0, :t + 1, 7]).all(), (t, n)
+            assert torch.equal(g[n][0][:, other], g0[n][0][:, other]), (t, n)
