@@ -82,7 +82,8 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a) {
   const int pieces = (a.D + C - 1) / C, nruns = (a.Ttot + a.run - 1) / a.run;
   const long e = (long)blockIdx.x * 256 + threadIdx.x;
   const long r = e / pieces;
-  const auto [c, nv] = conv_piece<C>(e % pieces, a.D);
+  const ConvPiece cp = conv_piece<C>(e % pieces, a.D);
+  const int c = cp.c, nv = cp.nv;
   if (r >= nruns) {  // the final histories
     const long k = r - nruns;
     if (!a.ht || k >= (long)a.N * (K - 1)) return;
@@ -112,29 +113,38 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a) {
     Piece<Tin, C, VEC> xn[CONV_PF];
 #pragma unroll
     for (int k = 0; k < CONV_PF; ++k) xn[k].load(x + (long)min(tb + CONV_PF + k, t1 - 1) * a.x_row, nv);
-#pragma unroll
-    for (int k = 0; k < CONV_PF; ++k) {
+    auto token = [&](int k) {
       const int t = tb + k;
-      if (t < t1) {
-        if (t >= se) {  // the next sequence starts with its own history
-          seq_of_token(a.cu_seqlens, a.N, a.Tseq, a.Ttot, t, s, sa, se);
+      float o[C];
 #pragma unroll
-          for (int m = 0; m < K - 1; ++m) load_ext<Tin, K, C, VEC>(a, s, sa, m - (K - 1), c, nv, xw[m]);
+      for (int i = 0; i < C; ++i) {
+        const float xv = xr[k].get(i);
+        float u = b[i];
+#pragma unroll
+        for (int m = 0; m < K - 1; ++m) u = fmaf(wt[m][i], xw[m][i], u);
+        u = fmaf(wt[K - 1][i], xv, u);
+        o[i] = a.silu ? u * sigmoid_acc(u) : u;
+#pragma unroll
+        for (int m = 0; m < K - 2; ++m) xw[m][i] = xw[m + 1][i];
+        xw[K - 2][i] = xv;
+      }
+      store_piece<Tin, C, VEC>(y + (long)t * a.D, o, nv);
+    };
+    if (tb + CONV_PF <= min(t1, se)) {  // inside one sequence: straight-line code
+#pragma unroll
+      for (int k = 0; k < CONV_PF; ++k) token(k);
+    } else {
+#pragma unroll
+      for (int k = 0; k < CONV_PF; ++k) {
+        const int t = tb + k;
+        if (t < t1) {
+          if (t >= se) {  // the next sequence starts with its own history
+            seq_of_token(a.cu_seqlens, a.N, a.Tseq, a.Ttot, t, s, sa, se);
+#pragma unroll
+            for (int m = 0; m < K - 1; ++m) load_ext<Tin, K, C, VEC>(a, s, sa, m - (K - 1), c, nv, xw[m]);
+          }
+          token(k);
         }
-        float o[C];
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
-          const float xv = xr[k].get(i);
-          float u = b[i];
-#pragma unroll
-          for (int m = 0; m < K - 1; ++m) u = fmaf(wt[m][i], xw[m][i], u);
-          u = fmaf(wt[K - 1][i], xv, u);
-          o[i] = a.silu ? u * sigmoid_acc(u) : u;
-#pragma unroll
-          for (int m = 0; m < K - 2; ++m) xw[m][i] = xw[m + 1][i];
-          xw[K - 2][i] = xv;
-        }
-        store_piece<Tin, C, VEC>(y + (long)t * a.D, o, nv);
       }
     }
 #pragma unroll
@@ -255,29 +265,21 @@ __global__ __launch_bounds__(64 * CONV_BWAVES) void k_conv_bwd(ConvArgs a) {
     const Tin *x = static_cast<const Tin*>(a.x) + c, *dy = static_cast<const Tin*>(a.dy) + c;
     const int tstop = min(t1 + K - 1, a.Ttot);
     bool done = false;
-    for (int tb = t0; tb < tstop && !done; tb += CONV_PF) {
-      Piece<Tin, C, VEC> xb[CONV_PF], gb[CONV_PF];
+    Piece<Tin, C, VEC> xb[CONV_PF], gb[CONV_PF], xn[CONV_PF], gn[CONV_PF];
+    auto load = [&](int tb, Piece<Tin, C, VEC>(&xp)[CONV_PF], Piece<Tin, C, VEC>(&gp)[CONV_PF]) {
 #pragma unroll
       for (int k = 0; k < CONV_PF; ++k) {
         const long row = min(tb + k, tstop - 1);
-        xb[k].load(x + row * a.x_row, nl);
-        gb[k].load(dy + row * a.D, nl);
+        xp[k].load(x + row * a.x_row, nl);
+        gp[k].load(dy + row * a.D, nl);
       }
-#pragma unroll
-      for (int k = 0; k < CONV_PF; ++k) {
-        const int t = tb + k;
-        if (t >= tstop || done) continue;
-        if (t >= se) {
-#pragma unroll
-          for (int m = 0; m < K - 1; ++m) put(t - (K - 1) + m, acc[m]);
-          if (t >= t1) {
-            done = true;
-            continue;
-          }
-          seq_of_token(a.cu_seqlens, a.N, a.Tseq, a.Ttot, t, s, sa, se);
-          enter(t);
-        }
-        const bool mine = t < t1;
+    };
+    load(t0, xb, gb);
+    for (int tb = t0; tb < tstop && !done; tb += CONV_PF) {
+      load(tb + CONV_PF, xn, gn);  // in flight while this block is worked on
+      // du of token tb + k, its part of the open rows and (mine) of dw and dbias;
+      // row t - (K - 1) is then complete in acc[0]
+      auto token = [&](int k, bool mine) {
 #pragma unroll
         for (int i = 0; i < C; ++i) {
           const float xv = xb[k].get(i);
@@ -302,13 +304,47 @@ __global__ __launch_bounds__(64 * CONV_BWAVES) void k_conv_bwd(ConvArgs a) {
           for (int m = 0; m < K - 2; ++m) xw[m][i] = xw[m + 1][i];
           xw[K - 2][i] = xv;
         }
-        put(t - (K - 1), acc[0]);
+      };
+      auto next_row = [&]() {
 #pragma unroll
         for (int i = 0; i < C; ++i) {
 #pragma unroll
           for (int m = 0; m < K - 1; ++m) acc[m][i] = acc[m + 1][i];
           acc[K - 1][i] = 0.f;
         }
+      };
+      if (tb - (K - 1) >= max(t0, sa) && tb + CONV_PF <= min(t1, se)) {
+        // the block and the rows it completes are this run's, inside one sequence
+#pragma unroll
+        for (int k = 0; k < CONV_PF; ++k) {
+          token(k, true);
+          store_piece<Tin, C, VEC>(static_cast<Tin*>(a.dx) + (long)(tb + k - (K - 1)) * a.D + c, acc[0], nv);
+          next_row();
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < CONV_PF; ++k) {
+          const int t = tb + k;
+          if (t >= tstop || done) continue;
+          if (t >= se) {
+#pragma unroll
+            for (int m = 0; m < K - 1; ++m) put(t - (K - 1) + m, acc[m]);
+            if (t >= t1) {
+              done = true;
+              continue;
+            }
+            seq_of_token(a.cu_seqlens, a.N, a.Tseq, a.Ttot, t, s, sa, se);
+            enter(t);
+          }
+          token(k, t < t1);
+          put(t - (K - 1), acc[0]);
+          next_row();
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < CONV_PF; ++k) {
+        xb[k] = xn[k];
+        gb[k] = gn[k];
       }
     }
     if (!done) {  // the tokens end here, or the walk stopped inside a sequence past t1
