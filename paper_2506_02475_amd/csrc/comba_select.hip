@@ -910,10 +910,25 @@ __global__ __launch_bounds__(16 * select_ck(N)) void k_select_bwd(SelectArgs a) 
   }
 }
 
-// dB, dC of every (token, group, state): the channel blocks' partial sums in
-// order, four values a thread.
+// The sums after the main kernel, in one launch: the first `nbc` workgroups add dB
+// and dC of every (token, group, state) over the channel blocks, four values a
+// thread, the others dA, dD and dbias over the segments; both in order.
 template <typename Tin>
-__global__ __launch_bounds__(256) void k_select_dbc(SelectArgs a) {
+__global__ __launch_bounds__(256) void k_select_sums(SelectArgs a, int nbc) {
+  if ((int)blockIdx.x >= nbc) {
+    const int w = a.N + 2;
+    const long n = (long)a.D * w, e = (long)(blockIdx.x - nbc) * 256 + threadIdx.x;
+    if (e >= n) return;
+    float sum = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < a.S * a.segs; ++s) sum += a.dap[s * n + e];
+    const int k = e % w;
+    const long c = e / w;
+    if (k < a.N) a.dA[c * a.N + k] = sum;
+    else if (k == a.N) { if (a.dD) a.dD[c] = sum; }
+    else if (a.dbias) a.dbias[c] = sum;
+    return;
+  }
   const int N2 = 2 * a.N;
   const long n = (long)a.Ttot * a.G * N2;
   const long e = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
@@ -935,21 +950,6 @@ __global__ __launch_bounds__(256) void k_select_dbc(SelectArgs a) {
   store_elem(out + 1, v.y);
   store_elem(out + 2, v.z);
   store_elem(out + 3, v.w);
-}
-
-// dA, dD and dbias: the segments' partial sums in order.
-__global__ __launch_bounds__(256) void k_select_dparam(SelectArgs a) {
-  const int N2 = a.N + 2;
-  const long n = (long)a.D * N2;
-  const long e = (long)blockIdx.x * 256 + threadIdx.x;
-  if (e >= n) return;
-  float sum = 0.f;
-  for (int s = 0; s < a.S * a.segs; ++s) sum += a.dap[s * n + e];
-  const int k = e % N2;
-  const long c = e / N2;
-  if (k < a.N) a.dA[c * a.N + k] = sum;
-  else if (k == a.N) { if (a.dD) a.dD[c] = sum; }
-  else if (a.dbias) a.dbias[c] = sum;
 }
 
 // One token per row: a lane holds 4 states of one channel, consecutive lanes
@@ -1067,9 +1067,9 @@ static hipError_t run_bwd(const SelectArgs& a) {
     else if (a.z) k_select_bwd<Tin, N, CPL, false, true><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
     else k_select_bwd<Tin, N, CPL, false, false><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
   }
-  const long nbc = (long)a.Ttot * a.G * 2 * N / 4, np = (long)a.D * (N + 2);
-  if (nbc > 0) k_select_dbc<Tin><<<(unsigned)((nbc + 255) / 256), 256, 0, a.stream>>>(a);
-  k_select_dparam<<<(unsigned)((np + 255) / 256), 256, 0, a.stream>>>(a);
+  const long nbc = ((long)a.Ttot * a.G * 2 * N / 4 + 255) / 256, np = ((long)a.D * (N + 2) + 255) / 256;
+  if (nbc + np > INT32_MAX) return hipErrorInvalidValue;
+  k_select_sums<Tin><<<(unsigned)(nbc + np), 256, 0, a.stream>>>(a, (int)nbc);
   return hipGetLastError();
 }
 

@@ -80,16 +80,23 @@ def bind(lib):
 
 # ---- argument checks -------------------------------------------------------
 def _code(t, name):
-    import torch
-
     if t.get_device() < 0:
         raise CombaError("comba: tensors must be on a GPU device")
-    dt = t.dtype
-    if dt is torch.bfloat16:
-        return COMBA_BF16
-    if dt is torch.float32:
-        return COMBA_F32
-    raise CombaError("comba: %s must be bfloat16 or float32" % name)
+    code = _codes().get(t.dtype)
+    if code is None:
+        raise CombaError("comba: %s must be bfloat16 or float32" % name)
+    return code
+
+
+_CODES = {}
+
+
+def _codes():
+    if not _CODES:
+        import torch
+
+        _CODES.update({torch.bfloat16: COMBA_BF16, torch.float32: COMBA_F32})
+    return _CODES
 
 
 def _dense(name, t, shape, dtype, dev):
@@ -274,13 +281,12 @@ def comba_conv_step(x, w, bias, state, *, slots=None, activation="silu", stream=
     if len(shape) != 2 or len(taps) != 2 or taps[0] != shape[1] or len(pool) != 3:
         raise CombaError("comba: x must be [B,D], w [D,K] and state [S,K-1,D]")
     B, D = shape
-    K, dt = taps[1], x.dtype
+    K, dt, f32 = taps[1], x.dtype, torch.float32
     shp = _CONV.pack(B, 1, D, K, B, 0, 0, code, _activation(activation, _CONV_ACT),
                      _row("x", x, 1, shape, dt, dev))
     y = x.new_empty(shape)
     _run(load_library().comba_conv_step(
-        shp, x.data_ptr(), _dense("w", w, taps, torch.float32, dev),
-        _dense("bias", bias, (D,), torch.float32, dev),
+        shp, x.data_ptr(), _dense("w", w, taps, f32, dev), _dense("bias", bias, (D,), f32, dev),
         _dense("state", state, (pool[0], K - 1, D), dt, dev), _slots(slots, B, dev), pool[0],
         y.data_ptr(), _on(stream, dev, y)))
     return y
