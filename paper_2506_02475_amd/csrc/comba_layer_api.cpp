@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "comba_layer.h"
 #include "comba_layer_launch.h"
 
@@ -91,59 +93,152 @@ struct SelectLayout {
   size_t ck, bcp, dap, segF, segdt, total;
 };
 
-// Cuts rows into segments when their workgroups, one per CU, leave CUs idle or
-// wait for a long row: the main kernel then runs over segments side by side,
-// after a first pass over all but one segment of each row that is cut (`pre` of
-// the main kernel's time per token).  Packed rows of up to a CU's share of all
-// tokens stay whole.  Takes the number with the least time, counted in tokens
-// walked one after the other (`launch`: the first pass's launch and the
-// segments' starts).  Measured, whole rows / segments, us: 16 states, one row of
-// 8,192 tokens, 2,048 channels: forward 387 / 167, backward 1,022 / 361; 1,000
-// tokens: forward 54 / 31; 4 rows of 4,096, which fill the CUs: 219 whole, 297 to
-// 321 cut.
-void select_segments(comba::SelectArgs* a, bool bwd) {
+// `count` sequences' workgroups of `tokens` each, one per channel block.
+struct Batch {
+  double tokens;
+  int64_t count;
+};
+
+// Tokens walked one after the other until the batches, in their order, are done by
+// `cus` CUs with one workgroup each (`start`: a workgroup's own, in tokens).
+double makespan(const Batch* batch, int n, int64_t blocks, int cus, double start) {
+  struct Load {
+    double t;
+    int cus;
+  } load[comba::SEL_LIST + 19] = {{0, cus}};
+  auto later = [](const Load& x, const Load& y) { return x.t > y.t; };
+  int m = 1;
+  double all = 0, last = 0;
+  for (int i = 0; i < n; ++i) {
+    int64_t need = batch[i].count * blocks;
+    const double t = batch[i].tokens + start;
+    if (need >= 4 * cus) {  // whole rounds at once
+      const int64_t k = need / cus - 2;
+      all += (double)k * t;
+      need -= k * cus;
+    }
+    while (need > 0) {  // the CUs that are free first
+      std::pop_heap(load, load + m, later);
+      Load& f = load[m - 1];
+      const int k = need < f.cus ? (int)need : f.cus;
+      need -= k;
+      const Load done{f.t + t, k};
+      if (done.t > last) last = done.t;
+      if (k < f.cus) {
+        f.cus -= k;
+        std::push_heap(load, load + m, later);
+        ++m;
+      }
+      load[m - 1] = done;
+      std::push_heap(load, load + m, later);
+    }
+  }
+  return all + last;
+}
+
+// The work rows.  Sequences are cut into segments where their workgroups, one per
+// CU, leave CUs idle or wait for a long one: the main kernel then runs over segments
+// side by side, after a first pass over all but one segment of each sequence that is
+// cut.  Packed sequences of up to a CU's share of all tokens stay whole; without
+// host offsets all do.  Takes the number of segments whose workgroups, one after
+// the other to the first free CU, are done first; times in tokens of the main
+// kernel (`pre`: the first pass's per token; `launch`: its launch; `start`: a
+// workgroup's first loads and segment ends), fitted to 56 batches measured at 1 to
+// 32 segments, over which the choice is 1.5% above the best on average.  Whole /
+// cut, us, 16 states, 2,048 channels, forward and backward: one row of 8,192 tokens
+// 341 / 155 and 884 / 312; of 1,000: 49 / 31 and 122 / 62; 4 rows of 2,048, which
+// fill the CUs, 93 / 149 and 242 / 309; ten packed sequences of 1 to 15,777 tokens,
+// 36,283 in all, forward 670 / 491; 20 of 777, one of 9,000 and two more 387 / 400.
+void select_rows(comba::SelectArgs* a, bool bwd, comba::SelectRows* q) {
   a->segs = 1;
   a->seglen = a->segmin = 1 << 30;
-  const int64_t tile = comba::select_tile(a->N);
+  q->rows = a->S;
+  q->n = 0;
+  const int32_t* cu = a->cu_host;
+  int32_t tokens[comba::SEL_LIST];  // of the longest sequences, the longest first
+  if (cu) {
+    for (int s = 0; s < a->S; ++s) {
+      const int32_t len = cu[s + 1] - cu[s];
+      if (q->n == comba::SEL_LIST && len <= tokens[q->n - 1]) continue;
+      int i = q->n < comba::SEL_LIST ? q->n++ : q->n - 1;
+      for (; i > 0 && tokens[i - 1] < len; --i) {
+        tokens[i] = tokens[i - 1];
+        q->seq[i] = q->seq[i - 1];
+      }
+      tokens[i] = len;
+      q->seq[i] = s;
+    }
+    for (int i = 0; i <= q->n; ++i) q->at[i] = i;
+  }
+  const int64_t tile = comba::select_tile(a->N), blocks = (int64_t)a->G * a->nblk;
   if (a->longest < 2 * tile || a->S == 0) return;  // short, or not known
   int dev = 0, cus = 0;
   if (hipGetDevice(&dev) != hipSuccess ||
       hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
     return;
-  const double pre = bwd ? 0.25 : 0.6, launch = bwd ? 64 : 128;
-  const double blocks = (double)a->G * a->nblk, share = (double)a->Ttot * blocks / cus;
-  auto rounds = [&](double rows) { return (double)(((int64_t)(rows * blocks) + cus - 1) / cus); };
-  const double longest = (double)a->longest;
-  if (a->cu_host && longest <= share) return;
-  double best = a->cu_host ? longest : rounds(a->S) * longest;
-  for (int p = 2; p <= 32; p *= 2) {
-    const int64_t len = (a->longest + p * tile - 1) / (p * tile) * tile, n = (a->longest + len - 1) / len;
-    if (n < 2) break;
-    double t = launch;
-    if (!a->cu_host) {
-      t += (rounds((double)a->S * n) + pre * rounds((double)a->S * (n - 1))) * (double)len;
+  const double share = (double)a->Ttot * blocks / cus;
+  if (cu && (double)a->longest <= share) return;
+  const double pre = bwd ? 0.27 : 0.5, launch = bwd ? 110 : 186, start = bwd ? 60 : 50;
+  int ncut = 0;  // packed sequences that may be cut
+  while (cu && ncut < q->n && (double)tokens[ncut] > share) ++ncut;
+  // the 16 longest whole sequences as batches, the others only in the share
+  Batch batch[comba::SEL_LIST + 18];
+  const int few = std::min(q->n, ncut + 16);
+  auto whole = [&](int i, int end, int n) {
+    for (; i < end; ++i) batch[n++] = {(double)tokens[i], 1};
+    return n;
+  };
+  int n = cu ? whole(0, few, 0) : 1;
+  if (!cu) batch[0] = {(double)a->longest, a->S};
+  auto rounds = [&] { return std::max(makespan(batch, n, blocks, cus, start), share); };
+  double best = rounds();
+  for (int p = 2; p <= 32; p += p < 8 ? 1 : p < 16 ? 2 : 8) {
+    const int64_t len = (a->longest + p * tile - 1) / (p * tile) * tile, segs = (a->longest + len - 1) / len;
+    if (segs < 2) break;
+    Batch first{(double)len, 0};
+    int64_t rows = a->S;
+    if (launch + std::max((double)len, share) + pre * (double)len >= best) continue;
+    if (!cu) {
+      first.count = (segs - 1) * a->S;
+      batch[0] = first;
+      batch[1] = {(double)(a->longest - (segs - 1) * len), a->S};
+      n = 2;
     } else {
-      int64_t first = 0;  // tokens of the first pass
-      for (int i = 0; i < a->S; ++i) {
-        const int64_t tokens = a->cu_host[i + 1] - a->cu_host[i];
-        if ((double)tokens > share) first += (tokens - 1) / len * len;
+      int i = ncut;
+      while (i < few && tokens[i] > len) ++i;
+      n = whole(ncut, i, 0);
+      Batch& cut = batch[n++];
+      for (int k = 0; k < ncut; ++k) {
+        const int64_t c = (tokens[k] - 1) / len;
+        first.count += c;
+        batch[n++] = {(double)(tokens[k] - c * len), 1};
       }
-      const double f = (double)first * blocks / cus;
-      t += ((double)len > share ? (double)len : share) + pre * ((double)len > f ? (double)len : f);
+      cut = first;
+      n = whole(i, few, n);
     }
-    if (t < best && (int64_t)a->S * n * a->G * a->nblk <= INT32_MAX) {
+    rows += first.count;
+    const double t = launch + rounds() + pre * makespan(&first, 1, blocks, cus, start);
+    if (t < best && rows * blocks <= INT32_MAX) {
       best = t;
-      a->segs = (int)n;
+      a->segs = (int)segs;
       a->seglen = (int)len;
-      a->segmin = a->cu_host ? (int)share : 0;
+      a->segmin = cu ? (int)share : 0;
+      q->rows = (int)rows;
     }
   }
+  if (!cu || a->segs == 1) return;
+  // the listed sequences by their segments' length
+  int i = ncut;
+  while (i < q->n && tokens[i] > a->seglen) ++i;
+  std::rotate(q->seq, q->seq + ncut, q->seq + i);
+  std::rotate(tokens, tokens + ncut, tokens + i);
+  for (int k = 0; k < q->n; ++k)
+    q->at[k + 1] = q->at[k] + (tokens[k] > a->segmin ? (tokens[k] + a->seglen - 1) / a->seglen : 1);
 }
 
-// Workspace of a forward, or (save) of a saving forward and its backward, whose
-// segments are chosen apart.
-SelectLayout select_layout(const comba::SelectArgs& a0, bool save) {
-  comba::SelectArgs a = a0;
+// The call's work rows, and the workspace of a forward, or (save) of a saving
+// forward and its backward, whose segments are chosen apart.
+SelectLayout select_layout(comba::SelectArgs* a, bool save, bool bwd, comba::SelectRows* q) {
   SelectLayout L{};
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -151,20 +246,23 @@ SelectLayout select_layout(const comba::SelectArgs& a0, bool save) {
     off += round_up(bytes);
     return at;
   };
-  select_segments(&a, false);
-  size_t segs = a.segs;
+  size_t cut = 0, all = 0;  // work rows with kept ends of segments; the backward's
+  auto plan = [&](bool dir) {
+    select_rows(a, dir, q);
+    if (a->segs > 1) cut = std::max(cut, (size_t)q->rows);
+    if (dir) all = q->rows;
+  };
+  if (save) plan(!bwd);
+  plan(bwd);
   if (save) {
-    select_segments(&a, true);
     // states: a sequence's start at tok0 / select_ck + its number, which leaves
     // room for a partial interval per sequence
-    L.ck = take(((size_t)a.Ttot / comba::select_ck(a.N) + a.S + 1) * a.D * a.N * sizeof(float));
-    L.bcp = take((size_t)a.G * a.nblk * a.Ttot * 2 * a.N * sizeof(float));
-    L.dap = take((size_t)a.S * a.segs * a.D * (a.N + 2) * sizeof(float));
-    if ((size_t)a.segs > segs) segs = a.segs;
+    L.ck = take(((size_t)a->Ttot / comba::select_ck(a->N) + a->S + 1) * a->D * a->N * sizeof(float));
+    L.bcp = take((size_t)a->G * a->nblk * a->Ttot * 2 * a->N * sizeof(float));
+    L.dap = take(all * a->D * (a->N + 2) * sizeof(float));
   }
-  const size_t rows = segs > 1 ? (size_t)a.S * segs * a.D : 0;
-  L.segF = take(rows * a.N * sizeof(float));
-  L.segdt = take(rows * sizeof(float));
+  L.segF = take(cut * a->D * a->N * sizeof(float));
+  L.segdt = take(cut * a->D * sizeof(float));
   L.total = off + kAlign;
   return L;
 }
@@ -231,17 +329,17 @@ comba_status select_fwd(bool save, const comba_select_shape* shape, const void* 
   if (st != COMBA_OK) return st;
   if ((a.Ttot > 0 && !y) || !ws) return COMBA_ERR_NULL;
   if (!aligned(y, a.bf16 ? 2 : 4) || !aligned(ht, 4) || !aligned(ws, kAlign)) return COMBA_ERR_ALIGN;
-  const SelectLayout L = select_layout(a, save);
+  comba::SelectRows q;
+  const SelectLayout L = select_layout(&a, save, false, &q);
   if (ws_bytes < L.total) return COMBA_ERR_WORKSPACE;
   a.y = y;
   a.ht = ht;
   char* base = static_cast<char*>(ws);
   if (save) a.ck = reinterpret_cast<float*>(base + L.ck);
-  select_segments(&a, false);
   a.segF = reinterpret_cast<float*>(base + L.segF);
   a.segdt = reinterpret_cast<float*>(base + L.segdt);
   a.stream = static_cast<hipStream_t>(stream);
-  return done(comba::launch_select_fwd(a));
+  return done(comba::launch_select_fwd(a, q));
 }
 
 // ---- group norm ---------------------------------------------------------------
@@ -366,12 +464,14 @@ comba_status comba_conv_step(const comba_conv_shape* shape, const void* x, const
 
 size_t comba_select_fwd_workspace_bytes(const comba_select_shape* shape) {
   comba::SelectArgs a;
-  return select_args(shape, &a) == COMBA_OK ? select_layout(a, false).total : 0;
+  comba::SelectRows q;
+  return select_args(shape, &a) == COMBA_OK ? select_layout(&a, false, false, &q).total : 0;
 }
 
 size_t comba_select_bwd_workspace_bytes(const comba_select_shape* shape) {
   comba::SelectArgs a;
-  return select_args(shape, &a) == COMBA_OK ? select_layout(a, true).total : 0;
+  comba::SelectRows q;
+  return select_args(shape, &a) == COMBA_OK ? select_layout(&a, true, false, &q).total : 0;
 }
 
 comba_status comba_select_fwd(const comba_select_shape* shape, const void* u, const void* delta,
@@ -411,13 +511,13 @@ comba_status comba_select_bwd(const comba_select_shape* shape, const void* u, co
       !aligned(dz, e) || !aligned(dht, 4) || !aligned(dA, 4) || !aligned(dD, 4) ||
       !aligned(ddelta_bias, 4) || !aligned(dh0, 4) || !aligned(ws, kAlign))
     return COMBA_ERR_ALIGN;
-  const SelectLayout L = select_layout(a, true);
+  comba::SelectRows q;
+  const SelectLayout L = select_layout(&a, true, true, &q);
   if (ws_bytes < L.total) return COMBA_ERR_WORKSPACE;
   char* base = static_cast<char*>(ws);
   a.ck = reinterpret_cast<float*>(base + L.ck);
   a.bcp = reinterpret_cast<float*>(base + L.bcp);
   a.dap = reinterpret_cast<float*>(base + L.dap);
-  select_segments(&a, true);
   a.segF = reinterpret_cast<float*>(base + L.segF);
   a.segdt = reinterpret_cast<float*>(base + L.segdt);
   a.dy = dy;
@@ -432,7 +532,7 @@ comba_status comba_select_bwd(const comba_select_shape* shape, const void* u, co
   a.dbias = delta_bias ? ddelta_bias : nullptr;
   a.dh0 = dh0;
   a.stream = static_cast<hipStream_t>(stream);
-  return done(comba::launch_select_bwd(a));
+  return done(comba::launch_select_bwd(a, q));
 }
 
 comba_status comba_select_step(const comba_select_shape* shape, const void* u, const void* delta,

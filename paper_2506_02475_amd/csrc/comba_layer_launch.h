@@ -44,7 +44,7 @@ constexpr int select_ck(int N) { return N == 8 ? 32 : 48; }
 constexpr int select_tile(int N) { return N == 8 ? 64 : 96; }
 
 struct SelectArgs {
-  bool bf16, softplus, vec;  // vec: whole groups of channels in one load (set by the launchers)
+  bool bf16, softplus;
   int D, N, G, S, Tseq, Ttot;  // S sequences
   const int32_t* cu_seqlens;
   const int32_t* cu_host;  // the host's copy, or NULL (host code only)
@@ -65,19 +65,29 @@ struct SelectArgs {
   void *du, *ddelta, *dz, *dB, *dC;
   float *dA, *dD, *dbias, *dh0;
   int nblk;      // channel blocks per group
-  // rows of more than `segmin` tokens cut into up to `segs` segments of `seglen`
-  // tokens: each segment's end from zero and the sum of its steps
+  // sequences of more than `segmin` tokens cut into up to `segs` segments of
+  // `seglen` tokens; a work row is a segment or a whole sequence: each segment's end
+  // from zero and the sum of its steps
   int segs, seglen, segmin;
-  float* segF;   // [sequence][segment][D][N]
-  float* segdt;  // [sequence][segment][D]
+  float* segF;   // [work row][D][N]
+  float* segdt;  // [work row][D]
   float* bcp;    // [channel block][token][2 N] partial dB, dC of one block's channels
-  float* dap;    // [sequence][segment][D][N + 2] partial dA, dD, dbias
+  float* dap;    // [work row][D][N + 2] partial dA, dD, dbias
   hipStream_t stream;
+};
+// The work rows in the order of their workgroups.  Packed sequences with host
+// offsets: rows at[i] .. at[i + 1] - 1 are the segments of sequence seq[i], the
+// longest work first; the sequences not listed follow whole, in their own order.
+constexpr int SEL_LIST = 32;
+struct SelectRows {
+  int rows, n;
+  int32_t seq[SEL_LIST];
+  int16_t at[SEL_LIST + 1];  // up to 32 segments each
 };
 // Channels of one workgroup of the backward, and its blocks per group.
 constexpr int select_block_channels(int N) { return 512 / N; }
-hipError_t launch_select_fwd(const SelectArgs& a);
-hipError_t launch_select_bwd(const SelectArgs& a);
+hipError_t launch_select_fwd(const SelectArgs& a, const SelectRows& q);
+hipError_t launch_select_bwd(const SelectArgs& a, const SelectRows& q);
 hipError_t launch_select_step(const SelectArgs& a);
 
 struct GroupNormArgs {

@@ -7,8 +7,7 @@
 // (channel, state, token), and these, not the bytes, bound every long call.
 //
 // Layout of a wave: CW channels x N states.  A lane holds CPL = 2 channels x 4
-// states (four channels of decays and states spilled: 2,440 us instead of 410 at
-// 4 x 4,096 tokens, 4,096 channels, 16 states) (lane group ng = lane / CG takes states 4 ng .. 4 ng + 3, lane cg = lane
+// states (lane group ng = lane / CG takes states 4 ng .. 4 ng + 3, lane cg = lane
 // % CG takes channels CPL cg ..), so that sums over states are three in-lane
 // adds and log2(N / 4) lane exchanges for CPL channels at once, and sums over
 // channels (the gradients of B and C) start with in-lane adds as well.
@@ -74,47 +73,63 @@ __device__ __forceinline__ float or_zero(const float* p, const float* any, int c
   return p ? v : 0.f;
 }
 
-// What a workgroup works on: a segment of a sequence and a block of CW channels
-// of one group.  Two neighbouring blocks, which share the 128-byte lines of their
-// rows, go to workgroups eight apart and so to the same XCD.
+// What a workgroup works on: a work row (a segment of a sequence) and a block of CW
+// channels of one group.  Two neighbouring blocks, which share the 128-byte lines
+// of their rows, go to workgroups eight apart and so to the same XCD.
 struct SelBlock {
   int seq, seg, blk, g;  // sequence, its segment, channel block (of all groups), group
+  int row0;              // the work row of the sequence's first segment
   int c0, cend;          // channels [c0, cend)
   int tok0, len;         // the sequence's tokens
   int t0, t1;            // the segment's tokens, counted in the sequence
   int nseg;              // the sequence's segments (at least one)
 };
 template <int CW>
-__device__ __forceinline__ SelBlock sel_block(const SelectArgs& a) {
+__device__ __forceinline__ SelBlock sel_block(const SelectArgs& a, const SelectRows& q) {
   const int Dg = a.D / a.G, nblk = (Dg + CW - 1) / CW, nb = a.G * nblk;
   int b = blockIdx.x;
   if ((b | 15) < (int)gridDim.x) b = (b & ~15) | ((b & 7) << 1) | ((b >> 3) & 1);
   SelBlock s;
-  const int r = b / nb;
+  const int r = b / nb, l = lane_id();
+  int most = 1;  // segments that have a work row
   s.blk = b - r * nb;
-  s.seq = r / a.segs;
-  s.seg = r - s.seq * a.segs;
-  if (a.cu_seqlens && a.S > 1 && a.S <= 64) {
-    // packed: the longest work first (lane l ranks sequence l by its segments'
-    // length), so that no long one starts when the others are done
-    const int l = lane_id();
-    int n = l < a.S ? a.cu_seqlens[l + 1] - a.cu_seqlens[l] : 0;
-    n = n > a.segmin ? min(n, a.seglen) : n;
-    int rank = 0;
-    for (int j = 0; j < a.S; ++j) {
-      const int m = __builtin_amdgcn_readlane(n, j);
-      rank += m > n || (m == n && j < l);
+  if (q.n > 0) {
+    const int at = l < q.n ? q.at[l] : INT32_MAX, seq = l < q.n ? q.seq[l] : INT32_MAX;
+    const int listed = q.at[q.n];
+    if (r < listed) {
+      const int i = __builtin_popcountll(__ballot(at <= r)) - 1;
+      s.row0 = __builtin_amdgcn_readlane(at, i);
+      s.seq = __builtin_amdgcn_readlane(seq, i);
+      most = (i + 1 < q.n ? __builtin_amdgcn_readlane(at, i + 1) : listed) - s.row0;
+    } else {  // the (r - listed)-th of the others
+      s.row0 = r;
+      s.seq = r - listed;
+      for (int k = 0; k < SEL_LIST; ++k) s.seq = r - listed + __builtin_popcountll(__ballot(seq <= s.seq));
     }
-    s.seq = __builtin_ctzll(__ballot(l < a.S && rank == s.seq));
+  } else {
+    s.seq = r / a.segs;
+    s.row0 = s.seq * a.segs;
+    most = a.segs;
+    if (a.cu_seqlens && a.S > 1 && a.S <= 64) {
+      // no host offsets: lane l ranks sequence l by its length
+      const int n = l < a.S ? a.cu_seqlens[l + 1] - a.cu_seqlens[l] : 0;
+      int rank = 0;
+      for (int j = 0; j < a.S; ++j) {
+        const int m = __builtin_amdgcn_readlane(n, j);
+        rank += m > n || (m == n && j < l);
+      }
+      s.seq = __builtin_ctzll(__ballot(l < a.S && rank == r));
+    }
   }
+  s.seg = r - s.row0;
   s.g = s.blk / nblk;
   s.c0 = s.g * Dg + (s.blk - s.g * nblk) * CW;
   s.cend = min(s.c0 + CW, (s.g + 1) * Dg);
   int t1;
   seq_range(a.cu_seqlens, s.seq, a.Tseq, a.Ttot, s.tok0, t1);
   s.len = t1 - s.tok0;
-  const bool cut = s.len > a.segmin;
-  s.nseg = cut ? min((s.len + a.seglen - 1) / a.seglen, a.segs) : 1;
+  const bool cut = most > 1 && s.len > a.segmin;
+  s.nseg = cut ? min((s.len + a.seglen - 1) / a.seglen, most) : 1;
   s.t0 = cut ? min(s.len, s.seg * a.seglen) : (s.seg > 0 ? s.len : 0);
   s.t1 = cut ? min(s.len, s.t0 + a.seglen) : s.len;
   return s;
@@ -134,7 +149,7 @@ __device__ __forceinline__ void sel_slot(int slot, int& ch, int& n) {
 // (REV: the decayed gradient of the state that enters it) and, per channel, the
 // sum of its steps, whose exponential is the segment's decay product.
 template <typename Tin, int N, int CPL, bool VEC, bool REV>
-__global__ __launch_bounds__(64 * sel_waves(N)) void k_select_seg(SelectArgs a) {
+__global__ __launch_bounds__(64 * sel_waves(N)) void k_select_seg(SelectArgs a, SelectRows q) {
   constexpr int L = 8, W = sel_waves(N);
   using S = SelTile<N, CPL>;
   constexpr int LN = S::LN, CG = S::CG, CW = S::CW, NE = S::NE, TL = L / LN, TILE = L * W;
@@ -147,7 +162,7 @@ __global__ __launch_bounds__(64 * sel_waves(N)) void k_select_seg(SelectArgs a) 
   __shared__ __align__(16) WaveLds lds[W];
   __shared__ __align__(16) float ex[W][2][NE];
 
-  const SelBlock sb = sel_block<CW>(a);
+  const SelBlock sb = sel_block<CW>(a, q);
   // the last segment's end is nobody's start (REV: the first one's)
   if (sb.t0 >= sb.t1 || sb.seg == (REV ? 0 : sb.nseg - 1)) return;
   const int lane = lane_id(), w = wave_id_s(), ng = lane / CG, cg = lane % CG;
@@ -285,7 +300,7 @@ __global__ __launch_bounds__(64 * sel_waves(N)) void k_select_seg(SelectArgs a) 
     }
     __syncthreads();
   }
-  const long at = (long)(sb.seq * a.segs + sb.seg) * a.D;
+  const long at = (long)(sb.row0 + sb.seg) * a.D;
   int oc, on;
   sel_slot<N, CPL>(own, oc, on);
   if (own < NE && sb.c0 + oc < sb.cend) a.segF[(at + sb.c0 + oc) * N + on] = H;
@@ -311,14 +326,14 @@ __device__ __forceinline__ float seg_enter(const SelectArgs& a, const SelBlock& 
   const int m = REV ? sb.nseg - 1 - sb.seg : sb.seg;
 #pragma unroll 4
   for (int k = 0; k < m; ++k) {
-    const long at = (long)(sb.seq * a.segs + (REV ? sb.nseg - 1 - k : k)) * a.D + c;
+    const long at = (long)(sb.row0 + (REV ? sb.nseg - 1 - k : k)) * a.D + c;
     h = fmaf(__builtin_amdgcn_exp2f(A2 * a.segdt[at]), h, a.segF[at * N + n]);
   }
   return h;
 }
 
 template <typename Tin, int N, int CPL, int L, int W, bool VEC, bool Z>
-__global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
+__global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a, SelectRows q) {
   using S = SelTile<N, CPL>;
   constexpr int LN = S::LN, CG = S::CG, CW = S::CW, NE = S::NE, TL = L / LN, TILE = L * W;
   constexpr int NB = L * N / 64;        // states of a B or C row that a lane loads
@@ -332,7 +347,7 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
   // replaces by the state at its start
   __shared__ __align__(16) float ex[W][2][NE];
 
-  const SelBlock sb = sel_block<CW>(a);
+  const SelBlock sb = sel_block<CW>(a, q);
   const int lane = lane_id(), w = wave_id_s(), ng = lane / CG, cg = lane % CG;
   const int cl = sb.c0 + cg * CPL, nv = max(0, min(CPL, sb.cend - cl));  // the lane's channels
   const int len = sb.t1;  // the segment's end
@@ -443,27 +458,27 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
     const bool live = t0 < len;  // a chunk past the end leaves the state as it is
     if (live) {
 #pragma unroll
-    for (int t = 0; t < L; ++t) {
-      __builtin_amdgcn_sched_barrier(0);
-      float dt[CPL], xu[CPL], Bv[4], Cv[4];
-      lds_get<CPL>(&my.dt[t][cg * CPL], dt);
-      lds_get<CPL>(&my.xu[t][cg * CPL], xu);
-      lds_get<4>(&my.B[t][ng * 4], Bv);
-      lds_get<4>(&my.C[t][ng * 4], Cv);
+      for (int t = 0; t < L; ++t) {
+        __builtin_amdgcn_sched_barrier(0);
+        float dt[CPL], xu[CPL], Bv[4], Cv[4];
+        lds_get<CPL>(&my.dt[t][cg * CPL], dt);
+        lds_get<CPL>(&my.xu[t][cg * CPL], xu);
+        lds_get<4>(&my.B[t][ng * 4], Bv);
+        lds_get<4>(&my.C[t][ng * 4], Cv);
 #pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        sdt[i] += dt[i];
-        float s = 0.f;
+        for (int i = 0; i < CPL; ++i) {
+          sdt[i] += dt[i];
+          float s = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          dec[t][i][j] = __builtin_amdgcn_exp2f(dt[i] * A2[i][j]);
-          h[i][j] = t == 0 ? xu[i] * Bv[j] : fmaf(dec[t][i][j], h[i][j], xu[i] * Bv[j]);
-          s = j == 0 ? Cv[0] * h[i][0] : fmaf(Cv[j], h[i][j], s);
+          for (int j = 0; j < 4; ++j) {
+            dec[t][i][j] = __builtin_amdgcn_exp2f(dt[i] * A2[i][j]);
+            h[i][j] = t == 0 ? xu[i] * Bv[j] : fmaf(dec[t][i][j], h[i][j], xu[i] * Bv[j]);
+            s = j == 0 ? Cv[0] * h[i][0] : fmaf(Cv[j], h[i][j], s);
+          }
+          asm("" : "+v"(s));  // formed here: deferred, every token's states would stay in registers
+          yp[t * CPL + i] = s;
         }
-        asm("" : "+v"(s));  // formed here: deferred, every token's states would stay in registers
-        yp[t * CPL + i] = s;
       }
-    }
     }
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
@@ -547,7 +562,7 @@ __global__ __launch_bounds__(64 * W) void k_select_fwd(SelectArgs a) {
 // ends, and a second pass forms the states (kept in registers) and then the
 // gradients.  dB and dC of the workgroup's channels go to a partial sum.
 template <typename Tin, int N, int CPL, bool VEC, bool Z>
-__global__ __launch_bounds__(16 * select_ck(N)) void k_select_bwd(SelectArgs a) {
+__global__ __launch_bounds__(16 * select_ck(N)) void k_select_bwd(SelectArgs a, SelectRows q) {
   constexpr int L = 4, W = select_ck(N) / L;
   using S = SelTile<N, CPL>;
   constexpr int LN = S::LN, CG = S::CG, CW = S::CW, NE = S::NE, TL = (L + LN - 1) / LN, TILE = L * W;
@@ -563,7 +578,7 @@ __global__ __launch_bounds__(16 * select_ck(N)) void k_select_bwd(SelectArgs a) 
   // the owner replaces by the state at its start and the gradient at its end
   __shared__ __align__(16) float ex[W][3][NE];
 
-  const SelBlock sb = sel_block<CW>(a);
+  const SelBlock sb = sel_block<CW>(a, q);
   const int lane = lane_id(), w = wave_id_s(), ng = lane / CG, cg = lane % CG;
   const int cl = sb.c0 + cg * CPL, nv = max(0, min(CPL, sb.cend - cl));
   const int len = sb.t1, tile0 = sb.t0 / TILE;  // the segment's tiles: none past the sequence's end
@@ -892,7 +907,7 @@ __global__ __launch_bounds__(16 * select_ck(N)) void k_select_bwd(SelectArgs a) 
     red[w * 3 * NE + (1 * CPL + i) * 64 + lane] = dbias[i];
   }
   __syncthreads();
-  const long part = (long)(sb.seq * a.segs + sb.seg) * a.D;
+  const long part = (long)(sb.row0 + sb.seg) * a.D;
   if (has) {
     float v = ex[0][0][threadIdx.x];
 #pragma unroll
@@ -914,14 +929,14 @@ __global__ __launch_bounds__(16 * select_ck(N)) void k_select_bwd(SelectArgs a) 
 // and dC of every (token, group, state) over the channel blocks, four values a
 // thread, the others dA, dD and dbias over the segments; both in order.
 template <typename Tin>
-__global__ __launch_bounds__(256) void k_select_sums(SelectArgs a, int nbc) {
+__global__ __launch_bounds__(256) void k_select_sums(SelectArgs a, int rows, int nbc) {
   if ((int)blockIdx.x >= nbc) {
     const int w = a.N + 2;
     const long n = (long)a.D * w, e = (long)(blockIdx.x - nbc) * 256 + threadIdx.x;
     if (e >= n) return;
     float sum = 0.f;
 #pragma unroll 4
-    for (int s = 0; s < a.S * a.segs; ++s) sum += a.dap[s * n + e];
+    for (int s = 0; s < rows; ++s) sum += a.dap[s * n + e];
     const int k = e % w;
     const long c = e / w;
     if (k < a.N) a.dA[c * a.N + k] = sum;
@@ -1035,41 +1050,41 @@ static bool rows_vec(const SelectArgs& a, int C, int nb, bool bwd) {
 }
 
 template <typename Tin, int N, bool REV>
-static void run_seg(const SelectArgs& a, unsigned grid) {
+static void run_seg(const SelectArgs& a, const SelectRows& q, unsigned grid) {
   if (a.segs <= 1) return;
-  if (rows_vec(a, SEL_CPL, N / 8, REV)) k_select_seg<Tin, N, SEL_CPL, true, REV><<<grid, 64 * sel_waves(N), 0, a.stream>>>(a);
-  else k_select_seg<Tin, N, SEL_CPL, false, REV><<<grid, 64 * sel_waves(N), 0, a.stream>>>(a);
+  if (rows_vec(a, SEL_CPL, N / 8, REV)) k_select_seg<Tin, N, SEL_CPL, true, REV><<<grid, 64 * sel_waves(N), 0, a.stream>>>(a, q);
+  else k_select_seg<Tin, N, SEL_CPL, false, REV><<<grid, 64 * sel_waves(N), 0, a.stream>>>(a, q);
 }
 
 template <typename Tin, int N>
-static hipError_t run_fwd(const SelectArgs& a) {
+static hipError_t run_fwd(const SelectArgs& a, const SelectRows& q) {
   constexpr int CPL = SEL_CPL, L = 8, W = sel_waves(N);
   static_assert(SelTile<N, CPL>::CW == select_block_channels(N), "one block of channels throughout");
-  const unsigned grid = (unsigned)a.S * a.segs * a.G * a.nblk;
-  run_seg<Tin, N, false>(a, grid);
+  const unsigned grid = (unsigned)q.rows * a.G * a.nblk;
+  run_seg<Tin, N, false>(a, q, grid);
   const bool vec = rows_vec(a, CPL, L * N / 64, false);
-  if (vec && a.z) k_select_fwd<Tin, N, CPL, L, W, true, true><<<grid, 64 * W, 0, a.stream>>>(a);
-  else if (vec) k_select_fwd<Tin, N, CPL, L, W, true, false><<<grid, 64 * W, 0, a.stream>>>(a);
-  else if (a.z) k_select_fwd<Tin, N, CPL, L, W, false, true><<<grid, 64 * W, 0, a.stream>>>(a);
-  else k_select_fwd<Tin, N, CPL, L, W, false, false><<<grid, 64 * W, 0, a.stream>>>(a);
+  if (vec && a.z) k_select_fwd<Tin, N, CPL, L, W, true, true><<<grid, 64 * W, 0, a.stream>>>(a, q);
+  else if (vec) k_select_fwd<Tin, N, CPL, L, W, true, false><<<grid, 64 * W, 0, a.stream>>>(a, q);
+  else if (a.z) k_select_fwd<Tin, N, CPL, L, W, false, true><<<grid, 64 * W, 0, a.stream>>>(a, q);
+  else k_select_fwd<Tin, N, CPL, L, W, false, false><<<grid, 64 * W, 0, a.stream>>>(a, q);
   return hipGetLastError();
 }
 
 template <typename Tin, int N>
-static hipError_t run_bwd(const SelectArgs& a) {
+static hipError_t run_bwd(const SelectArgs& a, const SelectRows& q) {
   constexpr int CPL = SEL_CPL;
-  const unsigned grid = (unsigned)a.S * a.segs * a.G * a.nblk;
+  const unsigned grid = (unsigned)q.rows * a.G * a.nblk;
   if (grid > 0) {
-    run_seg<Tin, N, true>(a, grid);
+    run_seg<Tin, N, true>(a, q, grid);
     const bool vec = rows_vec(a, CPL, N >= 16 ? N / 16 : 1, true);
-    if (vec && a.z) k_select_bwd<Tin, N, CPL, true, true><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
-    else if (vec) k_select_bwd<Tin, N, CPL, true, false><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
-    else if (a.z) k_select_bwd<Tin, N, CPL, false, true><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
-    else k_select_bwd<Tin, N, CPL, false, false><<<grid, 16 * select_ck(N), 0, a.stream>>>(a);
+    if (vec && a.z) k_select_bwd<Tin, N, CPL, true, true><<<grid, 16 * select_ck(N), 0, a.stream>>>(a, q);
+    else if (vec) k_select_bwd<Tin, N, CPL, true, false><<<grid, 16 * select_ck(N), 0, a.stream>>>(a, q);
+    else if (a.z) k_select_bwd<Tin, N, CPL, false, true><<<grid, 16 * select_ck(N), 0, a.stream>>>(a, q);
+    else k_select_bwd<Tin, N, CPL, false, false><<<grid, 16 * select_ck(N), 0, a.stream>>>(a, q);
   }
   const long nbc = ((long)a.Ttot * a.G * 2 * N / 4 + 255) / 256, np = ((long)a.D * (N + 2) + 255) / 256;
   if (nbc + np > INT32_MAX) return hipErrorInvalidValue;
-  k_select_sums<Tin><<<(unsigned)(nbc + np), 256, 0, a.stream>>>(a, (int)nbc);
+  k_select_sums<Tin><<<(unsigned)(nbc + np), 256, 0, a.stream>>>(a, q.rows, (int)nbc);
   return hipGetLastError();
 }
 
@@ -1089,15 +1104,15 @@ static hipError_t run_step(const SelectArgs& a) {
   return (long)a.S * a.D * (N / 4) >= 4L * 1024 * 256 ? step_rows<Tin, N, 4>(a) : step_rows<Tin, N, 1>(a);
 }
 
-#define SELECT_DISPATCH(fn, a)                                                              \
-  ((a).N == 8    ? ((a).bf16 ? fn<bf16_t, 8>(a) : fn<float, 8>(a))                          \
-   : (a).N == 16 ? ((a).bf16 ? fn<bf16_t, 16>(a) : fn<float, 16>(a))                        \
-   : (a).N == 32 ? ((a).bf16 ? fn<bf16_t, 32>(a) : fn<float, 32>(a)) : hipErrorInvalidValue)
+#define SELECT_DISPATCH(fn, ...)                                                                       \
+  (a.N == 8    ? (a.bf16 ? fn<bf16_t, 8>(__VA_ARGS__) : fn<float, 8>(__VA_ARGS__))                     \
+   : a.N == 16 ? (a.bf16 ? fn<bf16_t, 16>(__VA_ARGS__) : fn<float, 16>(__VA_ARGS__))                   \
+   : a.N == 32 ? (a.bf16 ? fn<bf16_t, 32>(__VA_ARGS__) : fn<float, 32>(__VA_ARGS__)) : hipErrorInvalidValue)
 
-hipError_t launch_select_fwd(const SelectArgs& a) {
-  return a.S == 0 ? hipSuccess : SELECT_DISPATCH(run_fwd, a);
+hipError_t launch_select_fwd(const SelectArgs& a, const SelectRows& q) {
+  return a.S == 0 ? hipSuccess : SELECT_DISPATCH(run_fwd, a, q);
 }
-hipError_t launch_select_bwd(const SelectArgs& a) { return SELECT_DISPATCH(run_bwd, a); }
+hipError_t launch_select_bwd(const SelectArgs& a, const SelectRows& q) { return SELECT_DISPATCH(run_bwd, a, q); }
 hipError_t launch_select_step(const SelectArgs& a) {
   return a.S == 0 ? hipSuccess : SELECT_DISPATCH(run_step, a);
 }

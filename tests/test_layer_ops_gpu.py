@@ -597,6 +597,11 @@ SEGMENTED = [
     ("two_rows_n32", dict(B=2, T=900, D=20, N=32, z=False, dht=True)),
     ("no_states", dict(B=1, T=700, D=33, N=16, h0=False, off=1)),
     ("packed", dict(D=24, N=16, lens=[1100, 1, 0, 64, 700, 129], host=True, dht=True)),
+    ("packed_many", dict(D=24, N=16, lens=[7, 60, 0, 33] * 15 + [1300, 5, 0, 900, 200], host=True,
+                         dht=True)),
+    ("packed_many_f32", dict(D=72, N=8, lens=[1, 0, 2] * 40 + [1000], dtype="f32", host=True,
+                             dht=True)),
+    ("packed_mixed", dict(D=3000, N=16, lens=[900, 400, 150, 30, 400], z=False, host=True)),
 ]
 
 
