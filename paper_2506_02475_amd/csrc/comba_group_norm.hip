@@ -6,16 +6,24 @@
 //
 // Bound by bytes: every value is read and written once.  A group's channels lie
 // in the registers of a team of 1..64 lanes (a power of two) or of a workgroup of
-// 256, KV pieces of four per lane, so that mean and variance are two passes over
-// registers.  A team keeps its group and walks rows, with weight and bias
-// (backward: and their gradients' sums) in registers.  Groups of more than 4,096
-// channels read x again from the caches (k_group_norm_wide).
+// 256 or 512, KV pieces of four per lane, so that mean and variance are two passes
+// over registers.  A team keeps its group and walks rows, the next row's loads in
+// flight, with weight and bias (backward: and their gradients' sums) in registers.
+// 16,384 x 4,096 channels in groups of 128, gated, bf16: forward 84 us (4.8 TB/s),
+// backward 134 us and 5 for the sums (5.0 TB/s); x in fp32, 2,048 channels: 45 us.
+//
+// Groups of more than 8,192 channels read x again from the caches
+// (k_group_norm_wide), at a higher cost: 8,192 rows of one group of 8,192 channels
+// take 87 us forward and 166 backward in registers, of 12,000 from the caches 325
+// and 948; one group of 4,096 from the caches 443 and 929 for 16,384 rows, not 86
+// and 156.
 #include "comba_layer_device.hpp"
 #include "comba_layer_launch.h"
 
 namespace comba {
 
-constexpr int GN_C = 4;  // channels of a piece
+constexpr int GN_C = 4;        // channels of a piece
+constexpr int GN_WIDE = 1024;  // threads where a group's channels do not fit registers
 
 // Sum over the lanes of a team (team: a power of two up to 64), the same in every lane.
 __device__ __forceinline__ float team_sum(float x, int team) {
@@ -48,20 +56,23 @@ __device__ __forceinline__ float act_slope(comba_activation act, float t, float&
   return s * (1.f - s);
 }
 
-// Sum over a workgroup of 256, the same in every thread.
+// Sum over a workgroup of TH threads, the same in every thread.
+template <int TH>
 __device__ __forceinline__ float block_sum(float x, float* lds) {
   x = team_sum(x, 64);
   if (lane_id() == 0) lds[wave_id()] = x;
   __syncthreads();
-  const float s = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < TH / 64; ++i) s += lds[i];
   __syncthreads();
   return s;
 }
 
-// The same over the team: a wave's lanes, or the workgroup.
-template <bool BLOCK>
+// The same over the team: a wave's lanes (TEAM 0), or a workgroup of TEAM threads.
+template <int TEAM>
 __device__ __forceinline__ float gn_sum(float x, int team, float* lds) {
-  if constexpr (BLOCK) return block_sum(x, lds);
+  if constexpr (TEAM > 0) return block_sum<TEAM>(x, lds);
   return team_sum(x, team);
 }
 
@@ -70,11 +81,11 @@ struct GnTeam {
   int chunks;  // row chunks: team (group, chunk) takes rows chunk, chunk + chunks, ..
 };
 
-template <typename Tx, typename To, int KV, bool VEC, bool BLOCK, bool BWD>
-__global__ __launch_bounds__(256) void k_group_norm(GroupNormArgs a, GnTeam tm) {
-  __shared__ float lds[4];
-  const int m = a.C / a.G, team = tm.team;
-  const long id = ((long)blockIdx.x * 256 + threadIdx.x) / team;
+template <typename Tx, typename To, int KV, bool VEC, int TEAM, bool BWD>
+__global__ __launch_bounds__(TEAM > 0 ? TEAM : 256) void k_group_norm(GroupNormArgs a, GnTeam tm) {
+  __shared__ float lds[TEAM / 64 + 1];
+  const int m = a.C / a.G, team = TEAM > 0 ? TEAM : tm.team;
+  const long id = ((long)blockIdx.x * blockDim.x + threadIdx.x) / team;
   const int l = threadIdx.x & (team - 1);
   const int g = id % a.G, chunk = id / a.G;
   if (chunk >= tm.chunks) return;  // whole teams
@@ -120,7 +131,7 @@ __global__ __launch_bounds__(256) void k_group_norm(GroupNormArgs a, GnTeam tm) 
         sum += v[k][i];
       }
     if (r + tm.chunks < a.rows) load(r + tm.chunks);
-    const float mean = gn_sum<BLOCK>(sum, team, lds) * inv;
+    const float mean = gn_sum<TEAM>(sum, team, lds) * inv;
 #pragma unroll
     for (int k = 0; k < KV; ++k)
 #pragma unroll
@@ -128,7 +139,7 @@ __global__ __launch_bounds__(256) void k_group_norm(GroupNormArgs a, GnTeam tm) 
         v[k][i] = i < nv[k] ? v[k][i] - mean : 0.f;
         sq = fmaf(v[k][i], v[k][i], sq);
       }
-    const float rstd = rsqrtf(gn_sum<BLOCK>(sq, team, lds) * inv + a.eps);
+    const float rstd = rsqrtf(gn_sum<TEAM>(sq, team, lds) * inv + a.eps);
     if constexpr (!BWD) {
 #pragma unroll
       for (int k = 0; k < KV; ++k) {
@@ -161,8 +172,8 @@ __global__ __launch_bounds__(256) void k_group_norm(GroupNormArgs a, GnTeam tm) 
         }
         if (z) store_piece<To, GN_C, VEC>(static_cast<To*>(a.dz) + r * a.C + c[k], dz, nv[k]);
       }
-      s1 = gn_sum<BLOCK>(s1, team, lds) * inv;
-      s2 = gn_sum<BLOCK>(s2, team, lds) * inv;
+      s1 = gn_sum<TEAM>(s1, team, lds) * inv;
+      s2 = gn_sum<TEAM>(s2, team, lds) * inv;
 #pragma unroll
       for (int k = 0; k < KV; ++k) {
         float dx[GN_C];
@@ -184,68 +195,101 @@ __global__ __launch_bounds__(256) void k_group_norm(GroupNormArgs a, GnTeam tm) 
   }
 }
 
-// Groups too wide for registers: a workgroup per (group, chunk of rows).
-template <typename Tx, typename To, bool BWD>
-__global__ __launch_bounds__(256) void k_group_norm_wide(GroupNormArgs a, GnTeam tm) {
-  __shared__ float lds[4];
+// Groups too wide for registers: a workgroup per (group, chunk of rows), which
+// reads its rows again from the caches.
+template <typename Tx, typename To, bool VEC, bool BWD>
+__global__ __launch_bounds__(GN_WIDE) void k_group_norm_wide(GroupNormArgs a, GnTeam tm) {
+  __shared__ float lds[GN_WIDE / 64];
   const int m = a.C / a.G, g = blockIdx.x % a.G, chunk = blockIdx.x / a.G;
   const float inv = 1.f / m;
   const To *zt = static_cast<const To*>(a.z), *dyt = static_cast<const To*>(a.dy);
-  float* pw = BWD ? a.part + (long)chunk * 2 * a.C + g * m : nullptr;
+  const float *wt = a.w ? a.w + (long)g * m : nullptr, *bt = a.b ? a.b + (long)g * m : nullptr;
+  float* pw = BWD ? a.part + (long)chunk * 2 * a.C + (long)g * m : nullptr;
+  // fn(first channel, channels) for every piece of the thread
+  auto pieces = [&](auto fn) {
+    for (int c = threadIdx.x * GN_C; c < m; c += GN_WIDE * GN_C) fn(c, min(GN_C, m - c));
+  };
   if constexpr (BWD) {
-    for (int c = threadIdx.x; c < m; c += 256) pw[c] = pw[a.C + c] = 0.f;
+    pieces([&](int c, int nv) {
+      for (int i = 0; i < nv; ++i) pw[c + i] = pw[a.C + c + i] = 0.f;
+    });
   }
   for (long r = chunk; r < a.rows; r += tm.chunks) {
-    const Tx* x = static_cast<const Tx*>(a.x) + r * a.x_row + g * m;
-    const To* z = zt ? zt + r * a.z_row + g * m : nullptr;
+    const Tx* x = static_cast<const Tx*>(a.x) + r * a.x_row + (long)g * m;
+    const To* z = zt ? zt + r * a.z_row + (long)g * m : nullptr;
     float sum = 0.f, sq = 0.f;
-    for (int c = threadIdx.x; c < m; c += 256) sum += to_f(x[c]);
-    const float mean = block_sum(sum, lds) * inv;
-    for (int c = threadIdx.x; c < m; c += 256) {
-      const float d = to_f(x[c]) - mean;
-      sq = fmaf(d, d, sq);
-    }
-    const float rstd = rsqrtf(block_sum(sq, lds) * inv + a.eps);
-    auto norm = [&](int c, float& xh, float& wv) {
-      wv = a.w ? a.w[g * m + c] : 1.f;
-      xh = (to_f(x[c]) - mean) * rstd;
-      return fmaf(xh, wv, a.b ? a.b[g * m + c] : 0.f);
-    };
+    pieces([&](int c, int nv) {
+      Piece<Tx, GN_C, VEC> p;
+      p.load(x + c, nv);
+#pragma unroll
+      for (int i = 0; i < GN_C; ++i) sum += i < nv ? p.get(i) : 0.f;
+    });
+    const float mean = block_sum<GN_WIDE>(sum, lds) * inv;
+    pieces([&](int c, int nv) {
+      Piece<Tx, GN_C, VEC> p;
+      p.load(x + c, nv);
+#pragma unroll
+      for (int i = 0; i < GN_C; ++i) {
+        const float d = i < nv ? p.get(i) - mean : 0.f;
+        sq = fmaf(d, d, sq);
+      }
+    });
+    const float rstd = rsqrtf(block_sum<GN_WIDE>(sq, lds) * inv + a.eps);
     if constexpr (!BWD) {
-      To* y = static_cast<To*>(a.y) + r * a.C + g * m;
-      for (int c = threadIdx.x; c < m; c += 256) {
-        float xh, wv;
-        const float n = norm(c, xh, wv);
-        store_elem(y + c, z ? n * act_of(a.act, to_f(z[c])) : act_of(a.act, n));
-      }
+      pieces([&](int c, int nv) {
+        Piece<Tx, GN_C, VEC> p;
+        Piece<To, GN_C, VEC> pz;
+        p.load(x + c, nv);
+        if (z) pz.load(z + c, nv);
+        float y[GN_C];
+#pragma unroll
+        for (int i = 0; i < GN_C; ++i) {
+          const int at = c + min(i, nv - 1);
+          const float n = fmaf((p.get(i) - mean) * rstd, wt ? wt[at] : 1.f, bt ? bt[at] : 0.f);
+          y[i] = z ? n * act_of(a.act, pz.get(i)) : act_of(a.act, n);
+        }
+        store_piece<To, GN_C, VEC>(static_cast<To*>(a.y) + r * a.C + (long)g * m + c, y, nv);
+      });
     } else {
-      const To* dy = dyt + r * a.C + g * m;
-      Tx* dx = static_cast<Tx*>(a.dx) + r * a.C + g * m;
+      const long row = r * a.C + (long)g * m;
       float s1 = 0.f, s2 = 0.f;
-      auto grad = [&](int c, float& xh, float& dn, float& dz) {
-        float wv, y;
-        const float n = norm(c, xh, wv), gv = to_f(dy[c]);
-        const float sl = act_slope(a.act, z ? to_f(z[c]) : n, y);
-        dn = gv * (z ? y : sl);
-        dz = gv * n * sl;
-        return dn * wv;
+      // fn(i, xh, dn, dn w, dz) for every channel of a piece
+      auto grad = [&](int c, int nv, auto fn) {
+        Piece<Tx, GN_C, VEC> p;
+        Piece<To, GN_C, VEC> pz, py;
+        p.load(x + c, nv);
+        if (z) pz.load(z + c, nv);
+        py.load(dyt + row + c, nv);
+#pragma unroll
+        for (int i = 0; i < GN_C; ++i) {
+          const int at = c + min(i, nv - 1);
+          const float wv = wt ? wt[at] : 1.f, xh = (p.get(i) - mean) * rstd;
+          const float n = fmaf(xh, wv, bt ? bt[at] : 0.f), gv = py.get(i);
+          float y;
+          const float sl = act_slope(a.act, z ? pz.get(i) : n, y), dn = gv * (z ? y : sl);
+          fn(i, xh, dn, dn * wv, gv * n * sl);
+        }
       };
-      for (int c = threadIdx.x; c < m; c += 256) {
-        float xh, dn, dz;
-        const float gw = grad(c, xh, dn, dz);
-        s1 += gw;
-        s2 = fmaf(gw, xh, s2);
-        pw[c] = fmaf(dn, xh, pw[c]);
-        pw[a.C + c] += dn;
-      }
-      s1 = block_sum(s1, lds) * inv;
-      s2 = block_sum(s2, lds) * inv;
-      for (int c = threadIdx.x; c < m; c += 256) {
-        float xh, dn, dz;
-        const float gw = grad(c, xh, dn, dz);
-        if (z) store_elem(static_cast<To*>(a.dz) + r * a.C + g * m + c, dz);
-        store_elem(dx + c, rstd * (gw - s1 - xh * s2));
-      }
+      pieces([&](int c, int nv) {
+        grad(c, nv, [&](int i, float xh, float dn, float gw, float) {
+          if (i >= nv) return;
+          s1 += gw;
+          s2 = fmaf(gw, xh, s2);
+          pw[c + i] = fmaf(dn, xh, pw[c + i]);
+          pw[a.C + c + i] += dn;
+        });
+      });
+      s1 = block_sum<GN_WIDE>(s1, lds) * inv;
+      s2 = block_sum<GN_WIDE>(s2, lds) * inv;
+      pieces([&](int c, int nv) {
+        float dx[GN_C], dz[GN_C];
+        grad(c, nv, [&](int i, float xh, float, float gw, float d) {
+          dx[i] = rstd * (gw - s1 - xh * s2);
+          dz[i] = d;
+        });
+        if (z) store_piece<To, GN_C, VEC>(static_cast<To*>(a.dz) + row + c, dz, nv);
+        store_piece<Tx, GN_C, VEC>(static_cast<Tx*>(a.dx) + row + c, dx, nv);
+      });
     }
   }
 }
@@ -280,10 +324,11 @@ static GnTeam gn_team(const GroupNormArgs& a, int& kv) {
   GnTeam t{};
   t.team = 1;
   while (t.team < 64 && t.team * 2 < pieces) t.team *= 2;
-  if (pieces > 4 * 64) t.team = 256;
+  if (pieces > 4 * 64) t.team = pieces > 4 * 256 ? 512 : 256;
   const int need = (pieces + t.team - 1) / t.team;
   kv = need <= 2 ? 2 : need <= 4 ? 4 : 0;
-  const long lanes = (long)a.G * (kv ? t.team : 256);
+  if (!kv) t.team = GN_WIDE;
+  const long lanes = (long)a.G * t.team;
   long chunks = 256L * GN_LANES / lanes;  // lanes per CU
   chunks = chunks < 1 ? 1 : chunks > a.rows ? a.rows : chunks;
   t.chunks = (int)chunks;
@@ -305,20 +350,25 @@ static hipError_t run_group_norm(const GroupNormArgs& a0) {
     auto ok = [&](const void* p, size_t eb, long row) {
       return !p || ((uintptr_t)p % (GN_C * eb) == 0 && row % GN_C == 0);
     };
+    // four channels in one load or store, or one by one (slices that are not aligned
+    // to four values; 16,384 x 4,096, groups of 128: 81 / 144 us forward, 145 / 277 backward)
     const bool vec = (a.C / a.G) % GN_C == 0 && ok(a.x, sizeof(Tx), a.x_row) && ok(a.z, sizeof(To), a.z_row) &&
                      ok(a.y, sizeof(To), a.C) && ok(a.dy, sizeof(To), a.C) && ok(a.dx, sizeof(Tx), a.C) &&
                      ok(a.dz, sizeof(To), a.C);
-    const long threads = (long)t.chunks * a.G * (kv ? t.team : 256), grid = (threads + 255) / 256;
+    const int th = t.team > 64 ? t.team : 256;
+    const long grid = ((long)t.chunks * a.G * t.team + th - 1) / th;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-#define GN_LAUNCH(KV, BLOCK)                                                                       \
-  if (vec) k_group_norm<Tx, To, KV, true, BLOCK, BWD><<<(unsigned)grid, 256, 0, a.stream>>>(a, t); \
-  else k_group_norm<Tx, To, KV, false, BLOCK, BWD><<<(unsigned)grid, 256, 0, a.stream>>>(a, t);
-    if (kv == 2 && t.team < 256) { GN_LAUNCH(2, false) }
-    else if (kv == 4 && t.team < 256) { GN_LAUNCH(4, false) }
-    else if (kv == 2) { GN_LAUNCH(2, true) }
-    else if (kv == 4) { GN_LAUNCH(4, true) }
-    else k_group_norm_wide<Tx, To, BWD><<<(unsigned)grid, 256, 0, a.stream>>>(a, t);
+#define GN_LAUNCH(KV, TEAM)                                                                      \
+  if (vec) k_group_norm<Tx, To, KV, true, TEAM, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t); \
+  else k_group_norm<Tx, To, KV, false, TEAM, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t);
+    if (kv == 2 && t.team <= 64) { GN_LAUNCH(2, 0) }
+    else if (kv == 4 && t.team <= 64) { GN_LAUNCH(4, 0) }
+    else if (kv == 2) { GN_LAUNCH(2, 256) }
+    else if (kv == 4 && t.team == 256) { GN_LAUNCH(4, 256) }
+    else if (kv == 4) { GN_LAUNCH(4, 512) }
 #undef GN_LAUNCH
+    else if (vec) k_group_norm_wide<Tx, To, true, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t);
+    else k_group_norm_wide<Tx, To, false, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t);
   }
   if (BWD && (a.dw || a.db))
     k_group_norm_dw<<<(unsigned)((2L * a.C + 63) / 64), 64 * GN_WAVES, 0, a.stream>>>(a);

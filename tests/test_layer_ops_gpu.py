@@ -360,6 +360,10 @@ NORM = [
     ("no_affine", dict(rows=8, C=256, G=2, affine=False, gate=True)),
     ("one_row", dict(rows=1, C=2048, G=16, xt="f32", gate=True)),
     ("many_rows", dict(rows=9000, C=128, G=2, gate=True)),
+    ("bf16_odd_6001", dict(rows=5, C=6001, G=1, gate=True, off=1)),
+    ("f32_in_two_groups_8k", dict(rows=270, C=16384, G=2, xt="f32", gate=True)),
+    ("bf16_beyond_registers", dict(rows=600, C=9000, G=1, gate=True)),
+    ("f32_beyond_registers_odd", dict(rows=5, C=24603, G=3, dtype="f32", gate=True, off=1)),
 ]
 
 
