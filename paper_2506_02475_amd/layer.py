@@ -78,6 +78,13 @@ def bind(lib):
         fn.argtypes, fn.restype = [P], Z
 
 
+def _like(t, dtype=None):
+    """An uninitialised contiguous tensor of t's shape (half the host time of new_empty)."""
+    import torch
+
+    return torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format)
+
+
 # ---- argument checks -------------------------------------------------------
 def _code(t, name):
     if t.get_device() < 0:
@@ -225,7 +232,7 @@ def _conv_shape(x, w, bias, h0, activation, cu_seqlens, cu_seqlens_host):
     B, T, D = shape
     K = w.shape[1]
     N, cu, host = _seqs(B, cu_seqlens, cu_seqlens_host, dev)
-    row = _row("x", x, 2, shape, x.dtype, dev)
+    row = 0 if x.is_contiguous() else _row("x", x, 2, shape, x.dtype, dev)
     shp = _CONV.pack(B, T, D, K, N, cu, _host_ptr(host), code, _activation(activation, _CONV_ACT),
                      row)
     ptrs = (x.data_ptr(), _dense("w", w, (D, K), torch.float32, dev),
@@ -243,7 +250,7 @@ def comba_conv_fwd(x, w, bias=None, h0=None, *, activation="silu", cu_seqlens=No
     before its first token, oldest first (None: zeros); ht: those before its next."""
     shp, _host, ptrs, state, dev = _conv_shape(x, w, bias, h0, activation, cu_seqlens,
                                                cu_seqlens_host)
-    y = x.new_empty(x.shape)
+    y = _like(x)
     ht = x.new_empty(state) if output_final_state else None
     _run(load_library().comba_conv_fwd(shp, *ptrs, y.data_ptr(), _ptr(ht),
                                        _on(stream, dev, y, ht)))
@@ -260,7 +267,7 @@ def comba_conv_bwd(x, w, bias, h0, dy, dht=None, *, activation="silu", cu_seqlen
     shp, _host, ptrs, state, dev = _conv_shape(x, w, bias, h0, activation, cu_seqlens,
                                                cu_seqlens_host)
     grads = (_dense("dy", dy, x.shape, x.dtype, dev), _dense("dht", dht, state, x.dtype, dev))
-    out = {"dx": x.new_empty(x.shape), "dw": torch.empty_like(w),
+    out = {"dx": _like(x), "dw": torch.empty_like(w),
            "dbias": None if bias is None else torch.empty_like(bias),
            "dh0": x.new_empty(state) if need_dh0 else None}
     ws = _workspace(lib.comba_conv_workspace_bytes, shp, workspace, x.device)
@@ -283,8 +290,8 @@ def comba_conv_step(x, w, bias, state, *, slots=None, activation="silu", stream=
     B, D = shape
     K, dt, f32 = taps[1], x.dtype, torch.float32
     shp = _CONV.pack(B, 1, D, K, B, 0, 0, code, _activation(activation, _CONV_ACT),
-                     _row("x", x, 1, shape, dt, dev))
-    y = x.new_empty(shape)
+                     0 if x.is_contiguous() else _row("x", x, 1, shape, dt, dev))
+    y = _like(x)
     _run(load_library().comba_conv_step(
         shp, x.data_ptr(), _dense("w", w, taps, f32, dev), _dense("bias", bias, (D,), f32, dev),
         _dense("state", state, (pool[0], K - 1, D), dt, dev), _slots(slots, B, dev), pool[0],
@@ -316,7 +323,8 @@ def _select_shape(lead, u, delta, A, B, C, D, z, delta_bias, delta_softplus, N, 
     else:
         batch, T = shape[0], shape[1]
     shp = _SELECT.pack(batch, T, width, n, G, N, cu, _host_ptr(host), code,
-                       1 if delta_softplus else 0, _row("u", u, lead, shape, dt, dev),
+                       1 if delta_softplus else 0,
+                       0 if u.is_contiguous() else _row("u", u, lead, shape, dt, dev),
                        _row("delta", delta, lead, shape, dt, dev),
                        _row("z", z, lead, shape, dt, dev), _row("B", B, lead, want, dt, dev),
                        _row("C", C, lead, want, dt, dev))
@@ -339,7 +347,7 @@ def _select(save, u, delta, A, B, C, D, z, delta_bias, h0, delta_softplus, cu_se
                                     host)
     state = (S, u.shape[2], n)
     h0p = _dense("h0", h0, state, torch.float32, u.get_device())
-    y = u.new_empty(u.shape)
+    y = _like(u)
     ht = A.new_empty(state) if output_final_state else None
     size = lib.comba_select_bwd_workspace_bytes if save else lib.comba_select_fwd_workspace_bytes
     ws = _workspace(size, shp, workspace, u.device)
@@ -392,11 +400,11 @@ def comba_select_bwd(u, delta, A, B, C, D, z, delta_bias, h0, dy, dht=None, *, w
     state = (S, u.shape[2], n)
     given = (_dense("h0", h0, state, f32, dev), _dense("dy", dy, u.shape, u.dtype, dev),
              _dense("dht", dht, state, f32, dev))
-    out = {"du": u.new_empty(u.shape), "ddelta": u.new_empty(u.shape),
-           "dA": A.new_empty(A.shape), "dB": u.new_empty(bshape), "dC": u.new_empty(bshape),
-           "dD": None if D is None else A.new_empty(D.shape),
-           "dz": None if z is None else u.new_empty(u.shape),
-           "ddelta_bias": None if delta_bias is None else A.new_empty(delta_bias.shape),
+    out = {"du": _like(u), "ddelta": _like(u),
+           "dA": _like(A), "dB": _like(B), "dC": _like(C),
+           "dD": None if D is None else _like(D),
+           "dz": None if z is None else _like(u),
+           "ddelta_bias": None if delta_bias is None else _like(delta_bias),
            "dh0": A.new_empty(state) if need_dh0 else None}
     if workspace is None or workspace.numel() < lib.comba_select_bwd_workspace_bytes(shp):
         raise CombaError("comba: comba_select_bwd needs the workspace filled by "
@@ -421,7 +429,7 @@ def comba_select_step(u, delta, A, B, C, D, z, delta_bias, state, *, slots=None,
     shp, ptrs, n, _ = _select_shape(1, u, delta, A, B, C, D, z, delta_bias, delta_softplus, rows,
                                     0, None)
     dev = u.get_device()
-    y = u.new_empty(shape)
+    y = _like(u)
     _run(load_library().comba_select_step(
         shp, *ptrs, _dense("state", state, (pool[0], shape[1], n), torch.float32, dev),
         _slots(slots, rows, dev), pool[0], y.data_ptr(), _on(stream, dev, y)))
@@ -446,7 +454,8 @@ def _norm_shape(x, groups, weight, bias, z, activation, eps, out):
     C = shape[-1]
     shp = _NORM.pack(x.numel() // C, C, groups, xc,
                      COMBA_BF16 if out is torch.bfloat16 else COMBA_F32,
-                     _activation(activation, _NORM_ACT), eps, _row("x", x, lead, shape, dt, dev),
+                     _activation(activation, _NORM_ACT), eps,
+                     0 if x.is_contiguous() else _row("x", x, lead, shape, dt, dev),
                      _row("z", z, lead, shape, out, dev))
     ptrs = (x.data_ptr(), _dense("weight", weight, (C,), f32, dev),
             _dense("bias", bias, (C,), f32, dev), None if z is None else z.data_ptr())
@@ -462,7 +471,7 @@ def comba_group_norm_fwd(x, groups, weight=None, bias=None, z=None, *, activatio
     ``out_dtype`` (default: the dtype of z, else of x); x is float32 or of that dtype."""
     out = out_dtype or (x.dtype if z is None else z.dtype)
     shp, ptrs = _norm_shape(x, groups, weight, bias, z, activation, eps, out)
-    y = x.new_empty(x.shape, dtype=out)
+    y = _like(x, out)
     _run(load_library().comba_group_norm_fwd(shp, *ptrs, y.data_ptr(),
                                              _on(stream, x.get_device(), y)))
     return y
@@ -475,9 +484,9 @@ def comba_group_norm_bwd(x, groups, weight, bias, z, dy, *, activation="silu", e
     lib = load_library()
     shp, ptrs = _norm_shape(x, groups, weight, bias, z, activation, eps, dy.dtype)
     dyp = _dense("dy", dy, x.shape, dy.dtype, x.get_device())
-    out = {"dx": x.new_empty(x.shape), "dz": None if z is None else dy.new_empty(x.shape),
-           "dweight": None if weight is None else weight.new_empty(weight.shape),
-           "dbias": None if bias is None else bias.new_empty(bias.shape)}
+    out = {"dx": _like(x), "dz": None if z is None else _like(dy),
+           "dweight": None if weight is None else _like(weight),
+           "dbias": None if bias is None else _like(bias)}
     ws = _workspace(lib.comba_group_norm_workspace_bytes, shp, workspace, x.device)
     _run(lib.comba_group_norm_bwd(shp, *ptrs, dyp, _ptr(out["dx"]), _ptr(out["dz"]),
                                   _ptr(out["dweight"]), _ptr(out["dbias"]), ws.data_ptr(),
