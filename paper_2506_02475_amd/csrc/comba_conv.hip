@@ -417,11 +417,16 @@ static bool conv_vec(const ConvArgs& a, int C) {
          ok(a.dy) && ok(a.dht) && ok(a.dx) && ok(a.dh0);
 }
 
-// Channels of a thread of the backward (2 / 4 / 8, with the sums: 96 / 99 / 133 us at 4 x
-// 4,096 tokens, 4,096 channels, bf16; eight leave too few waves).
-constexpr int CONV_BC = 4;
+// Channels of a thread of the backward: two give twice the waves, four read and
+// write wider, from 64 MiB of x on.  us, two / four channels, with the sums: bf16
+// 300 tokens x 256 channels 9.4 / 11.9; 1,000 x 2,048 11.8 / 13.2; 16,384 x 2,048 45.9 /
+// 49.5; 16,384 x 4,096 105 / 105; 16,384 x 5,000 142 / 134; fp32 1,000 x 2,048 12.3 / 14.3;
+// 16,384 x 2,048 90.3 / 88.8.  (Eight leave too few waves: 133 at 16,384 x 4,096.)
+static int conv_bc(const ConvArgs& a) {
+  return (long)a.Ttot * a.D * (a.bf16 ? 2 : 4) <= 64L << 20 ? 2 : 4;
+}
 int conv_bwd_runs(const ConvArgs& a) {
-  const int tokens = conv_run(a, CONV_BC) * CONV_BWAVES;
+  const int tokens = conv_run(a, conv_bc(a)) * CONV_BWAVES;
   return (a.Ttot + tokens - 1) / tokens;
 }
 
@@ -455,17 +460,22 @@ static hipError_t run_conv_step(const ConvArgs& a) {
   return (long)a.N * a.D * (int)sizeof(Tin) >= 4L * 512 * 256 * 8 ? conv_step_rows<Tin, K, 4>(a)
                                                                    : conv_step_rows<Tin, K, 1>(a);
 }
+template <typename Tin, int K, int C>
+static void conv_bwd_main(const ConvArgs& a, unsigned grid) {
+  if (conv_vec(a, C)) k_conv_bwd<Tin, K, C, true><<<grid, 64 * CONV_BWAVES, 0, a.stream>>>(a);
+  else k_conv_bwd<Tin, K, C, false><<<grid, 64 * CONV_BWAVES, 0, a.stream>>>(a);
+}
 template <typename Tin, int K>
 static hipError_t run_conv_bwd(const ConvArgs& a0) {
-  constexpr int C = CONV_BC;
+  const int C = conv_bc(a0);
   ConvArgs a = a0;
   a.run = conv_run(a, C);
   a.nruns = conv_bwd_runs(a);
   const long pgs = ((a.D + C - 1) / C + 63) / 64, grid = pgs * a.nruns;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   if (grid > 0) {
-    if (conv_vec(a, C)) k_conv_bwd<Tin, K, C, true><<<(unsigned)grid, 64 * CONV_BWAVES, 0, a.stream>>>(a);
-    else k_conv_bwd<Tin, K, C, false><<<(unsigned)grid, 64 * CONV_BWAVES, 0, a.stream>>>(a);
+    if (C == 2) conv_bwd_main<Tin, K, 2>(a, (unsigned)grid);
+    else conv_bwd_main<Tin, K, 4>(a, (unsigned)grid);
   }
   const long nb = ((long)(K + 1) * a.D + CONV_DCOLS - 1) / CONV_DCOLS + (a.dh0 ? a.N : 0);
   k_conv_dw<Tin, K><<<(unsigned)nb, 256, 0, a.stream>>>(a);

@@ -163,6 +163,38 @@ def test_conv_longer_runs():
         _hold(n, gr[n], rg[n], b)
 
 
+@pytest.mark.parametrize("dtype,T,D", [("bf16", 8200, 4100), ("bf16", 8200, 4099),
+                                       ("f32", 4110, 4100), ("f32", 4110, 4099)])
+def test_conv_large_inputs(dtype, T, D):
+    """Beyond 64 MiB of x, checked on some channels (no channel meets another)."""
+    import torch
+
+    import paper_2506_02475_amd as comba
+
+    _log("conv large %s %d" % (dtype, D))
+    torch.manual_seed(D)
+    dt, lens = _dt(dtype), [T - 1300, 1, 0, 1299]
+    spans, _ = _spans(1, 0, lens)
+    x, dy = (torch.randn(1, T, D, device="cuda").to(dt) for _ in range(2))
+    h0, dht = (torch.randn(4, 3, D, device="cuda").to(dt) for _ in range(2))
+    w, b = torch.randn(D, 4, device="cuda") * 0.5, torch.randn(D, device="cuda")
+    call = _packed(lens, True)
+    y, ht = comba.comba_conv_fwd(x, w, b, h0, **call)
+    gr = comba.comba_conv_bwd(x, w, b, h0, dy, dht, **call)
+    at = [0, 1, 5, 2050, D - 4, D - 3, D - 2, D - 1]
+    cx, cdy, ch0, cdht = (_np(t[..., at]) for t in (x[0], dy[0], h0, dht))
+    cw, cb = _np(w[at]), _np(b[at])
+    ry, rht = ref.conv_fwd(cx, cw, cb, ch0, spans)
+    rg = ref.conv_bwd(cx, cw, cb, ch0, cdy, cdht, spans)
+    bf16 = dtype == "bf16"
+    _hold("y", y[0][:, at], ry, bf16)
+    assert np.array_equal(_np(ht[..., at]), rht)
+    _hold("dx", gr["dx"][0][:, at], rg["dx"], bf16)
+    _hold("dh0", gr["dh0"][..., at], rg["dh0"], bf16)
+    _hold("dw", gr["dw"][at], rg["dw"], False)
+    _hold("dbias", gr["dbias"][at], rg["dbias"], False)
+
+
 @pytest.mark.parametrize("dtype,D,K,off", [("bf16", 72, 4, 8), ("bf16", 35, 3, 1), ("f32", 20, 2, 4)])
 def test_conv_steps_follow_the_prompt(dtype, D, K, off):
     """Steps through slots of a larger pool, one padding row per step, against the prompt."""
