@@ -94,12 +94,14 @@ typedef struct {
  *   NULL; h0, ht [num_seqs,D,N] fp32 or NULL.
  * Few long rows (packed ones only with cu_seqlens_host) are cut into segments
  * that run side by side; the choice follows from the shape and the device.
- * The workspace holds comba_select_fwd_workspace_bytes; the saving form keeps
- * the states that the backward needs in a workspace of
- * comba_select_bwd_workspace_bytes, which comba_select_bwd takes unmodified
- * together with the same shape and inputs.
+ * The workspace holds comba_select_fwd_workspace_bytes.  The saving form's holds
+ * comba_select_save_bytes and keeps the states that the backward needs:
+ * comba_select_bwd takes it as `saved`, unmodified, together with the same shape
+ * and inputs and a workspace of its own (comba_select_bwd_workspace_bytes, which
+ * need not live between the two).
  */
 size_t comba_select_fwd_workspace_bytes(const comba_select_shape *shape);
+size_t comba_select_save_bytes(const comba_select_shape *shape);
 size_t comba_select_bwd_workspace_bytes(const comba_select_shape *shape);
 comba_status comba_select_fwd(const comba_select_shape *shape, const void *u, const void *delta,
                               const float *A, const void *Bm, const void *Cm, const float *Dskip,
@@ -122,7 +124,8 @@ comba_status comba_select_bwd(const comba_select_shape *shape, const void *u, co
                               const void *z, const float *delta_bias, const float *h0,
                               const void *dy, const float *dht, void *du, void *ddelta, float *dA,
                               void *dB, void *dC, float *dD, void *dz, float *ddelta_bias,
-                              float *dh0, void *ws, size_t ws_bytes, void *stream);
+                              float *dh0, const void *saved, size_t saved_bytes, void *ws,
+                              size_t ws_bytes, void *stream);
 /* One token per row (T = 1): y [B,D]; state [num_slots,D,N] fp32, in place. */
 comba_status comba_select_step(const comba_select_shape *shape, const void *u, const void *delta,
                                const float *A, const void *Bm, const void *Cm, const float *Dskip,

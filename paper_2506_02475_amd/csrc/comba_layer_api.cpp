@@ -236,9 +236,16 @@ void select_rows(comba::SelectArgs* a, bool bwd, comba::SelectRows* q) {
     q->at[k + 1] = q->at[k] + (tokens[k] > a->segmin ? (tokens[k] + a->seglen - 1) / a->seglen : 1);
 }
 
-// The call's work rows, and the workspace of a forward, or (save) of a saving
-// forward and its backward, whose segments are chosen apart.
-SelectLayout select_layout(comba::SelectArgs* a, bool save, bool bwd, comba::SelectRows* q) {
+// The states kept for the backward: a sequence's start at tok0 / select_ck + its
+// number, which leaves room for a partial interval per sequence.
+size_t select_kept_bytes(const comba::SelectArgs& a) {
+  return ((size_t)a.Ttot / comba::select_ck(a.N) + a.S + 1) * a.D * a.N * sizeof(float);
+}
+
+// The call's work rows and the layout of its workspace: of a forward, a saving
+// forward (whose first part the backward reads) or a backward.
+enum class Use { kFwd, kSave, kBwd };
+SelectLayout select_layout(comba::SelectArgs* a, Use use, comba::SelectRows* q) {
   SelectLayout L{};
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -246,21 +253,13 @@ SelectLayout select_layout(comba::SelectArgs* a, bool save, bool bwd, comba::Sel
     off += round_up(bytes);
     return at;
   };
-  size_t cut = 0, all = 0;  // work rows with kept ends of segments; the backward's
-  auto plan = [&](bool dir) {
-    select_rows(a, dir, q);
-    if (a->segs > 1) cut = std::max(cut, (size_t)q->rows);
-    if (dir) all = q->rows;
-  };
-  if (save) plan(!bwd);
-  plan(bwd);
-  if (save) {
-    // states: a sequence's start at tok0 / select_ck + its number, which leaves
-    // room for a partial interval per sequence
-    L.ck = take(((size_t)a->Ttot / comba::select_ck(a->N) + a->S + 1) * a->D * a->N * sizeof(float));
+  select_rows(a, use == Use::kBwd, q);
+  if (use == Use::kSave) L.ck = take(select_kept_bytes(*a));
+  if (use == Use::kBwd) {
     L.bcp = take((size_t)a->G * a->nblk * a->Ttot * 2 * a->N * sizeof(float));
-    L.dap = take(all * a->D * (a->N + 2) * sizeof(float));
+    L.dap = take((size_t)q->rows * a->D * (a->N + 2) * sizeof(float));
   }
+  const size_t cut = a->segs > 1 ? q->rows : 0;  // work rows with kept ends of segments
   L.segF = take(cut * a->D * a->N * sizeof(float));
   L.segdt = take(cut * a->D * sizeof(float));
   L.total = off + kAlign;
@@ -318,6 +317,12 @@ comba_status select_inputs(comba::SelectArgs* a, const void* u, const void* delt
   return COMBA_OK;
 }
 
+size_t select_bytes(const comba_select_shape* shape, Use use) {
+  comba::SelectArgs a;
+  comba::SelectRows q;
+  return select_args(shape, &a) == COMBA_OK ? select_layout(&a, use, &q).total : 0;
+}
+
 comba_status select_fwd(bool save, const comba_select_shape* shape, const void* u, const void* delta,
                         const float* A, const void* Bm, const void* Cm, const float* Dskip,
                         const void* z, const float* bias, const float* h0, void* y, float* ht,
@@ -330,7 +335,7 @@ comba_status select_fwd(bool save, const comba_select_shape* shape, const void* 
   if ((a.Ttot > 0 && !y) || !ws) return COMBA_ERR_NULL;
   if (!aligned(y, a.bf16 ? 2 : 4) || !aligned(ht, 4) || !aligned(ws, kAlign)) return COMBA_ERR_ALIGN;
   comba::SelectRows q;
-  const SelectLayout L = select_layout(&a, save, false, &q);
+  const SelectLayout L = select_layout(&a, save ? Use::kSave : Use::kFwd, &q);
   if (ws_bytes < L.total) return COMBA_ERR_WORKSPACE;
   a.y = y;
   a.ht = ht;
@@ -463,15 +468,15 @@ comba_status comba_conv_step(const comba_conv_shape* shape, const void* x, const
 }
 
 size_t comba_select_fwd_workspace_bytes(const comba_select_shape* shape) {
-  comba::SelectArgs a;
-  comba::SelectRows q;
-  return select_args(shape, &a) == COMBA_OK ? select_layout(&a, false, false, &q).total : 0;
+  return select_bytes(shape, Use::kFwd);
+}
+
+size_t comba_select_save_bytes(const comba_select_shape* shape) {
+  return select_bytes(shape, Use::kSave);
 }
 
 size_t comba_select_bwd_workspace_bytes(const comba_select_shape* shape) {
-  comba::SelectArgs a;
-  comba::SelectRows q;
-  return select_args(shape, &a) == COMBA_OK ? select_layout(&a, true, false, &q).total : 0;
+  return select_bytes(shape, Use::kBwd);
 }
 
 comba_status comba_select_fwd(const comba_select_shape* shape, const void* u, const void* delta,
@@ -496,26 +501,27 @@ comba_status comba_select_bwd(const comba_select_shape* shape, const void* u, co
                               const void* z, const float* delta_bias, const float* h0,
                               const void* dy, const float* dht, void* du, void* ddelta, float* dA,
                               void* dB, void* dC, float* dD, void* dz, float* ddelta_bias,
-                              float* dh0, void* ws, size_t ws_bytes, void* stream) {
+                              float* dh0, const void* saved, size_t saved_bytes, void* ws,
+                              size_t ws_bytes, void* stream) {
   comba::SelectArgs a;
   comba_status st = select_args(shape, &a);
   if (st != COMBA_OK) return st;
   st = select_inputs(&a, u, delta, A, Bm, Cm, Dskip, z, delta_bias, h0);
   if (st != COMBA_OK) return st;
   const bool tok = a.Ttot > 0;
-  if (!dA || !ws || (Dskip && !dD) || (delta_bias && !ddelta_bias) ||
+  if (!dA || !saved || !ws || (Dskip && !dD) || (delta_bias && !ddelta_bias) ||
       (tok && (!dy || !du || !ddelta || !dB || !dC || (z && !dz))))
     return COMBA_ERR_NULL;
   const size_t e = a.bf16 ? 2 : 4;
   if (!aligned(dy, e) || !aligned(du, e) || !aligned(ddelta, e) || !aligned(dB, e) || !aligned(dC, e) ||
       !aligned(dz, e) || !aligned(dht, 4) || !aligned(dA, 4) || !aligned(dD, 4) ||
-      !aligned(ddelta_bias, 4) || !aligned(dh0, 4) || !aligned(ws, kAlign))
+      !aligned(ddelta_bias, 4) || !aligned(dh0, 4) || !aligned(saved, kAlign) || !aligned(ws, kAlign))
     return COMBA_ERR_ALIGN;
   comba::SelectRows q;
-  const SelectLayout L = select_layout(&a, true, true, &q);
-  if (ws_bytes < L.total) return COMBA_ERR_WORKSPACE;
+  const SelectLayout L = select_layout(&a, Use::kBwd, &q);
+  if (saved_bytes < select_kept_bytes(a) || ws_bytes < L.total) return COMBA_ERR_WORKSPACE;
   char* base = static_cast<char*>(ws);
-  a.ck = reinterpret_cast<float*>(base + L.ck);
+  a.kept = static_cast<const float*>(saved);
   a.bcp = reinterpret_cast<float*>(base + L.bcp);
   a.dap = reinterpret_cast<float*>(base + L.dap);
   a.segF = reinterpret_cast<float*>(base + L.segF);

@@ -54,7 +54,9 @@ struct SelectArgs {
   const float *A, *Dskip, *bias, *h0;
   void* y;
   float* ht;
-  float* ck;  // states at every select_ck(N)-th token of each sequence, or NULL
+  // states at every select_ck(N)-th token of each sequence: written (or NULL), read
+  float* ck;
+  const float* kept;
   // step
   float* state;
   const int32_t* slots;

@@ -617,7 +617,7 @@ __global__ __launch_bounds__(16 * select_ck(N)) void k_select_bwd(SelectArgs a, 
   RowsAt tb(a.Bm, last, a.b_row * EB), tc(a.Cm, last, a.c_row * EB);
   RowsAt tdu(a.du, last, yb), tdd(a.ddelta, last, yb), tdz(a.dz, last, yb);
   RowsAt tbc(a.bcp, (long)sb.blk * a.Ttot + last, 2 * N * 4);
-  const float* ck = a.ck + (long)(sb.tok0 / select_ck(N) + sb.seq + max(ntiles - 1, 0)) * a.D * N;
+  const float* ck = a.kept + (long)(sb.tok0 / select_ck(N) + sb.seq + max(ntiles - 1, 0)) * a.D * N;
   auto load = [&](int tile) {
     const int rows = min(len - tile * TILE, TILE);
     const auto ru = tu.rows(rows), rd = td.rows(rows), rb = tb.rows(rows), rc = tc.rows(rows);

@@ -66,14 +66,15 @@ def bind(lib):
                        ("comba_conv_step", [P] * 6 + [_I32, P, P]),
                        ("comba_select_fwd", [P] * 13 + [Z, P]),
                        ("comba_select_fwd_save", [P] * 13 + [Z, P]),
-                       ("comba_select_bwd", [P] * 22 + [Z, P]),
+                       ("comba_select_bwd", [P] * 22 + [Z, P, Z, P]),
                        ("comba_select_step", [P] * 11 + [_I32, P, P]),
                        ("comba_group_norm_fwd", [P] * 7),
                        ("comba_group_norm_bwd", [P] * 11 + [Z, P])):
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, I
     for name in ("comba_conv_workspace_bytes", "comba_select_fwd_workspace_bytes",
-                 "comba_select_bwd_workspace_bytes", "comba_group_norm_workspace_bytes"):
+                 "comba_select_save_bytes", "comba_select_bwd_workspace_bytes",
+                 "comba_group_norm_workspace_bytes"):
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = [P], Z
 
@@ -349,7 +350,7 @@ def _select(save, u, delta, A, B, C, D, z, delta_bias, h0, delta_softplus, cu_se
     h0p = _dense("h0", h0, state, torch.float32, u.get_device())
     y = _like(u)
     ht = A.new_empty(state) if output_final_state else None
-    size = lib.comba_select_bwd_workspace_bytes if save else lib.comba_select_fwd_workspace_bytes
+    size = lib.comba_select_save_bytes if save else lib.comba_select_fwd_workspace_bytes
     ws = _workspace(size, shp, workspace, u.device)
     fn = lib.comba_select_fwd_save if save else lib.comba_select_fwd
     _run(fn(shp, *ptrs, h0p, y.data_ptr(), _ptr(ht), ws.data_ptr(), ws.numel(),
@@ -383,8 +384,9 @@ def comba_select_fwd_save(u, delta, A, B, C, D=None, z=None, delta_bias=None, h0
 
 def comba_select_bwd(u, delta, A, B, C, D, z, delta_bias, h0, dy, dht=None, *, workspace,
                      delta_softplus=True, cu_seqlens=None, cu_seqlens_host=None, need_dh0=True,
-                     stream=None):
-    """Backward of comba_select_fwd_save from dy [B,T,D] (dtype of u) and dht [S,D,N] float32.
+                     scratch=None, stream=None):
+    """Backward of comba_select_fwd_save from dy [B,T,D] (dtype of u) and dht [S,D,N] float32,
+    with the ``workspace`` it filled; ``scratch``: memory for the call itself, made if absent.
     Returns dict du, ddelta, dz, dB, dC (dtype of u), dA, dD, ddelta_bias, dh0 (float32); the
     entries of absent inputs are None."""
     import torch
@@ -406,13 +408,15 @@ def comba_select_bwd(u, delta, A, B, C, D, z, delta_bias, h0, dy, dht=None, *, w
            "dz": None if z is None else _like(u),
            "ddelta_bias": None if delta_bias is None else _like(delta_bias),
            "dh0": A.new_empty(state) if need_dh0 else None}
-    if workspace is None or workspace.numel() < lib.comba_select_bwd_workspace_bytes(shp):
+    if workspace is None or workspace.numel() < lib.comba_select_save_bytes(shp):
         raise CombaError("comba: comba_select_bwd needs the workspace filled by "
                          "comba_select_fwd_save")
+    ws = _workspace(lib.comba_select_bwd_workspace_bytes, shp, scratch, u.device)
     _run(lib.comba_select_bwd(
         shp, *ptrs, *given, *(_ptr(out[k]) for k in ("du", "ddelta", "dA", "dB", "dC", "dD", "dz",
                                                      "ddelta_bias", "dh0")),
-        workspace.data_ptr(), workspace.numel(), _on(stream, dev, *out.values())))
+        workspace.data_ptr(), workspace.numel(), ws.data_ptr(), ws.numel(),
+        _on(stream, dev, ws, *out.values())))
     return out
 
 
@@ -570,9 +574,13 @@ def comba_conv(x, w, bias=None, h0=None, *, activation="silu", cu_seqlens=None,
 def comba_select(u, delta, A, B, C, D=None, z=None, delta_bias=None, h0=None, *,
                  delta_softplus=True, cu_seqlens=None, cu_seqlens_host=None):
     """Differentiable comba_select_fwd: (y, ht); gradients flow to every tensor.  Each call
-    keeps its workspace until the backward has run."""
+    keeps a state every 48 tokens (N = 8: 32) until the backward has run."""
     kw = dict(delta_softplus=delta_softplus, cu_seqlens=cu_seqlens,
               cu_seqlens_host=cu_seqlens_host)
+    import torch
+
+    if not torch.is_grad_enabled():
+        return comba_select_fwd(u, delta, A, B, C, D, z, delta_bias, h0, **kw)
     return _functions()["select"].apply(u, delta, A, B, C, D, z, delta_bias, h0, kw)
 
 

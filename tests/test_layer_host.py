@@ -50,18 +50,21 @@ CALLS = {
     "comba_select_fwd": ("u delta A B C D? z? bias? h0? y ht? ws", "ws"),
     "comba_select_fwd_save": ("u delta A B C D? z? bias? h0? y ht? ws", "ws"),
     "comba_select_bwd": ("u delta A B C D? z? bias? h0? dy dht? du ddelta dA dB dC dD dz dbias "
-                         "dh0? ws", "ws"),
+                         "dh0? saved saved_bytes ws", "ws"),
     "comba_select_step": ("u delta A B C D? z? bias? state slots? num_slots y", None),
     "comba_group_norm_fwd": ("x w? b? z? y", None),
     "comba_group_norm_bwd": ("x w? b? z? dy dx dz dw? db? ws", "ws"),
 }
 
 
+SIZES = {"num_slots": 4, "saved_bytes": BIG}
+
+
 def call(name, shp, ws_bytes=BIG, **over):
     names, ws = CALLS[name]
     args = []
     for n in names.split():
-        v = over.get(n.rstrip("?"), 4 if n == "num_slots" else FAKE)
+        v = over.get(n.rstrip("?"), SIZES.get(n, FAKE))
         args.append(v)
     if ws:
         args.append(ws_bytes)
@@ -81,7 +84,8 @@ def test_layer_header_is_exported_and_bound():
     declared = comba.exported_symbols("comba_layer.h")
     assert declared == sorted(list(CALLS) + [
         "comba_conv_workspace_bytes", "comba_select_fwd_workspace_bytes",
-        "comba_select_bwd_workspace_bytes", "comba_group_norm_workspace_bytes"])
+        "comba_select_save_bytes", "comba_select_bwd_workspace_bytes",
+        "comba_group_norm_workspace_bytes"])
     out = subprocess.run(["nm", "-D", "--defined-only", comba.library_path()],
                          capture_output=True, text=True, check=True).stdout
     exported = {line.split()[-1] for line in out.splitlines() if line.strip()}
@@ -96,7 +100,7 @@ def test_layer_header_is_exported_and_bound():
 def test_required_pointers(name):
     assert call(name, None) == ENULL
     for n in CALLS[name][0].split():
-        if n.endswith("?") or n == "num_slots":
+        if n.endswith("?") or n in SIZES:
             continue
         assert call(name, shape_of(name), **{n: None}) == ENULL, n
 
@@ -105,9 +109,9 @@ def test_required_pointers(name):
 def test_misaligned_pointers(name):
     for n in CALLS[name][0].split():
         n = n.rstrip("?")
-        if n == "num_slots":
+        if n in SIZES:
             continue
-        bad = FAKE + (128 if n == "ws" else 1)
+        bad = FAKE + (128 if n in ("ws", "saved") else 1)
         assert call(name, shape_of(name), **{n: bad}) == EALIGN, n
 
 
@@ -133,6 +137,7 @@ def test_select_shapes(over, code):
     lib = comba.load_library()
     assert lib.comba_select_fwd_workspace_bytes(ctypes.byref(select(**over))) == 0
     assert lib.comba_select_bwd_workspace_bytes(ctypes.byref(select(**over))) == 0
+    assert lib.comba_select_save_bytes(ctypes.byref(select(**over))) == 0
 
 
 @pytest.mark.parametrize("over,code", [
@@ -165,16 +170,19 @@ def test_workspaces():
     lib = comba.load_library()
     for name, size, shp in (("comba_conv_bwd", lib.comba_conv_workspace_bytes, conv()),
                             ("comba_select_fwd", lib.comba_select_fwd_workspace_bytes, select()),
-                            ("comba_select_fwd_save", lib.comba_select_bwd_workspace_bytes,
-                             select()),
+                            ("comba_select_fwd_save", lib.comba_select_save_bytes, select()),
                             ("comba_select_bwd", lib.comba_select_bwd_workspace_bytes, select()),
                             ("comba_group_norm_bwd", lib.comba_group_norm_workspace_bytes, norm())):
         n = size(ctypes.byref(shp))
         assert n > 0
         assert call(name, shp, ws_bytes=n - 1) == EWS, name
-    # the states kept for the backward dominate: one per 32 tokens and sequence
-    long = select(B=1, T=32000, num_seqs=1)
-    assert lib.comba_select_bwd_workspace_bytes(ctypes.byref(long)) >= 1000 * 32 * 16 * 4
+    # the states kept for the backward: one per 48 tokens (8 states a channel: 32) and sequence
+    for n, every in ((16, 48), (8, 32)):
+        long = select(B=1, T=32000, num_seqs=1, N=n)
+        kept = (32000 // every + 2) * 32 * n * 4
+        assert lib.comba_select_save_bytes(ctypes.byref(long)) >= kept
+        assert call("comba_select_bwd", long, saved_bytes=kept - 1) == EWS
+        assert lib.comba_select_bwd_workspace_bytes(ctypes.byref(long)) >= 32000 * 2 * n * 4
 
 
 def test_tokens_need_a_sequence():
