@@ -6,7 +6,7 @@
 // Streaming kernels, bound by bytes: a thread holds C consecutive channels and
 // walks a run of tokens with the K - 1 previous rows in registers, so a row is
 // read once but for the runs' first K - 1 rows.  4 x 4,096 tokens, 4,096 channels,
-// 4 taps, bf16: forward 54 us (5.0 TB/s), backward 92 us (4.4 TB/s: the runs' own
+// 4 taps, bf16: forward 49 us (5.5 TB/s), backward 92 us (4.4 TB/s: the runs' own
 // rows; 9% more is read again at their ends) and 6 for the sums.
 #include "comba_layer_device.hpp"
 #include "comba_layer_launch.h"
@@ -19,7 +19,8 @@ constexpr int CONV_BWAVES = 4;    // runs of a workgroup of the backward
 // Tokens per run: 32, or 16 or 8 where 32 would leave less than three waves a
 // SIMD (a run reads K - 1 rows more than its own; the backward forms as many du
 // more).  us by run 8 / 16 / 32 / 64, bf16: forward 16,384 tokens x 4,096 channels
-// 84 / 68 / 59 / 64; 18,384 x 2,048: 41 / 34 / 39 / 36; 1,000 x 2,048: 12 / 12 / 18 / 29.
+// 54 / 50 / 49 / 51; 16,384 x 2,048: 29 / 26 / 26 / 27; 1,000 x 2,048: 5.3 / 5.9 / 7.8 /
+// 12; backward 137 / 113 / 99 / 103; 72 / 54 / 46 / 46; 12 / 12 / 16 / 23.
 static int conv_run(const ConvArgs& a, int C) {
   const long items = (long)a.Ttot * ((a.D + C - 1) / C);
   return items >= 32L * 192 * 1024 ? 32 : items >= 16L * 64 * 1024 ? 16 : 8;
@@ -45,33 +46,23 @@ __device__ __forceinline__ void seq_of_token(const int32_t* __restrict__ cu, int
   se = min(max(cu[lo + 1], t + 1), Ttot);
 }
 
-// Channels of a piece, of which nv exist (a piece past D reads the last one's place).
-struct ConvPiece {
-  int c, nv;
-};
-template <int C>
-__device__ __forceinline__ ConvPiece conv_piece(int p, int D) {
-  const int c = min(p * C, max(0, D - 1) / C * C);
-  return {c, min(C, D - c)};
-}
-
 template <int K, int C>
-__device__ __forceinline__ void load_taps(const float* __restrict__ w, int c, int nv, float (&wt)[K][C]) {
+__device__ __forceinline__ void load_taps(const float* __restrict__ w, int c, float (&wt)[K][C]) {
 #pragma unroll
   for (int i = 0; i < C; ++i)
 #pragma unroll
-    for (int j = 0; j < K; ++j) wt[j][i] = w[(long)(c + min(i, nv - 1)) * K + j];
+    for (int j = 0; j < K; ++j) wt[j][i] = w[(long)(c + i) * K + j];
 }
 
 // Row `pos` of sequence s (negative: its history) as floats.
-template <typename Tin, int K, int C, bool VEC>
-__device__ __forceinline__ void load_ext(const ConvArgs& a, int s, int sa, int pos, int c, int nv,
+template <typename Tin, int K, int C>
+__device__ __forceinline__ void load_ext(const ConvArgs& a, int s, int sa, int pos, int c,
                                          float (&v)[C]) {
-  Piece<Tin, C, VEC> p;
+  Piece<Tin, C, true> p;
   if (pos >= 0) {
-    p.load(static_cast<const Tin*>(a.x) + (long)(sa + pos) * a.x_row + c, nv);
+    p.load(static_cast<const Tin*>(a.x) + (long)(sa + pos) * a.x_row + c, C);
   } else if (a.h0) {
-    p.load(static_cast<const Tin*>(a.h0) + ((long)s * (K - 1) + (K - 1) + pos) * a.D + c, nv);
+    p.load(static_cast<const Tin*>(a.h0) + ((long)s * (K - 1) + (K - 1) + pos) * a.D + c, C);
   } else {
     p.zero();
   }
@@ -79,13 +70,12 @@ __device__ __forceinline__ void load_ext(const ConvArgs& a, int s, int sa, int p
   for (int i = 0; i < C; ++i) v[i] = p.get(i);
 }
 
-template <typename Tin, int K, int C, bool VEC>
+template <typename Tin, int K, int C>
 __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a) {
-  const int pieces = (a.D + C - 1) / C, nruns = (a.Ttot + a.run - 1) / a.run;
+  const int pieces = a.D / C, nruns = (a.Ttot + a.run - 1) / a.run;
   const long e = (long)blockIdx.x * 256 + threadIdx.x;
   const long r = e / pieces;
-  const ConvPiece cp = conv_piece<C>(e % pieces, a.D);
-  const int c = cp.c, nv = cp.nv;
+  const int c = e % pieces * C;
   if (r >= nruns) {  // the final histories
     const long k = r - nruns;
     if (!a.ht || k >= (long)a.N * (K - 1)) return;
@@ -93,28 +83,28 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a) {
     int sa, se;
     seq_range(a.cu_seqlens, s, a.Tseq, a.Ttot, sa, se);
     float v[C];
-    load_ext<Tin, K, C, VEC>(a, s, sa, se - sa - (K - 1) + j, c, nv, v);
-    store_piece<Tin, C, VEC>(static_cast<Tin*>(a.ht) + k * a.D + c, v, nv);
+    load_ext<Tin, K, C>(a, s, sa, se - sa - (K - 1) + j, c, v);
+    store_piece<Tin, C, true>(static_cast<Tin*>(a.ht) + k * a.D + c, v, C);
     return;
   }
   const int t0 = r * a.run, t1 = min(t0 + a.run, a.Ttot);
   float wt[K][C], b[C], xw[K - 1][C];
-  load_taps<K, C>(a.w, c, nv, wt);
+  load_taps<K, C>(a.w, c, wt);
 #pragma unroll
-  for (int i = 0; i < C; ++i) b[i] = a.bias ? a.bias[c + min(i, nv - 1)] : 0.f;
+  for (int i = 0; i < C; ++i) b[i] = a.bias ? a.bias[c + i] : 0.f;
   const Tin* x = static_cast<const Tin*>(a.x) + c;
   Tin* y = static_cast<Tin*>(a.y) + c;
   int s, sa, se;
   seq_of_token(a.cu_seqlens, a.N, a.Tseq, a.Ttot, t0, s, sa, se);
 #pragma unroll
-  for (int m = 0; m < K - 1; ++m) load_ext<Tin, K, C, VEC>(a, s, sa, t0 - sa - (K - 1) + m, c, nv, xw[m]);
-  Piece<Tin, C, VEC> xr[CONV_PF];
+  for (int m = 0; m < K - 1; ++m) load_ext<Tin, K, C>(a, s, sa, t0 - sa - (K - 1) + m, c, xw[m]);
+  Piece<Tin, C, true> xr[CONV_PF];
 #pragma unroll
-  for (int k = 0; k < CONV_PF; ++k) xr[k].load(x + (long)min(t0 + k, t1 - 1) * a.x_row, nv);
+  for (int k = 0; k < CONV_PF; ++k) xr[k].load(x + (long)min(t0 + k, t1 - 1) * a.x_row, C);
   for (int tb = t0; tb < t1; tb += CONV_PF) {
-    Piece<Tin, C, VEC> xn[CONV_PF];
+    Piece<Tin, C, true> xn[CONV_PF];
 #pragma unroll
-    for (int k = 0; k < CONV_PF; ++k) xn[k].load(x + (long)min(tb + CONV_PF + k, t1 - 1) * a.x_row, nv);
+    for (int k = 0; k < CONV_PF; ++k) xn[k].load(x + (long)min(tb + CONV_PF + k, t1 - 1) * a.x_row, C);
     auto token = [&](int k) {
       const int t = tb + k;
       float o[C];
@@ -130,7 +120,7 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a) {
         for (int m = 0; m < K - 2; ++m) xw[m][i] = xw[m + 1][i];
         xw[K - 2][i] = xv;
       }
-      store_piece<Tin, C, VEC>(y + (long)t * a.D, o, nv);
+      store_piece<Tin, C, true>(y + (long)t * a.D, o, C);
     };
     if (tb + CONV_PF <= min(t1, se)) {  // inside one sequence: straight-line code
 #pragma unroll
@@ -143,7 +133,7 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a) {
           if (t >= se) {  // the next sequence starts with its own history
             seq_of_token(a.cu_seqlens, a.N, a.Tseq, a.Ttot, t, s, sa, se);
 #pragma unroll
-            for (int m = 0; m < K - 1; ++m) load_ext<Tin, K, C, VEC>(a, s, sa, m - (K - 1), c, nv, xw[m]);
+            for (int m = 0; m < K - 1; ++m) load_ext<Tin, K, C>(a, s, sa, m - (K - 1), c, xw[m]);
           }
           token(k);
         }
@@ -157,20 +147,20 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a) {
 // One token per row; the state's rows move up by one.  A thread takes its
 // channels of R rows, so that the taps, twice a row's bytes, are read once.  64
 // rows of 4,096 channels: 3.2 us, less than the host takes for the call.
-template <typename Tin, int K, int C, bool VEC, int R>
+template <typename Tin, int K, int C, int R>
 __global__ __launch_bounds__(256) void k_conv_step(ConvArgs a) {
-  const int pieces = (a.D + C - 1) / C;
+  const int pieces = a.D / C;
   const long e = (long)blockIdx.x * 256 + threadIdx.x;
   const long row0 = e / pieces * R;
   if (row0 >= a.N) return;
-  const auto [c, nv] = conv_piece<C>(e % pieces, a.D);
+  const int c = e % pieces * C;
   int slot[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const long row = min(row0 + r, (long)a.N - 1);
     slot[r] = a.slots ? a.slots[row] : (int)row;
   }
-  Piece<Tin, C, VEC> p[R][K];
+  Piece<Tin, C, true> p[R][K];
   Tin* st[R];
   bool on[R];
 #pragma unroll
@@ -179,14 +169,14 @@ __global__ __launch_bounds__(256) void k_conv_step(ConvArgs a) {
     st[r] = static_cast<Tin*>(a.state) + (long)(on[r] ? slot[r] : 0) * (K - 1) * a.D + c;
     if (a.num_slots > 0) {
 #pragma unroll
-      for (int j = 0; j < K - 1; ++j) p[r][j].load(st[r] + (long)j * a.D, nv);
+      for (int j = 0; j < K - 1; ++j) p[r][j].load(st[r] + (long)j * a.D, C);
     }
-    p[r][K - 1].load(static_cast<const Tin*>(a.x) + min(row0 + r, (long)a.N - 1) * a.x_row + c, nv);
+    p[r][K - 1].load(static_cast<const Tin*>(a.x) + min(row0 + r, (long)a.N - 1) * a.x_row + c, C);
   }
   float wt[K][C], b[C];
-  load_taps<K, C>(a.w, c, nv, wt);
+  load_taps<K, C>(a.w, c, wt);
 #pragma unroll
-  for (int i = 0; i < C; ++i) b[i] = a.bias ? a.bias[c + min(i, nv - 1)] : 0.f;
+  for (int i = 0; i < C; ++i) b[i] = a.bias ? a.bias[c + i] : 0.f;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     if (row0 + r >= a.N) break;
@@ -201,10 +191,10 @@ __global__ __launch_bounds__(256) void k_conv_step(ConvArgs a) {
       }
       o[i] = on[r] ? (a.silu ? u * sigmoid_acc(u) : u) : 0.f;
     }
-    store_piece<Tin, C, VEC>(static_cast<Tin*>(a.y) + (row0 + r) * a.D + c, o, nv);
+    store_piece<Tin, C, true>(static_cast<Tin*>(a.y) + (row0 + r) * a.D + c, o, C);
     if (on[r]) {
 #pragma unroll
-      for (int j = 0; j < K - 1; ++j) store_piece<Tin, C, VEC>(st[r] + (long)j * a.D, v[j + 1], nv);
+      for (int j = 0; j < K - 1; ++j) store_piece<Tin, C, true>(st[r] + (long)j * a.D, v[j + 1], C);
     }
   }
 }
@@ -214,15 +204,14 @@ __global__ __launch_bounds__(256) void k_conv_step(ConvArgs a) {
 // and keeps the K rows still open in registers.  Rows before a sequence's first
 // token are its history's; dht adds to the last K - 1 extended rows.  A run's dw
 // and dbias are summed over the workgroup's runs in LDS.
-template <typename Tin, int K, int C, bool VEC>
+template <typename Tin, int K, int C>
 __global__ __launch_bounds__(64 * CONV_BWAVES) void k_conv_bwd(ConvArgs a) {
   __shared__ float part[CONV_BWAVES][K + 1][C][64];
-  const int pieces = (a.D + C - 1) / C, pgs = (pieces + 63) / 64;
+  const int pieces = a.D / C, pgs = (pieces + 63) / 64;
   const int pg = blockIdx.x % pgs, rb = blockIdx.x / pgs;
   const int lane = lane_id(), w = wave_id_s();
   const int piece = pg * 64 + lane;
-  const ConvPiece cp = conv_piece<C>(piece, a.D);
-  const int c = cp.c, nl = cp.nv, nv = piece < pieces ? nl : 0;  // channels loaded, stored
+  const int c = min(piece, pieces - 1) * C, nv = piece < pieces ? C : 0;  // channels stored
   const int t0 = (rb * CONV_BWAVES + w) * a.run, t1 = min(t0 + a.run, a.Ttot);
   float dw[K][C], db[C];
 #pragma unroll
@@ -233,14 +222,14 @@ __global__ __launch_bounds__(64 * CONV_BWAVES) void k_conv_bwd(ConvArgs a) {
   }
   if (t0 < a.Ttot) {
     float wt[K][C], b[C], xw[K - 1][C], acc[K][C];
-    load_taps<K, C>(a.w, c, nl, wt);
+    load_taps<K, C>(a.w, c, wt);
 #pragma unroll
-    for (int i = 0; i < C; ++i) b[i] = a.bias ? a.bias[c + min(i, nl - 1)] : 0.f;
+    for (int i = 0; i < C; ++i) b[i] = a.bias ? a.bias[c + i] : 0.f;
     int s, sa, se;
     seq_of_token(a.cu_seqlens, a.N, a.Tseq, a.Ttot, t0, s, sa, se);
     auto enter = [&](int t) {  // the window before token t of sequence s
 #pragma unroll
-      for (int m = 0; m < K - 1; ++m) load_ext<Tin, K, C, VEC>(a, s, sa, t - sa - (K - 1) + m, c, nl, xw[m]);
+      for (int m = 0; m < K - 1; ++m) load_ext<Tin, K, C>(a, s, sa, t - sa - (K - 1) + m, c, xw[m]);
 #pragma unroll
       for (int m = 0; m < K; ++m)
 #pragma unroll
@@ -255,26 +244,26 @@ __global__ __launch_bounds__(64 * CONV_BWAVES) void k_conv_bwd(ConvArgs a) {
 #pragma unroll
       for (int i = 0; i < C; ++i) o[i] = v[i];
       if (a.dht && tail >= 0) {
-        Piece<Tin, C, VEC> p;
-        p.load(static_cast<const Tin*>(a.dht) + ((long)s * (K - 1) + tail) * a.D + c, nl);
+        Piece<Tin, C, true> p;
+        p.load(static_cast<const Tin*>(a.dht) + ((long)s * (K - 1) + tail) * a.D + c, C);
 #pragma unroll
         for (int i = 0; i < C; ++i) o[i] += p.get(i);
       }
       Tin* at = tok ? static_cast<Tin*>(a.dx) + (long)r * a.D + c
                     : static_cast<Tin*>(a.dh0) + ((long)s * (K - 1) + ext) * a.D + c;
-      store_piece<Tin, C, VEC>(at, o, nv);
+      store_piece<Tin, C, true>(at, o, nv);
     };
     enter(t0);
     const Tin *x = static_cast<const Tin*>(a.x) + c, *dy = static_cast<const Tin*>(a.dy) + c;
     const int tstop = min(t1 + K - 1, a.Ttot);
     bool done = false;
-    Piece<Tin, C, VEC> xb[CONV_PF], gb[CONV_PF], xn[CONV_PF], gn[CONV_PF];
-    auto load = [&](int tb, Piece<Tin, C, VEC>(&xp)[CONV_PF], Piece<Tin, C, VEC>(&gp)[CONV_PF]) {
+    Piece<Tin, C, true> xb[CONV_PF], gb[CONV_PF], xn[CONV_PF], gn[CONV_PF];
+    auto load = [&](int tb, Piece<Tin, C, true>(&xp)[CONV_PF], Piece<Tin, C, true>(&gp)[CONV_PF]) {
 #pragma unroll
       for (int k = 0; k < CONV_PF; ++k) {
         const long row = min(tb + k, tstop - 1);
-        xp[k].load(x + row * a.x_row, nl);
-        gp[k].load(dy + row * a.D, nl);
+        xp[k].load(x + row * a.x_row, C);
+        gp[k].load(dy + row * a.D, C);
       }
     };
     load(t0, xb, gb);
@@ -321,7 +310,7 @@ __global__ __launch_bounds__(64 * CONV_BWAVES) void k_conv_bwd(ConvArgs a) {
 #pragma unroll
         for (int k = 0; k < CONV_PF; ++k) {
           token(k, true);
-          store_piece<Tin, C, VEC>(static_cast<Tin*>(a.dx) + (long)(tb + k - (K - 1)) * a.D + c, acc[0], nv);
+          store_piece<Tin, C, true>(static_cast<Tin*>(a.dx) + (long)(tb + k - (K - 1)) * a.D + c, acc[0], nv);
           next_row();
         }
       } else {
@@ -407,10 +396,11 @@ __global__ __launch_bounds__(256) void k_conv_dw(ConvArgs a) {
   }
 }
 
-// Whether every piece of C channels is loaded and stored at once, or channel by
-// channel (4 x 4,096 tokens, 4,096 channels: 51 / 131 us forward, 98 / 177 backward;
-// a step of 512 rows 7.8 / 13.5).
-static bool conv_vec(const ConvArgs& a, int C) {
+// Whether the width and the alignment of every tensor allow C channels a thread, as
+// one load or store; else it takes two or one (the step: one).  Forward, us with two /
+// one: bf16 16,384 x 4,094 and 4,095 54 / 66; eight channels loaded one by one
+// would take 137.
+static bool conv_fits(const ConvArgs& a, int C) {
   const long m = C * (a.bf16 ? 2 : 4);
   auto ok = [&](const void* p) { return !p || (uintptr_t)p % m == 0; };
   return a.D % C == 0 && a.x_row % C == 0 && ok(a.x) && ok(a.h0) && ok(a.y) && ok(a.ht) && ok(a.state) &&
@@ -425,33 +415,44 @@ static bool conv_vec(const ConvArgs& a, int C) {
 static int conv_bc(const ConvArgs& a) {
   return (long)a.Ttot * a.D * (a.bf16 ? 2 : 4) <= 64L << 20 ? 2 : 4;
 }
+// (From the shape alone: the workspace is sized before there are tensors.)
+static int conv_bwd_run(const ConvArgs& a) { return conv_run(a, conv_bc(a)); }
 int conv_bwd_runs(const ConvArgs& a) {
-  const int tokens = conv_run(a, conv_bc(a)) * CONV_BWAVES;
+  const int tokens = conv_bwd_run(a) * CONV_BWAVES;
   return (a.Ttot + tokens - 1) / tokens;
 }
 
-template <typename Tin, int K>
-static hipError_t run_conv_fwd(const ConvArgs& a0) {
-  constexpr int C = 16 / (int)sizeof(Tin);
-  ConvArgs a = a0;
-  const long pieces = (a.D + C - 1) / C;
+template <typename Tin, int K, int C>
+static hipError_t conv_fwd_main(ConvArgs a) {
   a.run = conv_run(a, C);
-  const long items = ((long)(a.Ttot + a.run - 1) / a.run + (a.ht ? (long)a.N * (K - 1) : 0)) * pieces;
+  const long items = ((long)(a.Ttot + a.run - 1) / a.run + (a.ht ? (long)a.N * (K - 1) : 0)) * (a.D / C);
   const long grid = (items + 255) / 256;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   if (grid == 0) return hipSuccess;
-  if (conv_vec(a, C)) k_conv_fwd<Tin, K, C, true><<<(unsigned)grid, 256, 0, a.stream>>>(a);
-  else k_conv_fwd<Tin, K, C, false><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  k_conv_fwd<Tin, K, C><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  return hipGetLastError();
+}
+template <typename Tin, int K>
+static hipError_t run_conv_fwd(const ConvArgs& a) {
+  // two channels, in fp32 four where they fit (bf16, us with 8 / 4 / 2: 16,384 x 4,096 52.8 /
+  // 52.8 / 48.5; 16,384 x 2,048 30.2 / 26.8 / 25.8; 1,000 x 2,048 7.5 / 5.8 / 5.3; fp32 with 4 / 2:
+  // 16,384 x 4,096 108.7 / 111.7; 16,384 x 2,048 44.6 / 48.1)
+  if constexpr (sizeof(Tin) == 4) {
+    if (conv_fits(a, 4)) return conv_fwd_main<Tin, K, 4>(a);
+  }
+  return conv_fits(a, 2) ? conv_fwd_main<Tin, K, 2>(a) : conv_fwd_main<Tin, K, 1>(a);
+}
+template <typename Tin, int K, int C, int R>
+static hipError_t conv_step_main(const ConvArgs& a) {
+  const long grid = ((long)((a.N + R - 1) / R) * (a.D / C) + 255) / 256;
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  k_conv_step<Tin, K, C, R><<<(unsigned)grid, 256, 0, a.stream>>>(a);
   return hipGetLastError();
 }
 template <typename Tin, int K, int R>
 static hipError_t conv_step_rows(const ConvArgs& a) {
   constexpr int C = 8 / (int)sizeof(Tin);
-  const long grid = ((long)((a.N + R - 1) / R) * ((a.D + C - 1) / C) + 255) / 256;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  if (conv_vec(a, C)) k_conv_step<Tin, K, C, true, R><<<(unsigned)grid, 256, 0, a.stream>>>(a);
-  else k_conv_step<Tin, K, C, false, R><<<(unsigned)grid, 256, 0, a.stream>>>(a);
-  return hipGetLastError();
+  return conv_fits(a, C) ? conv_step_main<Tin, K, C, R>(a) : conv_step_main<Tin, K, 1, R>(a);
 }
 template <typename Tin, int K>
 static hipError_t run_conv_step(const ConvArgs& a) {
@@ -461,22 +462,20 @@ static hipError_t run_conv_step(const ConvArgs& a) {
                                                                    : conv_step_rows<Tin, K, 1>(a);
 }
 template <typename Tin, int K, int C>
-static void conv_bwd_main(const ConvArgs& a, unsigned grid) {
-  if (conv_vec(a, C)) k_conv_bwd<Tin, K, C, true><<<grid, 64 * CONV_BWAVES, 0, a.stream>>>(a);
-  else k_conv_bwd<Tin, K, C, false><<<grid, 64 * CONV_BWAVES, 0, a.stream>>>(a);
+static hipError_t conv_bwd_main(const ConvArgs& a) {
+  const long pgs = (a.D / C + 63) / 64, grid = pgs * a.nruns;
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  if (grid > 0) k_conv_bwd<Tin, K, C><<<(unsigned)grid, 64 * CONV_BWAVES, 0, a.stream>>>(a);
+  return hipSuccess;
 }
 template <typename Tin, int K>
 static hipError_t run_conv_bwd(const ConvArgs& a0) {
-  const int C = conv_bc(a0);
   ConvArgs a = a0;
-  a.run = conv_run(a, C);
+  a.run = conv_bwd_run(a);
   a.nruns = conv_bwd_runs(a);
-  const long pgs = ((a.D + C - 1) / C + 63) / 64, grid = pgs * a.nruns;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  if (grid > 0) {
-    if (C == 2) conv_bwd_main<Tin, K, 2>(a, (unsigned)grid);
-    else conv_bwd_main<Tin, K, 4>(a, (unsigned)grid);
-  }
+  const hipError_t st = conv_bc(a) == 4 && conv_fits(a, 4) ? conv_bwd_main<Tin, K, 4>(a)
+                        : conv_fits(a, 2) ? conv_bwd_main<Tin, K, 2>(a) : conv_bwd_main<Tin, K, 1>(a);
+  if (st != hipSuccess) return st;
   const long nb = ((long)(K + 1) * a.D + CONV_DCOLS - 1) / CONV_DCOLS + (a.dh0 ? a.N : 0);
   k_conv_dw<Tin, K><<<(unsigned)nb, 256, 0, a.stream>>>(a);
   return hipGetLastError();

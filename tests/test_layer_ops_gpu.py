@@ -109,6 +109,8 @@ CONV = [
     ("packed", dict(D=72, K=4, lens=[1, 0, 2, 31, 32, 33, 0, 3, 130, 5], host=True, dht=True)),
     ("packed_dev_only", dict(D=40, K=3, lens=[64, 1, 1, 1, 0, 200], dtype="f32")),
     ("packed_odd", dict(D=33, K=4, lens=[2, 2, 2, 2, 2, 2, 60], off=5, dht=True)),
+    ("f32_pairs", dict(B=2, T=37, D=22, K=3, dtype="f32", off=2, dht=True)),
+    ("bf16_pairs", dict(B=2, T=70, D=50, K=2, off=2, act="none")),
 ]
 
 
