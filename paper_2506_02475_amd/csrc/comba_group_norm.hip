@@ -6,7 +6,7 @@
 //
 // Bound by bytes: every value is read and written once.  A group's channels lie
 // in the registers of a team of 1..64 lanes (a power of two) or of a workgroup of
-// 256 or 512, KV pieces of four per lane, so that mean and variance are two passes
+// 256 or 512, KV pieces of C channels per lane, so that mean and variance are two passes
 // over registers.  A team keeps its group and walks rows, the next row's loads in
 // flight, with weight and bias (backward: and their gradients' sums) in registers.
 // 16,384 x 4,096 channels in groups of 128, gated, bf16: forward 84 us (4.8 TB/s),
@@ -22,7 +22,7 @@
 
 namespace comba {
 
-constexpr int GN_C = 4;        // channels of a piece
+constexpr int GN_C = 4;        // channels of an aligned piece
 constexpr int GN_WIDE = 1024;  // threads where a group's channels do not fit registers
 
 // Sum over the lanes of a team (team: a power of two up to 64), the same in every lane.
@@ -81,7 +81,7 @@ struct GnTeam {
   int chunks;  // row chunks: team (group, chunk) takes rows chunk, chunk + chunks, ..
 };
 
-template <typename Tx, typename To, int KV, bool VEC, int TEAM, bool BWD>
+template <typename Tx, typename To, int KV, int C, int TEAM, bool BWD>
 __global__ __launch_bounds__(TEAM > 0 ? TEAM : 256) void k_group_norm(GroupNormArgs a, GnTeam tm) {
   __shared__ float lds[TEAM / 64 + 1];
   const int m = a.C / a.G, team = TEAM > 0 ? TEAM : tm.team;
@@ -89,97 +89,108 @@ __global__ __launch_bounds__(TEAM > 0 ? TEAM : 256) void k_group_norm(GroupNormA
   const int l = threadIdx.x & (team - 1);
   const int g = id % a.G, chunk = id / a.G;
   if (chunk >= tm.chunks) return;  // whole teams
+  // where not everything fits registers: each row loaded when it is due, and the
+  // sums of dw and db in LDS
+  constexpr bool LEAN = BWD && TEAM == 512 && C == 1;
+  __shared__ float kept[2][LEAN ? KV : 1][LEAN ? TEAM : 1];
   int c[KV], nv[KV];
-  float w[KV][GN_C], b[KV][GN_C], dw[KV][GN_C], db[KV][GN_C];
+  float w[KV][C], b[KV][C], dw[KV][C], db[KV][C];
 #pragma unroll
   for (int k = 0; k < KV; ++k) {
-    const int at = (k * team + l) * GN_C;  // in the group
-    nv[k] = max(0, min(GN_C, m - at));
+    const int at = (k * team + l) * C;  // in the group
+    nv[k] = at < m ? C : 0;
     c[k] = g * m + (nv[k] > 0 ? at : 0);
 #pragma unroll
-    for (int i = 0; i < GN_C; ++i) {
-      const bool on = i < nv[k];
+    for (int i = 0; i < C; ++i) {
+      const bool on = nv[k] > 0;
       w[k][i] = on ? (a.w ? a.w[c[k] + i] : 1.f) : 0.f;
       b[k][i] = on && a.b ? a.b[c[k] + i] : 0.f;
-      dw[k][i] = db[k][i] = 0.f;
+      if constexpr (LEAN) kept[0][k][l] = kept[1][k][l] = 0.f;
+      else dw[k][i] = db[k][i] = 0.f;
     }
   }
   const float inv = 1.f / m;
   const Tx* x = static_cast<const Tx*>(a.x);
   const To *z = static_cast<const To*>(a.z), *dy = static_cast<const To*>(a.dy);
-  Piece<Tx, GN_C, VEC> px[KV];
-  Piece<To, GN_C, VEC> pz[KV], py[KV];
+  Piece<Tx, C, true> px[KV];
+  Piece<To, C, true> pz[KV], py[KV];
   auto load = [&](long r) {
 #pragma unroll
     for (int k = 0; k < KV; ++k) {
-      px[k].load(x + r * a.x_row + c[k], max(nv[k], 1));
-      if (z) pz[k].load(z + r * a.z_row + c[k], max(nv[k], 1));
-      if constexpr (BWD) py[k].load(dy + r * a.C + c[k], max(nv[k], 1));
+      px[k].load(x + r * a.x_row + c[k], C);
+      if (z) pz[k].load(z + r * a.z_row + c[k], C);
+      if constexpr (BWD) py[k].load(dy + r * a.C + c[k], C);
     }
   };
-  if (chunk < a.rows) load(chunk);
+  if (!LEAN && chunk < a.rows) load(chunk);
   for (long r = chunk; r < a.rows; r += tm.chunks) {
-    float v[KV][GN_C], zv[KV][GN_C], gv[KV][GN_C], sum = 0.f, sq = 0.f;
+    float v[KV][C], zv[KV][C], gv[KV][C], sum = 0.f, sq = 0.f;
+    if constexpr (LEAN) load(r);
 #pragma unroll
     for (int k = 0; k < KV; ++k)
 #pragma unroll
-      for (int i = 0; i < GN_C; ++i) {
-        const bool on = i < nv[k];
+      for (int i = 0; i < C; ++i) {
+        const bool on = nv[k] > 0;
         v[k][i] = on ? px[k].get(i) : 0.f;
         zv[k][i] = on && z ? pz[k].get(i) : 0.f;
         if constexpr (BWD) gv[k][i] = on ? py[k].get(i) : 0.f;
         sum += v[k][i];
       }
-    if (r + tm.chunks < a.rows) load(r + tm.chunks);
+    if (!LEAN && r + tm.chunks < a.rows) load(r + tm.chunks);
     const float mean = gn_sum<TEAM>(sum, team, lds) * inv;
 #pragma unroll
     for (int k = 0; k < KV; ++k)
 #pragma unroll
-      for (int i = 0; i < GN_C; ++i) {
-        v[k][i] = i < nv[k] ? v[k][i] - mean : 0.f;
+      for (int i = 0; i < C; ++i) {
+        v[k][i] = nv[k] > 0 ? v[k][i] - mean : 0.f;
         sq = fmaf(v[k][i], v[k][i], sq);
       }
     const float rstd = rsqrtf(gn_sum<TEAM>(sq, team, lds) * inv + a.eps);
     if constexpr (!BWD) {
 #pragma unroll
       for (int k = 0; k < KV; ++k) {
-        float y[GN_C];
+        float y[C];
 #pragma unroll
-        for (int i = 0; i < GN_C; ++i) {
+        for (int i = 0; i < C; ++i) {
           const float n = fmaf(v[k][i] * rstd, w[k][i], b[k][i]);
           y[i] = z ? n * act_of(a.act, zv[k][i]) : act_of(a.act, n);
         }
-        store_piece<To, GN_C, VEC>(static_cast<To*>(a.y) + r * a.C + c[k], y, nv[k]);
+        store_piece<To, C, true>(static_cast<To*>(a.y) + r * a.C + c[k], y, nv[k]);
       }
     } else {
       float s1 = 0.f, s2 = 0.f;
 #pragma unroll
       for (int k = 0; k < KV; ++k) {
-        float dz[GN_C];
+        float dz[C];
 #pragma unroll
-        for (int i = 0; i < GN_C; ++i) {
+        for (int i = 0; i < C; ++i) {
           const float xh = v[k][i] * rstd, n = fmaf(xh, w[k][i], b[k][i]);
           float y;
           const float sl = act_slope(a.act, z ? zv[k][i] : n, y);
           const float dn = gv[k][i] * (z ? y : sl);
           dz[i] = gv[k][i] * n * sl;
-          dw[k][i] = fmaf(dn, xh, dw[k][i]);
-          db[k][i] += dn;
+          if constexpr (LEAN) {
+            kept[0][k][l] = fmaf(dn, xh, kept[0][k][l]);
+            kept[1][k][l] += dn;
+          } else {
+            dw[k][i] = fmaf(dn, xh, dw[k][i]);
+            db[k][i] += dn;
+          }
           v[k][i] = xh;
           gv[k][i] = dn * w[k][i];
           s1 += gv[k][i];
           s2 = fmaf(gv[k][i], xh, s2);
         }
-        if (z) store_piece<To, GN_C, VEC>(static_cast<To*>(a.dz) + r * a.C + c[k], dz, nv[k]);
+        if (z) store_piece<To, C, true>(static_cast<To*>(a.dz) + r * a.C + c[k], dz, nv[k]);
       }
       s1 = gn_sum<TEAM>(s1, team, lds) * inv;
       s2 = gn_sum<TEAM>(s2, team, lds) * inv;
 #pragma unroll
       for (int k = 0; k < KV; ++k) {
-        float dx[GN_C];
+        float dx[C];
 #pragma unroll
-        for (int i = 0; i < GN_C; ++i) dx[i] = rstd * (gv[k][i] - s1 - v[k][i] * s2);
-        store_piece<Tx, GN_C, VEC>(static_cast<Tx*>(a.dx) + r * a.C + c[k], dx, nv[k]);
+        for (int i = 0; i < C; ++i) dx[i] = rstd * (gv[k][i] - s1 - v[k][i] * s2);
+        store_piece<Tx, C, true>(static_cast<Tx*>(a.dx) + r * a.C + c[k], dx, nv[k]);
       }
     }
   }
@@ -187,17 +198,17 @@ __global__ __launch_bounds__(TEAM > 0 ? TEAM : 256) void k_group_norm(GroupNormA
 #pragma unroll
     for (int k = 0; k < KV; ++k)
 #pragma unroll
-      for (int i = 0; i < GN_C; ++i)
-        if (i < nv[k]) {
-          a.part[((long)chunk * 2 + 0) * a.C + c[k] + i] = dw[k][i];
-          a.part[((long)chunk * 2 + 1) * a.C + c[k] + i] = db[k][i];
+      for (int i = 0; i < C; ++i)
+        if (nv[k] > 0) {
+          a.part[((long)chunk * 2 + 0) * a.C + c[k] + i] = LEAN ? kept[0][k][l] : dw[k][i];
+          a.part[((long)chunk * 2 + 1) * a.C + c[k] + i] = LEAN ? kept[1][k][l] : db[k][i];
         }
   }
 }
 
 // Groups too wide for registers: a workgroup per (group, chunk of rows), which
 // reads its rows again from the caches.
-template <typename Tx, typename To, bool VEC, bool BWD>
+template <typename Tx, typename To, int C, bool BWD>
 __global__ __launch_bounds__(GN_WIDE) void k_group_norm_wide(GroupNormArgs a, GnTeam tm) {
   __shared__ float lds[GN_WIDE / 64];
   const int m = a.C / a.G, g = blockIdx.x % a.G, chunk = blockIdx.x / a.G;
@@ -205,64 +216,64 @@ __global__ __launch_bounds__(GN_WIDE) void k_group_norm_wide(GroupNormArgs a, Gn
   const To *zt = static_cast<const To*>(a.z), *dyt = static_cast<const To*>(a.dy);
   const float *wt = a.w ? a.w + (long)g * m : nullptr, *bt = a.b ? a.b + (long)g * m : nullptr;
   float* pw = BWD ? a.part + (long)chunk * 2 * a.C + (long)g * m : nullptr;
-  // fn(first channel, channels) for every piece of the thread
+  // fn(first channel) for every piece of the thread
   auto pieces = [&](auto fn) {
-    for (int c = threadIdx.x * GN_C; c < m; c += GN_WIDE * GN_C) fn(c, min(GN_C, m - c));
+    for (int c = threadIdx.x * C; c < m; c += GN_WIDE * C) fn(c);
   };
   if constexpr (BWD) {
-    pieces([&](int c, int nv) {
-      for (int i = 0; i < nv; ++i) pw[c + i] = pw[a.C + c + i] = 0.f;
+    pieces([&](int c) {
+      for (int i = 0; i < C; ++i) pw[c + i] = pw[a.C + c + i] = 0.f;
     });
   }
   for (long r = chunk; r < a.rows; r += tm.chunks) {
     const Tx* x = static_cast<const Tx*>(a.x) + r * a.x_row + (long)g * m;
     const To* z = zt ? zt + r * a.z_row + (long)g * m : nullptr;
     float sum = 0.f, sq = 0.f;
-    pieces([&](int c, int nv) {
-      Piece<Tx, GN_C, VEC> p;
-      p.load(x + c, nv);
+    pieces([&](int c) {
+      Piece<Tx, C, true> p;
+      p.load(x + c, C);
 #pragma unroll
-      for (int i = 0; i < GN_C; ++i) sum += i < nv ? p.get(i) : 0.f;
+      for (int i = 0; i < C; ++i) sum += p.get(i);
     });
     const float mean = block_sum<GN_WIDE>(sum, lds) * inv;
-    pieces([&](int c, int nv) {
-      Piece<Tx, GN_C, VEC> p;
-      p.load(x + c, nv);
+    pieces([&](int c) {
+      Piece<Tx, C, true> p;
+      p.load(x + c, C);
 #pragma unroll
-      for (int i = 0; i < GN_C; ++i) {
-        const float d = i < nv ? p.get(i) - mean : 0.f;
+      for (int i = 0; i < C; ++i) {
+        const float d = p.get(i) - mean;
         sq = fmaf(d, d, sq);
       }
     });
     const float rstd = rsqrtf(block_sum<GN_WIDE>(sq, lds) * inv + a.eps);
     if constexpr (!BWD) {
-      pieces([&](int c, int nv) {
-        Piece<Tx, GN_C, VEC> p;
-        Piece<To, GN_C, VEC> pz;
-        p.load(x + c, nv);
-        if (z) pz.load(z + c, nv);
-        float y[GN_C];
+      pieces([&](int c) {
+        Piece<Tx, C, true> p;
+        Piece<To, C, true> pz;
+        p.load(x + c, C);
+        if (z) pz.load(z + c, C);
+        float y[C];
 #pragma unroll
-        for (int i = 0; i < GN_C; ++i) {
-          const int at = c + min(i, nv - 1);
+        for (int i = 0; i < C; ++i) {
+          const int at = c + i;
           const float n = fmaf((p.get(i) - mean) * rstd, wt ? wt[at] : 1.f, bt ? bt[at] : 0.f);
           y[i] = z ? n * act_of(a.act, pz.get(i)) : act_of(a.act, n);
         }
-        store_piece<To, GN_C, VEC>(static_cast<To*>(a.y) + r * a.C + (long)g * m + c, y, nv);
+        store_piece<To, C, true>(static_cast<To*>(a.y) + r * a.C + (long)g * m + c, y, C);
       });
     } else {
       const long row = r * a.C + (long)g * m;
       float s1 = 0.f, s2 = 0.f;
       // fn(i, xh, dn, dn w, dz) for every channel of a piece
-      auto grad = [&](int c, int nv, auto fn) {
-        Piece<Tx, GN_C, VEC> p;
-        Piece<To, GN_C, VEC> pz, py;
-        p.load(x + c, nv);
-        if (z) pz.load(z + c, nv);
-        py.load(dyt + row + c, nv);
+      auto grad = [&](int c, auto fn) {
+        Piece<Tx, C, true> p;
+        Piece<To, C, true> pz, py;
+        p.load(x + c, C);
+        if (z) pz.load(z + c, C);
+        py.load(dyt + row + c, C);
 #pragma unroll
-        for (int i = 0; i < GN_C; ++i) {
-          const int at = c + min(i, nv - 1);
+        for (int i = 0; i < C; ++i) {
+          const int at = c + i;
           const float wv = wt ? wt[at] : 1.f, xh = (p.get(i) - mean) * rstd;
           const float n = fmaf(xh, wv, bt ? bt[at] : 0.f), gv = py.get(i);
           float y;
@@ -270,9 +281,8 @@ __global__ __launch_bounds__(GN_WIDE) void k_group_norm_wide(GroupNormArgs a, Gn
           fn(i, xh, dn, dn * wv, gv * n * sl);
         }
       };
-      pieces([&](int c, int nv) {
-        grad(c, nv, [&](int i, float xh, float dn, float gw, float) {
-          if (i >= nv) return;
+      pieces([&](int c) {
+        grad(c, [&](int i, float xh, float dn, float gw, float) {
           s1 += gw;
           s2 = fmaf(gw, xh, s2);
           pw[c + i] = fmaf(dn, xh, pw[c + i]);
@@ -281,14 +291,14 @@ __global__ __launch_bounds__(GN_WIDE) void k_group_norm_wide(GroupNormArgs a, Gn
       });
       s1 = block_sum<GN_WIDE>(s1, lds) * inv;
       s2 = block_sum<GN_WIDE>(s2, lds) * inv;
-      pieces([&](int c, int nv) {
-        float dx[GN_C], dz[GN_C];
-        grad(c, nv, [&](int i, float xh, float, float gw, float d) {
+      pieces([&](int c) {
+        float dx[C], dz[C];
+        grad(c, [&](int i, float xh, float, float gw, float d) {
           dx[i] = rstd * (gw - s1 - xh * s2);
           dz[i] = d;
         });
-        if (z) store_piece<To, GN_C, VEC>(static_cast<To*>(a.dz) + row + c, dz, nv);
-        store_piece<Tx, GN_C, VEC>(static_cast<Tx*>(a.dx) + row + c, dx, nv);
+        if (z) store_piece<To, C, true>(static_cast<To*>(a.dz) + row + c, dz, C);
+        store_piece<Tx, C, true>(static_cast<Tx*>(a.dx) + row + c, dx, C);
       });
     }
   }
@@ -350,8 +360,9 @@ static hipError_t run_group_norm(const GroupNormArgs& a0) {
     auto ok = [&](const void* p, size_t eb, long row) {
       return !p || ((uintptr_t)p % (GN_C * eb) == 0 && row % GN_C == 0);
     };
-    // four channels in one load or store, or one by one (slices that are not aligned
-    // to four values; 16,384 x 4,096, groups of 128: 81 / 144 us forward, 145 / 277 backward)
+    // pieces of four channels, or of one for other groups and for slices that are not
+    // aligned to four (bf16, 16,384 x 4,096, groups of 128: 83 / 107 us forward, 149 / 197
+    // backward; pieces of four loaded one by one 139 and 274)
     const bool vec = (a.C / a.G) % GN_C == 0 && ok(a.x, sizeof(Tx), a.x_row) && ok(a.z, sizeof(To), a.z_row) &&
                      ok(a.y, sizeof(To), a.C) && ok(a.dy, sizeof(To), a.C) && ok(a.dx, sizeof(Tx), a.C) &&
                      ok(a.dz, sizeof(To), a.C);
@@ -359,16 +370,16 @@ static hipError_t run_group_norm(const GroupNormArgs& a0) {
     const long grid = ((long)t.chunks * a.G * t.team + th - 1) / th;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
 #define GN_LAUNCH(KV, TEAM)                                                                      \
-  if (vec) k_group_norm<Tx, To, KV, true, TEAM, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t); \
-  else k_group_norm<Tx, To, KV, false, TEAM, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t);
+  if (vec) k_group_norm<Tx, To, KV, GN_C, TEAM, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t); \
+  else k_group_norm<Tx, To, KV * GN_C, 1, TEAM, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t);
     if (kv == 2 && t.team <= 64) { GN_LAUNCH(2, 0) }
     else if (kv == 4 && t.team <= 64) { GN_LAUNCH(4, 0) }
     else if (kv == 2) { GN_LAUNCH(2, 256) }
     else if (kv == 4 && t.team == 256) { GN_LAUNCH(4, 256) }
     else if (kv == 4) { GN_LAUNCH(4, 512) }
 #undef GN_LAUNCH
-    else if (vec) k_group_norm_wide<Tx, To, true, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t);
-    else k_group_norm_wide<Tx, To, false, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t);
+    else if (vec) k_group_norm_wide<Tx, To, GN_C, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t);
+    else k_group_norm_wide<Tx, To, 1, BWD><<<(unsigned)grid, th, 0, a.stream>>>(a, t);
   }
   if (BWD && (a.dw || a.db))
     k_group_norm_dw<<<(unsigned)((2L * a.C + 63) / 64), 64 * GN_WAVES, 0, a.stream>>>(a);
