@@ -85,7 +85,7 @@ template <typename Tx, typename To, int KV, int C, int TEAM, bool BWD>
 __global__ __launch_bounds__(TEAM > 0 ? TEAM : 256) void k_group_norm(GroupNormArgs a, GnTeam tm) {
   __shared__ float lds[TEAM / 64 + 1];
   const int m = a.C / a.G, team = TEAM > 0 ? TEAM : tm.team;
-  const long id = ((long)blockIdx.x * blockDim.x + threadIdx.x) / team;
+  const long id = ((long)blockIdx.x * (TEAM > 0 ? TEAM : 256) + threadIdx.x) / team;
   const int l = threadIdx.x & (team - 1);
   const int g = id % a.G, chunk = id / a.G;
   if (chunk >= tm.chunks) return;  // whole teams
