@@ -502,6 +502,19 @@ def comba_group_norm_bwd(x, groups, weight, bias, z, dy, *, activation="silu", e
 _FNS = {}
 
 
+def _kept_offsets(cu_seqlens_host):
+    """The backward's own copy of the host offsets: the caller's buffer may be filled anew
+    before the backward runs.  (The device's offsets are saved as a tensor, so that writing
+    them in between raises as for every other input.)"""
+    import numpy as np
+
+    if cu_seqlens_host is None or getattr(cu_seqlens_host, "is_cuda", False):  # refused later
+        return cu_seqlens_host
+    if hasattr(cu_seqlens_host, "detach"):
+        cu_seqlens_host = cu_seqlens_host.detach().numpy()
+    return np.array(cu_seqlens_host)
+
+
 def _functions():
     if _FNS:
         return _FNS
@@ -512,40 +525,43 @@ def _functions():
 
     class Conv(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, x, w, bias, h0, kw):
+        def forward(ctx, x, w, bias, h0, cu_seqlens, kw):
             ctx.set_materialize_grads(False)
-            ctx.save_for_backward(x, w, bias, h0)
+            ctx.save_for_backward(x, w, bias, h0, cu_seqlens)
             ctx.kw = kw
-            return comba_conv_fwd(x, w, bias, h0, **kw)
+            return comba_conv_fwd(x, w, bias, h0, cu_seqlens=cu_seqlens, **kw)
 
         @staticmethod
         def backward(ctx, dy, dht):
-            x, w, bias, h0 = ctx.saved_tensors
+            x, w, bias, h0, cu_seqlens = ctx.saved_tensors
             dy = torch.zeros_like(x, memory_format=torch.contiguous_format) if dy is None \
                 else dy.contiguous()
             gr = comba_conv_bwd(x, w, bias, h0, dy, None if dht is None else dht.contiguous(),
-                                need_dh0=h0 is not None and ctx.needs_input_grad[3], **ctx.kw)
-            return needed(ctx, (gr["dx"], gr["dw"], gr["dbias"], gr["dh0"], None))
+                                need_dh0=h0 is not None and ctx.needs_input_grad[3],
+                                cu_seqlens=cu_seqlens, **ctx.kw)
+            return needed(ctx, (gr["dx"], gr["dw"], gr["dbias"], gr["dh0"], None, None))
 
     class Select(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, u, delta, A, B, C, D, z, bias, h0, kw):
+        def forward(ctx, u, delta, A, B, C, D, z, bias, h0, cu_seqlens, kw):
             ctx.set_materialize_grads(False)
-            y, ht, ws = comba_select_fwd_save(u, delta, A, B, C, D, z, bias, h0, **kw)
-            ctx.save_for_backward(u, delta, A, B, C, D, z, bias, h0, ws)
+            y, ht, ws = comba_select_fwd_save(u, delta, A, B, C, D, z, bias, h0,
+                                              cu_seqlens=cu_seqlens, **kw)
+            ctx.save_for_backward(u, delta, A, B, C, D, z, bias, h0, cu_seqlens, ws)
             ctx.kw = kw
             return y, ht
 
         @staticmethod
         def backward(ctx, dy, dht):
-            u, delta, A, B, C, D, z, bias, h0, ws = ctx.saved_tensors
+            u, delta, A, B, C, D, z, bias, h0, cu_seqlens, ws = ctx.saved_tensors
             dy = torch.zeros_like(u, memory_format=torch.contiguous_format) if dy is None \
                 else dy.contiguous()
             gr = comba_select_bwd(u, delta, A, B, C, D, z, bias, h0, dy,
                                   None if dht is None else dht.contiguous(), workspace=ws,
-                                  need_dh0=h0 is not None and ctx.needs_input_grad[8], **ctx.kw)
+                                  need_dh0=h0 is not None and ctx.needs_input_grad[8],
+                                  cu_seqlens=cu_seqlens, **ctx.kw)
             names = ("du", "ddelta", "dA", "dB", "dC", "dD", "dz", "ddelta_bias", "dh0")
-            return needed(ctx, tuple(gr[n] for n in names) + (None,))
+            return needed(ctx, tuple(gr[n] for n in names) + (None, None))
 
     class GroupNorm(torch.autograd.Function):
         @staticmethod
@@ -567,21 +583,21 @@ def _functions():
 def comba_conv(x, w, bias=None, h0=None, *, activation="silu", cu_seqlens=None,
                cu_seqlens_host=None):
     """Differentiable comba_conv_fwd: (y, ht); gradients flow to x, w, bias and h0."""
-    kw = dict(activation=activation, cu_seqlens=cu_seqlens, cu_seqlens_host=cu_seqlens_host)
-    return _functions()["conv"].apply(x, w, bias, h0, kw)
+    kw = dict(activation=activation, cu_seqlens_host=_kept_offsets(cu_seqlens_host))
+    return _functions()["conv"].apply(x, w, bias, h0, cu_seqlens, kw)
 
 
 def comba_select(u, delta, A, B, C, D=None, z=None, delta_bias=None, h0=None, *,
                  delta_softplus=True, cu_seqlens=None, cu_seqlens_host=None):
     """Differentiable comba_select_fwd: (y, ht); gradients flow to every tensor.  Each call
     keeps a state every 48 tokens (N = 8: 32) until the backward has run."""
-    kw = dict(delta_softplus=delta_softplus, cu_seqlens=cu_seqlens,
-              cu_seqlens_host=cu_seqlens_host)
+    kw = dict(delta_softplus=delta_softplus, cu_seqlens_host=_kept_offsets(cu_seqlens_host))
     import torch
 
     if not torch.is_grad_enabled():
-        return comba_select_fwd(u, delta, A, B, C, D, z, delta_bias, h0, **kw)
-    return _functions()["select"].apply(u, delta, A, B, C, D, z, delta_bias, h0, kw)
+        return comba_select_fwd(u, delta, A, B, C, D, z, delta_bias, h0, cu_seqlens=cu_seqlens,
+                                **kw)
+    return _functions()["select"].apply(u, delta, A, B, C, D, z, delta_bias, h0, cu_seqlens, kw)
 
 
 def comba_group_norm(x, groups, weight=None, bias=None, z=None, *, activation="silu", eps=1e-5,
