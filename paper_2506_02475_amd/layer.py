@@ -519,6 +519,7 @@ def _functions():
     if _FNS:
         return _FNS
     import torch
+    from torch.autograd.function import once_differentiable  # the kernels leave no graph
 
     def needed(ctx, grads):
         return tuple(g if n else None for g, n in zip(grads, ctx.needs_input_grad))
@@ -532,6 +533,7 @@ def _functions():
             return comba_conv_fwd(x, w, bias, h0, cu_seqlens=cu_seqlens, **kw)
 
         @staticmethod
+        @once_differentiable
         def backward(ctx, dy, dht):
             x, w, bias, h0, cu_seqlens = ctx.saved_tensors
             dy = torch.zeros_like(x, memory_format=torch.contiguous_format) if dy is None \
@@ -552,6 +554,7 @@ def _functions():
             return y, ht
 
         @staticmethod
+        @once_differentiable
         def backward(ctx, dy, dht):
             u, delta, A, B, C, D, z, bias, h0, cu_seqlens, ws = ctx.saved_tensors
             dy = torch.zeros_like(u, memory_format=torch.contiguous_format) if dy is None \
@@ -571,6 +574,7 @@ def _functions():
             return comba_group_norm_fwd(x, groups, weight, bias, z, out_dtype=out_dtype, **kw)
 
         @staticmethod
+        @once_differentiable
         def backward(ctx, dy):
             x, weight, bias, z = ctx.saved_tensors
             gr = comba_group_norm_bwd(x, ctx.groups, weight, bias, z, dy.contiguous(), **ctx.kw)

@@ -103,3 +103,18 @@ def test_the_backward_has_the_forwards_host_offsets(fakes, op, tensor):
     y.sum().backward()
     assert [c[1:] for c in fakes.calls] == [([0, 2, 6], [0, 2, 6])] * 2
     assert torch.equal(x.grad, torch.full_like(x, 2.0))
+
+
+@pytest.mark.parametrize("op", ["conv", "select", "norm"])
+def test_second_derivatives_raise(fakes, op):
+    """The backward's gradients have no graph of their own: with a product upstream a gradient
+    penalty would otherwise lose the operator's part without a word."""
+    import torch
+
+    v = torch.randn(8, requires_grad=True)
+    x = torch.randn(1, 6, 8)
+    y = _ops(x * (v * v))[op]()
+    g, = torch.autograd.grad(y.square().sum(), v, create_graph=True)
+    assert torch.isfinite(g).all()
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.square().sum().backward()
