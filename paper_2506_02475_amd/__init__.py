@@ -198,6 +198,19 @@ def _host_offsets(cu_seqlens_host, n):
     return a
 
 
+def _kept_offsets(cu_seqlens_host):
+    """The backward's own copy of the host offsets: the caller's buffer may be filled anew
+    before the backward runs.  (The device's offsets are saved as a tensor, so that writing
+    them in between raises as for every other input.)"""
+    import numpy as np
+
+    if cu_seqlens_host is None or getattr(cu_seqlens_host, "is_cuda", False):  # refused later
+        return cu_seqlens_host
+    if hasattr(cu_seqlens_host, "detach"):
+        cu_seqlens_host = cu_seqlens_host.detach().numpy()
+    return np.array(cu_seqlens_host)
+
+
 def fwd_workspace_bytes(B, T, H, dk, dv, *, num_seqs=None, varlen=False, bf16=True) -> int:
     N = B if num_seqs is None else num_seqs
     shp = _make_shape(B, T, H, dk, dv, N, ctypes.c_void_p(1) if varlen else None,
@@ -625,7 +638,8 @@ def comba_chunk(q, k, v, g, beta, d, h0=None, *, beta_tilde=None, cu_seqlens=Non
     global _CHUNK_FN
     if _CHUNK_FN is None:
         _CHUNK_FN = _autograd_function()
-    return _CHUNK_FN.apply(q, k, v, g, beta, d, h0, beta_tilde, cu_seqlens, cu_seqlens_host)
+    return _CHUNK_FN.apply(q, k, v, g, beta, d, h0, beta_tilde, cu_seqlens,
+                           _kept_offsets(cu_seqlens_host))
 
 
 from . import layer  # noqa: E402  (after the helpers that it takes from here)

@@ -18,7 +18,8 @@ from __future__ import annotations
 import ctypes
 import struct
 
-from . import (COMBA_BF16, COMBA_F32, CombaError, _check, _host_offsets, _ptr, load_library)
+from . import (COMBA_BF16, COMBA_F32, CombaError, _check, _host_offsets, _kept_offsets, _ptr,
+               load_library)
 
 __all__ = ["comba_conv_fwd", "comba_conv_bwd", "comba_conv_step", "comba_conv",
            "comba_select_fwd", "comba_select_fwd_save", "comba_select_bwd", "comba_select_step",
@@ -500,19 +501,6 @@ def comba_group_norm_bwd(x, groups, weight, bias, z, dy, *, activation="silu", e
 
 # ---- torch.autograd ---------------------------------------------------------------
 _FNS = {}
-
-
-def _kept_offsets(cu_seqlens_host):
-    """The backward's own copy of the host offsets: the caller's buffer may be filled anew
-    before the backward runs.  (The device's offsets are saved as a tensor, so that writing
-    them in between raises as for every other input.)"""
-    import numpy as np
-
-    if cu_seqlens_host is None or getattr(cu_seqlens_host, "is_cuda", False):  # refused later
-        return cu_seqlens_host
-    if hasattr(cu_seqlens_host, "detach"):
-        cu_seqlens_host = cu_seqlens_host.detach().numpy()
-    return np.array(cu_seqlens_host)
 
 
 def _functions():
