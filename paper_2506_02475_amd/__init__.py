@@ -583,6 +583,7 @@ def comba_chunk_bwd_saved_in_dtype(q, k, v, g, beta, d, h0, dO, dht=None, *, wor
 
 def _autograd_function():
     import torch
+    from torch.autograd.function import once_differentiable  # the kernels leave no graph
 
     class _ChunkComba(torch.autograd.Function):
         """The training pair as one differentiable op: comba_chunk_fwd_save in
@@ -602,6 +603,7 @@ def _autograd_function():
             return o, ht
 
         @staticmethod
+        @once_differentiable
         def backward(ctx, do, dht):
             q, k, v, g, beta, d, h0, beta_tilde, cu_seqlens, ws = ctx.saved_tensors
             if do is None:

@@ -45,3 +45,17 @@ def test_the_backward_has_the_forwards_host_offsets(calls, tensor):
     o.sum().backward()
     assert calls == [[0, 2, 6]] * 2
     assert torch.equal(v.grad, torch.full_like(v, 2.0))
+
+
+def test_second_derivatives_raise(calls):
+    """The backward's gradients have no graph of their own: with a product upstream a gradient
+    penalty would otherwise lose the operator's part without a word."""
+    import torch
+
+    s = torch.randn(4, requires_grad=True)
+    v = torch.randn(1, 6, 2, 4) * (s * s)
+    o, _ = comba.comba_chunk(*_args(v))
+    g, = torch.autograd.grad(o.square().sum(), s, create_graph=True)
+    assert torch.isfinite(g).all()
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.square().sum().backward()
