@@ -533,8 +533,11 @@ def _functions():
 
     class Select(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, u, delta, A, B, C, D, z, bias, h0, cu_seqlens, kw):
+        def forward(ctx, u, delta, A, B, C, D, z, bias, h0, cu_seqlens, kw, grad):
             ctx.set_materialize_grads(False)
+            if not (grad and any(ctx.needs_input_grad)):  # no backward: no states kept for it
+                return comba_select_fwd(u, delta, A, B, C, D, z, bias, h0, cu_seqlens=cu_seqlens,
+                                        **kw)
             y, ht, ws = comba_select_fwd_save(u, delta, A, B, C, D, z, bias, h0,
                                               cu_seqlens=cu_seqlens, **kw)
             ctx.save_for_backward(u, delta, A, B, C, D, z, bias, h0, cu_seqlens, ws)
@@ -552,7 +555,7 @@ def _functions():
                                   need_dh0=h0 is not None and ctx.needs_input_grad[8],
                                   cu_seqlens=cu_seqlens, **ctx.kw)
             names = ("du", "ddelta", "dA", "dB", "dC", "dD", "dz", "ddelta_bias", "dh0")
-            return needed(ctx, tuple(gr[n] for n in names) + (None, None))
+            return needed(ctx, tuple(gr[n] for n in names) + (None, None, None))
 
     class GroupNorm(torch.autograd.Function):
         @staticmethod
@@ -581,15 +584,13 @@ def comba_conv(x, w, bias=None, h0=None, *, activation="silu", cu_seqlens=None,
 
 def comba_select(u, delta, A, B, C, D=None, z=None, delta_bias=None, h0=None, *,
                  delta_softplus=True, cu_seqlens=None, cu_seqlens_host=None):
-    """Differentiable comba_select_fwd: (y, ht); gradients flow to every tensor.  Each call
-    keeps a state every 48 tokens (N = 8: 32) until the backward has run."""
+    """Differentiable comba_select_fwd: (y, ht); gradients flow to every tensor.  A call
+    that a backward can follow keeps a state every 48 tokens (N = 8: 32) until it has run."""
     kw = dict(delta_softplus=delta_softplus, cu_seqlens_host=_kept_offsets(cu_seqlens_host))
     import torch
 
-    if not torch.is_grad_enabled():
-        return comba_select_fwd(u, delta, A, B, C, D, z, delta_bias, h0, cu_seqlens=cu_seqlens,
-                                **kw)
-    return _functions()["select"].apply(u, delta, A, B, C, D, z, delta_bias, h0, cu_seqlens, kw)
+    return _functions()["select"].apply(u, delta, A, B, C, D, z, delta_bias, h0, cu_seqlens, kw,
+                                        torch.is_grad_enabled())
 
 
 def comba_group_norm(x, groups, weight=None, bias=None, z=None, *, activation="silu", eps=1e-5,

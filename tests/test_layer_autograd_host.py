@@ -118,3 +118,35 @@ def test_second_derivatives_raise(fakes, op):
     assert torch.isfinite(g).all()
     with pytest.raises(RuntimeError, match="once_differentiable"):
         g.square().sum().backward()
+
+
+@pytest.mark.parametrize("op", ["conv", "select", "norm"])
+def test_forward_mode_raises_without_grad_mode_too(fakes, op):
+    """Forward-mode differentiation does not depend on grad mode: a result without its tangent
+    would read as a derivative of zero."""
+    import torch
+    import torch.autograd.forward_ad as fwad
+
+    with fwad.dual_level(), torch.no_grad():
+        x = fwad.make_dual(torch.randn(1, 6, 8), torch.ones(1, 6, 8))
+        with pytest.raises(RuntimeError, match="forward mode AD|jvp"):
+            _ops(x)[op]()
+
+
+def test_states_are_kept_only_for_a_backward(fakes):
+    import torch
+
+    def names(x):
+        del fakes.calls[:]
+        _ops(x)["select"]()
+        return [c[0] for c in fakes.calls]
+
+    x = torch.randn(1, 6, 8)
+    assert names(x) == ["select_fwd"]  # grad mode, but nothing to differentiate
+    assert names(x.clone().requires_grad_()) == ["select_fwd_save"]
+    with torch.no_grad():
+        assert names(x.clone().requires_grad_()) == ["select_fwd"]
+    with torch.inference_mode():
+        assert names(x) == ["select_fwd"]
+    y = _ops(x)["select"]()
+    assert not y.requires_grad
