@@ -13,7 +13,8 @@
  *  - Rows: the inputs named with a `*_row` field are [tokens] rows that lie
  *    `*_row` elements apart (0: contiguous), so that a column slice of a wider
  *    projection is taken as it lies; a row's own elements are contiguous.
- *    Every other tensor is C-contiguous.
+ *    comba_select_fwd, _fwd_save and _bwd take rows up to 2^22 elements apart,
+ *    the other calls any distance.  Every other tensor is C-contiguous.
  *  - Alignment: every pointer needs its element's size only, a workspace 256
  *    bytes.  Calls are fastest where rows start at multiples of 16 bytes.
  *  - Token-free calls are valid as in comba.h: states pass through.

@@ -54,13 +54,15 @@ comba_status check_rows(const Shape* s, Rows* r) {
   return COMBA_OK;
 }
 
-// Rows of up to 4M values: the byte offsets inside a tile of 96 rows stay below 2^31.
+// Rows of up to 4M values.
 constexpr int64_t kMaxRow = (int64_t)1 << 22;
 
-// The elements between rows of a named input: given, or contiguous.
-bool row_stride(int64_t given, int64_t width, long* row) {
+// The elements between the `rows` rows of a named input: given, or contiguous.  Kernels
+// address rows in 64 bits, but for the scan's tiles (`tiles`), whose byte offsets
+// inside 96 rows have to stay below 2^31.
+bool row_stride(int64_t given, int64_t width, int64_t rows, bool tiles, long* row) {
   *row = given == 0 ? width : given;
-  return *row >= width && *row <= kMaxRow;
+  return *row >= width && *row <= (tiles ? kMaxRow : ((int64_t)1 << 60) / std::max<int64_t>(rows, 1));
 }
 
 // ---- convolution -------------------------------------------------------------
@@ -81,7 +83,7 @@ comba_status conv_args(const comba_conv_shape* s, comba::ConvArgs* a) {
   a->Tseq = r.Tseq;
   a->Ttot = r.Ttot;
   a->cu_seqlens = s->cu_seqlens;
-  return row_stride(s->x_row, s->D, &a->x_row) ? COMBA_OK : COMBA_ERR_SHAPE;
+  return row_stride(s->x_row, s->D, r.Ttot, false, &a->x_row) ? COMBA_OK : COMBA_ERR_SHAPE;
 }
 
 size_t conv_ws_bytes(const comba::ConvArgs& a) {
@@ -266,7 +268,7 @@ SelectLayout select_layout(comba::SelectArgs* a, Use use, comba::SelectRows* q) 
   return L;
 }
 
-comba_status select_args(const comba_select_shape* s, comba::SelectArgs* a) {
+comba_status select_args(const comba_select_shape* s, comba::SelectArgs* a, bool tiles = true) {
   if (!s) return COMBA_ERR_NULL;
   if (!dtype_ok(s->in_dtype)) return COMBA_ERR_DTYPE;
   if (s->N != 8 && s->N != 16 && s->N != 32) return COMBA_ERR_SHAPE;
@@ -290,9 +292,11 @@ comba_status select_args(const comba_select_shape* s, comba::SelectArgs* a) {
   a->nblk = (s->D / s->G + bc - 1) / bc;
   if ((int64_t)a->S * a->G * a->nblk > INT32_MAX) return COMBA_ERR_SHAPE;
   const int64_t gn = (int64_t)s->G * s->N;
-  if (!row_stride(s->u_row, s->D, &a->u_row) || !row_stride(s->delta_row, s->D, &a->delta_row) ||
-      !row_stride(s->z_row, s->D, &a->z_row) || !row_stride(s->b_row, gn, &a->b_row) ||
-      !row_stride(s->c_row, gn, &a->c_row))
+  auto row = [&](int64_t given, int64_t width, long* to) {
+    return row_stride(given, width, r.Ttot, tiles, to);
+  };
+  if (!row(s->u_row, s->D, &a->u_row) || !row(s->delta_row, s->D, &a->delta_row) ||
+      !row(s->z_row, s->D, &a->z_row) || !row(s->b_row, gn, &a->b_row) || !row(s->c_row, gn, &a->c_row))
     return COMBA_ERR_SHAPE;
   return COMBA_OK;
 }
@@ -366,8 +370,10 @@ comba_status group_norm_args(const comba_group_norm_shape* s, comba::GroupNormAr
   a->C = s->C;
   a->G = s->G;
   a->eps = s->eps;
-  return row_stride(s->x_row, s->C, &a->x_row) && row_stride(s->z_row, s->C, &a->z_row) ? COMBA_OK
-                                                                                       : COMBA_ERR_SHAPE;
+  return row_stride(s->x_row, s->C, s->rows, false, &a->x_row) &&
+                 row_stride(s->z_row, s->C, s->rows, false, &a->z_row)
+             ? COMBA_OK
+             : COMBA_ERR_SHAPE;
 }
 
 comba_status group_norm_inputs(comba::GroupNormArgs* a, const comba_group_norm_shape* s, const void* x,
@@ -546,7 +552,7 @@ comba_status comba_select_step(const comba_select_shape* shape, const void* u, c
                                const void* z, const float* delta_bias, float* state,
                                const int32_t* slots, int32_t num_slots, void* y, void* stream) {
   comba::SelectArgs a;
-  comba_status st = select_args(shape, &a);
+  comba_status st = select_args(shape, &a, false);
   if (st != COMBA_OK) return st;
   if (a.cu_seqlens || shape->T != 1 || num_slots < 0) return COMBA_ERR_SHAPE;
   st = select_inputs(&a, u, delta, A, Bm, Cm, Dskip, z, delta_bias, nullptr);

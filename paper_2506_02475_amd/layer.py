@@ -119,9 +119,13 @@ def _dense(name, t, shape, dtype, dev):
     return t.data_ptr()
 
 
-def _row(name, t, lead, shape, dtype, dev):
+_SCAN_ROW = 1 << 22  # the scan's tiles hold rows up to this many elements apart
+
+
+def _row(name, t, lead, shape, dtype, dev, limit=None):
     """Elements between token rows of ``t`` (``lead`` leading dimensions of tokens,
-    then a row): a row's elements are contiguous, the rows evenly spaced."""
+    then a row): a row's elements are contiguous, the rows evenly spaced and at most
+    ``limit`` elements apart."""
     if t is None:
         return 0
     if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
@@ -149,6 +153,9 @@ def _row(name, t, lead, shape, dtype, dev):
         return 0
     if row < n:
         raise CombaError("comba: the rows of %s overlap" % name)
+    if limit is not None and row > limit:
+        raise CombaError("comba: the rows of %s lie %d elements apart, at most %d are supported: "
+                         "pass a contiguous copy" % (name, row, limit))
     return row
 
 
@@ -321,15 +328,16 @@ def _select_shape(lead, u, delta, A, B, C, D, z, delta_bias, delta_softplus, N, 
     else:
         raise CombaError("comba: B and C must be [..,G,N] or [..,N]")
     if lead == 1:
-        batch, T = shape[0], 1
+        batch, T, far = shape[0], 1, None
     else:
-        batch, T = shape[0], shape[1]
+        batch, T, far = shape[0], shape[1], _SCAN_ROW
     shp = _SELECT.pack(batch, T, width, n, G, N, cu, _host_ptr(host), code,
                        1 if delta_softplus else 0,
-                       0 if u.is_contiguous() else _row("u", u, lead, shape, dt, dev),
-                       _row("delta", delta, lead, shape, dt, dev),
-                       _row("z", z, lead, shape, dt, dev), _row("B", B, lead, want, dt, dev),
-                       _row("C", C, lead, want, dt, dev))
+                       0 if u.is_contiguous() else _row("u", u, lead, shape, dt, dev, far),
+                       _row("delta", delta, lead, shape, dt, dev, far),
+                       _row("z", z, lead, shape, dt, dev, far),
+                       _row("B", B, lead, want, dt, dev, far),
+                       _row("C", C, lead, want, dt, dev, far))
     ptrs = (u.data_ptr(), delta.data_ptr(), _dense("A", A, ashape, f32, dev), B.data_ptr(),
             C.data_ptr(), _dense("D", D, (width,), f32, dev), None if z is None else z.data_ptr(),
             _dense("delta_bias", delta_bias, (width,), f32, dev))
@@ -368,7 +376,8 @@ def comba_select_fwd(u, delta, A, B, C, D=None, z=None, delta_bias=None, h0=None
     h_t = exp(dt A) h_{t-1} + dt u_t B_t,  y_t = (<C_t, h_t> + D u_t) silu(z_t).
     u, delta, z [B,T,D]; B, C [B,T,G,N] or [B,T,N] (G groups of channels), all of one dtype
     and each possibly a column slice; A [D,N], D, delta_bias [D], h0 [S,D,N] float32.
-    D, z, delta_bias and h0 may be None.  N: 8, 16 or 32."""
+    D, z, delta_bias and h0 may be None.  N: 8, 16 or 32.  Rows of a slice lie at most 2^22
+    elements apart."""
     y, ht, _ = _select(False, u, delta, A, B, C, D, z, delta_bias, h0, delta_softplus, cu_seqlens,
                        cu_seqlens_host, output_final_state, workspace, stream)
     return y, ht

@@ -214,3 +214,37 @@ def test_binding_refuses_before_the_library():
                 torch.zeros(2, 1, 8).expand(2, 3, 8), torch.zeros(2, 8, 3).transpose(1, 2)):
         with pytest.raises(comba.CombaError, match="x"):
             _row("x", bad, 2, tuple(bad.shape), f, dev)
+
+
+FAR = 1 << 23  # elements between rows: one token of each of a batch's long rows
+
+
+@pytest.mark.parametrize("name,rows", [
+    ("comba_conv_fwd", ("x_row",)), ("comba_conv_step", ("x_row",)),
+    ("comba_select_step", ("u_row", "delta_row", "z_row", "b_row", "c_row")),
+    ("comba_group_norm_fwd", ("x_row", "z_row"))])
+def test_rows_far_apart_are_taken(name, rows):
+    """They go on to the next check (a missing output); spans past 64-bit offsets do not."""
+    for r in rows:
+        assert call(name, shape_of(name, **{r: FAR}), y=None) == ENULL, r
+        assert call(name, shape_of(name, **{r: (1 << 57) // 10}), y=None) == ENULL, r
+        assert call(name, shape_of(name, **{r: 1 << 60}), y=None) == ESHAPE, r
+
+
+def test_the_scan_states_the_limit_of_its_rows():
+    """Its tiles address rows by 32-bit offsets: rows up to 2^22 elements apart, refused by
+    name above that."""
+    import torch
+
+    for r in ("u_row", "delta_row", "z_row", "b_row", "c_row"):
+        for name in ("comba_select_fwd", "comba_select_fwd_save", "comba_select_bwd"):
+            assert call(name, select(**{r: FAR})) == ESHAPE, (name, r)
+            missing = {"dA": None} if name.endswith("bwd") else {"y": None}
+            assert call(name, select(**{r: 1 << 22}), **missing) == ENULL, (name, r)
+    from paper_2506_02475_amd.layer import _row
+
+    far = torch.empty_strided((2, 1, 8), (FAR, FAR, 1), device="meta")
+    dev = far.get_device()
+    assert _row("z", far, 2, (2, 1, 8), torch.float32, dev) == FAR
+    with pytest.raises(comba.CombaError, match="rows of z .*4194304"):
+        _row("z", far, 2, (2, 1, 8), torch.float32, dev, 1 << 22)
