@@ -248,3 +248,25 @@ def test_the_scan_states_the_limit_of_its_rows():
     assert _row("z", far, 2, (2, 1, 8), torch.float32, dev) == FAR
     with pytest.raises(comba.CombaError, match="rows of z .*4194304"):
         _row("z", far, 2, (2, 1, 8), torch.float32, dev, 1 << 22)
+
+
+def test_a_workspace_has_to_be_device_memory():
+    """Host memory, or fewer bytes behind a view than it has elements, would be written past."""
+    import torch
+
+    from paper_2506_02475_amd.layer import _workspace
+
+    def size(shp):
+        return 1000
+
+    host = torch.empty(2000, dtype=torch.uint8)
+    with pytest.raises(comba.CombaError, match="workspace"):
+        _workspace(size, b"", host, torch.device("cuda", 0))
+    meta = torch.device("meta")
+    assert _workspace(size, b"", None, meta).numel() == 1000
+    small = torch.empty(999, dtype=torch.uint8, device=meta)
+    assert _workspace(size, b"", small, meta).numel() == 1000  # too small: made anew
+    good = torch.empty(1000, dtype=torch.uint8, device=meta)
+    assert _workspace(size, b"", good, meta) is good
+    with pytest.raises(comba.CombaError, match="workspace"):
+        _workspace(size, b"", good[:1].expand(5000), meta)
