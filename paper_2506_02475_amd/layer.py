@@ -220,14 +220,18 @@ def _run(status):
 
 def _on(stream, dev, *made):
     """The stream handle of a call.  Tensors that the call makes on another stream than
-    torch's current one are marked as used there, so that their memory is not given away
-    while the kernels still run."""
+    torch's current one: that stream first waits for the current one, whose work may still
+    use the memory that they were given, and they are marked as used there, so that it is
+    not given away while the kernels still run."""
     import torch
 
     here = torch._C._cuda_getCurrentRawStream(dev)
     if stream is None or stream == here:
         return here
-    ext = torch.cuda.ExternalStream(stream, device=dev)
+    # (an ExternalStream of handle 0, the default stream, would be another stream)
+    ext = torch.cuda.ExternalStream(stream, device=dev) if stream \
+        else torch.cuda.default_stream(dev)
+    ext.wait_stream(torch.cuda.current_stream(dev))
     for t in made:
         if t is not None:
             t.record_stream(ext)

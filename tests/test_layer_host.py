@@ -270,3 +270,37 @@ def test_a_workspace_has_to_be_device_memory():
     assert _workspace(size, b"", good, meta) is good
     with pytest.raises(comba.CombaError, match="workspace"):
         _workspace(size, b"", good[:1].expand(5000), meta)
+
+
+def test_another_stream_waits_for_the_current_one(monkeypatch):
+    """What a call makes comes from the current stream's memory, whose last users may still be
+    at work there: a stream given by handle has to wait for them before it writes."""
+    import torch
+
+    from paper_2506_02475_amd import layer
+
+    log = []
+
+    class Stream:
+        def __init__(self, handle, device=None):
+            self.handle = handle
+
+        def wait_stream(self, other):
+            log.append((self.handle, "waits for", other.handle))
+
+    class Made:
+        def record_stream(self, s):
+            log.append(("used on", s.handle))
+
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 7, raising=False)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: Stream(7))
+    assert layer._on(None, 0, Made()) == 7 and layer._on(7, 0, Made()) == 7
+    assert log == []
+    assert layer._on(9, 0, Made(), None) == 9
+    assert log == [(9, "waits for", 7), ("used on", 9)]
+    # handle 0 is the default stream
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda dev=None: Stream("default"))
+    del log[:]
+    assert layer._on(0, 0, Made()) == 0
+    assert log == [("default", "waits for", 7), ("used on", "default")]
