@@ -10,7 +10,7 @@ and, differentiable (torch.autograd), comba_conv, comba_select, comba_group_norm
 Activations are bfloat16 or float32 and so are their gradients and outputs;
 parameters, their gradients and the scan's states are float32.  Tensors may be
 column slices of a wider row (a projection's output) where noted; everything
-else is contiguous.  Packed sequences pass ``cu_seqlens`` (and, to have the
+else is contiguous, on the current device.  Packed sequences pass ``cu_seqlens`` (and, to have the
 offsets checked, ``cu_seqlens_host``) as in the package's other calls.
 """
 from __future__ import annotations
@@ -225,6 +225,9 @@ def _on(stream, dev, *made):
     not given away while the kernels still run."""
     import torch
 
+    if torch._C._cuda_getDevice() != dev:
+        raise CombaError("comba: the tensors are on device %d: make it the current device "
+                         "(torch.cuda.device)" % dev)
     here = torch._C._cuda_getCurrentRawStream(dev)
     if stream is None or stream == here:
         return here

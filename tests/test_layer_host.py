@@ -293,6 +293,7 @@ def test_another_stream_waits_for_the_current_one(monkeypatch):
             log.append(("used on", s.handle))
 
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 7, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: Stream(7))
     assert layer._on(None, 0, Made()) == 7 and layer._on(7, 0, Made()) == 7
@@ -304,3 +305,17 @@ def test_another_stream_waits_for_the_current_one(monkeypatch):
     del log[:]
     assert layer._on(0, 0, Made()) == 0
     assert log == [("default", "waits for", 7), ("used on", "default")]
+
+
+def test_tensors_of_another_device_than_the_current_one(monkeypatch):
+    """Their default stream has the handle of the current device's, so the kernels would run
+    on the wrong GPU, with pointers of the other."""
+    import torch
+
+    from paper_2506_02475_amd import layer
+
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    assert layer._on(None, 0) == 0
+    with pytest.raises(comba.CombaError, match="device 1.*current"):
+        layer._on(None, 1)
