@@ -42,8 +42,7 @@ def _work_rows(B=1, T=0, D=0, N=16, G=1, lens=None, **_):
 
     fwd = lib.comba_select_fwd_workspace_bytes(ctypes.byref(s))
     bwd = lib.comba_select_bwd_workspace_bytes(ctypes.byref(s))
-    rows = round((fwd - 256) / (D * (N + 1) * 4))
-    assert fwd == up(rows * D * N * 4) + up(rows * D * 4) + 256
+    rows = [r for r in range(2000) if fwd == up(r * D * N * 4) + up(r * D * 4) + 256][0]
     whole = up(parts * s.T * 2 * N * 4) + up(S * D * (N + 2) * 4) + 256
     return rows, bwd > whole
 
