@@ -93,6 +93,8 @@ typedef struct {
  *   u, delta, z, y [B,T,D] in_dtype (z or NULL); A [D,N] fp32 (negative for a
  *   decaying state); Bm, Cm [B,T,G,N] in_dtype; Dskip, delta_bias [D] fp32 or
  *   NULL; h0, ht [num_seqs,D,N] fp32 or NULL.
+ * Sequences times blocks of 512 / N channels (per group) may be up to 2^32 / 768
+ * (N = 8: 512) in a call.
  * Few long rows (packed ones only with cu_seqlens_host) are cut into segments
  * that run side by side; the choice follows from the shape and the device.
  * The workspace holds comba_select_fwd_workspace_bytes.  The saving form's holds

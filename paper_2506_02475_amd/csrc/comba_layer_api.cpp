@@ -91,6 +91,10 @@ size_t conv_ws_bytes(const comba::ConvArgs& a) {
 }
 
 // ---- selective scan -----------------------------------------------------------
+// Workgroups of a launch, which holds fewer than 2^32 threads: the tiles' have 512 or
+// 768 each.
+int64_t select_groups(int N) { return UINT32_MAX / (N == 8 ? 512 : 768); }
+
 struct SelectLayout {
   size_t ck, bcp, dap, segF, segdt, total;
 };
@@ -220,7 +224,7 @@ void select_rows(comba::SelectArgs* a, bool bwd, comba::SelectRows* q) {
     }
     rows += first.count;
     const double t = launch + rounds() + pre * makespan(&first, 1, blocks, cus, start);
-    if (t < best && rows * blocks <= INT32_MAX) {
+    if (t < best && rows * blocks <= select_groups(a->N)) {
       best = t;
       a->segs = (int)segs;
       a->seglen = (int)len;
@@ -290,7 +294,7 @@ comba_status select_args(const comba_select_shape* s, comba::SelectArgs* a, bool
   a->cu_seqlens = s->cu_seqlens;
   const int bc = comba::select_block_channels(s->N);
   a->nblk = (s->D / s->G + bc - 1) / bc;
-  if ((int64_t)a->S * a->G * a->nblk > INT32_MAX) return COMBA_ERR_SHAPE;
+  if (tiles && (int64_t)a->S * a->G * a->nblk > select_groups(s->N)) return COMBA_ERR_SHAPE;
   const int64_t gn = (int64_t)s->G * s->N;
   auto row = [&](int64_t given, int64_t width, long* to) {
     return row_stride(given, width, r.Ttot, tiles, to);

@@ -319,3 +319,17 @@ def test_tensors_of_another_device_than_the_current_one(monkeypatch):
     assert layer._on(None, 0) == 0
     with pytest.raises(comba.CombaError, match="device 1.*current"):
         layer._on(None, 1)
+
+
+def test_a_scan_of_more_workgroups_than_a_launch_holds():
+    """A launch has fewer than 2^32 threads: more sequences x channel blocks are refused before
+    the first of a call's launches, not by one of them."""
+    lib = comba.load_library()
+    for N, most in ((8, 2 ** 23 - 1), (16, (2 ** 32 - 1) // 768), (32, (2 ** 32 - 1) // 768)):
+        for S, fits in ((most, True), (most + 1, False)):
+            shp = select(B=S, num_seqs=S, T=1, D=512 // N, N=N)
+            assert call("comba_select_fwd", shp, y=None) == (ENULL if fits else ESHAPE), (N, S)
+            assert call("comba_select_bwd", shp, dA=None) == (ENULL if fits else ESHAPE), (N, S)
+            assert (lib.comba_select_save_bytes(ctypes.byref(shp)) > 0) == fits
+    S = 1 << 23  # the steps take several rows a thread
+    assert call("comba_select_step", select(B=S, num_seqs=S, T=1, D=32), y=None) == ENULL
