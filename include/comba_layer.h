@@ -95,6 +95,9 @@ typedef struct {
  *   NULL; h0, ht [num_seqs,D,N] fp32 or NULL.
  * Sequences times blocks of 512 / N channels (per group) may be up to 2^32 / 768
  * (N = 8: 512) in a call.
+ * The decays of several tokens (of a segment: all of its tokens) are multiplied in
+ * fp32 before they meet a state: where dt A > 0, a growth of more than 2^127 over
+ * them overflows, also before a state that is zero.
  * Few long rows (packed ones only with cu_seqlens_host) are cut into segments
  * that run side by side; the choice follows from the shape and the device.
  * The workspace holds comba_select_fwd_workspace_bytes.  The saving form's holds
