@@ -191,9 +191,9 @@ def _activation(name, allowed):
     return ACTIVATIONS[name]
 
 
-def _memory(given, device):
-    """A caller's workspace: as many bytes as elements, at least, on the device."""
-    if given.device != device or not given.is_contiguous():
+def _memory(given, here):
+    """A caller's workspace: as many bytes as elements, at least, ``here`` on the device."""
+    if not here or not given.is_contiguous():
         raise CombaError("comba: a workspace must be contiguous memory on the tensors' device")
     return given
 
@@ -204,7 +204,7 @@ def _workspace(fn, shp, given, device):
     nbytes = fn(shp)
     if nbytes == 0:
         _check(2)
-    if given is not None and _memory(given, device).numel() >= nbytes:
+    if given is not None and _memory(given, given.device == device).numel() >= nbytes:
         return given
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
@@ -225,10 +225,11 @@ def _on(stream, dev, *made):
     not given away while the kernels still run."""
     import torch
 
-    if torch._C._cuda_getDevice() != dev:
+    cuda = torch._C
+    if cuda._cuda_getDevice() != dev:
         raise CombaError("comba: the tensors are on device %d: make it the current device "
                          "(torch.cuda.device)" % dev)
-    here = torch._C._cuda_getCurrentRawStream(dev)
+    here = cuda._cuda_getCurrentRawStream(dev)
     if stream is None or stream == here:
         return here
     # (an ExternalStream of handle 0, the default stream, would be another stream)
@@ -432,8 +433,8 @@ def comba_select_bwd(u, delta, A, B, C, D, z, delta_bias, h0, dy, dht=None, *, w
            "dz": None if z is None else _like(u),
            "ddelta_bias": None if delta_bias is None else _like(delta_bias),
            "dh0": A.new_empty(state) if need_dh0 else None}
-    if workspace is None or \
-            _memory(workspace, u.device).numel() < lib.comba_select_save_bytes(shp):
+    if workspace is None or _memory(workspace, workspace.get_device() == dev).numel() \
+            < lib.comba_select_save_bytes(shp):
         raise CombaError("comba: comba_select_bwd needs the workspace filled by "
                          "comba_select_fwd_save")
     ws = _workspace(lib.comba_select_bwd_workspace_bytes, shp, scratch, u.device)
