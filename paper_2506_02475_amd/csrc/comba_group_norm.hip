@@ -14,9 +14,12 @@
 //
 // Groups of more than 8,192 channels read x again from the caches
 // (k_group_norm_wide), at a higher cost: 8,192 rows of one group of 8,192 channels
-// take 87 us forward and 166 backward in registers, of 12,000 from the caches 325
-// and 948; one group of 4,096 from the caches 443 and 929 for 16,384 rows, not 86
-// and 156.
+// take 87 us forward and 170 backward in registers, of 12,000 from the caches 336
+// and 966, 2.8 and 4.9 times their bytes at the copy rate (dw and db are read and
+// written per row there, and the gradient is formed twice); one group of 4,096 from the
+// caches 443 and 929 for 16,384 rows, not 88 and 158.  An odd width takes one channel a
+// piece: 8,192 rows of 8,191 channels 136 and 218 in bf16 (whose backward keeps 12 of its
+// registers in scratch), 152 and 290 in fp32.
 #include "comba_layer_device.hpp"
 #include "comba_layer_launch.h"
 
@@ -327,7 +330,7 @@ __global__ __launch_bounds__(64 * GN_WAVES) void k_group_norm_dw(GroupNormArgs a
 
 // The team of a group of m channels, and how many teams walk the rows: 1,024 lanes
 // per CU (bf16, 16,384 x 4,096 channels, groups of 128: 512 / 1,024 / 2,048 lanes
-// forward 102 / 84 / 92 us, backward 149 / 149 / 154).
+// forward 106 / 84 / 95 us, backward 164 / 155 / 166, whole calls with the sums).
 constexpr long GN_LANES = 1024;
 static GnTeam gn_team(const GroupNormArgs& a, int& kv) {
   const int m = a.C / a.G, pieces = (m + GN_C - 1) / GN_C;
@@ -361,8 +364,8 @@ static hipError_t run_group_norm(const GroupNormArgs& a0) {
       return !p || ((uintptr_t)p % (GN_C * eb) == 0 && row % GN_C == 0);
     };
     // pieces of four channels, or of one for other groups and for slices that are not
-    // aligned to four (bf16, 16,384 x 4,096, groups of 128: 83 / 107 us forward, 149 / 197
-    // backward; pieces of four loaded one by one 139 and 274)
+    // aligned to four (bf16, 16,384 x 4,096, groups of 128, whole calls: 84 / 106 us forward,
+    // 155 / 207 backward; pieces of four loaded one by one 139 and 274)
     const bool vec = (a.C / a.G) % GN_C == 0 && ok(a.x, sizeof(Tx), a.x_row) && ok(a.z, sizeof(To), a.z_row) &&
                      ok(a.y, sizeof(To), a.C) && ok(a.dy, sizeof(To), a.C) && ok(a.dx, sizeof(Tx), a.C) &&
                      ok(a.dz, sizeof(To), a.C);

@@ -205,7 +205,7 @@ __device__ __forceinline__ float sigmoid_acc(float x) {
 // log(1 + e^x) = max(x, 0) + log1p(e), e = e^-|x| in (0, 1], with
 // log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3.  2 artanh(s) / s is a
 // polynomial of degree 4 in s^2, fitted at Chebyshev points of [0, 1/9]
-// (relative error 4e-9).  (log(1 + e) itself would lose the low bits of a
+// (relative error 8e-9 as stored).  (log(1 + e) itself would lose the low bits of a
 // small e, and steps of 0.001 are ordinary here.)
 __device__ __forceinline__ float softplus_acc(float x) {
   const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(x));

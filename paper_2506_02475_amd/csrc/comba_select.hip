@@ -7,8 +7,8 @@
 // operations per (channel, state, token), and these, not the bytes, bound every
 // long call.  4 x 4,096 tokens, 4,096 channels, 16 states, gated, bf16: forward 352
 // us with 10 vector instructions per (channel, state, token), the vector units busy
-// 88% of the time (its bytes alone would take 108 us); backward 936 us with 25 and
-// 84%, and 50 us for its sums.
+// 88% of the time (its bytes alone would take 108 us); backward 936 us, with 25 and
+// 84% in its main kernel and 50 us of it for the sums.
 //
 // Layout of a wave: CW channels x N states.  A lane holds CPL = 2 channels x 4
 // states (lane group ng = lane / CG takes states 4 ng .. 4 ng + 3, lane cg = lane
@@ -24,6 +24,16 @@
 // second pass costs two operations more per value than a walk token by token,
 // but leaves W times as many waves.  Twelve waves are three a SIMD at 168
 // registers: forward 356 us, with eight 408, with six and two workgroups a CU 549.
+//
+// Eleven of the variants need more than 168 and keep 3 to 10 registers in scratch: the
+// gated fp32 backward of 16 states, the backward of 32 states (but ungated, aligned
+// bf16), the gated backward and the gated fp32 forward of 16 states for unaligned
+// rows.  Their scratch stays in the caches (the fp32 backward of 16 states writes 1,033
+// MiB, its results and partial sums 1,024), and they issue as densely (80 to 83% busy).
+// 4 x 4,096 tokens, 4,096 channels, gated, us of the calls, forward and backward: 8 states
+// bf16 235 and 594, fp32 267 and 613; 16 states 363 and 954, fp32 377 and 970; 32 states
+// 669 and 2,072, fp32 681 and 2,141; rows off by one element: 16 states 462 and 1,033, fp32
+// 494 and 1,157; 32 states 862 and 2,294, fp32 780 and 2,235; 8 states 346 and 771.
 #include "comba_layer_device.hpp"
 #include "comba_layer_launch.h"
 
@@ -1050,8 +1060,8 @@ __global__ __launch_bounds__(256) void k_select_step(SelectArgs a) {
 }
 
 // Whether every piece of C channels, and of nb states of a B or C row, is loaded and
-// stored at once, or value by value (4 x 4,096 tokens, 4,096 channels, 16 states: 383 /
-// 455 us forward, 956 / 1,014 backward).
+// stored at once, or value by value (4 x 4,096 tokens, 4,096 channels, 16 states: 363 /
+// 462 us forward, 954 / 1,033 backward).
 static bool rows_vec(const SelectArgs& a, int C, int nb, bool bwd) {
   const long eb = a.bf16 ? 2 : 4;
   auto ok = [&](const void* p, long row, long n) { return !p || ((uintptr_t)p % (n * eb) == 0 && row % n == 0); };
