@@ -113,6 +113,7 @@ def load_library():
             lib.comba_status_string.argtypes = [I]
             lib.comba_status_string.restype = ctypes.c_char_p
             layer.bind(lib)
+            block.bind(lib)
             _lib = lib
     return _lib
 
@@ -646,5 +647,7 @@ def comba_chunk(q, k, v, g, beta, d, h0=None, *, beta_tilde=None, cu_seqlens=Non
 
 from . import layer  # noqa: E402  (after the helpers that it takes from here)
 from .layer import *  # noqa: E402,F401,F403
+from . import block  # noqa: E402
+from .block import *  # noqa: E402,F401,F403
 
-__all__ += layer.__all__
+__all__ += layer.__all__ + block.__all__

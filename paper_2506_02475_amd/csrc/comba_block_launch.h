@@ -1,0 +1,66 @@
+// Internal interface between the host API (comba_block_api.cpp) and the kernels
+// of a block's operators.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "comba_block.h"
+
+namespace comba {
+
+constexpr int DC_CH = 64;  // tokens of a chunk
+constexpr int DC_BV = 32;  // value columns of a scan's workgroup
+
+struct DecayArgs {
+  bool bf16, g_f32, g_head;
+  int S, Tseq, Ttot;  // S sequences
+  const int32_t* cu_seqlens;
+  int H, Hq, Hk, Hv, dk, dv;
+  float scale;
+  long q_row, k_row, v_row, g_row;
+  const void *q, *k, *v, *g;
+  const float* h0;
+  void* o;
+  float* ht;
+  // states at every chunk's start, [chunk slot][H][dv][dk] in in_dtype: written (or
+  // NULL), read; a sequence's slots start at start / 64 + its number (fixed rows: at
+  // its number times the row's chunks)
+  void* kept;
+  // step
+  float* state;
+  const int32_t* slots;
+  int num_slots;
+  // backward
+  const void* dO;
+  const float* dht;
+  void *dq, *dk_, *dv_, *dg;
+  float* dh0;
+  void* dkept;  // gradients of the states at every chunk's end, laid out as `kept`
+  float *pq, *pk, *pv;  // [tokens][H][d] gradients of shared heads before their sum, or NULL
+  // sequences of more than seglen tokens run as segments of seglen (a multiple of 64)
+  // side by side, each from its true state: per segment slot and head its end from
+  // zero and its decay
+  int seglen;
+  float* segS;
+  float* segG;  // log2
+  hipStream_t stream;
+};
+// Slots of pieces of `unit` tokens.
+inline long decay_slots(const DecayArgs& a, long unit) {
+  const long per = (a.Tseq + unit - 1) / unit;
+  return a.cu_seqlens ? a.Ttot / unit + a.S : a.S * (per > 1 ? per : 1);
+}
+// Padded size of the key dimension: of a scan's tiles.
+inline int decay_dkp(int dk) { return dk <= 64 ? 64 : dk <= 128 ? 128 : 256; }
+inline int decay_splits(int dv) { return (dv + DC_BV - 1) / DC_BV; }
+// Floats of one segment's end: every split's accumulators.
+inline long decay_end_floats(const DecayArgs& a) {
+  return (long)decay_splits(a.dv) * DC_BV * decay_dkp(a.dk);
+}
+hipError_t launch_decay_fwd(const DecayArgs& a);
+hipError_t launch_decay_bwd(const DecayArgs& a);
+hipError_t launch_decay_step(const DecayArgs& a);
+
+}  // namespace comba

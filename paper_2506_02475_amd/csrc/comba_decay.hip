@@ -1,0 +1,911 @@
+// Linear attention with a decay for each head, in chunks of 64 tokens.  Per head,
+// with G_r the sum of a chunk's log-decays up to row r and S the state entering it:
+//
+//   o_r   = scale (sum_{j <= r} e^{G_r - G_j} (q_r . k_j) v_j + e^{G_r} S^T q_r)
+//   S'    = e^{G_end} S + sum_j e^{G_end - G_j} k_j v_j^T
+//   dS    = e^{G_end} dS' + scale sum_r e^{G_r} q_r do_r^T        (dS' of the next chunk)
+//   dq_r  = scale (sum_{j <= r} e^{G_r - G_j} (do_r . v_j) k_j + e^{G_r} S do_r)
+//   dk_j  = scale sum_{r >= j} e^{G_r - G_j} (do_r . v_j) q_r + e^{G_end - G_j} dS' v_j
+//   dv_j  = scale sum_{r >= j} e^{G_r - G_j} (q_r . k_j) do_r + e^{G_end - G_j} dS'^T k_j
+//   dg_t  = the sum over all pairs j < t <= r of a pair's weight times its products:
+//           both tokens in the chunk, one of them, or none (e^{G_end} <dS', S>).
+//
+// All differences of G are formed from sums in 64 bits; what is masked is never formed.
+#include "comba_block_launch.h"
+#include "comba_layer_device.hpp"
+
+namespace comba {
+
+// ---- matrix products -----------------------------------------------------------
+// Eight values of an operand along the summed index; bf16 on the bf16 matrix
+// instruction, fp32 on the fp32 one (eight of its steps of one value a lane).
+template <typename T> struct Frag;
+template <> struct Frag<bf16_t> {
+  bf16x8 x;
+};
+template <> struct Frag<float> {
+  float x[8];
+};
+__device__ __forceinline__ floatx4 mma(const Frag<bf16_t>& a, const Frag<bf16_t>& b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.x, b.x, c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx4 mma(const Frag<float>& a, const Frag<float>& b, floatx4 c) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[e], b.x[e], c, 0, 0, 0);
+  return c;
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ Frag<T> as_frag(const Piece<T, 8, VEC>& p) {
+  Frag<T> f;
+  if constexpr (is_f32<T>::value) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.x[e] = __uint_as_float(p.r[e]);
+  } else {
+    f.x = __builtin_bit_cast(bf16x8, make_uint4(p.r[0], p.r[1], p.r[2], p.r[3]));
+  }
+  return f;
+}
+// Two accumulators as an operand: the lane's rows 4 (l / 16) .. + 3 of both.
+template <typename T>
+__device__ __forceinline__ Frag<T> frag_of(const floatx4& a, const floatx4& b) {
+  Frag<T> f;
+  if constexpr (is_f32<T>::value) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f.x[e] = a[e], f.x[4 + e] = b[e];
+  } else {
+    f.x = __builtin_bit_cast(bf16x8, make_uint4(bf16_pair(a[0], a[1]), bf16_pair(a[2], a[3]),
+                                                bf16_pair(b[0], b[1]), bf16_pair(b[2], b[3])));
+  }
+  return f;
+}
+// From a tile of rows of LD elements (a multiple of 64, pieces of eight swizzled):
+// eight consecutive elements of row (lane % 16), from column col + 8 (lane / 16).
+template <int LD, typename T>
+__device__ __forceinline__ Frag<T> ld_row(const T* tile, int row, int col) {
+  const T* p = tile + sw16<LD>(row + (lane_id() & 15), col + 8 * (lane_id() >> 4));
+  Frag<T> f;
+  if constexpr (is_f32<T>::value) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    f.x[0] = a.x, f.x[1] = a.y, f.x[2] = a.z, f.x[3] = a.w;
+    f.x[4] = b.x, f.x[5] = b.y, f.x[6] = b.z, f.x[7] = b.w;
+  } else {
+    f.x = *reinterpret_cast<const bf16x8*>(p);
+  }
+  return f;
+}
+// Column col + lane % 16 at rows r0 .. r0 + 3 and r1 .. r1 + 3.
+template <int LD, typename T>
+__device__ __forceinline__ Frag<T> ld_col2(const T* tile, int r0, int r1, int col) {
+  const int s = lane_id() & 15;
+  Frag<T> f;
+  if constexpr (is_f32<T>::value) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      f.x[e] = tile[sw16<LD>(r0 + e, col + s)];
+      f.x[4 + e] = tile[sw16<LD>(r1 + e, col + s)];
+    }
+  } else {
+    const int at = s >> 2, c = col + 4 * (s & 3);
+    f.x = ld_tr8(tile, TrOff{sw16<LD>(r0 + at, c), sw16<LD>(r1 + at, c)});
+  }
+  return f;
+}
+// The same at rows r0 + 8 (lane / 16) .. + 7 ...
+template <int LD, typename T>
+__device__ __forceinline__ Frag<T> ld_col(const T* tile, int r0, int col) {
+  const int r = r0 + 8 * (lane_id() >> 4);
+  return ld_col2<LD>(tile, r, r + 4, col);
+}
+// ... and in the row order of frag_of: 4 (lane / 16) .. + 3 of two blocks of 16.
+template <int LD, typename T>
+__device__ __forceinline__ Frag<T> ld_col_acc(const T* tile, int r0, int col) {
+  const int r = r0 + 4 * (lane_id() >> 4);
+  return ld_col2<LD>(tile, r, r + 16, col);
+}
+template <int LD, typename T, bool VEC>
+__device__ __forceinline__ void st_row8(T* tile, int row, int col, const Piece<T, 8, VEC>& p) {
+  uint4* d = reinterpret_cast<uint4*>(tile + sw16<LD>(row, col));
+  d[0] = make_uint4(p.r[0], p.r[1], p.r[2], p.r[3]);
+  if constexpr (is_f32<T>::value) d[1] = make_uint4(p.r[4], p.r[5], p.r[6], p.r[7]);
+}
+// Four values at columns col .. col + 3 (a multiple of four).
+template <int LD, typename T>
+__device__ __forceinline__ void st_row4(T* tile, int row, int col, const floatx4& x) {
+  T* d = tile + sw16<LD>(row, col);
+  if constexpr (is_f32<T>::value) *reinterpret_cast<float4*>(d) = make_float4(x[0], x[1], x[2], x[3]);
+  else *reinterpret_cast<uint2*>(d) = make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
+}
+
+// ---- chunks and rows --------------------------------------------------------------
+// n tokens' rows of one head as a raw buffer: what lies behind the last row reads as
+// zeros, and stores there are dropped.
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t head_rows(const void* t, long tok, long row, long col, int n, int d) {
+  const T* p = static_cast<const T*>(t) + tok * row + col;
+  const unsigned bytes = n > 0 ? (unsigned)(((long)(n - 1) * row + d) * (long)sizeof(T)) : 0u;
+  return clip_rsrc(const_cast<T*>(p), bytes);
+}
+// Columns col .. col + 7 of row r; columns from d on are zeros.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(Piece<T, 8, VEC>& p, __amdgpu_buffer_rsrc_t rs, int r, unsigned row_bytes, int col,
+                                      int d) {
+  const unsigned off = (unsigned)r * row_bytes + (unsigned)col * (unsigned)sizeof(T);
+  if constexpr (VEC) p.load(rs, col < d ? off : BUF_OOB, 8);
+  else p.load(rs, off, d - col);
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ Frag<T> load_frag(__amdgpu_buffer_rsrc_t rs, int row, unsigned row_bytes, int col, int d) {
+  Piece<T, 8, VEC> p;
+  load8(p, rs, row + (lane_id() & 15), row_bytes, col + 8 * (lane_id() >> 4), d);
+  return as_frag<T, VEC>(p);
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store4c(__amdgpu_buffer_rsrc_t rs, int r, unsigned row_bytes, int col, int d,
+                                        const floatx4& x) {
+  const float v[4] = {x[0], x[1], x[2], x[3]};
+  const unsigned off = (unsigned)r * row_bytes + (unsigned)col * (unsigned)sizeof(T);
+  store_piece<T, 4, VEC>(rs, col < d ? off : BUF_OOB, v, d - col);
+}
+
+// The piece of a slot: sequence, its first token and length, the piece's number.  A
+// sequence's slots start at start / unit + its number (fixed rows: at its number times
+// `per`).  Offsets are clamped into the tokens whatever they hold.
+struct Slot {
+  int seq, piece, t0, len;
+};
+__device__ __forceinline__ Slot find_slot(const DecayArgs& a, int slot, int unit) {
+  Slot s;
+  if (!a.cu_seqlens) {
+    const int per = max((a.Tseq + unit - 1) / unit, 1);
+    s.seq = slot / per;
+    s.piece = slot % per;
+  } else {
+    int lo = 0, hi = a.S;  // the last sequence whose slots start at or before this one
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (min(max(a.cu_seqlens[mid], 0), a.Ttot) / unit + mid <= slot) lo = mid;
+      else hi = mid;
+    }
+    s.seq = lo;
+    s.piece = max(slot - (min(max(a.cu_seqlens[lo], 0), a.Ttot) / unit + lo), 0);
+  }
+  int b;
+  seq_range(a.cu_seqlens, s.seq, a.Tseq, a.Ttot, s.t0, b);
+  s.len = b - s.t0;
+  return s;
+}
+__device__ __forceinline__ int first_slot(const DecayArgs& a, const Slot& s, int unit) {
+  return a.cu_seqlens ? s.t0 / unit + s.seq : s.seq * max((a.Tseq + unit - 1) / unit, 1);
+}
+
+// A token's log-decay, and the sums over a chunk (lane = row, 64 bits, base 2).
+__device__ __forceinline__ float gate_of(const DecayArgs& a, long tok, int h) {
+  if (a.g_head) return static_cast<const float*>(a.g)[h];
+  const long at = tok * a.g_row + h;
+  return a.g_f32 ? static_cast<const float*>(a.g)[at] : bf2f(static_cast<const bf16_t*>(a.g)[at]);
+}
+__device__ __forceinline__ double gate_sum(float g) {
+  g = g < -128.f ? -128.f : g;
+  double x = (double)g * 1.4426950408889634074;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const double y = __shfl_up(x, d);
+    x += lane_id() >= d ? y : 0.0;
+  }
+  return x;
+}
+// Pair weights from two floats a sum: a difference keeps the accuracy of the 64 bits.
+struct Sums {
+  float hi[DC_CH], lo[DC_CH];
+};
+
+// fp32 as the sum of three bf16: products with an exact bf16 operand keep 24 bits.
+__device__ __forceinline__ void split3(float x, float y, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  uint32_t rest;
+  split2(x, y, hi, rest);
+  const float ax = x - __uint_as_float(hi << 16), ay = y - __uint_as_float(hi & 0xFFFF0000u);
+  split2(ax, ay, mid, lo);
+}
+
+// ---- the scans ---------------------------------------------------------------------
+// A workgroup walks the chunks of one segment of one sequence and head, and holds DC_BV
+// value columns of the state in fp32 accumulators (wave w: key rows w DK / 4 ..).
+// Forward: keys k, values v, weights e^{G_end - G_j}.  REV, for the states' gradients,
+// from the last chunk to the first: keys q, values do, weights scale e^{G_r}.
+// LOCAL: a segment's end from a zero state, for the segments behind it.
+// The weights multiply the value columns, of which a workgroup has few, and there
+// fp32 becomes three bf16 against the keys as they are: the state's sums keep 24 bits.
+template <typename T, int DK>
+struct ScanTiles {
+  static constexpr int VLD = is_f32<T>::value ? 64 : 128;  // weighted values (bf16: three terms), values
+  T k[DC_CH * DK], v[DC_CH * VLD], s[DC_BV * DK];
+  Sums g;
+};
+
+template <typename T, int DK, bool REV, bool LOCAL, bool VEC>
+__global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
+  constexpr bool F32 = is_f32<T>::value, OUT = !REV && !LOCAL;
+  constexpr int VLD = ScanTiles<T, DK>::VLD, NT = F32 ? 1 : 3, VCOL = DC_BV * NT;
+  constexpr int MT = DK / 64, KI = DK / 32;
+  __shared__ __align__(16) ScanTiles<T, DK> t;
+
+  // the splits of one head's state on one XCD (they read the same keys), heads dealt
+  // over the XCDs
+  const int NS = (a.dv + DC_BV - 1) / DC_BV;
+  const int id = blockIdx.x % (8 * NS), u = blockIdx.x / (8 * NS) * 8 + id % 8, split = id / 8;
+  if (u >= units) return;
+  const int slot = u / a.H, h = u % a.H, j0 = split * DC_BV;
+  const Slot sq = find_slot(a, slot, a.seglen);
+  const int first = sq.piece * a.seglen;
+  if (sq.piece > 0 && first >= sq.len) return;
+  const int n = min(a.seglen, sq.len - first), nc = (n + DC_CH - 1) / DC_CH;
+  const int base = first_slot(a, sq, a.seglen);
+  const int segs = max((sq.len + a.seglen - 1) / a.seglen, 1);
+  if (LOCAL && sq.piece == (REV ? 0 : segs - 1)) return;  // no segment comes after it
+  const int w = wave_id_s(), lane = lane_id(), r16 = lane & 15, g4 = lane >> 4;
+
+  const int hx = REV ? h / (a.H / a.Hq) : h / (a.H / a.Hk), hq = h / (a.H / a.Hq), hv = REV ? h : h / (a.H / a.Hv);
+  const long xrow = REV ? a.q_row : a.k_row, yrow = REV ? (long)a.H * a.dv : a.v_row;
+  const void *X = REV ? a.q : a.k, *Y = REV ? a.dO : a.v;
+  const long tok0 = (long)sq.t0 + first;
+
+  // ---- the state that enters
+  floatx4 S[MT][2];
+  const int row0 = w * (DK / 4) + 4 * g4;  // key rows row0 + 16 m + i, value columns j0 + 16 n + r16
+  auto each = [&](auto fn) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[m][c][i] = fn(S[m][c][i], row0 + 16 * m + i, j0 + 16 * c + r16);
+  };
+  const long ends = (long)NS * DC_BV * DK;  // floats of a segment's end
+  auto end_at = [&](int sl) {
+    return a.segS + ((long)sl * a.H + h) * ends + (((long)split * 4 + w) * 64 + lane) * (MT * 8);
+  };
+  const float* in = REV ? a.dht : a.h0;
+  const long sbase = ((long)sq.seq * a.H + h) * a.dk * a.dv;
+  {
+    double f = 0.;
+    if (!LOCAL) {
+      for (int p = 0; p < (REV ? segs - 1 - sq.piece : sq.piece); ++p)
+        f += a.segG[(long)(base + (REV ? sq.piece + 1 + p : p)) * a.H + h];
+    }
+    const float far = __builtin_amdgcn_exp2f((float)f);
+    each([&](float, int r, int c) {
+      return !LOCAL && in && r < a.dk && c < a.dv ? far * in[sbase + (long)r * a.dv + c] : 0.f;
+    });
+    if (!LOCAL && (REV ? sq.piece < segs - 1 : sq.piece > 0)) {
+      double between = 0.;
+      for (int p = 0; p < (REV ? segs - 1 - sq.piece : sq.piece); ++p) {  // the nearest first
+        const int sl = base + (REV ? sq.piece + 1 + p : sq.piece - 1 - p);
+        const float f2 = __builtin_amdgcn_exp2f((float)between);
+        const float4* e = reinterpret_cast<const float4*>(end_at(sl));
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const float4 x = e[m * 2 + c];
+            S[m][c][0] = fmaf(f2, x.x, S[m][c][0]);
+            S[m][c][1] = fmaf(f2, x.y, S[m][c][1]);
+            S[m][c][2] = fmaf(f2, x.z, S[m][c][2]);
+            S[m][c][3] = fmaf(f2, x.w, S[m][c][3]);
+          }
+        between += a.segG[(long)sl * a.H + h];
+      }
+    }
+  }
+
+  // ---- a chunk's inputs: the next one's loads are in flight while one is worked on
+  Piece<T, 8, VEC> pk[KI], pv, pq[OUT ? KI : 1];
+  float pg = 0.f;
+  auto load = [&](int c) {
+    const long tok = tok0 + (long)c * DC_CH;
+    const int m = min(DC_CH, n - c * DC_CH);
+    const auto rx = head_rows<T>(X, tok, xrow, (long)hx * a.dk, m, a.dk);
+    const auto ry = head_rows<T>(Y, tok, yrow, (long)hv * a.dv, m, a.dv);
+#pragma unroll
+    for (int it = 0; it < KI; ++it) {
+      const int idx = threadIdx.x + it * 256;
+      load8(pk[it], rx, idx / (DK / 8), (unsigned)xrow * sizeof(T), idx % (DK / 8) * 8, a.dk);
+    }
+    load8(pv, ry, threadIdx.x / 4, (unsigned)yrow * sizeof(T), j0 + threadIdx.x % 4 * 8, a.dv);
+    if constexpr (OUT) {
+      const auto rq = head_rows<T>(a.q, tok, a.q_row, (long)hq * a.dk, m, a.dk);
+#pragma unroll
+      for (int s = 0; s < KI; ++s)
+        load8(pq[s], rq, 16 * w + r16, (unsigned)a.q_row * sizeof(T), 32 * s + 8 * g4, a.dk);
+    }
+    pg = lane < m ? gate_of(a, tok + lane, h) : 0.f;
+  };
+  if (nc > 0) load(REV ? nc - 1 : 0);
+  const int kslot = first_slot(a, sq, DC_CH) + first / DC_CH;
+  double total = 0.;
+
+  for (int it = 0; it < nc; ++it) {
+    const int c = REV ? nc - 1 - it : it;
+    const int m = min(DC_CH, n - c * DC_CH);
+    // ---- staging
+    const double G = gate_sum(pg), Gend = __shfl(G, 63);
+    total += Gend;
+    {
+#pragma unroll
+      for (int i = 0; i < KI; ++i) {
+        const int idx = threadIdx.x + i * 256;
+        st_row8<DK>(t.k, idx / (DK / 8), idx % (DK / 8) * 8, pk[i]);
+      }
+      const float wt = REV ? a.scale * __builtin_amdgcn_exp2f((float)G) : __builtin_amdgcn_exp2f((float)(Gend - G));
+      const float f = __shfl(wt, 16 * w + lane / 4);
+      const int row = threadIdx.x / 4, col = threadIdx.x % 4 * 8;
+      if constexpr (F32) {
+        Piece<T, 8, VEC> x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x.r[e] = __float_as_uint(f * pv.get(e));
+        st_row8<VLD>(t.v, row, col, x);
+      } else {
+        Piece<T, 8, VEC> x[3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          split3(f * pv.get(2 * e), f * pv.get(2 * e + 1), x[0].r[e], x[1].r[e], x[2].r[e]);
+#pragma unroll
+        for (int e = 0; e < 3; ++e) st_row8<VLD>(t.v, row, 32 * e + col, x[e]);
+      }
+      if constexpr (OUT) {
+        st_row8<VLD>(t.v, row, VCOL + col, pv);
+        if (w == 0) {
+          t.g.hi[lane] = (float)G;
+          t.g.lo[lane] = (float)(G - (double)(float)G);
+        }
+      }
+    }
+    if (!LOCAL && (OUT || a.dkept)) {
+#pragma unroll
+      for (int mm = 0; mm < MT; ++mm)
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc) st_row4<DK>(t.s, 16 * cc + r16, row0 + 16 * mm, S[mm][cc]);
+    }
+    Frag<T> fq[OUT ? KI : 1];
+    if constexpr (OUT) {
+#pragma unroll
+      for (int s = 0; s < KI; ++s) fq[s] = as_frag<T, VEC>(pq[s]);
+    }
+    __syncthreads();
+    if (it + 1 < nc) load(REV ? c - 1 : c + 1);
+
+    // ---- the state kept for the backward
+    if (T* keep = LOCAL ? nullptr : static_cast<T*>(REV ? a.dkept : a.kept)) {
+      keep += ((long)(kslot + c) * a.H + h) * a.dv * a.dk;
+      for (int idx = threadIdx.x; idx < DC_BV * DK / 8; idx += 256) {
+        const int row = idx / (DK / 8), col = idx % (DK / 8) * 8;
+        if (j0 + row < a.dv && col < a.dk) {
+          const T* from = t.s + sw16<DK>(row, col);
+          T* to = keep + (long)(j0 + row) * a.dk + col;
+          if constexpr (VEC) {
+#pragma unroll
+            for (int e = 0; e < (int)sizeof(T) / 2; ++e)
+              reinterpret_cast<uint4*>(to)[e] = reinterpret_cast<const uint4*>(from)[e];
+          } else {
+            for (int e = 0; e < 8; ++e)
+              if (col + e < a.dk) to[e] = from[e];
+          }
+        }
+      }
+    }
+    // ---- outputs, transposed: lane r16 has row 16 w + r16, and four value columns
+    if constexpr (OUT) {
+      floatx4 A[4], oi[2], ot[2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) A[i] = zero4();
+      oi[0] = oi[1] = ot[0] = ot[1] = zero4();
+#pragma unroll
+      for (int s = 0; s < KI; ++s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i <= w) A[i] = mma(ld_row<DK>(t.k, 16 * i, 32 * s), fq[s], A[i]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) oi[i] = mma(ld_row<DK>(t.s, 16 * i, 32 * s), fq[s], oi[i]);
+      }
+      const int r = 16 * w + r16;
+      const float Gh = t.g.hi[r], Gl = t.g.lo[r];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i <= w) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = 16 * i + 4 * g4 + e;
+            float d = Gh - t.g.hi[j];
+            if constexpr (F32) d += Gl - t.g.lo[j];
+            A[i][e] = j <= r ? A[i][e] * __builtin_amdgcn_exp2f(d) : 0.f;
+          }
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (2 * s <= w) {
+          const Frag<T> p = frag_of<T>(A[2 * s], A[2 * s + 1]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) ot[i] = mma(ld_col_acc<VLD>(t.v, 32 * s, VCOL + 16 * i), p, ot[i]);
+        }
+      }
+      const long tok = tok0 + (long)c * DC_CH;
+      const long orow = (long)a.H * a.dv;
+      const auto ro = head_rows<T>(a.o, tok, orow, (long)h * a.dv, m, a.dv);
+      const float eg = a.scale * __builtin_amdgcn_exp2f(Gh);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        floatx4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(eg, oi[i][e], a.scale * ot[i][e]);
+        store4c<T, VEC>(ro, r, (unsigned)orow * sizeof(T), j0 + 16 * i + 4 * g4, a.dv, o);
+      }
+    }
+    // ---- the state behind the chunk
+    const float fade = __builtin_amdgcn_exp2f((float)Gend);
+    each([&](float x, int, int) { return x * fade; });
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      Frag<T> fv[2][NT];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < NT; ++e) fv[i][e] = ld_col<VLD>(t.v, 32 * s, 32 * e + 16 * i);
+#pragma unroll
+      for (int mm = 0; mm < MT; ++mm) {
+        const Frag<T> fk = ld_col<DK>(t.k, 32 * s, w * (DK / 4) + 16 * mm);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < NT; ++e) S[mm][i] = mma(fk, fv[i][e], S[mm][i]);
+      }
+    }
+    __syncthreads();
+  }
+
+  if constexpr (LOCAL) {
+    float4* e = reinterpret_cast<float4*>(end_at(slot));
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) e[m * 2 + c] = make_float4(S[m][c][0], S[m][c][1], S[m][c][2], S[m][c][3]);
+    if (split == 0 && threadIdx.x == 0) a.segG[(long)slot * a.H + h] = (float)total;
+  } else {
+    float* out = REV ? a.dh0 : a.ht;
+    if (out && sq.piece == (REV ? 0 : segs - 1)) {
+      each([&](float x, int r, int c) {
+        if (r < a.dk && c < a.dv) out[sbase + (long)r * a.dv + c] = x;
+        return x;
+      });
+    }
+  }
+}
+
+// ---- gradients of a chunk -----------------------------------------------------------
+// A workgroup forms one chunk's and head's dq, dk, dv and dg from its inputs, the state
+// that enters it and the gradient of the one that leaves it.  Wave w owns the rows
+// 16 w ..: of q in dq, of k and v in dk and dv.  All products are transposed, so that a
+// lane holds four consecutive columns of one row.
+template <typename T>
+struct GradTiles {
+  T q[DC_CH * 64], k[DC_CH * 64], s[64 * 64], d[64 * 64], w[DC_CH * DC_CH], p[DC_CH * DC_CH];
+  Sums g;
+  float row[DC_CH], col[4][DC_CH], far[DC_CH], part[4];
+};
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void k_decay_grad(DecayArgs a) {
+  constexpr bool F32 = is_f32<T>::value;
+  __shared__ __align__(16) GradTiles<T> t;
+  const int slot = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  const Slot sq = find_slot(a, slot, DC_CH);
+  const int first = sq.piece * DC_CH;
+  if (first >= sq.len) return;
+  const int m = min(DC_CH, sq.len - first);
+  const long tok = (long)sq.t0 + first;
+  const int w = wave_id_s(), lane = lane_id(), r16 = lane & 15, g4 = lane >> 4, r = 16 * w + r16;
+  const int dk = a.dk, dv = a.dv;
+  const auto rq = head_rows<T>(a.q, tok, a.q_row, (long)(h / (a.H / a.Hq)) * dk, m, dk);
+  const auto rk = head_rows<T>(a.k, tok, a.k_row, (long)(h / (a.H / a.Hk)) * dk, m, dk);
+  const auto rv = head_rows<T>(a.v, tok, a.v_row, (long)(h / (a.H / a.Hv)) * dv, m, dv);
+  const auto rdo = head_rows<T>(a.dO, tok, (long)a.H * dv, (long)h * dv, m, dv);
+  const unsigned bq = (unsigned)a.q_row * sizeof(T), bk = (unsigned)a.k_row * sizeof(T),
+                 bv = (unsigned)a.v_row * sizeof(T), bo = (unsigned)(a.H * dv) * (unsigned)sizeof(T);
+  const long at = ((long)slot * a.H + h) * dv * dk;
+  const auto rS = head_rows<T>(static_cast<const T*>(a.kept) + at, 0, dk, 0, dv, dk);
+  const auto rD = head_rows<T>(static_cast<const T*>(a.dkept) + at, 0, dk, 0, dv, dk);
+  const unsigned bs = (unsigned)dk * sizeof(T);
+
+  const double G = gate_sum(lane < m ? gate_of(a, tok + lane, h) : 0.f), Gend = __shfl(G, 63);
+  if (w == 0) {
+    t.g.hi[lane] = (float)G;
+    t.g.lo[lane] = (float)(G - (double)(float)G);
+  }
+  const float eg = a.scale * __builtin_amdgcn_exp2f((float)__shfl(G, r));        // of row r as a query
+  const float tail = __builtin_amdgcn_exp2f((float)(Gend - __shfl(G, r)));       // as a key
+  __syncthreads();
+
+  // ---- the pairs' products (q_r . k_j) and (do_r . v_j), lane: row r, j = 16 i + 4 g4 + e
+  floatx4 A[4], Bt[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) A[i] = Bt[i] = zero4();
+  for (int s = 0; s < dk; s += 32) {
+    const Frag<T> f = load_frag<T, VEC>(rq, 16 * w, bq, s, dk);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i <= w) A[i] = mma(load_frag<T, VEC>(rk, 16 * i, bk, s, dk), f, A[i]);
+  }
+  for (int s = 0; s < dv; s += 32) {
+    const Frag<T> f = load_frag<T, VEC>(rdo, 16 * w, bo, s, dv);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i <= w) Bt[i] = mma(load_frag<T, VEC>(rv, 16 * i, bv, s, dv), f, Bt[i]);
+  }
+  {
+    const float Gh = t.g.hi[r], Gl = t.g.lo[r];
+    floatx4 pair[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int j = 16 * i + 4 * g4 + e;
+        float d = Gh - t.g.hi[j];
+        if constexpr (F32) d += Gl - t.g.lo[j];
+        const float f = a.scale * __builtin_amdgcn_exp2f(d);
+        const float b = j <= r ? Bt[i][e] * f : 0.f;
+        pair[i][e] = j < r ? b * A[i][e] : 0.f;
+        A[i][e] = j <= r ? A[i][e] * f : 0.f;
+        Bt[i][e] = b;
+      }
+      st_row4<64>(t.p, r, 16 * i + 4 * g4, A[i]);
+      st_row4<64>(t.w, r, 16 * i + 4 * g4, Bt[i]);
+    }
+    // sums over the pairs j < t <= r for every t: over j as a product with a triangle of
+    // ones (bf16: of the pairs in two terms), then over the rows that remain.  Nothing is
+    // subtracted: where few pairs are left, row sums minus column sums would be rounding.
+    if (a.dg) {
+      floatx4 U[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) U[i] = zero4();
+      floatx4 tri;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) tri[e] = 4 * g4 + e < r16 ? 1.f : 0.f;
+      const floatx4 ones = {1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (2 * s > w) continue;
+        const Frag<T> hi = frag_of<T>(pair[2 * s], pair[2 * s + 1]);
+        Frag<T> lo{};
+        if constexpr (!F32) {
+          floatx4 x[2];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e / 4][e % 4] = pair[2 * s + e / 4][e % 4] - (float)hi.x[e];
+          lo = frag_of<T>(x[0], x[1]);
+        }
+#pragma unroll
+        for (int i = 2 * s; i < 4; ++i) {  // (block i's t against blocks 2 s and 2 s + 1 of j)
+          if (i > w) continue;
+          const Frag<T> l = frag_of<T>(i == 2 * s ? tri : ones, i == 2 * s ? zero4() : i == 2 * s + 1 ? tri : ones);
+          U[i] = mma(l, hi, U[i]);
+          if constexpr (!F32) U[i] = mma(l, lo, U[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int tt = 16 * i + 4 * g4 + e;
+          const float cs = sum16(r >= tt ? U[i][e] : 0.f);
+          if (r16 == 0) t.col[w][tt] = cs;
+        }
+    }
+  }
+  const Frag<T> fw[2] = {frag_of<T>(Bt[0], Bt[1]), frag_of<T>(Bt[2], Bt[3])};
+
+  // ---- dq and dk, 64 columns at a time
+  float xr = 0.f, yj = 0.f, carry = 0.f;
+  const long pq = (long)h * dk, pv = (long)h * dv;
+  const auto oq = a.pq ? head_rows<float>(a.pq, tok, (long)a.H * dk, pq, m, dk)
+                       : head_rows<T>(a.dq, tok, (long)a.H * dk, pq, m, dk);
+  const auto ok = a.pk ? head_rows<float>(a.pk, tok, (long)a.H * dk, pq, m, dk)
+                       : head_rows<T>(a.dk_, tok, (long)a.H * dk, pq, m, dk);
+  const auto ov = a.pv ? head_rows<float>(a.pv, tok, (long)a.H * dv, pv, m, dv)
+                       : head_rows<T>(a.dv_, tok, (long)a.H * dv, pv, m, dv);
+  auto put = [&](__amdgpu_buffer_rsrc_t rs, bool wide, int col, int d, const floatx4& x) {
+    if (wide) store4c<float, VEC>(rs, r, (unsigned)(a.H * d) * 4u, col, d, x);
+    else store4c<T, VEC>(rs, r, (unsigned)(a.H * d) * (unsigned)sizeof(T), col, d, x);
+  };
+  for (int c0 = 0; c0 < dk; c0 += 64) {
+    Piece<T, 8, VEC> x[2], y[2];
+    auto tile = [&](__amdgpu_buffer_rsrc_t rs, unsigned rb, int r0, int c, int d, Piece<T, 8, VEC>(&p)[2]) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int idx = threadIdx.x + 256 * i;
+        load8(p[i], rs, r0 + idx / 8, rb, c + idx % 8 * 8, d);
+      }
+    };
+    auto put_tile = [&](T* to, const Piece<T, 8, VEC>(&p)[2]) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int idx = threadIdx.x + 256 * i;
+        st_row8<64>(to, idx / 8, idx % 8 * 8, p[i]);
+      }
+    };
+    tile(rq, bq, 0, c0, dk, x);
+    tile(rk, bk, 0, c0, dk, y);
+    __syncthreads();
+    put_tile(t.q, x);
+    put_tile(t.k, y);
+    floatx4 aq[4], ak[4], iq[4], ik[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) aq[i] = ak[i] = iq[i] = ik[i] = zero4();
+    for (int v0 = 0; v0 < dv; v0 += 64) {
+      tile(rS, bs, v0, c0, dk, x);
+      tile(rD, bs, v0, c0, dk, y);
+      Frag<T> fo[2], fv[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        fo[s] = load_frag<T, VEC>(rdo, 16 * w, bo, v0 + 32 * s, dv);
+        fv[s] = load_frag<T, VEC>(rv, 16 * w, bv, v0 + 32 * s, dv);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) carry = fmaf(x[i].get(e), y[i].get(e), carry);
+      if (v0 > 0) __syncthreads();
+      put_tile(t.s, x);
+      put_tile(t.d, y);
+      __syncthreads();
+      if (v0 == 0) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const Frag<T> f = ld_col<64>(t.w, 32 * s, 16 * w);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            aq[i] = mma(ld_col_acc<64>(t.k, 32 * s, 16 * i), fw[s], aq[i]);
+            ak[i] = mma(ld_col<64>(t.q, 32 * s, 16 * i), f, ak[i]);
+          }
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          iq[i] = mma(ld_col<64>(t.s, 32 * s, 16 * i), fo[s], iq[i]);
+          ik[i] = mma(ld_col<64>(t.d, 32 * s, 16 * i), fv[s], ik[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int col = 16 * i + 4 * g4;
+      const T *qr = t.q + sw16<64>(r, col), *kr = t.k + sw16<64>(r, col);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x1 = eg * iq[i][e], y1 = tail * ik[i][e];
+        xr = fmaf(to_f(qr[e]), x1, xr);
+        yj = fmaf(to_f(kr[e]), y1, yj);
+        aq[i][e] += x1;
+        ak[i][e] += y1;
+      }
+      put(oq, a.pq, c0 + col, dk, aq[i]);
+      put(ok, a.pk, c0 + col, dk, ak[i]);
+    }
+  }
+  // ---- dv, 64 columns at a time
+  for (int v0 = 0; v0 < dv; v0 += 64) {
+    Piece<T, 8, VEC> x[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int idx = threadIdx.x + 256 * i;
+      load8(x[i], rdo, idx / 8, bo, v0 + idx % 8 * 8, dv);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int idx = threadIdx.x + 256 * i;
+      st_row8<64>(t.q, idx / 8, idx % 8 * 8, x[i]);
+    }
+    floatx4 av[4], iv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) av[i] = iv[i] = zero4();
+    for (int s = 0; s < dk; s += 32) {
+      const Frag<T> f = load_frag<T, VEC>(rk, 16 * w, bk, s, dk);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) iv[i] = mma(load_frag<T, VEC>(rD, v0 + 16 * i, bs, s, dk), f, iv[i]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const Frag<T> f = ld_col<64>(t.p, 32 * s, 16 * w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) av[i] = mma(ld_col<64>(t.q, 32 * s, 16 * i), f, av[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      floatx4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(tail, iv[i][e], av[i][e]);
+      put(ov, a.pv, v0 + 16 * i + 4 * g4, dv, o);
+    }
+  }
+  // ---- dg: pairs inside the chunk, with one token before or behind it, with both
+  if (!a.dg) return;
+  xr = sum_groups(xr);
+  yj = sum_groups(yj);
+  if (g4 == 0) {
+    t.row[r] = xr;
+    t.far[r] = yj;
+  }
+  carry = wave_sum(carry);
+  if (lane == 0) t.part[w] = carry;
+  __syncthreads();
+  if (w == 0) {
+    const int back = 63 - lane;  // lane l holds row 63 - l: suffix sums as prefix sums
+    float x = wave_prefix_sum(t.row[back]);
+    float y = wave_prefix_sum(t.far[lane]);
+    y = __shfl_up(y, 1);
+    x = __shfl(x, back);
+    const float both = __builtin_amdgcn_exp2f((float)Gend) * (((t.part[0] + t.part[1]) + t.part[2]) + t.part[3]);
+    const float in = ((t.col[0][lane] + t.col[1][lane]) + t.col[2][lane]) + t.col[3][lane];
+    const float dg = in + x + (lane > 0 ? y : 0.f) + both;
+    if (lane < m) {
+      const long to = (tok + lane) * a.H + h;
+      if (a.g_f32) static_cast<float*>(a.dg)[to] = dg;
+      else store_elem(static_cast<bf16_t*>(a.dg) + to, dg);
+    }
+  }
+}
+
+// Gradients of shared heads: the sum over the state heads that share one, in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void k_decay_shared(const float* __restrict__ p, T* __restrict__ out, long n, int heads,
+                                                      int per, int d) {
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
+    const long th = i / d;
+    const float* from = p + (th / heads * heads + th % heads) * per * d + i % d;
+    float s = 0.f;
+    for (int k = 0; k < per; ++k) s += from[(long)k * d];
+    store_elem(out + i, s);
+  }
+}
+
+// ---- one token -----------------------------------------------------------------------
+// Bound by the state, read and written once.  A workgroup takes COLS groups of C value
+// columns of one row and head; thread (i, c) the key rows i, i + 256 / COLS, ...
+template <typename T, int C, int COLS>
+__global__ __launch_bounds__(256) void k_decay_step(DecayArgs a) {
+  constexpr int RG = 256 / COLS;
+  __shared__ float ks[256], qs[256], red[RG][COLS * C];
+  const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, c = tid % COLS, rg = tid / COLS;
+  const int col = (blockIdx.z * COLS + c) * C;
+  const long slot = a.slots ? a.slots[b] : b;
+  T* o = static_cast<T*>(a.o) + ((long)b * a.H + h) * a.dv;
+  if (slot < 0 || slot >= a.num_slots) {  // padding
+    if (rg == 0)
+      for (int i = 0; i < C; ++i)
+        if (col + i < a.dv) store_elem(o + col + i, 0.f);
+    return;
+  }
+  const T* k = static_cast<const T*>(a.k) + b * a.k_row + (long)(h / (a.H / a.Hk)) * a.dk;
+  const T* q = static_cast<const T*>(a.q) + b * a.q_row + (long)(h / (a.H / a.Hq)) * a.dk;
+  const T* v = static_cast<const T*>(a.v) + b * a.v_row + (long)(h / (a.H / a.Hv)) * a.dv;
+  float g = gate_of(a, b, h);
+  g = g < -128.f ? -128.f : g;
+  const float alpha = __builtin_amdgcn_exp2f(LOG2E * g);
+  ks[tid] = tid < a.dk ? to_f(k[tid]) : 0.f;
+  qs[tid] = tid < a.dk ? to_f(q[tid]) : 0.f;
+  float vv[C], acc[C];
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    vv[i] = col + i < a.dv ? to_f(v[col + i]) : 0.f;
+    acc[i] = 0.f;
+  }
+  __syncthreads();
+  float* S = a.state + (slot * a.H + h) * (long)a.dk * a.dv + col;
+  if (col < a.dv) {
+#pragma unroll 8
+    for (int r = rg; r < a.dk; r += RG) {
+      float* p = S + (long)r * a.dv;
+      float x[C];
+      if constexpr (C == 4) {
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        const f32x4 s = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+        f32x4 y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = x[i] = fmaf(alpha, s[i], ks[r] * vv[i]);
+        __builtin_nontemporal_store(y, reinterpret_cast<f32x4*>(p));
+      } else {
+        x[0] = fmaf(alpha, *p, ks[r] * vv[0]);
+        *p = x[0];
+      }
+#pragma unroll
+      for (int i = 0; i < C; ++i) acc[i] = fmaf(qs[r], x[i], acc[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < C; ++i) red[rg][c * C + i] = acc[i];
+  __syncthreads();
+  const int out = blockIdx.z * COLS * C + tid;
+  if (tid < COLS * C && out < a.dv) {
+    float s = 0.f;
+    for (int i = 0; i < RG; ++i) s += red[i][tid];
+    store_elem(o + out, a.scale * s);
+  }
+}
+
+// ---- launches --------------------------------------------------------------------------
+template <typename T>
+static bool pieces8(const void* p, long row, int d) {
+  return d % 8 == 0 && (uintptr_t)p % 16 == 0 && row % (16 / (long)sizeof(T)) == 0;
+}
+
+template <typename T, bool REV, bool LOCAL, bool VEC>
+static hipError_t run_scan(const DecayArgs& a) {
+  const long units = decay_slots(a, a.seglen) * a.H, ns = decay_splits(a.dv);
+  if (units == 0) return hipSuccess;
+  const long grid = (units + 7) / 8 * 8 * ns;
+  if (grid > INT32_MAX / 256) return hipErrorInvalidValue;
+  switch (decay_dkp(a.dk)) {
+    case 64: k_decay_scan<T, 64, REV, LOCAL, VEC><<<(unsigned)grid, 256, 0, a.stream>>>(a, (int)units); break;
+    case 128: k_decay_scan<T, 128, REV, LOCAL, VEC><<<(unsigned)grid, 256, 0, a.stream>>>(a, (int)units); break;
+    default: k_decay_scan<T, 256, REV, LOCAL, VEC><<<(unsigned)grid, 256, 0, a.stream>>>(a, (int)units); break;
+  }
+  return hipGetLastError();
+}
+template <typename T, bool REV, bool VEC>
+static hipError_t run_scans(const DecayArgs& a) {
+  if (a.segS) {
+    const hipError_t e = run_scan<T, REV, true, VEC>(a);
+    if (e != hipSuccess) return e;
+  }
+  return run_scan<T, REV, false, VEC>(a);
+}
+
+template <typename T>
+static hipError_t run_fwd(const DecayArgs& a) {
+  const bool vec = pieces8<T>(a.q, a.q_row, a.dk) && pieces8<T>(a.k, a.k_row, a.dk) && pieces8<T>(a.v, a.v_row, a.dv) &&
+                   pieces8<T>(a.o, (long)a.H * a.dv, a.dv);
+  return vec ? run_scans<T, false, true>(a) : run_scans<T, false, false>(a);
+}
+hipError_t launch_decay_fwd(const DecayArgs& a) { return a.bf16 ? run_fwd<bf16_t>(a) : run_fwd<float>(a); }
+
+template <typename T>
+static hipError_t run_shared(const DecayArgs& a, const float* p, void* out, int heads, int d) {
+  const long n = (long)a.Ttot * heads * d;
+  const long grid = (n + 255) / 256;
+  k_decay_shared<T><<<(unsigned)(grid < 8192 ? grid : 8192), 256, 0, a.stream>>>(p, static_cast<T*>(out), n, heads,
+                                                                               a.H / heads, d);
+  return hipGetLastError();
+}
+template <typename T>
+static hipError_t run_bwd(const DecayArgs& a) {
+  const bool vec = pieces8<T>(a.q, a.q_row, a.dk) && pieces8<T>(a.k, a.k_row, a.dk) && pieces8<T>(a.v, a.v_row, a.dv) &&
+                   pieces8<T>(a.dO, (long)a.H * a.dv, a.dv) && pieces8<T>(a.dq, 0, a.dk) &&
+                   pieces8<T>(a.dk_, 0, a.dk) && pieces8<T>(a.dv_, 0, a.dv);
+  hipError_t e = vec ? run_scans<T, true, true>(a) : run_scans<T, true, false>(a);
+  if (e != hipSuccess || a.Ttot == 0) return e;
+  const long grid = decay_slots(a, DC_CH) * a.H;
+  if (grid > INT32_MAX / 256) return hipErrorInvalidValue;
+  if (vec) k_decay_grad<T, true><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  else k_decay_grad<T, false><<<(unsigned)grid, 256, 0, a.stream>>>(a);
+  e = hipGetLastError();
+  if (e == hipSuccess && a.pq) e = run_shared<T>(a, a.pq, a.dq, a.Hq, a.dk);
+  if (e == hipSuccess && a.pk) e = run_shared<T>(a, a.pk, a.dk_, a.Hk, a.dk);
+  if (e == hipSuccess && a.pv) e = run_shared<T>(a, a.pv, a.dv_, a.Hv, a.dv);
+  return e;
+}
+hipError_t launch_decay_bwd(const DecayArgs& a) { return a.bf16 ? run_bwd<bf16_t>(a) : run_bwd<float>(a); }
+
+template <typename T>
+static hipError_t run_step(const DecayArgs& a) {
+  if (a.S == 0) return hipSuccess;
+  const bool vec = a.dv % 4 == 0 && (uintptr_t)a.state % 16 == 0;
+  auto grid = [&](int cols) { return dim3(a.S, a.H, (a.dv + cols - 1) / cols); };
+  // few states: slices of 32 columns give more workgroups, so more CUs stream the states
+  if (!vec) k_decay_step<T, 1, 32><<<grid(32), 256, 0, a.stream>>>(a);
+  else if ((long)a.S * a.H * ((a.dv + 127) / 128) < 1024) k_decay_step<T, 4, 8><<<grid(32), 256, 0, a.stream>>>(a);
+  else k_decay_step<T, 4, 32><<<grid(128), 256, 0, a.stream>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_decay_step(const DecayArgs& a) { return a.bf16 ? run_step<bf16_t>(a) : run_step<float>(a); }
+
+}  // namespace comba
