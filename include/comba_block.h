@@ -1,6 +1,7 @@
 /*
  * comba_block.h -- a recurrent model's block beside comba.h's mixer: linear
- * attention with a decay for each head.  For training (forward
+ * attention with a decay for each head, and the norms after and before a block
+ * fused with its gate, residual scale and residual stream.  For training (forward
  * and backward), prompts (fixed rows or packed sequences, states that enter and
  * leave) and single tokens (states in slots, in place).
  *
@@ -76,6 +77,45 @@ comba_status comba_decay_bwd(const comba_decay_shape *shape, const void *q, cons
 comba_status comba_decay_step(const comba_decay_shape *shape, const void *q, const void *k,
                               const void *v, const void *g, float *state, const int32_t *slots,
                               int32_t num_slots, void *o, void *stream);
+
+/* ---- norms after and before a block, gate, residual scale, stream --------- */
+typedef struct {
+  int64_t rows;               /* tokens                                                   */
+  int32_t C;                  /* channels                                                 */
+  comba_dtype dtype;          /* of y, z, n and their gradients                           */
+  comba_dtype x_dtype;        /* of the stream x, r and their gradients: dtype, or fp32   */
+  comba_activation activation; /* of the gate                                             */
+  float eps;                  /* >= 0, added to the mean squares                          */
+  int64_t y_row, z_row, x_row; /* elements between rows (0: C)                            */
+} comba_block_norm_shape;
+
+/*
+ * A block's output y joins the residual stream x, and the next block's input n
+ * leaves it.  Per token, rms(u) = sqrt(mean(u^2) + eps) over its C channels:
+ *     p = y / rms(y) * post_weight   (p = y without post_weight),
+ *     t = p act(z)                   (t = p without the gate z),
+ *     r = x + scale t                (without x: r = scale t; without scale: 1),
+ *     n = r / rms(r) * weight        (not formed when weight is NULL).
+ *   y, z [rows,C]; x, r [rows,C]; n [rows,C]; post_weight, scale, weight [C] fp32 or
+ *   NULL.  n is formed from r before its rounding.
+ */
+comba_status comba_block_norm_fwd(const comba_block_norm_shape *shape, const void *y,
+                                  const void *x, const void *z, const float *post_weight,
+                                  const float *scale, const float *weight, void *r, void *n,
+                                  void *stream);
+/*
+ * From dr [rows,C] (x_dtype) and dn [rows,C] (either may be NULL: zeros): dy, dz
+ * (with z), dx (with x; NULL: not wanted), and dpost_weight, dscale, dweight [C] fp32
+ * where their parameter is given (each may be NULL).  Recomputes p, r and both
+ * norms; sums in a fixed order.
+ */
+size_t comba_block_norm_workspace_bytes(const comba_block_norm_shape *shape);
+comba_status comba_block_norm_bwd(const comba_block_norm_shape *shape, const void *y,
+                                  const void *x, const void *z, const float *post_weight,
+                                  const float *scale, const float *weight, const void *dr,
+                                  const void *dn, void *dy, void *dx, void *dz,
+                                  float *dpost_weight, float *dscale, float *dweight, void *ws,
+                                  size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

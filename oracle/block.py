@@ -92,8 +92,10 @@ def _rms(x, eps):
     return 1.0 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
 
 
-def _back(d, xh, rstd):
-    """Through xh = x rstd."""
+def _back(d, xh, rstd, terms=False):
+    """Through xh = x rstd (``terms``: the sum of its terms' absolute values)."""
+    if terms:
+        return rstd * (np.abs(d) + np.abs(xh) * np.abs(d * xh).mean(-1, keepdims=True))
     return rstd * (d - xh * (d * xh).mean(-1, keepdims=True))
 
 
@@ -107,7 +109,9 @@ def block_fwd(y, x, z, w1, sc, w2, activation="silu", eps=1e-6):
     return r, None if w2 is None else r * _rms(r, eps) * w2
 
 
-def block_bwd(y, x, z, w1, sc, w2, dr, dn, activation="silu", eps=1e-6):
+def block_bwd(y, x, z, w1, sc, w2, dr, dn, activation="silu", eps=1e-6, terms=False):
+    """``terms``: instead of the gradients, the sums of the absolute values of what is added and
+    subtracted for them (a norm of one channel leaves 1e-6 of its gradient's terms)."""
     y, x, z, w1, sc, w2, dr, dn = _f8(y, x, z, w1, sc, w2, dr, dn)
     r1 = None if w1 is None else _rms(y, eps)
     yh = y if w1 is None else y * r1
@@ -117,12 +121,16 @@ def block_bwd(y, x, z, w1, sc, w2, dr, dn, activation="silu", eps=1e-6):
     r = t if sc is None else sc * t
     r = r if x is None else x + r
     d = np.zeros_like(y) if dr is None else dr.copy()
+    if terms:
+        p, t, r, yh, gate, d = (np.abs(v) for v in (p, t, r, yh, gate, d))
+        slope = None if z is None else np.abs(slope)
+        w1, sc, w2, dn = (None if v is None else np.abs(v) for v in (w1, sc, w2, dn))
     out = {}
     if w2 is not None:
         r2 = _rms(r, eps)
         dn = np.zeros_like(y) if dn is None else dn
         out["dweight"] = (dn * r * r2).sum(0)
-        d = d + _back(dn * w2, r * r2, r2)
+        d = d + _back(dn * w2, r * r2, r2, terms)
     if x is not None:
         out["dx"] = d
     if sc is not None:
@@ -133,6 +141,6 @@ def block_bwd(y, x, z, w1, sc, w2, dr, dn, activation="silu", eps=1e-6):
         d = d * gate
     if w1 is not None:
         out["dpost_weight"] = (d * yh).sum(0)
-        d = _back(d * w1, yh, r1)
+        d = _back(d * w1, yh, r1, terms)
     out["dy"] = d
     return out

@@ -1,9 +1,11 @@
 """Operators of a recurrent model's block (include/comba_block.h): linear attention
-with a decay for each head.
+with a decay for each head, and the norms after and before a block fused with its
+gate, residual scale and residual stream.
 
     o, ht = comba_decay_fwd(q, k, v, g, h0)             # prompts; comba_decay_step: one token
+    r, n = comba_block_norm_fwd(y, x, weight, post_weight=w1, z=z, scale=s)
 
-and, differentiable (torch.autograd), comba_decay.  Types, slices, packed sequences,
+and, differentiable (torch.autograd), comba_decay and comba_block_norm.  Types, slices, packed sequences,
 streams and workspaces are those of the layer's operators (``layer.py``).
 """
 from __future__ import annotations
@@ -12,11 +14,12 @@ import ctypes
 import struct
 
 from . import COMBA_BF16, COMBA_F32, CombaError, _kept_offsets, _ptr, load_library
-from .layer import (_SCAN_ROW, _code, _dense, _host_ptr, _like, _memory, _on, _row, _run, _seqs,
+from .layer import (_NORM_ACT, _SCAN_ROW, _activation, _code, _dense, _host_ptr, _like, _memory, _on, _row, _run, _seqs,
                     _slots, _workspace)
 
 __all__ = ["comba_decay_fwd", "comba_decay_fwd_save", "comba_decay_bwd", "comba_decay_step",
-           "comba_decay", "CombaDecayShape"]
+           "comba_decay", "comba_block_norm_fwd", "comba_block_norm_bwd", "comba_block_norm",
+           "CombaDecayShape", "CombaBlockNormShape"]
 
 _I32, _I64, _P = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
 
@@ -29,7 +32,15 @@ class CombaDecayShape(ctypes.Structure):
                 ("k_row", _I64), ("v_row", _I64), ("g_row", _I64)]
 
 
+class CombaBlockNormShape(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("C", _I32), ("dtype", ctypes.c_int), ("x_dtype", ctypes.c_int),
+                ("activation", ctypes.c_int), ("eps", ctypes.c_float), ("y_row", _I64),
+                ("z_row", _I64), ("x_row", _I64)]
+
+
 _DECAY = struct.Struct("@iiiiiiiiiPPiiifqqqq")
+_NORM = struct.Struct("@qiiiifqqq")
+assert _NORM.size == ctypes.sizeof(CombaBlockNormShape)
 assert _DECAY.size == ctypes.sizeof(CombaDecayShape)
 
 
@@ -39,11 +50,13 @@ def bind(lib):
     for name, args in (("comba_decay_fwd", [P] * 9 + [Z, P]),
                        ("comba_decay_fwd_save", [P] * 9 + [Z, P]),
                        ("comba_decay_bwd", [P] * 14 + [Z, P, Z, P]),
-                       ("comba_decay_step", [P] * 7 + [_I32, P, P])):
+                       ("comba_decay_step", [P] * 7 + [_I32, P, P]),
+                       ("comba_block_norm_fwd", [P] * 10),
+                       ("comba_block_norm_bwd", [P] * 16 + [Z, P])):
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, I
     for name in ("comba_decay_fwd_workspace_bytes", "comba_decay_save_bytes",
-                 "comba_decay_bwd_workspace_bytes"):
+                 "comba_decay_bwd_workspace_bytes", "comba_block_norm_workspace_bytes"):
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = [P], Z
 
@@ -179,6 +192,70 @@ def comba_decay_step(q, k, v, g, state, *, slots=None, scale=None, stream=None):
     return o
 
 
+# ---- norms after and before a block ---------------------------------------------------
+def _norm_shape(y, x, weight, post_weight, z, scale, activation, eps, stream_dtype):
+    import torch
+
+    code, dev, dt, f32, shape = _code(y, "y"), y.get_device(), y.dtype, torch.float32, y.shape
+    lead = len(shape) - 1
+    if lead < 0 or shape[-1] < 1:
+        raise CombaError("comba: y must be [..,C]")
+    if stream_dtype is not dt and stream_dtype is not f32:
+        raise CombaError("comba: the stream must be float32 or of y's dtype")
+    C = shape[-1]
+    shp = _NORM.pack(y.numel() // C, C, code, COMBA_F32 if stream_dtype is f32 else COMBA_BF16,
+                     _activation(activation, _NORM_ACT), eps,
+                     0 if y.is_contiguous() else _row("y", y, lead, shape, dt, dev),
+                     _row("z", z, lead, shape, dt, dev),
+                     _row("x", x, lead, shape, stream_dtype, dev))
+    ptrs = (y.data_ptr(), _ptr(x), _ptr(z),
+            _dense("post_weight", post_weight, (C,), f32, dev),
+            _dense("scale", scale, (C,), f32, dev), _dense("weight", weight, (C,), f32, dev))
+    return shp, ptrs
+
+
+def comba_block_norm_fwd(y, x=None, weight=None, *, post_weight=None, z=None, scale=None,
+                         activation="silu", eps=1e-6, stream_dtype=None, stream=None):
+    """A block's output y [..,C] joins the residual stream x, and the next block's input leaves
+    it.  Returns (r, n): with rms(u) = sqrt(mean(u^2) + eps) over the channels,
+
+    p = y / rms(y) post_weight,  r = x + scale p act(z),  n = r / rms(r) weight.
+
+    y, x and z may be column slices; z and n have y's dtype, x and r are float32 or have it too
+    (without x: ``stream_dtype``, by default y's).  post_weight, scale and weight are [C] float32;
+    each of them, x and z may be None: no norm after the block, a scale of one, no norm before
+    the next (n is None), an empty stream, no gate."""
+    st = stream_dtype or (y.dtype if x is None else x.dtype)
+    shp, ptrs = _norm_shape(y, x, weight, post_weight, z, scale, activation, eps, st)
+    r = _like(y, st)
+    n = None if weight is None else _like(y)
+    _run(load_library().comba_block_norm_fwd(shp, *ptrs, r.data_ptr(), _ptr(n),
+                                             _on(stream, y.get_device(), r, n)))
+    return r, n
+
+
+def comba_block_norm_bwd(y, x, weight, dr, dn, *, post_weight=None, z=None, scale=None,
+                         activation="silu", eps=1e-6, need_dx=True, stream_dtype=None,
+                         workspace=None, stream=None):
+    """Backward of comba_block_norm_fwd from dr (the stream's dtype) and dn (y's), either of
+    which may be None.  Returns dict dy, dx, dz, dpost_weight, dscale, dweight (None where the
+    input is absent)."""
+    lib = load_library()
+    st = stream_dtype or (dr.dtype if dr is not None else y.dtype if x is None else x.dtype)
+    shp, ptrs = _norm_shape(y, x, weight, post_weight, z, scale, activation, eps, st)
+    dev = y.get_device()
+    grads = (_dense("dr", dr, y.shape, st, dev), _dense("dn", dn, y.shape, y.dtype, dev))
+    out = {"dy": _like(y), "dx": _like(y, st) if need_dx and x is not None else None,
+           "dz": None if z is None else _like(y),
+           "dpost_weight": None if post_weight is None else _like(post_weight),
+           "dscale": None if scale is None else _like(scale),
+           "dweight": None if weight is None else _like(weight)}
+    ws = _workspace(lib.comba_block_norm_workspace_bytes, shp, workspace, y.device)
+    _run(lib.comba_block_norm_bwd(shp, *ptrs, *grads, *(_ptr(t) for t in out.values()),
+                                  ws.data_ptr(), ws.numel(), _on(stream, dev, ws, *out.values())))
+    return out
+
+
 # ---- torch.autograd ---------------------------------------------------------------
 _FNS = {}
 
@@ -218,7 +295,30 @@ def _functions():
             names = ("dq", "dk", "dv", "dg", "dh0")
             return needed(ctx, tuple(gr[n] for n in names) + (None, None, None))
 
-    _FNS.update(decay=Decay)
+    class BlockNorm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, y, x, weight, post_weight, z, scale, kw):
+            ctx.set_materialize_grads(False)
+            ctx.save_for_backward(y, x, weight, post_weight, z, scale)
+            ctx.kw = kw
+            r, n = comba_block_norm_fwd(y, x, weight, post_weight=post_weight, z=z, scale=scale,
+                                        **kw)
+            ctx.stream_dtype = r.dtype
+            return r, n
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dr, dn):
+            y, x, weight, post_weight, z, scale = ctx.saved_tensors
+            kw = dict(ctx.kw, stream_dtype=ctx.stream_dtype)
+            gr = comba_block_norm_bwd(y, x, weight, None if dr is None else dr.contiguous(),
+                                      None if dn is None else dn.contiguous(),
+                                      post_weight=post_weight, z=z, scale=scale,
+                                      need_dx=ctx.needs_input_grad[1], **kw)
+            names = ("dy", "dx", "dweight", "dpost_weight", "dz", "dscale")
+            return needed(ctx, tuple(gr[n] for n in names) + (None,))
+
+    _FNS.update(decay=Decay, norm=BlockNorm)
     return _FNS
 
 
@@ -229,3 +329,10 @@ def comba_decay(q, k, v, g, h0=None, *, scale=None, cu_seqlens=None, cu_seqlens_
 
     kw = dict(scale=scale, cu_seqlens_host=_kept_offsets(cu_seqlens_host))
     return _functions()["decay"].apply(q, k, v, g, h0, cu_seqlens, kw, torch.is_grad_enabled())
+
+
+def comba_block_norm(y, x=None, weight=None, *, post_weight=None, z=None, scale=None,
+                     activation="silu", eps=1e-6, stream_dtype=None):
+    """Differentiable comba_block_norm_fwd: (r, n); gradients flow to every tensor."""
+    kw = dict(activation=activation, eps=eps, stream_dtype=stream_dtype)
+    return _functions()["norm"].apply(y, x, weight, post_weight, z, scale, kw)

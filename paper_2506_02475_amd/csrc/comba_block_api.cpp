@@ -184,6 +184,46 @@ comba_status decay_fwd(Use use, const comba_decay_shape* shape, const void* q, c
   return done(comba::launch_decay_fwd(a));
 }
 
+// ---- norms after and before a block ------------------------------------------------
+comba_status block_norm_args(const comba_block_norm_shape* s, comba::BlockNormArgs* a) {
+  if (!s) return COMBA_ERR_NULL;
+  if (!dtype_ok(s->dtype) || !dtype_ok(s->x_dtype)) return COMBA_ERR_DTYPE;
+  if (s->x_dtype != s->dtype && s->x_dtype != COMBA_F32) return COMBA_ERR_DTYPE;
+  if (s->activation != COMBA_ACT_NONE && s->activation != COMBA_ACT_SILU && s->activation != COMBA_ACT_SIGMOID)
+    return COMBA_ERR_SHAPE;
+  if (s->rows < 0 || s->rows > INT32_MAX || s->C <= 0 || s->C > kMaxRow || !(s->eps >= 0.f)) return COMBA_ERR_SHAPE;
+  *a = comba::BlockNormArgs{};
+  a->bf16 = s->dtype == COMBA_BF16;
+  a->x_bf16 = s->x_dtype == COMBA_BF16;
+  a->act = s->activation;
+  a->rows = s->rows;
+  a->C = s->C;
+  a->eps = s->eps;
+  return row_stride(s->y_row, s->C, s->rows, false, &a->y_row) && row_stride(s->z_row, s->C, s->rows, false, &a->z_row) &&
+                 row_stride(s->x_row, s->C, s->rows, false, &a->x_row)
+             ? COMBA_OK
+             : COMBA_ERR_SHAPE;
+}
+
+comba_status block_norm_inputs(comba::BlockNormArgs* a, const comba_block_norm_shape* s, const void* y, const void* x,
+                               const void* z, const float* w1, const float* sc, const float* w2) {
+  if (a->rows > 0 && !y) return COMBA_ERR_NULL;
+  if (!aligned(y, elem(s->dtype)) || !aligned(z, elem(s->dtype)) || !aligned(x, elem(s->x_dtype)) || !aligned(w1, 4) ||
+      !aligned(sc, 4) || !aligned(w2, 4))
+    return COMBA_ERR_ALIGN;
+  a->y = y;
+  a->x = x;
+  a->z = z;
+  a->w1 = w1;
+  a->sc = sc;
+  a->w2 = w2;
+  return COMBA_OK;
+}
+
+size_t block_norm_ws_bytes(const comba::BlockNormArgs& a) {
+  return round_up((size_t)comba::block_norm_bwd_blocks(a) * 3 * a.C * sizeof(float)) + kAlign;
+}
+
 }  // namespace
 
 extern "C" {
@@ -258,6 +298,55 @@ comba_status comba_decay_step(const comba_decay_shape* shape, const void* q, con
   a.o = o;
   a.stream = static_cast<hipStream_t>(stream);
   return done(comba::launch_decay_step(a));
+}
+
+comba_status comba_block_norm_fwd(const comba_block_norm_shape* shape, const void* y, const void* x, const void* z,
+                                  const float* post_weight, const float* scale, const float* weight, void* r, void* n,
+                                  void* stream) {
+  comba::BlockNormArgs a;
+  comba_status st = block_norm_args(shape, &a);
+  if (st != COMBA_OK) return st;
+  st = block_norm_inputs(&a, shape, y, x, z, post_weight, scale, weight);
+  if (st != COMBA_OK) return st;
+  if (a.rows > 0 && (!r || (weight && !n))) return COMBA_ERR_NULL;
+  if (!aligned(r, elem(shape->x_dtype)) || !aligned(n, elem(shape->dtype))) return COMBA_ERR_ALIGN;
+  a.r = r;
+  a.n = n;
+  a.stream = static_cast<hipStream_t>(stream);
+  return done(comba::launch_block_norm_fwd(a));
+}
+
+size_t comba_block_norm_workspace_bytes(const comba_block_norm_shape* shape) {
+  comba::BlockNormArgs a;
+  return block_norm_args(shape, &a) == COMBA_OK ? block_norm_ws_bytes(a) : 0;
+}
+
+comba_status comba_block_norm_bwd(const comba_block_norm_shape* shape, const void* y, const void* x, const void* z,
+                                  const float* post_weight, const float* scale, const float* weight, const void* dr,
+                                  const void* dn, void* dy, void* dx, void* dz, float* dpost_weight, float* dscale,
+                                  float* dweight, void* ws, size_t ws_bytes, void* stream) {
+  comba::BlockNormArgs a;
+  comba_status st = block_norm_args(shape, &a);
+  if (st != COMBA_OK) return st;
+  st = block_norm_inputs(&a, shape, y, x, z, post_weight, scale, weight);
+  if (st != COMBA_OK) return st;
+  if (!ws || (a.rows > 0 && (!dy || (z && !dz)))) return COMBA_ERR_NULL;
+  const size_t e = elem(shape->dtype), ex = elem(shape->x_dtype);
+  if (!aligned(dr, ex) || !aligned(dn, e) || !aligned(dy, e) || !aligned(dx, ex) || !aligned(dz, e) ||
+      !aligned(dpost_weight, 4) || !aligned(dscale, 4) || !aligned(dweight, 4) || !aligned(ws, kAlign))
+    return COMBA_ERR_ALIGN;
+  if (ws_bytes < block_norm_ws_bytes(a)) return COMBA_ERR_WORKSPACE;
+  a.dr = dr;
+  a.dn = weight ? dn : nullptr;
+  a.dy = dy;
+  a.dx = x ? dx : nullptr;
+  a.dz = dz;
+  a.dw1 = post_weight ? dpost_weight : nullptr;
+  a.dsc = scale ? dscale : nullptr;
+  a.dw2 = weight ? dweight : nullptr;
+  a.part = static_cast<float*>(ws);
+  a.stream = static_cast<hipStream_t>(stream);
+  return done(comba::launch_block_norm_bwd(a));
 }
 
 }  // extern "C"

@@ -63,4 +63,26 @@ hipError_t launch_decay_fwd(const DecayArgs& a);
 hipError_t launch_decay_bwd(const DecayArgs& a);
 hipError_t launch_decay_step(const DecayArgs& a);
 
+struct BlockNormArgs {
+  bool bf16, x_bf16;
+  comba_activation act;
+  long rows;
+  int C;
+  float eps;
+  long y_row, z_row, x_row;
+  const void *y, *x, *z;
+  const float *w1, *sc, *w2;
+  void *r, *n;
+  const void *dr, *dn;
+  void *dy, *dx, *dz;
+  float *dw1, *dsc, *dw2;
+  float* part;  // [blocks][3][C] partial sums of dw1, dsc, dw2
+  int blocks;
+  hipStream_t stream;
+};
+// Workgroups of the backward over the rows, which size its workspace.
+int block_norm_bwd_blocks(const BlockNormArgs& a);
+hipError_t launch_block_norm_fwd(const BlockNormArgs& a);
+hipError_t launch_block_norm_bwd(const BlockNormArgs& a);
+
 }  // namespace comba

@@ -28,37 +28,6 @@ namespace comba {
 constexpr int GN_C = 4;        // channels of an aligned piece
 constexpr int GN_WIDE = 1024;  // threads where a group's channels do not fit registers
 
-// Sum over the lanes of a team (team: a power of two up to 64), the same in every lane.
-__device__ __forceinline__ float team_sum(float x, int team) {
-  if (team > 1) x = xsum<0>(x);
-  if (team > 2) x = xsum<1>(x);
-  if (team > 4) x = xsum<2>(x);
-  if (team > 8) x = xsum<3>(x);
-  if (team > 16) x = xsum<4>(x);
-  if (team > 32) x = xsum<5>(x);
-  return x;
-}
-
-// act(t) and, for the backward, its slope.
-__device__ __forceinline__ float act_of(comba_activation act, float t) {
-  if (act == COMBA_ACT_NONE) return t;
-  const float s = sigmoid_acc(t);
-  return act == COMBA_ACT_SILU ? t * s : s;
-}
-__device__ __forceinline__ float act_slope(comba_activation act, float t, float& y) {
-  if (act == COMBA_ACT_NONE) {
-    y = t;
-    return 1.f;
-  }
-  const float s = sigmoid_acc(t);
-  if (act == COMBA_ACT_SILU) {
-    y = t * s;
-    return s * fmaf(t, 1.f - s, 1.f);
-  }
-  y = s;
-  return s * (1.f - s);
-}
-
 // Sum over a workgroup of TH threads, the same in every thread.
 template <int TH>
 __device__ __forceinline__ float block_sum(float x, float* lds) {
