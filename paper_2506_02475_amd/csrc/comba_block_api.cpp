@@ -124,7 +124,7 @@ DecayLayout decay_layout(const comba::DecayArgs& a, bool segments, Use use) {
     off += round_up(bytes);
     return at;
   };
-  if (use != Use::kFwd) L.kept = take(kept_bytes(a));
+  L.kept = take(kept_bytes(a));
   const size_t slots = segments ? (size_t)comba::decay_slots(a, a.seglen) * a.H : 0;
   L.segS = take(slots * comba::decay_end_floats(a) * sizeof(float));
   L.segG = take(slots * sizeof(float));
@@ -178,7 +178,7 @@ comba_status decay_fwd(Use use, const comba_decay_shape* shape, const void* q, c
   char* base = static_cast<char*>(ws);
   a.o = o;
   a.ht = ht;
-  if (use == Use::kSave) a.kept = base + L.kept;
+  a.kept = base + L.kept;
   set_segments(&a, L, segments, base);
   a.stream = static_cast<hipStream_t>(stream);
   return done(comba::launch_decay_fwd(a));

@@ -184,19 +184,67 @@ __device__ __forceinline__ float gate_of(const DecayArgs& a, long tok, int h) {
   const long at = tok * a.g_row + h;
   return a.g_f32 ? static_cast<const float*>(a.g)[at] : bf2f(static_cast<const bf16_t*>(a.g)[at]);
 }
+// The same of n tokens from tok on, one a lane, zeros behind them.  As two halves from a
+// raw buffer (bf16: the lower one from behind it), so that no load stands under a branch
+// and what is in flight is first touched where it is used.  Per head: `head`.
+struct Gates {
+  uint32_t lo, hi;
+  int n;
+  __device__ __forceinline__ void load(const DecayArgs& a, long tok, int h, int count) {
+    n = count;
+    const unsigned e = a.g_f32 ? 4 : 2, off = (unsigned)lane_id() * (unsigned)a.g_row * e;
+    const char* p = static_cast<const char*>(a.g) + (tok * a.g_row + h) * e;
+    const auto rs = clip_rsrc(const_cast<char*>(p), count > 0 && !a.g_head ? (unsigned)((count - 1) * (int)a.g_row + 1) * e : 0u);
+    hi = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, off + (e - 2), 0, 0);
+    lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, a.g_f32 ? off : BUF_OOB, 0, 0);
+  }
+  __device__ __forceinline__ float get(float head) const {
+    const float x = __uint_as_float(hi << 16 | lo);
+    return lane_id() < n ? x + head : 0.f;  // (per head x is zero, else head is)
+  }
+};
+template <int CTRL, int ROWMASK = 0xF>
+__device__ __forceinline__ double dpp_add(double x) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  const i32x2 u = __builtin_bit_cast(i32x2, x);
+  const i32x2 y = {__builtin_amdgcn_update_dpp(0, u[0], CTRL, ROWMASK, 0xF, false),
+                   __builtin_amdgcn_update_dpp(0, u[1], CTRL, ROWMASK, 0xF, false)};
+  return x + __builtin_bit_cast(double, y);
+}
+__device__ __forceinline__ double read_lane(double x, int lane) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  const i32x2 u = __builtin_bit_cast(i32x2, x);
+  return __builtin_bit_cast(double, i32x2{__builtin_amdgcn_readlane(u[0], lane), __builtin_amdgcn_readlane(u[1], lane)});
+}
 __device__ __forceinline__ double gate_sum(float g) {
   g = g < -128.f ? -128.f : g;
   double x = (double)g * 1.4426950408889634074;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const double y = __shfl_up(x, d);
-    x += lane_id() >= d ? y : 0.0;
-  }
-  return x;
+  x = dpp_add<0x111>(x);  // as wave_prefix_sum
+  x = dpp_add<0x112>(x);
+  x = dpp_add<0x114>(x);
+  x = dpp_add<0x118>(x);
+  x = dpp_add<0x142, 0xA>(x);
+  return dpp_add<0x143, 0xC>(x);
 }
 // Pair weights from two floats a sum: a difference keeps the accuracy of the 64 bits.
 struct Sums {
   float hi[DC_CH], lo[DC_CH];
+  // 2^(G - G_j) of four j from j0 on
+  template <bool BOTH>
+  __device__ __forceinline__ floatx4 weights(float gh, float gl, int j0) const {
+    const floatx4 h = *reinterpret_cast<const floatx4*>(hi + j0);
+    floatx4 d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) d[e] = gh - h[e];
+    if constexpr (BOTH) {
+      const floatx4 l = *reinterpret_cast<const floatx4*>(lo + j0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) d[e] += gl - l[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) d[e] = __builtin_amdgcn_exp2f(d[e]);
+    return d;
+  }
 };
 
 // fp32 as the sum of three bf16: products with an exact bf16 operand keep 24 bits.
@@ -208,26 +256,29 @@ __device__ __forceinline__ void split3(float x, float y, uint32_t& hi, uint32_t&
 }
 
 // ---- the scans ---------------------------------------------------------------------
-// A workgroup walks the chunks of one segment of one sequence and head, and holds DC_BV
-// value columns of the state in fp32 accumulators (wave w: key rows w DK / 4 ..).
-// Forward: keys k, values v, weights e^{G_end - G_j}.  REV, for the states' gradients,
-// from the last chunk to the first: keys q, values do, weights scale e^{G_r}.
-// LOCAL: a segment's end from a zero state, for the segments behind it.
+// A workgroup walks the chunks of one segment of one sequence and head, holds DC_BV value
+// columns of the state in fp32 accumulators (wave w: key rows w DK / 4 ..), and keeps what
+// it holds before each chunk.  Forward: keys k, values v, weights e^{G_end - G_j}.  REV,
+// for the states' gradients, from the last chunk to the first: keys q, values do, weights
+// scale e^{G_r}.  LOCAL: a segment's end from a zero state, for the segments behind it.
 // The weights multiply the value columns, of which a workgroup has few, and there
 // fp32 becomes three bf16 against the keys as they are: the state's sums keep 24 bits.
+//
+// Bound by the latency of a chunk's chain (its decays, the weighted values into LDS, their
+// products), not by what it moves: so two tiles in LDS, the next chunk being staged while
+// one is multiplied, one barrier a chunk, and loads two chunks ahead of their staging.
 template <typename T, int DK>
-struct ScanTiles {
-  static constexpr int VLD = is_f32<T>::value ? 64 : 128;  // weighted values (bf16: three terms), values
-  T k[DC_CH * DK], v[DC_CH * VLD], s[DC_BV * DK];
-  Sums g;
+struct ScanTile {
+  static constexpr int VLD = is_f32<T>::value ? 64 : 128;  // weighted values (bf16: three terms)
+  T k[DC_CH * DK], v[DC_CH * VLD];
 };
 
 template <typename T, int DK, bool REV, bool LOCAL, bool VEC>
 __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
-  constexpr bool F32 = is_f32<T>::value, OUT = !REV && !LOCAL;
-  constexpr int VLD = ScanTiles<T, DK>::VLD, NT = F32 ? 1 : 3, VCOL = DC_BV * NT;
+  constexpr bool F32 = is_f32<T>::value;
+  constexpr int VLD = ScanTile<T, DK>::VLD, NT = F32 ? 1 : 3;
   constexpr int MT = DK / 64, KI = DK / 32;
-  __shared__ __align__(16) ScanTiles<T, DK> t;
+  __shared__ __align__(16) ScanTile<T, DK> tiles[2];
 
   // the splits of one head's state on one XCD (they read the same keys), heads dealt
   // over the XCDs
@@ -244,10 +295,33 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
   if (LOCAL && sq.piece == (REV ? 0 : segs - 1)) return;  // no segment comes after it
   const int w = wave_id_s(), lane = lane_id(), r16 = lane & 15, g4 = lane >> 4;
 
-  const int hx = REV ? h / (a.H / a.Hq) : h / (a.H / a.Hk), hq = h / (a.H / a.Hq), hv = REV ? h : h / (a.H / a.Hv);
+  const int hx = REV ? h / (a.H / a.Hq) : h / (a.H / a.Hk), hv = REV ? h : h / (a.H / a.Hv);
   const long xrow = REV ? a.q_row : a.k_row, yrow = REV ? (long)a.H * a.dv : a.v_row;
   const void *X = REV ? a.q : a.k, *Y = REV ? a.dO : a.v;
   const long tok0 = (long)sq.t0 + first;
+
+  // ---- a chunk's inputs
+  struct Inputs {
+    Piece<T, 8, VEC> k[KI], v;
+    Gates g;
+  } in0, in1;
+  const float ghead = a.g_head ? static_cast<const float*>(a.g)[h] : 0.f;
+  auto load = [&](Inputs& in, int it) {  // the it-th chunk of the walk
+    const int c = REV ? nc - 1 - it : it;
+    const int m = it < nc ? min(DC_CH, n - c * DC_CH) : 0;  // (behind the last one: nothing)
+    const long tok = tok0 + (long)c * DC_CH;
+    const auto rx = head_rows<T>(X, tok, xrow, (long)hx * a.dk, m, a.dk);
+    const auto ry = head_rows<T>(Y, tok, yrow, (long)hv * a.dv, m, a.dv);
+    in.g.load(a, tok, h, m);
+    load8(in.v, ry, threadIdx.x / 4, (unsigned)yrow * sizeof(T), j0 + threadIdx.x % 4 * 8, a.dv);
+#pragma unroll
+    for (int i = 0; i < KI; ++i) {
+      const int idx = threadIdx.x + i * 256;
+      load8(in.k[i], rx, idx / (DK / 8), (unsigned)xrow * sizeof(T), idx % (DK / 8) * 8, a.dk);
+    }
+  };
+  load(in0, 0);
+  load(in1, 1);
 
   // ---- the state that enters
   floatx4 S[MT][2];
@@ -264,185 +338,100 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
   auto end_at = [&](int sl) {
     return a.segS + ((long)sl * a.H + h) * ends + (((long)split * 4 + w) * 64 + lane) * (MT * 8);
   };
-  const float* in = REV ? a.dht : a.h0;
+  const float* entering = REV ? a.dht : a.h0;
   const long sbase = ((long)sq.seq * a.H + h) * a.dk * a.dv;
   {
+    const int before = LOCAL ? 0 : REV ? segs - 1 - sq.piece : sq.piece;  // segments it has behind it
+    auto nth = [&](int p) { return base + (REV ? sq.piece + 1 + p : sq.piece - 1 - p); };  // the nearest first
     double f = 0.;
-    if (!LOCAL) {
-      for (int p = 0; p < (REV ? segs - 1 - sq.piece : sq.piece); ++p)
-        f += a.segG[(long)(base + (REV ? sq.piece + 1 + p : p)) * a.H + h];
-    }
+    for (int p = 0; p < before; ++p) f += a.segG[(long)nth(p) * a.H + h];
     const float far = __builtin_amdgcn_exp2f((float)f);
     each([&](float, int r, int c) {
-      return !LOCAL && in && r < a.dk && c < a.dv ? far * in[sbase + (long)r * a.dv + c] : 0.f;
+      return !LOCAL && entering && r < a.dk && c < a.dv ? far * entering[sbase + (long)r * a.dv + c] : 0.f;
     });
-    if (!LOCAL && (REV ? sq.piece < segs - 1 : sq.piece > 0)) {
-      double between = 0.;
-      for (int p = 0; p < (REV ? segs - 1 - sq.piece : sq.piece); ++p) {  // the nearest first
-        const int sl = base + (REV ? sq.piece + 1 + p : sq.piece - 1 - p);
-        const float f2 = __builtin_amdgcn_exp2f((float)between);
-        const float4* e = reinterpret_cast<const float4*>(end_at(sl));
+    double between = 0.;
+    for (int p = 0; p < before; ++p) {
+      const int sl = nth(p);
+      const float f2 = __builtin_amdgcn_exp2f((float)between);
+      const float4* e = reinterpret_cast<const float4*>(end_at(sl));
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const float4 x = e[m * 2 + c];
-            S[m][c][0] = fmaf(f2, x.x, S[m][c][0]);
-            S[m][c][1] = fmaf(f2, x.y, S[m][c][1]);
-            S[m][c][2] = fmaf(f2, x.z, S[m][c][2]);
-            S[m][c][3] = fmaf(f2, x.w, S[m][c][3]);
-          }
-        between += a.segG[(long)sl * a.H + h];
-      }
+        for (int c = 0; c < 2; ++c) {
+          const float4 x = e[m * 2 + c];
+          S[m][c][0] = fmaf(f2, x.x, S[m][c][0]);
+          S[m][c][1] = fmaf(f2, x.y, S[m][c][1]);
+          S[m][c][2] = fmaf(f2, x.z, S[m][c][2]);
+          S[m][c][3] = fmaf(f2, x.w, S[m][c][3]);
+        }
+      between += a.segG[(long)sl * a.H + h];
     }
   }
 
-  // ---- a chunk's inputs: the next one's loads are in flight while one is worked on
-  Piece<T, 8, VEC> pk[KI], pv, pq[OUT ? KI : 1];
-  float pg = 0.f;
-  auto load = [&](int c) {
-    const long tok = tok0 + (long)c * DC_CH;
-    const int m = min(DC_CH, n - c * DC_CH);
-    const auto rx = head_rows<T>(X, tok, xrow, (long)hx * a.dk, m, a.dk);
-    const auto ry = head_rows<T>(Y, tok, yrow, (long)hv * a.dv, m, a.dv);
-#pragma unroll
-    for (int it = 0; it < KI; ++it) {
-      const int idx = threadIdx.x + it * 256;
-      load8(pk[it], rx, idx / (DK / 8), (unsigned)xrow * sizeof(T), idx % (DK / 8) * 8, a.dk);
-    }
-    load8(pv, ry, threadIdx.x / 4, (unsigned)yrow * sizeof(T), j0 + threadIdx.x % 4 * 8, a.dv);
-    if constexpr (OUT) {
-      const auto rq = head_rows<T>(a.q, tok, a.q_row, (long)hq * a.dk, m, a.dk);
-#pragma unroll
-      for (int s = 0; s < KI; ++s)
-        load8(pq[s], rq, 16 * w + r16, (unsigned)a.q_row * sizeof(T), 32 * s + 8 * g4, a.dk);
-    }
-    pg = lane < m ? gate_of(a, tok + lane, h) : 0.f;
-  };
-  if (nc > 0) load(REV ? nc - 1 : 0);
-  const int kslot = first_slot(a, sq, DC_CH) + first / DC_CH;
   double total = 0.;
-
-  for (int it = 0; it < nc; ++it) {
-    const int c = REV ? nc - 1 - it : it;
-    const int m = min(DC_CH, n - c * DC_CH);
-    // ---- staging
-    const double G = gate_sum(pg), Gend = __shfl(G, 63);
+  auto stage = [&](ScanTile<T, DK>& t, const Inputs& in) {  // returns the chunk's decay
+    const double G = gate_sum(in.g.get(ghead)), Gend = read_lane(G, 63);
     total += Gend;
-    {
 #pragma unroll
-      for (int i = 0; i < KI; ++i) {
-        const int idx = threadIdx.x + i * 256;
-        st_row8<DK>(t.k, idx / (DK / 8), idx % (DK / 8) * 8, pk[i]);
-      }
-      const float wt = REV ? a.scale * __builtin_amdgcn_exp2f((float)G) : __builtin_amdgcn_exp2f((float)(Gend - G));
-      const float f = __shfl(wt, 16 * w + lane / 4);
-      const int row = threadIdx.x / 4, col = threadIdx.x % 4 * 8;
-      if constexpr (F32) {
-        Piece<T, 8, VEC> x;
+    for (int i = 0; i < KI; ++i) {
+      const int idx = threadIdx.x + i * 256;
+      st_row8<DK>(t.k, idx / (DK / 8), idx % (DK / 8) * 8, in.k[i]);
+    }
+    const float wt = REV ? a.scale * __builtin_amdgcn_exp2f((float)G) : __builtin_amdgcn_exp2f((float)(Gend - G));
+    const float f = __shfl(wt, 16 * w + lane / 4);
+    const int row = threadIdx.x / 4, col = threadIdx.x % 4 * 8;
+    if constexpr (F32) {
+      Piece<T, 8, VEC> x;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x.r[e] = __float_as_uint(f * pv.get(e));
-        st_row8<VLD>(t.v, row, col, x);
-      } else {
-        Piece<T, 8, VEC> x[3];
+      for (int e = 0; e < 8; ++e) x.r[e] = __float_as_uint(f * in.v.get(e));
+      st_row8<VLD>(t.v, row, col, x);
+    } else {
+      Piece<T, 8, VEC> x[3];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          split3(f * pv.get(2 * e), f * pv.get(2 * e + 1), x[0].r[e], x[1].r[e], x[2].r[e]);
+      for (int e = 0; e < 4; ++e)
+        split3(f * in.v.get(2 * e), f * in.v.get(2 * e + 1), x[0].r[e], x[1].r[e], x[2].r[e]);
 #pragma unroll
-        for (int e = 0; e < 3; ++e) st_row8<VLD>(t.v, row, 32 * e + col, x[e]);
-      }
-      if constexpr (OUT) {
-        st_row8<VLD>(t.v, row, VCOL + col, pv);
-        if (w == 0) {
-          t.g.hi[lane] = (float)G;
-          t.g.lo[lane] = (float)(G - (double)(float)G);
+      for (int e = 0; e < 3; ++e) st_row8<VLD>(t.v, row, 32 * e + col, x[e]);
+    }
+    return __builtin_amdgcn_exp2f((float)Gend);
+  };
+  // The state before a chunk, [dv][dk]: a lane has four key rows of a column (two tiles:
+  // exchanged to eight in a row).
+  const int kslot = first_slot(a, sq, DC_CH) + first / DC_CH;
+  auto keep = [&](int it) {
+    const int c = REV ? nc - 1 - it : it;
+    T* to = static_cast<T*>(REV ? a.dkept : a.kept) + ((long)(kslot + c) * a.H + h) * a.dv * a.dk;
+#pragma unroll
+    for (int cc = 0; cc < 2; ++cc) {
+      const int col = j0 + 16 * cc + r16;
+      if (col >= a.dv) continue;
+      T* at = to + (long)col * a.dk;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const float x[4] = {S[m][cc][0], S[m][cc][1], S[m][cc][2], S[m][cc][3]};
+        const int left = a.dk - row0 - 16 * m;
+        if constexpr (VEC && !F32 && MT > 1) {
+          if (m & 1) continue;
+          const floatx4 &u = S[m][cc], &v = S[m + 1][cc];
+          const uint4 y = row8_from_pieces(make_uint2(bf16_pair(u[0], u[1]), bf16_pair(u[2], u[3])),
+                                           make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])));
+          const int r = w * (DK / 4) + 16 * m + row8_col();
+          if (r < a.dk) *reinterpret_cast<uint4*>(at + r) = y;
+        } else {
+          store_piece<T, 4, VEC>(at + row0 + 16 * m, x, left);
         }
       }
     }
-    if (!LOCAL && (OUT || a.dkept)) {
-#pragma unroll
-      for (int mm = 0; mm < MT; ++mm)
-#pragma unroll
-        for (int cc = 0; cc < 2; ++cc) st_row4<DK>(t.s, 16 * cc + r16, row0 + 16 * mm, S[mm][cc]);
-    }
-    Frag<T> fq[OUT ? KI : 1];
-    if constexpr (OUT) {
-#pragma unroll
-      for (int s = 0; s < KI; ++s) fq[s] = as_frag<T, VEC>(pq[s]);
-    }
-    __syncthreads();
-    if (it + 1 < nc) load(REV ? c - 1 : c + 1);
-
-    // ---- the state kept for the backward
-    if (T* keep = LOCAL ? nullptr : static_cast<T*>(REV ? a.dkept : a.kept)) {
-      keep += ((long)(kslot + c) * a.H + h) * a.dv * a.dk;
-      for (int idx = threadIdx.x; idx < DC_BV * DK / 8; idx += 256) {
-        const int row = idx / (DK / 8), col = idx % (DK / 8) * 8;
-        if (j0 + row < a.dv && col < a.dk) {
-          const T* from = t.s + sw16<DK>(row, col);
-          T* to = keep + (long)(j0 + row) * a.dk + col;
-          if constexpr (VEC) {
-#pragma unroll
-            for (int e = 0; e < (int)sizeof(T) / 2; ++e)
-              reinterpret_cast<uint4*>(to)[e] = reinterpret_cast<const uint4*>(from)[e];
-          } else {
-            for (int e = 0; e < 8; ++e)
-              if (col + e < a.dk) to[e] = from[e];
-          }
-        }
-      }
-    }
-    // ---- outputs, transposed: lane r16 has row 16 w + r16, and four value columns
-    if constexpr (OUT) {
-      floatx4 A[4], oi[2], ot[2];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) A[i] = zero4();
-      oi[0] = oi[1] = ot[0] = ot[1] = zero4();
-#pragma unroll
-      for (int s = 0; s < KI; ++s) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i <= w) A[i] = mma(ld_row<DK>(t.k, 16 * i, 32 * s), fq[s], A[i]);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) oi[i] = mma(ld_row<DK>(t.s, 16 * i, 32 * s), fq[s], oi[i]);
-      }
-      const int r = 16 * w + r16;
-      const float Gh = t.g.hi[r], Gl = t.g.lo[r];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i <= w) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int j = 16 * i + 4 * g4 + e;
-            float d = Gh - t.g.hi[j];
-            if constexpr (F32) d += Gl - t.g.lo[j];
-            A[i][e] = j <= r ? A[i][e] * __builtin_amdgcn_exp2f(d) : 0.f;
-          }
-        }
-      }
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        if (2 * s <= w) {
-          const Frag<T> p = frag_of<T>(A[2 * s], A[2 * s + 1]);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) ot[i] = mma(ld_col_acc<VLD>(t.v, 32 * s, VCOL + 16 * i), p, ot[i]);
-        }
-      }
-      const long tok = tok0 + (long)c * DC_CH;
-      const long orow = (long)a.H * a.dv;
-      const auto ro = head_rows<T>(a.o, tok, orow, (long)h * a.dv, m, a.dv);
-      const float eg = a.scale * __builtin_amdgcn_exp2f(Gh);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        floatx4 o;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fmaf(eg, oi[i][e], a.scale * ot[i][e]);
-        store4c<T, VEC>(ro, r, (unsigned)orow * sizeof(T), j0 + 16 * i + 4 * g4, a.dv, o);
-      }
-    }
-    // ---- the state behind the chunk
-    const float fade = __builtin_amdgcn_exp2f((float)Gend);
-    each([&](float x, int, int) { return x * fade; });
+  };
+  float fade = stage(tiles[0], in0);
+  load(in0, 2);
+  __syncthreads();
+  auto step = [&](const ScanTile<T, DK>& t, ScanTile<T, DK>& next, Inputs& in, int it) {
+    const float f = fade;
+    fade = stage(next, in);
+    load(in, it + 3);
+    if (!LOCAL && (REV ? a.dkept : a.kept)) keep(it);
+    each([&](float x, int, int) { return x * f; });
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       Frag<T> fv[2][NT];
@@ -454,13 +443,19 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
       for (int mm = 0; mm < MT; ++mm) {
         const Frag<T> fk = ld_col<DK>(t.k, 32 * s, w * (DK / 4) + 16 * mm);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int e = 0; e < NT; ++e)
 #pragma unroll
-          for (int e = 0; e < NT; ++e) S[mm][i] = mma(fk, fv[i][e], S[mm][i]);
+          for (int i = 0; i < 2; ++i) S[mm][i] = mma(fk, fv[i][e], S[mm][i]);
       }
     }
     __syncthreads();
+  };
+  int it = 0;
+  for (; it + 1 < nc; it += 2) {
+    step(tiles[0], tiles[1], in1, it);
+    step(tiles[1], tiles[0], in0, it + 1);
   }
+  if (it < nc) step(tiles[0], tiles[1], in1, it);
 
   if constexpr (LOCAL) {
     float4* e = reinterpret_cast<float4*>(end_at(slot));
@@ -477,6 +472,129 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
         return x;
       });
     }
+  }
+}
+
+// ---- outputs of a chunk ----------------------------------------------------------------
+// A workgroup forms one chunk's and head's outputs from its inputs and the state that
+// enters it, 64 value columns at a time.  The products are transposed: lane r16 of wave w
+// has row 16 w + r16 and four consecutive columns, and the pairs' weights leave one
+// product in the registers that the next one takes them from.
+template <typename T, int DK>
+struct OutTiles {
+  T k[DC_CH * DK], s[64 * DK], v[DC_CH * 64];
+  Sums g;
+};
+
+template <typename T, int DK, bool VEC>
+__global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
+  constexpr bool F32 = is_f32<T>::value;
+  constexpr int KI = DK / 32;
+  __shared__ __align__(16) OutTiles<T, DK> t;
+  const int slot = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  const Slot sq = find_slot(a, slot, DC_CH);
+  const int first = sq.piece * DC_CH;
+  if (first >= sq.len) return;
+  const int m = min(DC_CH, sq.len - first);
+  const long tok = (long)sq.t0 + first;
+  const int w = wave_id_s(), lane = lane_id(), r16 = lane & 15, g4 = lane >> 4, r = 16 * w + r16;
+  const int dk = a.dk, dv = a.dv;
+  const auto rq = head_rows<T>(a.q, tok, a.q_row, (long)(h / (a.H / a.Hq)) * dk, m, dk);
+  const auto rk = head_rows<T>(a.k, tok, a.k_row, (long)(h / (a.H / a.Hk)) * dk, m, dk);
+  const auto rv = head_rows<T>(a.v, tok, a.v_row, (long)(h / (a.H / a.Hv)) * dv, m, dv);
+  const auto rS = head_rows<T>(static_cast<const T*>(a.kept) + ((long)slot * a.H + h) * dv * dk, 0, dk, 0, dv, dk);
+  const auto ro = head_rows<T>(a.o, tok, (long)a.H * dv, (long)h * dv, m, dv);
+  const unsigned bo = (unsigned)(a.H * dv) * (unsigned)sizeof(T);
+
+  Gates gates;
+  gates.load(a, tok, h, m);
+  Piece<T, 8, VEC> pk[KI], ps[KI], pv[2];
+#pragma unroll
+  for (int i = 0; i < KI; ++i) {
+    const int idx = threadIdx.x + 256 * i;
+    load8(pk[i], rk, idx / (DK / 8), (unsigned)a.k_row * sizeof(T), idx % (DK / 8) * 8, dk);
+  }
+  Frag<T> fq[KI];
+#pragma unroll
+  for (int s = 0; s < KI; ++s) fq[s] = load_frag<T, VEC>(rq, 16 * w, (unsigned)a.q_row * sizeof(T), 32 * s, dk);
+  auto load = [&](int v0) {  // a block of value columns
+#pragma unroll
+    for (int i = 0; i < KI; ++i) {
+      const int idx = threadIdx.x + 256 * i;
+      load8(ps[i], rS, v0 + idx / (DK / 8), (unsigned)dk * sizeof(T), idx % (DK / 8) * 8, dk);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int idx = threadIdx.x + 256 * i;
+      load8(pv[i], rv, idx / 8, (unsigned)a.v_row * sizeof(T), v0 + idx % 8 * 8, dv);
+    }
+  };
+  auto stage = [&] {
+#pragma unroll
+    for (int i = 0; i < KI; ++i) {
+      const int idx = threadIdx.x + 256 * i;
+      st_row8<DK>(t.s, idx / (DK / 8), idx % (DK / 8) * 8, ps[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int idx = threadIdx.x + 256 * i;
+      st_row8<64>(t.v, idx / 8, idx % 8 * 8, pv[i]);
+    }
+  };
+  load(0);
+  const double G = gate_sum(gates.get(a.g_head ? static_cast<const float*>(a.g)[h] : 0.f));
+  if (w == 0) {
+    t.g.hi[lane] = (float)G;
+    t.g.lo[lane] = (float)(G - (double)(float)G);
+  }
+#pragma unroll
+  for (int i = 0; i < KI; ++i) {
+    const int idx = threadIdx.x + 256 * i;
+    st_row8<DK>(t.k, idx / (DK / 8), idx % (DK / 8) * 8, pk[i]);
+  }
+  stage();
+  __syncthreads();
+
+  floatx4 A[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) A[i] = zero4();
+#pragma unroll
+  for (int s = 0; s < KI; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) A[i] = mma(ld_row<DK>(t.k, 16 * i, 32 * s), fq[s], A[i]);
+  const float Gh = t.g.hi[r], Gl = t.g.lo[r];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const floatx4 f = t.g.template weights<F32>(Gh, Gl, 16 * i + 4 * g4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) A[i][e] = 16 * i + 4 * g4 + e <= r ? A[i][e] * f[e] : 0.f;
+  }
+  const Frag<T> p[2] = {frag_of<T>(A[0], A[1]), frag_of<T>(A[2], A[3])};
+  const float eg = a.scale * __builtin_amdgcn_exp2f(Gh);
+  for (int v0 = 0;;) {
+    if (v0 + 64 < dv) load(v0 + 64);
+    floatx4 oi[4], ot[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) oi[i] = ot[i] = zero4();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int s = 0; s < KI; ++s) oi[i] = mma(ld_row<DK>(t.s, 16 * i, 32 * s), fq[s], oi[i]);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) ot[i] = mma(ld_col_acc<64>(t.v, 32 * s, 16 * i), p[s], ot[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      floatx4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(eg, oi[i][e], a.scale * ot[i][e]);
+      store4c<T, VEC>(ro, r, bo, v0 + 16 * i + 4 * g4, dv, o);
+    }
+    v0 += 64;
+    if (v0 >= dv) break;
+    __syncthreads();
+    stage();
+    __syncthreads();
   }
 }
 
@@ -515,7 +633,9 @@ __global__ __launch_bounds__(256) void k_decay_grad(DecayArgs a) {
   const auto rD = head_rows<T>(static_cast<const T*>(a.dkept) + at, 0, dk, 0, dv, dk);
   const unsigned bs = (unsigned)dk * sizeof(T);
 
-  const double G = gate_sum(lane < m ? gate_of(a, tok + lane, h) : 0.f), Gend = __shfl(G, 63);
+  Gates gates;
+  gates.load(a, tok, h, m);
+  const double G = gate_sum(gates.get(a.g_head ? static_cast<const float*>(a.g)[h] : 0.f)), Gend = read_lane(G, 63);
   if (w == 0) {
     t.g.hi[lane] = (float)G;
     t.g.lo[lane] = (float)(G - (double)(float)G);
@@ -545,16 +665,14 @@ __global__ __launch_bounds__(256) void k_decay_grad(DecayArgs a) {
     floatx4 pair[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      const floatx4 wt = t.g.template weights<F32>(Gh, Gl, 16 * i + 4 * g4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int j = 16 * i + 4 * g4 + e;
-        float d = Gh - t.g.hi[j];
-        if constexpr (F32) d += Gl - t.g.lo[j];
-        const float f = a.scale * __builtin_amdgcn_exp2f(d);
-        const float b = j <= r ? Bt[i][e] * f : 0.f;
+        const float f = a.scale * wt[e], b = Bt[i][e] * f, x = A[i][e] * f;
         pair[i][e] = j < r ? b * A[i][e] : 0.f;
-        A[i][e] = j <= r ? A[i][e] * f : 0.f;
-        Bt[i][e] = b;
+        A[i][e] = j <= r ? x : 0.f;
+        Bt[i][e] = j <= r ? b : 0.f;
       }
       st_row4<64>(t.p, r, 16 * i + 4 * g4, A[i]);
       st_row4<64>(t.w, r, 16 * i + 4 * g4, Bt[i]);
@@ -860,11 +978,24 @@ static hipError_t run_scans(const DecayArgs& a) {
   return run_scan<T, REV, false, VEC>(a);
 }
 
+template <typename T, bool VEC>
+static hipError_t run_out(const DecayArgs& a) {
+  if (a.Ttot == 0) return hipSuccess;
+  const unsigned grid = (unsigned)(decay_slots(a, DC_CH) * a.H);
+  switch (decay_dkp(a.dk)) {
+    case 64: k_decay_out<T, 64, VEC><<<grid, 256, 0, a.stream>>>(a); break;
+    case 128: k_decay_out<T, 128, VEC><<<grid, 256, 0, a.stream>>>(a); break;
+    default: k_decay_out<T, 256, VEC><<<grid, 256, 0, a.stream>>>(a); break;
+  }
+  return hipGetLastError();
+}
 template <typename T>
 static hipError_t run_fwd(const DecayArgs& a) {
   const bool vec = pieces8<T>(a.q, a.q_row, a.dk) && pieces8<T>(a.k, a.k_row, a.dk) && pieces8<T>(a.v, a.v_row, a.dv) &&
                    pieces8<T>(a.o, (long)a.H * a.dv, a.dv);
-  return vec ? run_scans<T, false, true>(a) : run_scans<T, false, false>(a);
+  const hipError_t e = vec ? run_scans<T, false, true>(a) : run_scans<T, false, false>(a);
+  if (e != hipSuccess) return e;
+  return vec ? run_out<T, true>(a) : run_out<T, false>(a);
 }
 hipError_t launch_decay_fwd(const DecayArgs& a) { return a.bf16 ? run_fwd<bf16_t>(a) : run_fwd<float>(a); }
 
