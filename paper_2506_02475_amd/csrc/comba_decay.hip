@@ -603,17 +603,301 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
 // that enters it and the gradient of the one that leaves it.  Wave w owns the rows
 // 16 w ..: of q in dq, of k and v in dk and dv.  All products are transposed, so that a
 // lane holds four consecutive columns of one row.
-template <typename T>
+// The chunk's four inputs lie in LDS whole; the values' tile makes room for the states',
+// 64 x 64 at a time with the next one's loads in flight.
+template <typename T, int DK, int DV>
 struct GradTiles {
+  static constexpr int VS = DV >= 128 ? DC_CH * DV : 2 * 64 * 64;
+  T q[DC_CH * DK], k[DC_CH * DK], o[DC_CH * DV], vs[VS], w[DC_CH * DC_CH];
+  Sums g;
+  float row[DC_CH], col[4][DC_CH], far[DC_CH], part[4];
+};
+
+// A tile of 64 rows, eight columns a piece: into registers, and from there into LDS.
+template <typename T, int COLS, bool VEC>
+struct Rows64 {
+  static constexpr int N = COLS / 32;
+  Piece<T, 8, VEC> p[N];
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, unsigned row_bytes, int r0, int c0, int d) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int idx = threadIdx.x + 256 * i;
+      load8(p[i], rs, r0 + idx / (COLS / 8), row_bytes, c0 + idx % (COLS / 8) * 8, d);
+    }
+  }
+  __device__ __forceinline__ void store(T* tile) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int idx = threadIdx.x + 256 * i;
+      st_row8<COLS>(tile, idx / (COLS / 8), idx % (COLS / 8) * 8, p[i]);
+    }
+  }
+};
+
+// The pairs of a chunk, lane: row r = 16 w + r16, j = 16 i + 4 g4 + e of A (q_r . k_j) and
+// B (do_r . v_j): both weighted and masked, and into col[w][t] the wave's part of the sum of
+// the pairs j < t <= r for every t: over j as a product with a triangle of ones (bf16: of
+// the pairs in two terms), then over the rows that remain.  Nothing is subtracted: where
+// few pairs are left, row sums minus column sums would be rounding.
+template <typename T, bool DG>
+__device__ __forceinline__ void weigh_pairs(floatx4 (&A)[4], floatx4 (&B)[4], const Sums& g, float scale, int w, float* col) {
+  constexpr bool F32 = is_f32<T>::value;
+  const int lane = lane_id(), r16 = lane & 15, g4 = lane >> 4, r = 16 * w + r16;
+  const float Gh = g.hi[r], Gl = g.lo[r];
+  floatx4 pair[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const floatx4 wt = g.template weights<F32>(Gh, Gl, 16 * i + 4 * g4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = 16 * i + 4 * g4 + e;
+      const float f = scale * wt[e], b = B[i][e] * f, x = A[i][e] * f;
+      pair[i][e] = j < r ? b * A[i][e] : 0.f;
+      A[i][e] = j <= r ? x : 0.f;
+      B[i][e] = j <= r ? b : 0.f;
+    }
+  }
+  if constexpr (DG) {
+    floatx4 U[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) U[i] = zero4();
+    floatx4 tri;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tri[e] = 4 * g4 + e < r16 ? 1.f : 0.f;
+    const floatx4 ones = {1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const Frag<T> hi = frag_of<T>(pair[2 * s], pair[2 * s + 1]);
+      Frag<T> lo{};
+      if constexpr (!F32) {
+        floatx4 x[2];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e / 4][e % 4] = pair[2 * s + e / 4][e % 4] - (float)hi.x[e];
+        lo = frag_of<T>(x[0], x[1]);
+      }
+#pragma unroll
+      for (int i = 2 * s; i < 4; ++i) {  // block i's t against blocks 2 s and 2 s + 1 of j
+        const Frag<T> l = frag_of<T>(i == 2 * s ? tri : ones, i == 2 * s ? zero4() : i == 2 * s + 1 ? tri : ones);
+        U[i] = mma(l, hi, U[i]);
+        if constexpr (!F32) U[i] = mma(l, lo, U[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int tt = 16 * i + 4 * g4 + e;
+        const float cs = sum16(r >= tt ? U[i][e] : 0.f);
+        if (r16 == 0) col[tt] = cs;
+      }
+  }
+}
+
+template <typename T, int DK, int DV, bool VEC>
+__global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 : 1) void k_decay_grad(DecayArgs a) {
+  constexpr int KS = DK / 32, VS = DV / 32, VT = DV / 16;
+  __shared__ __align__(16) GradTiles<T, DK, DV> t;
+  const int slot = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  const Slot sq = find_slot(a, slot, DC_CH);
+  const int first = sq.piece * DC_CH;
+  if (first >= sq.len) return;
+  const int m = min(DC_CH, sq.len - first);
+  const long tok = (long)sq.t0 + first;
+  const int w = wave_id_s(), lane = lane_id(), r16 = lane & 15, g4 = lane >> 4, r = 16 * w + r16;
+  const int dk = a.dk, dv = a.dv;
+  const long at = ((long)slot * a.H + h) * dv * dk;
+  const auto rS = head_rows<T>(static_cast<const T*>(a.kept) + at, 0, dk, 0, dv, dk);
+  const auto rD = head_rows<T>(static_cast<const T*>(a.dkept) + at, 0, dk, 0, dv, dk);
+  const unsigned bs = (unsigned)dk * sizeof(T);
+
+  Gates gates;
+  gates.load(a, tok, h, m);
+  Rows64<T, 64, VEC> xs, xd;  // the states' next tile
+  {
+    Rows64<T, DK, VEC> q, k;
+    Rows64<T, DV, VEC> o, v;
+    q.load(head_rows<T>(a.q, tok, a.q_row, (long)(h / (a.H / a.Hq)) * dk, m, dk), (unsigned)a.q_row * sizeof(T), 0, 0, dk);
+    k.load(head_rows<T>(a.k, tok, a.k_row, (long)(h / (a.H / a.Hk)) * dk, m, dk), (unsigned)a.k_row * sizeof(T), 0, 0, dk);
+    o.load(head_rows<T>(a.dO, tok, (long)a.H * dv, (long)h * dv, m, dv), (unsigned)(a.H * dv) * (unsigned)sizeof(T), 0, 0, dv);
+    v.load(head_rows<T>(a.v, tok, a.v_row, (long)(h / (a.H / a.Hv)) * dv, m, dv), (unsigned)a.v_row * sizeof(T), 0, 0, dv);
+    q.store(t.q);
+    k.store(t.k);
+    o.store(t.o);
+    v.store(t.vs);
+    xs.load(rS, bs, 0, 0, dk);
+    xd.load(rD, bs, 0, 0, dk);
+  }
+  const double G = gate_sum(gates.get(a.g_head ? static_cast<const float*>(a.g)[h] : 0.f)), Gend = read_lane(G, 63);
+  if (w == 0) {
+    t.g.hi[lane] = (float)G;
+    t.g.lo[lane] = (float)(G - (double)(float)G);
+  }
+  const double Gr = __shfl(G, r);
+  const float eg = a.scale * __builtin_amdgcn_exp2f((float)Gr);   // of row r as a query
+  const float tail = __builtin_amdgcn_exp2f((float)(Gend - Gr));  // as a key
+  __syncthreads();
+
+  // ---- the pairs
+  floatx4 A[4], Bt[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) A[i] = Bt[i] = zero4();
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const Frag<T> f = ld_row<DK>(t.q, 16 * w, 32 * s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) A[i] = mma(ld_row<DK>(t.k, 16 * i, 32 * s), f, A[i]);
+  }
+  Frag<T> fv[VS];
+#pragma unroll
+  for (int s = 0; s < VS; ++s) {
+    const Frag<T> f = ld_row<DV>(t.o, 16 * w, 32 * s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) Bt[i] = mma(ld_row<DV>(t.vs, 16 * i, 32 * s), f, Bt[i]);
+    fv[s] = ld_row<DV>(t.vs, 16 * w, 32 * s);
+  }
+  if (a.dg) weigh_pairs<T, true>(A, Bt, t.g, a.scale, w, t.col[w]);
+  else weigh_pairs<T, false>(A, Bt, t.g, a.scale, w, nullptr);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) st_row4<64>(t.w, r, 16 * i + 4 * g4, A[i]);
+  const Frag<T> fw[2] = {frag_of<T>(Bt[0], Bt[1]), frag_of<T>(Bt[2], Bt[3])};
+  __syncthreads();
+  // (the values' tile is free from here on)
+  T *ts = t.vs, *td = t.vs + 64 * 64;
+  xs.store(ts);
+  xd.store(td);
+  // ---- dv of the pairs
+  floatx4 av[VT], iv[VT];
+#pragma unroll
+  for (int i = 0; i < VT; ++i) av[i] = iv[i] = zero4();
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const Frag<T> f = ld_col<64>(t.w, 32 * s, 16 * w);
+#pragma unroll
+    for (int i = 0; i < VT; ++i) av[i] = mma(ld_col<DV>(t.o, 32 * s, 16 * i), f, av[i]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) st_row4<64>(t.w, r, 16 * i + 4 * g4, Bt[i]);
+  // (read behind the next barrier)
+
+  const long pq = (long)h * dk, pv = (long)h * dv;
+  auto rows_of = [&](float* wide, void* out, long col, int d) {
+    return wide ? head_rows<float>(wide, tok, (long)a.H * d, col, m, d) : head_rows<T>(out, tok, (long)a.H * d, col, m, d);
+  };
+  const auto oq = rows_of(a.pq, a.dq, pq, dk), ok = rows_of(a.pk, a.dk_, pq, dk), ov = rows_of(a.pv, a.dv_, pv, dv);
+  auto put = [&](__amdgpu_buffer_rsrc_t rs, bool wide, int col, int d, const floatx4& x) {
+    if (wide) store4c<float, VEC>(rs, r, (unsigned)(a.H * d) * 4u, col, d, x);
+    else store4c<T, VEC>(rs, r, (unsigned)(a.H * d) * (unsigned)sizeof(T), col, d, x);
+  };
+  // ---- dq and dk, 64 columns at a time, and the states' part of dv
+  float xr = 0.f, yj = 0.f, carry = 0.f;
+#pragma unroll 1
+  for (int n = 0; n < DK / 64; ++n) {
+    floatx4 iq[4], ik[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) iq[i] = ik[i] = zero4();
+#pragma unroll
+    for (int v = 0; v < DV / 64; ++v) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) carry = fmaf(xs.p[i].get(e), xd.p[i].get(e), carry);
+      const bool last = v + 1 == DV / 64;
+      if (!last || n + 1 < DK / 64) {
+        xs.load(rS, bs, last ? 0 : 64 * (v + 1), last ? 64 * (n + 1) : 64 * n, dk);
+        xd.load(rD, bs, last ? 0 : 64 * (v + 1), last ? 64 * (n + 1) : 64 * n, dk);
+      }
+      if (n + v > 0) __syncthreads();
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const Frag<T> fo = ld_row<DV>(t.o, 16 * w, 64 * v + 32 * s), fk = ld_row<DK>(t.k, 16 * w, 64 * n + 32 * s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          iq[i] = mma(ld_col<64>(ts, 32 * s, 16 * i), fo, iq[i]);
+          ik[i] = mma(ld_col<64>(td, 32 * s, 16 * i), fv[2 * v + s], ik[i]);
+          iv[4 * v + i] = mma(ld_row<64>(td, 16 * i, 32 * s), fk, iv[4 * v + i]);
+        }
+      }
+      __syncthreads();
+      if (!last || n + 1 < DK / 64) {
+        xs.store(ts);
+        xd.store(td);
+      }
+    }
+    // the states' parts by their rows' decays, then the pairs' on top
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int col = 64 * n + 16 * i + 4 * g4;
+      const T *qr = t.q + sw16<DK>(r, col), *kr = t.k + sw16<DK>(r, col);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        iq[i][e] *= eg;
+        ik[i][e] *= tail;
+        xr = fmaf(to_f(qr[e]), iq[i][e], xr);
+        yj = fmaf(to_f(kr[e]), ik[i][e], yj);
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const Frag<T> f = ld_col<64>(t.w, 32 * s, 16 * w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        iq[i] = mma(ld_col_acc<DK>(t.k, 32 * s, 64 * n + 16 * i), fw[s], iq[i]);
+        ik[i] = mma(ld_col<DK>(t.q, 32 * s, 64 * n + 16 * i), f, ik[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      put(oq, a.pq, 64 * n + 16 * i + 4 * g4, dk, iq[i]);
+      put(ok, a.pk, 64 * n + 16 * i + 4 * g4, dk, ik[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < VT; ++i) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) av[i][e] = fmaf(tail, iv[i][e], av[i][e]);
+    put(ov, a.pv, 16 * i + 4 * g4, dv, av[i]);
+  }
+  // ---- dg: pairs inside the chunk, with one token before or behind it, with both
+  if (!a.dg) return;
+  xr = sum_groups(xr);
+  yj = sum_groups(yj);
+  if (g4 == 0) {
+    t.row[r] = xr;
+    t.far[r] = yj;
+  }
+  carry = wave_sum(carry);
+  if (lane == 0) t.part[w] = carry;
+  __syncthreads();
+  if (w == 0) {
+    const int back = 63 - lane;  // lane l holds row 63 - l: suffix sums as prefix sums
+    float x = wave_prefix_sum(t.row[back]);
+    float y = wave_prefix_sum(t.far[lane]);
+    y = __shfl_up(y, 1);
+    x = __shfl(x, back);
+    const float both = __builtin_amdgcn_exp2f((float)Gend) * (((t.part[0] + t.part[1]) + t.part[2]) + t.part[3]);
+    const float in = ((t.col[0][lane] + t.col[1][lane]) + t.col[2][lane]) + t.col[3][lane];
+    const float dg = in + x + (lane > 0 ? y : 0.f) + both;
+    if (lane < m) {
+      const long to = (tok + lane) * a.H + h;
+      if (a.g_f32) static_cast<float*>(a.dg)[to] = dg;
+      else store_elem(static_cast<bf16_t*>(a.dg) + to, dg);
+    }
+  }
+}
+
+// Where the inputs do not fit LDS (fp32 with heads of more than 128): the same from
+// slices of 64 columns, the operands that LDS does not hold from the caches.
+template <typename T>
+struct WideTiles {
   T q[DC_CH * 64], k[DC_CH * 64], s[64 * 64], d[64 * 64], w[DC_CH * DC_CH], p[DC_CH * DC_CH];
   Sums g;
   float row[DC_CH], col[4][DC_CH], far[DC_CH], part[4];
 };
 
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void k_decay_grad(DecayArgs a) {
-  constexpr bool F32 = is_f32<T>::value;
-  __shared__ __align__(16) GradTiles<T> t;
+__global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
+  __shared__ __align__(16) WideTiles<T> t;
   const int slot = blockIdx.x / a.H, h = blockIdx.x % a.H;
   const Slot sq = find_slot(a, slot, DC_CH);
   const int first = sq.piece * DC_CH;
@@ -660,62 +944,12 @@ __global__ __launch_bounds__(256) void k_decay_grad(DecayArgs a) {
     for (int i = 0; i < 4; ++i)
       if (i <= w) Bt[i] = mma(load_frag<T, VEC>(rv, 16 * i, bv, s, dv), f, Bt[i]);
   }
-  {
-    const float Gh = t.g.hi[r], Gl = t.g.lo[r];
-    floatx4 pair[4];
+  if (a.dg) weigh_pairs<T, true>(A, Bt, t.g, a.scale, w, t.col[w]);
+  else weigh_pairs<T, false>(A, Bt, t.g, a.scale, w, nullptr);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const floatx4 wt = t.g.template weights<F32>(Gh, Gl, 16 * i + 4 * g4);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = 16 * i + 4 * g4 + e;
-        const float f = a.scale * wt[e], b = Bt[i][e] * f, x = A[i][e] * f;
-        pair[i][e] = j < r ? b * A[i][e] : 0.f;
-        A[i][e] = j <= r ? x : 0.f;
-        Bt[i][e] = j <= r ? b : 0.f;
-      }
-      st_row4<64>(t.p, r, 16 * i + 4 * g4, A[i]);
-      st_row4<64>(t.w, r, 16 * i + 4 * g4, Bt[i]);
-    }
-    // sums over the pairs j < t <= r for every t: over j as a product with a triangle of
-    // ones (bf16: of the pairs in two terms), then over the rows that remain.  Nothing is
-    // subtracted: where few pairs are left, row sums minus column sums would be rounding.
-    if (a.dg) {
-      floatx4 U[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) U[i] = zero4();
-      floatx4 tri;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) tri[e] = 4 * g4 + e < r16 ? 1.f : 0.f;
-      const floatx4 ones = {1.f, 1.f, 1.f, 1.f};
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        if (2 * s > w) continue;
-        const Frag<T> hi = frag_of<T>(pair[2 * s], pair[2 * s + 1]);
-        Frag<T> lo{};
-        if constexpr (!F32) {
-          floatx4 x[2];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e / 4][e % 4] = pair[2 * s + e / 4][e % 4] - (float)hi.x[e];
-          lo = frag_of<T>(x[0], x[1]);
-        }
-#pragma unroll
-        for (int i = 2 * s; i < 4; ++i) {  // (block i's t against blocks 2 s and 2 s + 1 of j)
-          if (i > w) continue;
-          const Frag<T> l = frag_of<T>(i == 2 * s ? tri : ones, i == 2 * s ? zero4() : i == 2 * s + 1 ? tri : ones);
-          U[i] = mma(l, hi, U[i]);
-          if constexpr (!F32) U[i] = mma(l, lo, U[i]);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int tt = 16 * i + 4 * g4 + e;
-          const float cs = sum16(r >= tt ? U[i][e] : 0.f);
-          if (r16 == 0) t.col[w][tt] = cs;
-        }
-    }
+  for (int i = 0; i < 4; ++i) {
+    st_row4<64>(t.p, r, 16 * i + 4 * g4, A[i]);
+    st_row4<64>(t.w, r, 16 * i + 4 * g4, Bt[i]);
   }
   const Frag<T> fw[2] = {frag_of<T>(Bt[0], Bt[1]), frag_of<T>(Bt[2], Bt[3])};
 
@@ -1007,6 +1241,31 @@ static hipError_t run_shared(const DecayArgs& a, const float* p, void* out, int 
                                                                                a.H / heads, d);
   return hipGetLastError();
 }
+template <typename T, int DK, bool VEC>
+static void grad_of(const DecayArgs& a, unsigned grid) {
+  switch (decay_dkp(a.dv)) {
+    case 64: k_decay_grad<T, DK, 64, VEC><<<grid, 256, 0, a.stream>>>(a); break;
+    case 128: k_decay_grad<T, DK, 128, VEC><<<grid, 256, 0, a.stream>>>(a); break;
+    default:
+      if constexpr (!is_f32<T>::value) k_decay_grad<T, DK, 256, VEC><<<grid, 256, 0, a.stream>>>(a);
+  }
+}
+template <typename T, bool VEC>
+static hipError_t run_grad(const DecayArgs& a, unsigned grid) {
+  if constexpr (is_f32<T>::value) {
+    if (a.dk > 128 || a.dv > 128) {
+      k_decay_grad_wide<T, VEC><<<grid, 256, 0, a.stream>>>(a);
+      return hipGetLastError();
+    }
+  }
+  switch (decay_dkp(a.dk)) {
+    case 64: grad_of<T, 64, VEC>(a, grid); break;
+    case 128: grad_of<T, 128, VEC>(a, grid); break;
+    default:
+      if constexpr (!is_f32<T>::value) grad_of<T, 256, VEC>(a, grid);
+  }
+  return hipGetLastError();
+}
 template <typename T>
 static hipError_t run_bwd(const DecayArgs& a) {
   const bool vec = pieces8<T>(a.q, a.q_row, a.dk) && pieces8<T>(a.k, a.k_row, a.dk) && pieces8<T>(a.v, a.v_row, a.dv) &&
@@ -1016,9 +1275,7 @@ static hipError_t run_bwd(const DecayArgs& a) {
   if (e != hipSuccess || a.Ttot == 0) return e;
   const long grid = decay_slots(a, DC_CH) * a.H;
   if (grid > INT32_MAX / 256) return hipErrorInvalidValue;
-  if (vec) k_decay_grad<T, true><<<(unsigned)grid, 256, 0, a.stream>>>(a);
-  else k_decay_grad<T, false><<<(unsigned)grid, 256, 0, a.stream>>>(a);
-  e = hipGetLastError();
+  e = vec ? run_grad<T, true>(a, (unsigned)grid) : run_grad<T, false>(a, (unsigned)grid);
   if (e == hipSuccess && a.pq) e = run_shared<T>(a, a.pq, a.dq, a.Hq, a.dk);
   if (e == hipSuccess && a.pk) e = run_shared<T>(a, a.pk, a.dk_, a.Hk, a.dk);
   if (e == hipSuccess && a.pv) e = run_shared<T>(a, a.pv, a.dv_, a.Hv, a.dv);
