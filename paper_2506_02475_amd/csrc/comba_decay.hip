@@ -58,11 +58,18 @@ __device__ __forceinline__ Frag<T> frag_of(const floatx4& a, const floatx4& b) {
   }
   return f;
 }
+// The lane's number as a value of its own: tile addresses formed from it stay where they
+// are used (the compiler would keep those of every tile in registers across a loop).
+__device__ __forceinline__ int fresh_lane() {
+  int l = lane_id();
+  asm volatile("" : "+v"(l));
+  return l;
+}
 // From a tile of rows of LD elements (a multiple of 64, pieces of eight swizzled):
 // eight consecutive elements of row (lane % 16), from column col + 8 (lane / 16).
 template <int LD, typename T>
-__device__ __forceinline__ Frag<T> ld_row(const T* tile, int row, int col) {
-  const T* p = tile + sw16<LD>(row + (lane_id() & 15), col + 8 * (lane_id() >> 4));
+__device__ __forceinline__ Frag<T> ld_row(const T* tile, int row, int col, int lane = lane_id()) {
+  const T* p = tile + sw16<LD>(row + (lane & 15), col + 8 * (lane >> 4));
   Frag<T> f;
   if constexpr (is_f32<T>::value) {
     const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
@@ -75,8 +82,8 @@ __device__ __forceinline__ Frag<T> ld_row(const T* tile, int row, int col) {
 }
 // Column col + lane % 16 at rows r0 .. r0 + 3 and r1 .. r1 + 3.
 template <int LD, typename T>
-__device__ __forceinline__ Frag<T> ld_col2(const T* tile, int r0, int r1, int col) {
-  const int s = lane_id() & 15;
+__device__ __forceinline__ Frag<T> ld_col2(const T* tile, int r0, int r1, int col, int lane) {
+  const int s = lane & 15;
   Frag<T> f;
   if constexpr (is_f32<T>::value) {
 #pragma unroll
@@ -92,15 +99,15 @@ __device__ __forceinline__ Frag<T> ld_col2(const T* tile, int r0, int r1, int co
 }
 // The same at rows r0 + 8 (lane / 16) .. + 7 ...
 template <int LD, typename T>
-__device__ __forceinline__ Frag<T> ld_col(const T* tile, int r0, int col) {
-  const int r = r0 + 8 * (lane_id() >> 4);
-  return ld_col2<LD>(tile, r, r + 4, col);
+__device__ __forceinline__ Frag<T> ld_col(const T* tile, int r0, int col, int lane = lane_id()) {
+  const int r = r0 + 8 * (lane >> 4);
+  return ld_col2<LD>(tile, r, r + 4, col, lane);
 }
 // ... and in the row order of frag_of: 4 (lane / 16) .. + 3 of two blocks of 16.
 template <int LD, typename T>
-__device__ __forceinline__ Frag<T> ld_col_acc(const T* tile, int r0, int col) {
-  const int r = r0 + 4 * (lane_id() >> 4);
-  return ld_col2<LD>(tile, r, r + 16, col);
+__device__ __forceinline__ Frag<T> ld_col_acc(const T* tile, int r0, int col, int lane = lane_id()) {
+  const int r = r0 + 4 * (lane >> 4);
+  return ld_col2<LD>(tile, r, r + 16, col, lane);
 }
 template <int LD, typename T, bool VEC>
 __device__ __forceinline__ void st_row8(T* tile, int row, int col, const Piece<T, 8, VEC>& p) {
@@ -634,6 +641,22 @@ struct Rows64 {
   }
 };
 
+// A row's pairs, as frag_of left them, into a tile of rows r and columns j.
+template <typename T>
+__device__ __forceinline__ void st_pairs(T* tile, int r, const Frag<T> (&f)[2]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    T* d = tile + sw16<64>(r, 16 * i + 4 * (lane_id() >> 4));
+    if constexpr (is_f32<T>::value) {
+      const float* x = f[i / 2].x + 4 * (i & 1);
+      *reinterpret_cast<float4*>(d) = make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+      const uint4 u = __builtin_bit_cast(uint4, f[i / 2].x);
+      *reinterpret_cast<uint2*>(d) = i & 1 ? make_uint2(u.z, u.w) : make_uint2(u.x, u.y);
+    }
+  }
+}
+
 // The pairs of a chunk, lane: row r = 16 w + r16, j = 16 i + 4 g4 + e of A (q_r . k_j) and
 // B (do_r . v_j): both weighted and masked, and into col[w][t] the wave's part of the sum of
 // the pairs j < t <= r for every t: over j as a product with a triangle of ones (bf16: of
@@ -757,28 +780,17 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
   }
   if (a.dg) weigh_pairs<T, true>(A, Bt, t.g, a.scale, w, t.col[w]);
   else weigh_pairs<T, false>(A, Bt, t.g, a.scale, w, nullptr);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) st_row4<64>(t.w, r, 16 * i + 4 * g4, A[i]);
+  const Frag<T> fp[2] = {frag_of<T>(A[0], A[1]), frag_of<T>(A[2], A[3])};
   const Frag<T> fw[2] = {frag_of<T>(Bt[0], Bt[1]), frag_of<T>(Bt[2], Bt[3])};
+  st_pairs(t.w, r, fw);
   __syncthreads();
   // (the values' tile is free from here on)
   T *ts = t.vs, *td = t.vs + 64 * 64;
   xs.store(ts);
   xd.store(td);
-  // ---- dv of the pairs
-  floatx4 av[VT], iv[VT];
+  floatx4 iv[VT];
 #pragma unroll
-  for (int i = 0; i < VT; ++i) av[i] = iv[i] = zero4();
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const Frag<T> f = ld_col<64>(t.w, 32 * s, 16 * w);
-#pragma unroll
-    for (int i = 0; i < VT; ++i) av[i] = mma(ld_col<DV>(t.o, 32 * s, 16 * i), f, av[i]);
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 4; ++i) st_row4<64>(t.w, r, 16 * i + 4 * g4, Bt[i]);
-  // (read behind the next barrier)
+  for (int i = 0; i < VT; ++i) iv[i] = zero4();
 
   const long pq = (long)h * dk, pv = (long)h * dv;
   auto rows_of = [&](float* wide, void* out, long col, int d) {
@@ -807,15 +819,17 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
         xs.load(rS, bs, last ? 0 : 64 * (v + 1), last ? 64 * (n + 1) : 64 * n, dk);
         xd.load(rD, bs, last ? 0 : 64 * (v + 1), last ? 64 * (n + 1) : 64 * n, dk);
       }
-      if (n + v > 0) __syncthreads();
+      __syncthreads();
+      const int l = fresh_lane();
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const Frag<T> fo = ld_row<DV>(t.o, 16 * w, 64 * v + 32 * s), fk = ld_row<DK>(t.k, 16 * w, 64 * n + 32 * s);
+        const Frag<T> fo = ld_row<DV>(t.o, 16 * w, 64 * v + 32 * s, l),
+                      fk = ld_row<DK>(t.k, 16 * w, 64 * n + 32 * s, l);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          iq[i] = mma(ld_col<64>(ts, 32 * s, 16 * i), fo, iq[i]);
-          ik[i] = mma(ld_col<64>(td, 32 * s, 16 * i), fv[2 * v + s], ik[i]);
-          iv[4 * v + i] = mma(ld_row<64>(td, 16 * i, 32 * s), fk, iv[4 * v + i]);
+          iq[i] = mma(ld_col<64>(ts, 32 * s, 16 * i, l), fo, iq[i]);
+          ik[i] = mma(ld_col<64>(td, 32 * s, 16 * i, l), fv[2 * v + s], ik[i]);
+          iv[4 * v + i] = mma(ld_row<64>(td, 16 * i, 32 * s, l), fk, iv[4 * v + i]);
         }
       }
       __syncthreads();
@@ -825,9 +839,10 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
       }
     }
     // the states' parts by their rows' decays, then the pairs' on top
+    const int l = fresh_lane();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int col = 64 * n + 16 * i + 4 * g4;
+      const int col = 64 * n + 16 * i + 4 * (l >> 4);
       const T *qr = t.q + sw16<DK>(r, col), *kr = t.k + sw16<DK>(r, col);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -839,11 +854,11 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const Frag<T> f = ld_col<64>(t.w, 32 * s, 16 * w);
+      const Frag<T> f = ld_col<64>(t.w, 32 * s, 16 * w, l);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        iq[i] = mma(ld_col_acc<DK>(t.k, 32 * s, 64 * n + 16 * i), fw[s], iq[i]);
-        ik[i] = mma(ld_col<DK>(t.q, 32 * s, 64 * n + 16 * i), f, ik[i]);
+        iq[i] = mma(ld_col_acc<DK>(t.k, 32 * s, 64 * n + 16 * i, l), fw[s], iq[i]);
+        ik[i] = mma(ld_col<DK>(t.q, 32 * s, 64 * n + 16 * i, l), f, ik[i]);
       }
     }
 #pragma unroll
@@ -852,12 +867,22 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
       put(ok, a.pk, 64 * n + 16 * i + 4 * g4, dk, ik[i]);
     }
   }
+  // ---- dv: the states' part by its rows' decays, the pairs' on top
+  __syncthreads();
+  st_pairs(t.w, r, fp);
+  __syncthreads();
 #pragma unroll
-  for (int i = 0; i < VT; ++i) {
+  for (int i = 0; i < VT; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) av[i][e] = fmaf(tail, iv[i][e], av[i][e]);
-    put(ov, a.pv, 16 * i + 4 * g4, dv, av[i]);
+    for (int e = 0; e < 4; ++e) iv[i][e] *= tail;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const Frag<T> f = ld_col<64>(t.w, 32 * s, 16 * w);
+#pragma unroll
+    for (int i = 0; i < VT; ++i) iv[i] = mma(ld_col<DV>(t.o, 32 * s, 16 * i), f, iv[i]);
   }
+#pragma unroll
+  for (int i = 0; i < VT; ++i) put(ov, a.pv, 16 * i + 4 * g4, dv, iv[i]);
   // ---- dg: pairs inside the chunk, with one token before or behind it, with both
   if (!a.dg) return;
   xr = sum_groups(xr);
