@@ -100,7 +100,7 @@ comba_status decay_args(const comba_decay_shape* s, comba::DecayArgs* a, bool* s
   if (tiles) {
     cut(a, longest, segments);
     // workgroups of a launch, which holds fewer than 2^31 threads
-    const int64_t most = INT32_MAX / 256 - 64;
+    const int64_t most = INT32_MAX / 512 - 64;
     if (comba::decay_slots(*a, a->seglen) > most / ((int64_t)a->H * comba::decay_splits(a->dv)) ||
         comba::decay_slots(*a, comba::DC_CH) > most / a->H)
       return COMBA_ERR_SHAPE;

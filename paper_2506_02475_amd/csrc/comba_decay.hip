@@ -58,6 +58,17 @@ __device__ __forceinline__ Frag<T> frag_of(const floatx4& a, const floatx4& b) {
   }
   return f;
 }
+// Element offset in a tile of rows of LD bf16 (a multiple of 64; fp32: twice the bytes),
+// whose pieces of eight are exchanged inside a row so that what one access touches falls
+// on distinct ones of the 64 banks: 16 rows of one piece (operands along a row), rows r ..
+// r + 3 and r + 8 .. r + 11 of two pieces (operands down the rows), four rows of four
+// (weighted values on their way in).
+template <int LD>
+__device__ __forceinline__ int swz(int row, int col) {
+  const int x = LD == 64 ? ((row & 2) << 1) | ((row >> 2) & 2) | ((row >> 2) & 1)
+                         : ((row & 3) << 2) | ((row >> 2) & 2) | ((row >> 2) & 1);
+  return row * LD + ((((col >> 3) ^ x) << 3) | (col & 7));
+}
 // The lane's number as a value of its own: tile addresses formed from it stay where they
 // are used (the compiler would keep those of every tile in registers across a loop).
 __device__ __forceinline__ int fresh_lane() {
@@ -65,11 +76,11 @@ __device__ __forceinline__ int fresh_lane() {
   asm volatile("" : "+v"(l));
   return l;
 }
-// From a tile of rows of LD elements (a multiple of 64, pieces of eight swizzled):
+// From such a tile:
 // eight consecutive elements of row (lane % 16), from column col + 8 (lane / 16).
 template <int LD, typename T>
 __device__ __forceinline__ Frag<T> ld_row(const T* tile, int row, int col, int lane = lane_id()) {
-  const T* p = tile + sw16<LD>(row + (lane & 15), col + 8 * (lane >> 4));
+  const T* p = tile + swz<LD>(row + (lane & 15), col + 8 * (lane >> 4));
   Frag<T> f;
   if constexpr (is_f32<T>::value) {
     const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
@@ -88,12 +99,12 @@ __device__ __forceinline__ Frag<T> ld_col2(const T* tile, int r0, int r1, int co
   if constexpr (is_f32<T>::value) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      f.x[e] = tile[sw16<LD>(r0 + e, col + s)];
-      f.x[4 + e] = tile[sw16<LD>(r1 + e, col + s)];
+      f.x[e] = tile[swz<LD>(r0 + e, col + s)];
+      f.x[4 + e] = tile[swz<LD>(r1 + e, col + s)];
     }
   } else {
     const int at = s >> 2, c = col + 4 * (s & 3);
-    f.x = ld_tr8(tile, TrOff{sw16<LD>(r0 + at, c), sw16<LD>(r1 + at, c)});
+    f.x = ld_tr8(tile, TrOff{swz<LD>(r0 + at, c), swz<LD>(r1 + at, c)});
   }
   return f;
 }
@@ -111,14 +122,14 @@ __device__ __forceinline__ Frag<T> ld_col_acc(const T* tile, int r0, int col, in
 }
 template <int LD, typename T, bool VEC>
 __device__ __forceinline__ void st_row8(T* tile, int row, int col, const Piece<T, 8, VEC>& p) {
-  uint4* d = reinterpret_cast<uint4*>(tile + sw16<LD>(row, col));
+  uint4* d = reinterpret_cast<uint4*>(tile + swz<LD>(row, col));
   d[0] = make_uint4(p.r[0], p.r[1], p.r[2], p.r[3]);
   if constexpr (is_f32<T>::value) d[1] = make_uint4(p.r[4], p.r[5], p.r[6], p.r[7]);
 }
 // Four values at columns col .. col + 3 (a multiple of four).
 template <int LD, typename T>
 __device__ __forceinline__ void st_row4(T* tile, int row, int col, const floatx4& x) {
-  T* d = tile + sw16<LD>(row, col);
+  T* d = tile + swz<LD>(row, col);
   if constexpr (is_f32<T>::value) *reinterpret_cast<float4*>(d) = make_float4(x[0], x[1], x[2], x[3]);
   else *reinterpret_cast<uint2*>(d) = make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
 }
@@ -132,13 +143,18 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t head_rows(const void* t, long 
   const unsigned bytes = n > 0 ? (unsigned)(((long)(n - 1) * row + d) * (long)sizeof(T)) : 0u;
   return clip_rsrc(const_cast<T*>(p), bytes);
 }
-// Columns col .. col + 7 of row r; columns from d on are zeros.
+// Columns col .. col + C - 1 of row r; columns from d on are zeros.
+template <typename T, int C, bool VEC>
+__device__ __forceinline__ void load_piece(Piece<T, C, VEC>& p, __amdgpu_buffer_rsrc_t rs, int r, unsigned row_bytes,
+                                           int col, int d) {
+  const unsigned off = (unsigned)r * row_bytes + (unsigned)col * (unsigned)sizeof(T);
+  if constexpr (VEC) p.load(rs, col < d ? off : BUF_OOB, C);
+  else p.load(rs, off, d - col);
+}
 template <typename T, bool VEC>
 __device__ __forceinline__ void load8(Piece<T, 8, VEC>& p, __amdgpu_buffer_rsrc_t rs, int r, unsigned row_bytes, int col,
                                       int d) {
-  const unsigned off = (unsigned)r * row_bytes + (unsigned)col * (unsigned)sizeof(T);
-  if constexpr (VEC) p.load(rs, col < d ? off : BUF_OOB, 8);
-  else p.load(rs, off, d - col);
+  load_piece<T, 8, VEC>(p, rs, r, row_bytes, col, d);
 }
 template <typename T, bool VEC>
 __device__ __forceinline__ Frag<T> load_frag(__amdgpu_buffer_rsrc_t rs, int row, unsigned row_bytes, int col, int d) {
@@ -264,8 +280,8 @@ __device__ __forceinline__ void split3(float x, float y, uint32_t& hi, uint32_t&
 
 // ---- the scans ---------------------------------------------------------------------
 // A workgroup walks the chunks of one segment of one sequence and head, holds DC_BV value
-// columns of the state in fp32 accumulators (wave w: key rows w DK / 4 ..), and keeps what
-// it holds before each chunk.  Forward: keys k, values v, weights e^{G_end - G_j}.  REV,
+// columns of the state in fp32 accumulators (wave w: key rows (w % 4) DK / 4 .., columns
+// 16 (w / 4) ..), and keeps what it holds before each chunk.  Forward: keys k, values v, weights e^{G_end - G_j}.  REV,
 // for the states' gradients, from the last chunk to the first: keys q, values do, weights
 // scale e^{G_r}.  LOCAL: a segment's end from a zero state, for the segments behind it.
 // The weights multiply the value columns, of which a workgroup has few, and there
@@ -274,6 +290,7 @@ __device__ __forceinline__ void split3(float x, float y, uint32_t& hi, uint32_t&
 // Bound by the latency of a chunk's chain (its decays, the weighted values into LDS, their
 // products), not by what it moves: so two tiles in LDS, the next chunk being staged while
 // one is multiplied, one barrier a chunk, and loads two chunks ahead of their staging.
+constexpr int SCAN_THREADS = 512;
 template <typename T, int DK>
 struct ScanTile {
   static constexpr int VLD = is_f32<T>::value ? 64 : 128;  // weighted values (bf16: three terms)
@@ -281,10 +298,10 @@ struct ScanTile {
 };
 
 template <typename T, int DK, bool REV, bool LOCAL, bool VEC>
-__global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
+__global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int units) {
   constexpr bool F32 = is_f32<T>::value;
   constexpr int VLD = ScanTile<T, DK>::VLD, NT = F32 ? 1 : 3;
-  constexpr int MT = DK / 64, KI = DK / 32;
+  constexpr int MT = DK / 64;
   __shared__ __align__(16) ScanTile<T, DK> tiles[2];
 
   // the splits of one head's state on one XCD (they read the same keys), heads dealt
@@ -300,7 +317,8 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
   const int base = first_slot(a, sq, a.seglen);
   const int segs = max((sq.len + a.seglen - 1) / a.seglen, 1);
   if (LOCAL && sq.piece == (REV ? 0 : segs - 1)) return;  // no segment comes after it
-  const int w = wave_id_s(), lane = lane_id(), r16 = lane & 15, g4 = lane >> 4;
+  const int wave = wave_id_s(), w = wave & 3, lane = lane_id(), r16 = lane & 15, g4 = lane >> 4;
+  const int c0 = 16 * (wave >> 2);  // of the workgroup's columns
 
   const int hx = REV ? h / (a.H / a.Hq) : h / (a.H / a.Hk), hv = REV ? h : h / (a.H / a.Hv);
   const long xrow = REV ? a.q_row : a.k_row, yrow = REV ? (long)a.H * a.dv : a.v_row;
@@ -309,7 +327,8 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
 
   // ---- a chunk's inputs
   struct Inputs {
-    Piece<T, 8, VEC> k[KI], v;
+    Piece<T, 8, VEC> k[MT];
+    Piece<T, 4, VEC> v;
     Gates g;
   } in0, in1;
   const float ghead = a.g_head ? static_cast<const float*>(a.g)[h] : 0.f;
@@ -320,10 +339,10 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
     const auto rx = head_rows<T>(X, tok, xrow, (long)hx * a.dk, m, a.dk);
     const auto ry = head_rows<T>(Y, tok, yrow, (long)hv * a.dv, m, a.dv);
     in.g.load(a, tok, h, m);
-    load8(in.v, ry, threadIdx.x / 4, (unsigned)yrow * sizeof(T), j0 + threadIdx.x % 4 * 8, a.dv);
+    load_piece(in.v, ry, threadIdx.x / 8, (unsigned)yrow * sizeof(T), j0 + threadIdx.x % 8 * 4, a.dv);
 #pragma unroll
-    for (int i = 0; i < KI; ++i) {
-      const int idx = threadIdx.x + i * 256;
+    for (int i = 0; i < MT; ++i) {
+      const int idx = threadIdx.x + i * SCAN_THREADS;
       load8(in.k[i], rx, idx / (DK / 8), (unsigned)xrow * sizeof(T), idx % (DK / 8) * 8, a.dk);
     }
   };
@@ -331,19 +350,17 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
   load(in1, 1);
 
   // ---- the state that enters
-  floatx4 S[MT][2];
-  const int row0 = w * (DK / 4) + 4 * g4;  // key rows row0 + 16 m + i, value columns j0 + 16 n + r16
+  floatx4 S[MT];
+  const int row0 = w * (DK / 4) + 4 * g4, scol = j0 + c0 + r16;  // key rows row0 + 16 m + i, value column
   auto each = [&](auto fn) {
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) S[m][c][i] = fn(S[m][c][i], row0 + 16 * m + i, j0 + 16 * c + r16);
+      for (int i = 0; i < 4; ++i) S[m][i] = fn(S[m][i], row0 + 16 * m + i, scol);
   };
   const long ends = (long)NS * DC_BV * DK;  // floats of a segment's end
   auto end_at = [&](int sl) {
-    return a.segS + ((long)sl * a.H + h) * ends + (((long)split * 4 + w) * 64 + lane) * (MT * 8);
+    return a.segS + ((long)sl * a.H + h) * ends + (((long)split * 8 + wave) * 64 + lane) * (MT * 4);
   };
   const float* entering = REV ? a.dht : a.h0;
   const long sbase = ((long)sq.seq * a.H + h) * a.dk * a.dv;
@@ -362,15 +379,13 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
       const float f2 = __builtin_amdgcn_exp2f((float)between);
       const float4* e = reinterpret_cast<const float4*>(end_at(sl));
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const float4 x = e[m * 2 + c];
-          S[m][c][0] = fmaf(f2, x.x, S[m][c][0]);
-          S[m][c][1] = fmaf(f2, x.y, S[m][c][1]);
-          S[m][c][2] = fmaf(f2, x.z, S[m][c][2]);
-          S[m][c][3] = fmaf(f2, x.w, S[m][c][3]);
-        }
+      for (int m = 0; m < MT; ++m) {
+        const float4 x = e[m];
+        S[m][0] = fmaf(f2, x.x, S[m][0]);
+        S[m][1] = fmaf(f2, x.y, S[m][1]);
+        S[m][2] = fmaf(f2, x.z, S[m][2]);
+        S[m][3] = fmaf(f2, x.w, S[m][3]);
+      }
       between += a.segG[(long)sl * a.H + h];
     }
   }
@@ -380,53 +395,50 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
     const double G = gate_sum(in.g.get(ghead)), Gend = read_lane(G, 63);
     total += Gend;
 #pragma unroll
-    for (int i = 0; i < KI; ++i) {
-      const int idx = threadIdx.x + i * 256;
+    for (int i = 0; i < MT; ++i) {
+      const int idx = threadIdx.x + i * SCAN_THREADS;
       st_row8<DK>(t.k, idx / (DK / 8), idx % (DK / 8) * 8, in.k[i]);
     }
     const float wt = REV ? a.scale * __builtin_amdgcn_exp2f((float)G) : __builtin_amdgcn_exp2f((float)(Gend - G));
-    const float f = __shfl(wt, 16 * w + lane / 4);
-    const int row = threadIdx.x / 4, col = threadIdx.x % 4 * 8;
+    const float f = __shfl(wt, 8 * wave + lane / 8);
+    const int row = threadIdx.x / 8, col = threadIdx.x % 8 * 4;
+    const float x[4] = {f * in.v.get(0), f * in.v.get(1), f * in.v.get(2), f * in.v.get(3)};
     if constexpr (F32) {
-      Piece<T, 8, VEC> x;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x.r[e] = __float_as_uint(f * in.v.get(e));
-      st_row8<VLD>(t.v, row, col, x);
+      st_row4<VLD>(t.v, row, col, floatx4{x[0], x[1], x[2], x[3]});
     } else {
-      Piece<T, 8, VEC> x[3];
+      uint2 y[3];
+      split3(x[0], x[1], y[0].x, y[1].x, y[2].x);
+      split3(x[2], x[3], y[0].y, y[1].y, y[2].y);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        split3(f * in.v.get(2 * e), f * in.v.get(2 * e + 1), x[0].r[e], x[1].r[e], x[2].r[e]);
-#pragma unroll
-      for (int e = 0; e < 3; ++e) st_row8<VLD>(t.v, row, 32 * e + col, x[e]);
+      for (int e = 0; e < 3; ++e) *reinterpret_cast<uint2*>(t.v + swz<VLD>(row, 32 * e + col)) = y[e];
     }
     return __builtin_amdgcn_exp2f((float)Gend);
   };
   // The state before a chunk, [dv][dk]: a lane has four key rows of a column (two tiles:
-  // exchanged to eight in a row).
+  // exchanged to eight in a row).  No store stands under a branch: what waits for the
+  // loads behind it counts the memory operations in between, and would count too few.
   const int kslot = first_slot(a, sq, DC_CH) + first / DC_CH;
   auto keep = [&](int it) {
     const int c = REV ? nc - 1 - it : it;
     T* to = static_cast<T*>(REV ? a.dkept : a.kept) + ((long)(kslot + c) * a.H + h) * a.dv * a.dk;
+    const auto rs = clip_rsrc(to, (unsigned)(a.dv * a.dk) * (unsigned)sizeof(T));  // (columns from dv on: dropped)
+    const unsigned at = (unsigned)(scol * a.dk) * (unsigned)sizeof(T);
+    if constexpr (VEC && !F32 && MT > 1) {
+      typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 #pragma unroll
-    for (int cc = 0; cc < 2; ++cc) {
-      const int col = j0 + 16 * cc + r16;
-      if (col >= a.dv) continue;
-      T* at = to + (long)col * a.dk;
+      for (int m = 0; m < MT; m += 2) {
+        const floatx4 &u = S[m], &v = S[m + 1];
+        const uint4 y = row8_from_pieces(make_uint2(bf16_pair(u[0], u[1]), bf16_pair(u[2], u[3])),
+                                         make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])));
+        const int r = w * (DK / 4) + 16 * m + row8_col();
+        __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{y.x, y.y, y.z, y.w}, rs, r < a.dk ? at + 2 * r : BUF_OOB, 0, 0);
+      }
+    } else {
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        const float x[4] = {S[m][cc][0], S[m][cc][1], S[m][cc][2], S[m][cc][3]};
-        const int left = a.dk - row0 - 16 * m;
-        if constexpr (VEC && !F32 && MT > 1) {
-          if (m & 1) continue;
-          const floatx4 &u = S[m][cc], &v = S[m + 1][cc];
-          const uint4 y = row8_from_pieces(make_uint2(bf16_pair(u[0], u[1]), bf16_pair(u[2], u[3])),
-                                           make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])));
-          const int r = w * (DK / 4) + 16 * m + row8_col();
-          if (r < a.dk) *reinterpret_cast<uint4*>(at + r) = y;
-        } else {
-          store_piece<T, 4, VEC>(at + row0 + 16 * m, x, left);
-        }
+        const int r = row0 + 16 * m;
+        const float x[4] = {S[m][0], S[m][1], S[m][2], S[m][3]};
+        store_piece<T, 4, VEC>(rs, r < a.dk ? at + r * (unsigned)sizeof(T) : BUF_OOB, x, a.dk - r);
       }
     }
   };
@@ -436,23 +448,19 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
   auto step = [&](const ScanTile<T, DK>& t, ScanTile<T, DK>& next, Inputs& in, int it) {
     const float f = fade;
     fade = stage(next, in);
+    if (!LOCAL) keep(it);
     load(in, it + 3);
-    if (!LOCAL && (REV ? a.dkept : a.kept)) keep(it);
     each([&](float x, int, int) { return x * f; });
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      Frag<T> fv[2][NT];
+      Frag<T> fv[NT];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int e = 0; e < NT; ++e) fv[e] = ld_col<VLD>(t.v, 32 * s, 32 * e + c0);
 #pragma unroll
-        for (int e = 0; e < NT; ++e) fv[i][e] = ld_col<VLD>(t.v, 32 * s, 32 * e + 16 * i);
+      for (int m = 0; m < MT; ++m) {
+        const Frag<T> fk = ld_col<DK>(t.k, 32 * s, w * (DK / 4) + 16 * m);
 #pragma unroll
-      for (int mm = 0; mm < MT; ++mm) {
-        const Frag<T> fk = ld_col<DK>(t.k, 32 * s, w * (DK / 4) + 16 * mm);
-#pragma unroll
-        for (int e = 0; e < NT; ++e)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) S[mm][i] = mma(fk, fv[i][e], S[mm][i]);
+        for (int e = 0; e < NT; ++e) S[m] = mma(fk, fv[e], S[m]);
       }
     }
     __syncthreads();
@@ -467,9 +475,7 @@ __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a, int units) {
   if constexpr (LOCAL) {
     float4* e = reinterpret_cast<float4*>(end_at(slot));
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) e[m * 2 + c] = make_float4(S[m][c][0], S[m][c][1], S[m][c][2], S[m][c][3]);
+    for (int m = 0; m < MT; ++m) e[m] = make_float4(S[m][0], S[m][1], S[m][2], S[m][3]);
     if (split == 0 && threadIdx.x == 0) a.segG[(long)slot * a.H + h] = (float)total;
   } else {
     float* out = REV ? a.dh0 : a.ht;
@@ -646,7 +652,7 @@ template <typename T>
 __device__ __forceinline__ void st_pairs(T* tile, int r, const Frag<T> (&f)[2]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    T* d = tile + sw16<64>(r, 16 * i + 4 * (lane_id() >> 4));
+    T* d = tile + swz<64>(r, 16 * i + 4 * (lane_id() >> 4));
     if constexpr (is_f32<T>::value) {
       const float* x = f[i / 2].x + 4 * (i & 1);
       *reinterpret_cast<float4*>(d) = make_float4(x[0], x[1], x[2], x[3]);
@@ -843,7 +849,7 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int col = 64 * n + 16 * i + 4 * (l >> 4);
-      const T *qr = t.q + sw16<DK>(r, col), *kr = t.k + sw16<DK>(r, col);
+      const T *qr = t.q + swz<DK>(r, col), *kr = t.k + swz<DK>(r, col);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         iq[i][e] *= eg;
@@ -1054,7 +1060,7 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int col = 16 * i + 4 * g4;
-      const T *qr = t.q + sw16<64>(r, col), *kr = t.k + sw16<64>(r, col);
+      const T *qr = t.q + swz<64>(r, col), *kr = t.k + swz<64>(r, col);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float x1 = eg * iq[i][e], y1 = tail * ik[i][e];
@@ -1220,11 +1226,11 @@ static hipError_t run_scan(const DecayArgs& a) {
   const long units = decay_slots(a, a.seglen) * a.H, ns = decay_splits(a.dv);
   if (units == 0) return hipSuccess;
   const long grid = (units + 7) / 8 * 8 * ns;
-  if (grid > INT32_MAX / 256) return hipErrorInvalidValue;
+  if (grid > INT32_MAX / SCAN_THREADS) return hipErrorInvalidValue;
   switch (decay_dkp(a.dk)) {
-    case 64: k_decay_scan<T, 64, REV, LOCAL, VEC><<<(unsigned)grid, 256, 0, a.stream>>>(a, (int)units); break;
-    case 128: k_decay_scan<T, 128, REV, LOCAL, VEC><<<(unsigned)grid, 256, 0, a.stream>>>(a, (int)units); break;
-    default: k_decay_scan<T, 256, REV, LOCAL, VEC><<<(unsigned)grid, 256, 0, a.stream>>>(a, (int)units); break;
+    case 64: k_decay_scan<T, 64, REV, LOCAL, VEC><<<(unsigned)grid, SCAN_THREADS, 0, a.stream>>>(a, (int)units); break;
+    case 128: k_decay_scan<T, 128, REV, LOCAL, VEC><<<(unsigned)grid, SCAN_THREADS, 0, a.stream>>>(a, (int)units); break;
+    default: k_decay_scan<T, 256, REV, LOCAL, VEC><<<(unsigned)grid, SCAN_THREADS, 0, a.stream>>>(a, (int)units); break;
   }
   return hipGetLastError();
 }
