@@ -278,6 +278,80 @@ __device__ __forceinline__ void split3(float x, float y, uint32_t& hi, uint32_t&
   split2(ax, ay, mid, lo);
 }
 
+// ---- kept states -------------------------------------------------------------------
+// A state [dv][dk] lies in blocks of 16 rows and CB columns, a block in the order in which
+// a wave's lanes hold it, 16 bytes a lane: lane p has row p % 16 and the p / 16-th piece of
+// the block's columns (bf16, 32 columns: in row8_col's order).  A wave so writes whole
+// lines; rows and columns behind the heads' sizes are kept too, as the zeros they are.
+template <typename T, int DK>
+struct StateLayout {
+  static constexpr int CB = is_f32<T>::value || DK == 64 ? 16 : 32;
+  static constexpr int E = 16 / (int)sizeof(T);  // values of a lane
+  static constexpr int PB = 16 * CB / E;         // pieces of a block
+  int blocks;                                    // side by side
+  unsigned bytes;
+  __device__ __forceinline__ StateLayout(int dk, int dv)
+      : blocks((dk + CB - 1) / CB), bytes((unsigned)(((dv + 15) & ~15) * blocks * CB) * (unsigned)sizeof(T)) {}
+  // byte offset of a block's piece p; what lies outside the state is behind its bytes
+  __device__ __forceinline__ unsigned at(int vblk, int cblk, int p) const {
+    return cblk < blocks ? (unsigned)((vblk * blocks + cblk) * PB + p) * 16u : BUF_OOB;
+  }
+  static __device__ __forceinline__ int col_of(int p) {  // first column of piece p in its block
+    const int g = p >> 4;
+    return E * (CB == 32 && E == 8 ? ((g & 1) << 1) | (g >> 1) : g);
+  }
+};
+// A tile of 64 rows (value columns) and COLS key columns of a kept state, through registers
+// into LDS.
+template <typename T, int DK, int COLS>
+struct StateTile {
+  typedef StateLayout<T, DK> L;
+  static constexpr int N = 64 * COLS / L::E / 256;
+  typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+  u32x4_t r[N];
+  static __device__ __forceinline__ void where(int i, int& vblk, int& cblk, int& p) {
+    const int idx = threadIdx.x + 256 * i, b = idx / L::PB;
+    p = idx % L::PB;
+    vblk = b / (COLS / L::CB);
+    cblk = b % (COLS / L::CB);
+  }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, const L& l, int v0, int c0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int vblk, cblk, p;
+      where(i, vblk, cblk, p);
+      r[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, l.at(v0 / 16 + vblk, c0 / L::CB + cblk, p), 0, 0));
+    }
+  }
+  __device__ __forceinline__ void store(T* tile) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int vblk, cblk, p;
+      where(i, vblk, cblk, p);
+      *reinterpret_cast<u32x4_t*>(tile + swz<COLS>(16 * vblk + (p & 15), L::CB * cblk + L::col_of(p))) = r[i];
+    }
+  }
+  // sum of the products with another tile
+  __device__ __forceinline__ float dot(const StateTile& o, float s) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (is_f32<T>::value) {
+          s = fmaf(__uint_as_float(r[i][e]), __uint_as_float(o.r[i][e]), s);
+        } else {
+          s = fmaf(__uint_as_float(r[i][e] << 16), __uint_as_float(o.r[i][e] << 16), s);
+          s = fmaf(__uint_as_float(r[i][e] & 0xFFFF0000u), __uint_as_float(o.r[i][e] & 0xFFFF0000u), s);
+        }
+      }
+    return s;
+  }
+};
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t state_rsrc(const void* kept, long slot_head, unsigned bytes) {
+  return clip_rsrc(const_cast<char*>(static_cast<const char*>(kept)) + slot_head * (long)bytes, bytes);
+}
+
 // ---- the scans ---------------------------------------------------------------------
 // A workgroup walks the chunks of one segment of one sequence and head, holds DC_BV value
 // columns of the state in fp32 accumulators (wave w: key rows (w % 4) DK / 4 .., columns
@@ -291,18 +365,23 @@ __device__ __forceinline__ void split3(float x, float y, uint32_t& hi, uint32_t&
 // products), not by what it moves: so two tiles in LDS, the next chunk being staged while
 // one is multiplied, one barrier a chunk, and loads two chunks ahead of their staging.
 constexpr int SCAN_THREADS = 512;
+// Keys; weighted values (bf16: three terms, fp32: both tiles' side by side).
 template <typename T, int DK>
-struct ScanTile {
-  static constexpr int VLD = is_f32<T>::value ? 64 : 128;  // weighted values (bf16: three terms)
-  T k[DC_CH * DK], v[DC_CH * VLD];
+struct ScanTiles {
+  static constexpr bool F32 = is_f32<T>::value;
+  static constexpr int VLD = F32 ? 64 : 128;
+  T key[2][DC_CH * DK], val[F32 ? 1 : 2][DC_CH * VLD];
+  float wts[2][DC_CH], fades[4];  // of chunk c: the rows' weights [c % 2], its decay [c % 4]
+  __device__ __forceinline__ T* v(int b) { return val[F32 ? 0 : b]; }
+  static __device__ __forceinline__ int col(int b) { return F32 ? 32 * b : 0; }
 };
 
 template <typename T, int DK, bool REV, bool LOCAL, bool VEC>
 __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int units) {
   constexpr bool F32 = is_f32<T>::value;
-  constexpr int VLD = ScanTile<T, DK>::VLD, NT = F32 ? 1 : 3;
+  constexpr int VLD = ScanTiles<T, DK>::VLD, NT = F32 ? 1 : 3;
   constexpr int MT = DK / 64;
-  __shared__ __align__(16) ScanTile<T, DK> tiles[2];
+  __shared__ __align__(16) ScanTiles<T, DK> t;
 
   // the splits of one head's state on one XCD (they read the same keys), heads dealt
   // over the XCDs
@@ -329,16 +408,24 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
   struct Inputs {
     Piece<T, 8, VEC> k[MT];
     Piece<T, 4, VEC> v;
-    Gates g;
   } in0, in1;
+  Gates g0, g1;
   const float ghead = a.g_head ? static_cast<const float*>(a.g)[h] : 0.f;
-  auto load = [&](Inputs& in, int it) {  // the it-th chunk of the walk
+  auto tokens = [&](int it, long& tok) {  // of the it-th chunk of the walk (behind the last one: none)
     const int c = REV ? nc - 1 - it : it;
-    const int m = it < nc ? min(DC_CH, n - c * DC_CH) : 0;  // (behind the last one: nothing)
-    const long tok = tok0 + (long)c * DC_CH;
+    tok = tok0 + (long)c * DC_CH;
+    return it < nc ? min(DC_CH, n - c * DC_CH) : 0;
+  };
+  auto load_gates = [&](Gates& g, int it) {  // (wave 0's: the others' lie behind the buffer)
+    long tok;
+    const int m = tokens(it, tok);
+    g.load(a, tok, h, wave == 0 ? m : 0);
+  };
+  auto load = [&](Inputs& in, int it) {
+    long tok;
+    const int m = tokens(it, tok);
     const auto rx = head_rows<T>(X, tok, xrow, (long)hx * a.dk, m, a.dk);
     const auto ry = head_rows<T>(Y, tok, yrow, (long)hv * a.dv, m, a.dv);
-    in.g.load(a, tok, h, m);
     load_piece(in.v, ry, threadIdx.x / 8, (unsigned)yrow * sizeof(T), j0 + threadIdx.x % 8 * 4, a.dv);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -346,6 +433,8 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
       load8(in.k[i], rx, idx / (DK / 8), (unsigned)xrow * sizeof(T), idx % (DK / 8) * 8, a.dk);
     }
   };
+  load_gates(g0, 0);
+  load_gates(g1, 1);
   load(in0, 0);
   load(in1, 1);
 
@@ -390,75 +479,90 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
     }
   }
 
+  // A chunk's decay and its rows' weights, by wave 0, a step before they are used
   double total = 0.;
-  auto stage = [&](ScanTile<T, DK>& t, const Inputs& in) {  // returns the chunk's decay
-    const double G = gate_sum(in.g.get(ghead)), Gend = read_lane(G, 63);
+  auto weigh = [&](const Gates& g, int it) {
+    if (wave != 0) return;
+    const double G = gate_sum(g.get(ghead)), Gend = read_lane(G, 63);
     total += Gend;
+    t.wts[it & 1][lane] = REV ? a.scale * __builtin_amdgcn_exp2f((float)G) : __builtin_amdgcn_exp2f((float)(Gend - G));
+    if (lane == 0) t.fades[it & 3] = __builtin_amdgcn_exp2f((float)Gend);
+  };
+  auto stage = [&](int b, const Inputs& in, int it) {  // into tile b
+    const float f = t.wts[it & 1][threadIdx.x / 8];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int idx = threadIdx.x + i * SCAN_THREADS;
-      st_row8<DK>(t.k, idx / (DK / 8), idx % (DK / 8) * 8, in.k[i]);
+      st_row8<DK>(t.key[b], idx / (DK / 8), idx % (DK / 8) * 8, in.k[i]);
     }
-    const float wt = REV ? a.scale * __builtin_amdgcn_exp2f((float)G) : __builtin_amdgcn_exp2f((float)(Gend - G));
-    const float f = __shfl(wt, 8 * wave + lane / 8);
-    const int row = threadIdx.x / 8, col = threadIdx.x % 8 * 4;
+    const int row = threadIdx.x / 8, col = threadIdx.x % 8 * 4 + t.col(b);
     const float x[4] = {f * in.v.get(0), f * in.v.get(1), f * in.v.get(2), f * in.v.get(3)};
     if constexpr (F32) {
-      st_row4<VLD>(t.v, row, col, floatx4{x[0], x[1], x[2], x[3]});
+      st_row4<VLD>(t.v(b), row, col, floatx4{x[0], x[1], x[2], x[3]});
     } else {
       uint2 y[3];
       split3(x[0], x[1], y[0].x, y[1].x, y[2].x);
       split3(x[2], x[3], y[0].y, y[1].y, y[2].y);
 #pragma unroll
-      for (int e = 0; e < 3; ++e) *reinterpret_cast<uint2*>(t.v + swz<VLD>(row, 32 * e + col)) = y[e];
+      for (int e = 0; e < 3; ++e) *reinterpret_cast<uint2*>(t.v(b) + swz<VLD>(row, 32 * e + col)) = y[e];
     }
-    return __builtin_amdgcn_exp2f((float)Gend);
   };
-  // The state before a chunk, [dv][dk]: a lane has four key rows of a column (two tiles:
-  // exchanged to eight in a row).  No store stands under a branch: what waits for the
-  // loads behind it counts the memory operations in between, and would count too few.
+  // The state before a chunk: a lane has four key rows of a value column (bf16: exchanged to
+  // eight in a row).  No store stands under a branch: what waits for the loads behind it
+  // counts the memory operations in between, and would count too few.
+  const StateLayout<T, DK> layout(a.dk, a.dv);
   const int kslot = first_slot(a, sq, DC_CH) + first / DC_CH;
+  const int vblk = (j0 + c0) / 16;
   auto keep = [&](int it) {
     const int c = REV ? nc - 1 - it : it;
-    T* to = static_cast<T*>(REV ? a.dkept : a.kept) + ((long)(kslot + c) * a.H + h) * a.dv * a.dk;
-    const auto rs = clip_rsrc(to, (unsigned)(a.dv * a.dk) * (unsigned)sizeof(T));  // (columns from dv on: dropped)
-    const unsigned at = (unsigned)(scol * a.dk) * (unsigned)sizeof(T);
-    if constexpr (VEC && !F32 && MT > 1) {
-      typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+    const auto rs = state_rsrc<T>(REV ? a.dkept : a.kept, (long)(kslot + c) * a.H + h, layout.bytes);
+    typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+    auto put = [&](int cblk, int p, uint4 y) {
+      __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{y.x, y.y, y.z, y.w}, rs, layout.at(vblk, cblk, p), 0, 0);
+    };
+    if constexpr (F32) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) put(w * MT + m, lane, __builtin_bit_cast(uint4, S[m]));
+    } else if constexpr (MT == 1) {
+      const uint32_t x = bf16_pair(S[0][0], S[0][1]), y = bf16_pair(S[0][2], S[0][3]);
+      const auto u = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+      const auto v = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+      // (both lanes of a pair have the eight: the odd ones store behind the state)
+      put(g4 & 1 ? layout.blocks : w, r16 + 16 * (g4 >> 1), make_uint4(u[0], v[0], u[1], v[1]));
+    } else {
 #pragma unroll
       for (int m = 0; m < MT; m += 2) {
         const floatx4 &u = S[m], &v = S[m + 1];
-        const uint4 y = row8_from_pieces(make_uint2(bf16_pair(u[0], u[1]), bf16_pair(u[2], u[3])),
-                                         make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])));
-        const int r = w * (DK / 4) + 16 * m + row8_col();
-        __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{y.x, y.y, y.z, y.w}, rs, r < a.dk ? at + 2 * r : BUF_OOB, 0, 0);
-      }
-    } else {
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const int r = row0 + 16 * m;
-        const float x[4] = {S[m][0], S[m][1], S[m][2], S[m][3]};
-        store_piece<T, 4, VEC>(rs, r < a.dk ? at + r * (unsigned)sizeof(T) : BUF_OOB, x, a.dk - r);
+        put(w * (MT / 2) + m / 2, lane,
+            row8_from_pieces(make_uint2(bf16_pair(u[0], u[1]), bf16_pair(u[2], u[3])),
+                             make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]))));
       }
     }
   };
-  float fade = stage(tiles[0], in0);
+  weigh(g0, 0);
+  weigh(g1, 1);
+  load_gates(g0, 2);
+  load_gates(g1, 3);
+  __syncthreads();
+  stage(0, in0, 0);
   load(in0, 2);
   __syncthreads();
-  auto step = [&](const ScanTile<T, DK>& t, ScanTile<T, DK>& next, Inputs& in, int it) {
-    const float f = fade;
-    fade = stage(next, in);
+  auto step = [&](int b, Inputs& in, Gates& g, int it) {
+    const float f = t.fades[it & 3];
+    stage(b ^ 1, in, it + 1);
     if (!LOCAL) keep(it);
     load(in, it + 3);
+    weigh(g, it + 2);
+    load_gates(g, it + 4);
     each([&](float x, int, int) { return x * f; });
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       Frag<T> fv[NT];
 #pragma unroll
-      for (int e = 0; e < NT; ++e) fv[e] = ld_col<VLD>(t.v, 32 * s, 32 * e + c0);
+      for (int e = 0; e < NT; ++e) fv[e] = ld_col<VLD>(t.v(b), 32 * s, 32 * e + c0 + t.col(b));
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        const Frag<T> fk = ld_col<DK>(t.k, 32 * s, w * (DK / 4) + 16 * m);
+        const Frag<T> fk = ld_col<DK>(t.key[b], 32 * s, w * (DK / 4) + 16 * m);
 #pragma unroll
         for (int e = 0; e < NT; ++e) S[m] = mma(fk, fv[e], S[m]);
       }
@@ -467,10 +571,10 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
   };
   int it = 0;
   for (; it + 1 < nc; it += 2) {
-    step(tiles[0], tiles[1], in1, it);
-    step(tiles[1], tiles[0], in0, it + 1);
+    step(0, in1, g0, it);
+    step(1, in0, g1, it + 1);
   }
-  if (it < nc) step(tiles[0], tiles[1], in1, it);
+  if (it < nc) step(0, in1, g0, it);
 
   if constexpr (LOCAL) {
     float4* e = reinterpret_cast<float4*>(end_at(slot));
@@ -515,13 +619,15 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
   const auto rq = head_rows<T>(a.q, tok, a.q_row, (long)(h / (a.H / a.Hq)) * dk, m, dk);
   const auto rk = head_rows<T>(a.k, tok, a.k_row, (long)(h / (a.H / a.Hk)) * dk, m, dk);
   const auto rv = head_rows<T>(a.v, tok, a.v_row, (long)(h / (a.H / a.Hv)) * dv, m, dv);
-  const auto rS = head_rows<T>(static_cast<const T*>(a.kept) + ((long)slot * a.H + h) * dv * dk, 0, dk, 0, dv, dk);
+  const StateLayout<T, DK> layout(dk, dv);
+  const auto rS = state_rsrc<T>(a.kept, (long)slot * a.H + h, layout.bytes);
   const auto ro = head_rows<T>(a.o, tok, (long)a.H * dv, (long)h * dv, m, dv);
   const unsigned bo = (unsigned)(a.H * dv) * (unsigned)sizeof(T);
 
   Gates gates;
   gates.load(a, tok, h, m);
-  Piece<T, 8, VEC> pk[KI], ps[KI], pv[2];
+  Piece<T, 8, VEC> pk[KI], pv[2];
+  StateTile<T, DK, DK> ps;
 #pragma unroll
   for (int i = 0; i < KI; ++i) {
     const int idx = threadIdx.x + 256 * i;
@@ -531,11 +637,7 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
 #pragma unroll
   for (int s = 0; s < KI; ++s) fq[s] = load_frag<T, VEC>(rq, 16 * w, (unsigned)a.q_row * sizeof(T), 32 * s, dk);
   auto load = [&](int v0) {  // a block of value columns
-#pragma unroll
-    for (int i = 0; i < KI; ++i) {
-      const int idx = threadIdx.x + 256 * i;
-      load8(ps[i], rS, v0 + idx / (DK / 8), (unsigned)dk * sizeof(T), idx % (DK / 8) * 8, dk);
-    }
+    ps.load(rS, layout, v0, 0);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int idx = threadIdx.x + 256 * i;
@@ -543,11 +645,7 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
     }
   };
   auto stage = [&] {
-#pragma unroll
-    for (int i = 0; i < KI; ++i) {
-      const int idx = threadIdx.x + 256 * i;
-      st_row8<DK>(t.s, idx / (DK / 8), idx % (DK / 8) * 8, ps[i]);
-    }
+    ps.store(t.s);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int idx = threadIdx.x + 256 * i;
@@ -734,14 +832,13 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
   const long tok = (long)sq.t0 + first;
   const int w = wave_id_s(), lane = lane_id(), r16 = lane & 15, g4 = lane >> 4, r = 16 * w + r16;
   const int dk = a.dk, dv = a.dv;
-  const long at = ((long)slot * a.H + h) * dv * dk;
-  const auto rS = head_rows<T>(static_cast<const T*>(a.kept) + at, 0, dk, 0, dv, dk);
-  const auto rD = head_rows<T>(static_cast<const T*>(a.dkept) + at, 0, dk, 0, dv, dk);
-  const unsigned bs = (unsigned)dk * sizeof(T);
+  const StateLayout<T, DK> layout(dk, dv);
+  const auto rS = state_rsrc<T>(a.kept, (long)slot * a.H + h, layout.bytes);
+  const auto rD = state_rsrc<T>(a.dkept, (long)slot * a.H + h, layout.bytes);
 
   Gates gates;
   gates.load(a, tok, h, m);
-  Rows64<T, 64, VEC> xs, xd;  // the states' next tile
+  StateTile<T, DK, 64> xs, xd;  // the states' next tile
   {
     Rows64<T, DK, VEC> q, k;
     Rows64<T, DV, VEC> o, v;
@@ -753,8 +850,8 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
     k.store(t.k);
     o.store(t.o);
     v.store(t.vs);
-    xs.load(rS, bs, 0, 0, dk);
-    xd.load(rD, bs, 0, 0, dk);
+    xs.load(rS, layout, 0, 0);
+    xd.load(rD, layout, 0, 0);
   }
   const double G = gate_sum(gates.get(a.g_head ? static_cast<const float*>(a.g)[h] : 0.f)), Gend = read_lane(G, 63);
   if (w == 0) {
@@ -816,14 +913,11 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
     for (int i = 0; i < 4; ++i) iq[i] = ik[i] = zero4();
 #pragma unroll
     for (int v = 0; v < DV / 64; ++v) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) carry = fmaf(xs.p[i].get(e), xd.p[i].get(e), carry);
+      carry = xs.dot(xd, carry);
       const bool last = v + 1 == DV / 64;
       if (!last || n + 1 < DK / 64) {
-        xs.load(rS, bs, last ? 0 : 64 * (v + 1), last ? 64 * (n + 1) : 64 * n, dk);
-        xd.load(rD, bs, last ? 0 : 64 * (v + 1), last ? 64 * (n + 1) : 64 * n, dk);
+        xs.load(rS, layout, last ? 0 : 64 * (v + 1), last ? 64 * (n + 1) : 64 * n);
+        xd.load(rD, layout, last ? 0 : 64 * (v + 1), last ? 64 * (n + 1) : 64 * n);
       }
       __syncthreads();
       const int l = fresh_lane();
@@ -943,10 +1037,10 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
   const auto rdo = head_rows<T>(a.dO, tok, (long)a.H * dv, (long)h * dv, m, dv);
   const unsigned bq = (unsigned)a.q_row * sizeof(T), bk = (unsigned)a.k_row * sizeof(T),
                  bv = (unsigned)a.v_row * sizeof(T), bo = (unsigned)(a.H * dv) * (unsigned)sizeof(T);
-  const long at = ((long)slot * a.H + h) * dv * dk;
-  const auto rS = head_rows<T>(static_cast<const T*>(a.kept) + at, 0, dk, 0, dv, dk);
-  const auto rD = head_rows<T>(static_cast<const T*>(a.dkept) + at, 0, dk, 0, dv, dk);
-  const unsigned bs = (unsigned)dk * sizeof(T);
+  typedef StateLayout<T, 256> Layout;  // (fp32: the same for every size)
+  const Layout layout(dk, dv);
+  const auto rS = state_rsrc<T>(a.kept, (long)slot * a.H + h, layout.bytes);
+  const auto rD = state_rsrc<T>(a.dkept, (long)slot * a.H + h, layout.bytes);
 
   Gates gates;
   gates.load(a, tok, h, m);
@@ -999,6 +1093,7 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
   };
   for (int c0 = 0; c0 < dk; c0 += 64) {
     Piece<T, 8, VEC> x[2], y[2];
+    StateTile<T, 256, 64> xs, xd;
     auto tile = [&](__amdgpu_buffer_rsrc_t rs, unsigned rb, int r0, int c, int d, Piece<T, 8, VEC>(&p)[2]) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -1022,21 +1117,18 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) aq[i] = ak[i] = iq[i] = ik[i] = zero4();
     for (int v0 = 0; v0 < dv; v0 += 64) {
-      tile(rS, bs, v0, c0, dk, x);
-      tile(rD, bs, v0, c0, dk, y);
+      xs.load(rS, layout, v0, c0);
+      xd.load(rD, layout, v0, c0);
       Frag<T> fo[2], fv[2];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         fo[s] = load_frag<T, VEC>(rdo, 16 * w, bo, v0 + 32 * s, dv);
         fv[s] = load_frag<T, VEC>(rv, 16 * w, bv, v0 + 32 * s, dv);
       }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) carry = fmaf(x[i].get(e), y[i].get(e), carry);
+      carry = xs.dot(xd, carry);
       if (v0 > 0) __syncthreads();
-      put_tile(t.s, x);
-      put_tile(t.d, y);
+      xs.store(t.s);
+      xd.store(t.d);
       __syncthreads();
       if (v0 == 0) {
 #pragma unroll
@@ -1074,6 +1166,19 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
     }
   }
   // ---- dv, 64 columns at a time
+  // rows v .. of the state's gradient, eight columns from s + 8 g4: two of a lane's pieces
+  auto state_frag = [&](int v, int s) {
+    const int col = s + 8 * g4;
+    Frag<T> f;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const auto u = __builtin_amdgcn_raw_buffer_load_b128(
+          rD, layout.at(v / 16, col / 16, (col % 16 / 4 + half) * 16 + r16), 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f.x[4 * half + e] = __uint_as_float(u[e]);
+    }
+    return f;
+  };
   for (int v0 = 0; v0 < dv; v0 += 64) {
     Piece<T, 8, VEC> x[2];
 #pragma unroll
@@ -1093,7 +1198,7 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
     for (int s = 0; s < dk; s += 32) {
       const Frag<T> f = load_frag<T, VEC>(rk, 16 * w, bk, s, dk);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) iv[i] = mma(load_frag<T, VEC>(rD, v0 + 16 * i, bs, s, dk), f, iv[i]);
+      for (int i = 0; i < 4; ++i) iv[i] = mma(state_frag(v0 + 16 * i, s), f, iv[i]);
     }
     __syncthreads();
 #pragma unroll
