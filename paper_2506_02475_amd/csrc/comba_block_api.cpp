@@ -56,16 +56,23 @@ comba_status check_rows(const comba_decay_shape* s, comba::DecayArgs* a, int64_t
   return COMBA_OK;
 }
 
-// Tokens of a segment.
+// Sequences that run as segments of `seglen` tokens side by side.  A scan's workgroup takes
+// 0.9 us a chunk alone, and the CUs together 1.2 us for a chunk of one workgroup each; the
+// first pass, which finds the segments' states, adds half of that and a launch.  So a
+// sequence is cut where its own walk is longer than two shares of a CU and some, into
+// segments of which every CU gets two.  Whole / cut, us of a forward, 16 heads of 128: one
+// row of 1,000 tokens 25 / 25, of 4,096 69 / 54, of 16,384 287 / 176; two rows of 4,096
+// 83 / 94, four 154 / 196; ten packed sequences of 1 to 15,777 tokens, 36,283 in all,
+// 430 / 412; 4 heads, one row of 65,536 791 / 184.  (Packed without host offsets: as
+// if one sequence had all tokens; what is shorter than a segment stays whole.)
 void cut(comba::DecayArgs* a, int64_t longest, bool* segments) {
   int dev = 0, cus = 0;
   if (hipGetDevice(&dev) != hipSuccess ||
       hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
     cus = 256;
-  const int64_t groups = (int64_t)a->H * comba::decay_splits(a->dv);
-  int64_t len = (int64_t)a->Ttot * groups / (2 * cus);
-  len = std::max<int64_t>((len + 63) / 64 * 64, 256);
-  *segments = longest > len && (a->cu_seqlens || a->S * groups < cus);
+  const int64_t share = (int64_t)a->Ttot * a->H * comba::decay_splits(a->dv) / cus;
+  const int64_t len = std::max<int64_t>((share / 2 + 63) / 64 * 64, 256);
+  *segments = longest > 2 * share + 600 && longest > len;
   a->seglen = *segments ? (int)len : a->cu_seqlens ? 1 << 30 : std::max(a->Tseq, 1);
 }
 

@@ -1244,15 +1244,26 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
 }
 
 // Gradients of shared heads: the sum over the state heads that share one, in their order.
-template <typename T>
-__global__ __launch_bounds__(256) void k_decay_shared(const float* __restrict__ p, T* __restrict__ out, long n, int heads,
-                                                      int per, int d) {
+// Four values a thread where the head's size allows (bf16, 16,384 tokens, 16 heads of 64 in
+// fp32 to 4: 22 us value by value).
+template <typename T, int C>
+__global__ __launch_bounds__(256) void k_decay_shared(const float* __restrict__ p, T* __restrict__ out, long n, int per,
+                                                      int d) {
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
-    const long th = i / d;
-    const float* from = p + (th / heads * heads + th % heads) * per * d + i % d;
-    float s = 0.f;
-    for (int k = 0; k < per; ++k) s += from[(long)k * d];
-    store_elem(out + i, s);
+    const unsigned w = (unsigned)(d / C);
+    const long head = i / w;
+    const float* from = p + head * per * d + (i - head * w) * C;
+    float s[C];
+#pragma unroll
+    for (int e = 0; e < C; ++e) s[e] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < per; ++k) {
+      Piece<float, C, true> x;
+      x.load(from + (long)k * d, C);
+#pragma unroll
+      for (int e = 0; e < C; ++e) s[e] += x.get(e);
+    }
+    store_piece<T, C, true>(out + i * C, s, C);
   }
 }
 
@@ -1371,10 +1382,11 @@ hipError_t launch_decay_fwd(const DecayArgs& a) { return a.bf16 ? run_fwd<bf16_t
 
 template <typename T>
 static hipError_t run_shared(const DecayArgs& a, const float* p, void* out, int heads, int d) {
-  const long n = (long)a.Ttot * heads * d;
-  const long grid = (n + 255) / 256;
-  k_decay_shared<T><<<(unsigned)(grid < 8192 ? grid : 8192), 256, 0, a.stream>>>(p, static_cast<T*>(out), n, heads,
-                                                                               a.H / heads, d);
+  const int c = d % 4 == 0 && (uintptr_t)out % (4 * sizeof(T)) == 0 ? 4 : 1;
+  const long n = (long)a.Ttot * heads * d / c, blocks = (n + 255) / 256;
+  const unsigned grid = (unsigned)(blocks < 16384 ? blocks : 16384);
+  if (c == 4) k_decay_shared<T, 4><<<grid, 256, 0, a.stream>>>(p, static_cast<T*>(out), n, a.H / heads, d);
+  else k_decay_shared<T, 1><<<grid, 256, 0, a.stream>>>(p, static_cast<T*>(out), n, a.H / heads, d);
   return hipGetLastError();
 }
 template <typename T, int DK, bool VEC>
