@@ -552,8 +552,6 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
     stage(b ^ 1, in, it + 1);
     if (!LOCAL) keep(it);
     load(in, it + 3);
-    weigh(g, it + 2);
-    load_gates(g, it + 4);
     each([&](float x, int, int) { return x * f; });
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -567,6 +565,8 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
         for (int e = 0; e < NT; ++e) S[m] = mma(fk, fv[e], S[m]);
       }
     }
+    weigh(g, it + 2);
+    load_gates(g, it + 4);
     __syncthreads();
   };
   int it = 0;
