@@ -62,38 +62,58 @@ def bind(lib):
 
 
 # ---- linear attention with a decay per head ------------------------------------------
+def _heads(name, t, lead, first, dtype, dev, far):
+    """(heads, head size, elements between token rows) of q, k or v."""
+    shape = t.shape
+    if len(shape) != lead + 2 or shape[:lead] != first or t.dtype is not dtype \
+            or t.get_device() != dev:
+        raise CombaError("comba: %s must be %s %s on the device"
+                         % (name, str(dtype).replace("torch.", ""), list(first) + ["heads", "d"]))
+    h, d = shape[-2], shape[-1]
+    if t.is_contiguous():
+        return h, d, 0
+    if lead == 1:  # (a step's common slice, without the general check's loops)
+        row, head, one = t.stride()
+        if one == 1 and head == d and row >= h * d:
+            return h, d, row
+    return h, d, _row(name, t, lead, shape, dtype, dev, far)
+
+
 def _decay_shape(lead, q, k, v, g, scale, N, cu, host):
     """(shape struct, pointers, (H, dk, dv)) of a call whose tensors have ``lead`` leading
     dimensions of tokens."""
     import torch
 
     code, dev, dt, f32 = _code(q, "q"), q.get_device(), q.dtype, torch.float32
-    qs, ks, vs, gs = q.shape, k.shape, v.shape, g.shape
-    if len(qs) != lead + 2 or len(ks) != lead + 2 or len(vs) != lead + 2 or qs[-1] != ks[-1]:
-        raise CombaError("comba: q, k and v must be [..,heads,d], q and k of one size")
-    first = qs[:lead]
+    far = None if lead == 1 else _SCAN_ROW
+    first, gs, gt = q.shape[:lead], g.shape, g.dtype
+    Hq, dk, q_row = _heads("q", q, lead, first, dt, dev, far)
+    Hk, dk2, k_row = _heads("k", k, lead, first, dt, dev, far)
+    Hv, dv, v_row = _heads("v", v, lead, first, dt, dev, far)
+    if dk != dk2:
+        raise CombaError("comba: q and k must have one head size")
     per_head = len(gs) == 1
     if not per_head and (len(gs) != lead + 1 or gs[:lead] != first):
         raise CombaError("comba: g must be [..,H], or [H] for constants of the heads")
-    H, Hq, Hk, Hv, dk, dv = gs[-1], qs[-2], ks[-2], vs[-2], qs[-1], vs[-1]
-    if min(H, Hq, Hk, Hv) < 1 or H % Hq or H % Hk or H % Hv:
+    H = gs[-1]
+    if H < 1 or Hq < 1 or Hk < 1 or Hv < 1 or H % Hq or H % Hk or H % Hv:
         raise CombaError("comba: the heads of q, k and v must divide those of g")
     if not (1 <= dk <= 256 and 1 <= dv <= 256):
         raise CombaError("comba: head sizes must be 1..256")
-    gt = g.dtype
     if gt is not f32 and (per_head or gt is not dt):
         raise CombaError("comba: g must be float32%s" % ("" if per_head else ", or of q's dtype"))
     if per_head:
         _dense("g", g, gs, f32, dev)
-    far = None if lead == 1 else _SCAN_ROW
     shp = _DECAY.pack(first[0], 1 if lead == 1 else first[1], H, Hq, Hk, Hv, dk, dv, N, cu,
                       _host_ptr(host), code, COMBA_F32 if gt is f32 else COMBA_BF16,
-                      1 if per_head else 0, dk ** -0.5 if scale is None else scale,
-                      0 if q.is_contiguous() else _row("q", q, lead, qs, dt, dev, far),
-                      _row("k", k, lead, first + (Hk, dk), dt, dev, far),
-                      _row("v", v, lead, first + (Hv, dv), dt, dev, far),
-                      0 if per_head else _row("g", g, lead, first + (H,), gt, dev, far))
+                      1 if per_head else 0, dk ** -0.5 if scale is None else scale, q_row, k_row,
+                      v_row, 0 if per_head else _row("g", g, lead, first + (H,), gt, dev, far))
     return shp, (q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr()), (H, dk, dv), dev
+
+
+def _outputs(v, H):
+    """An uninitialised contiguous o: as v, with H heads."""
+    return _like(v) if v.shape[-2] == H else v.new_empty(v.shape[:-2] + (H, v.shape[-1]))
 
 
 def _decay(save, q, k, v, g, h0, scale, cu_seqlens, cu_seqlens_host, output_final_state,
@@ -108,7 +128,7 @@ def _decay(save, q, k, v, g, h0, scale, cu_seqlens, cu_seqlens_host, output_fina
     shp, ptrs, (H, dk, dv), dev = _decay_shape(2, q, k, v, g, scale, S, cu, host)
     state = (S, H, dk, dv)
     h0p = _dense("h0", h0, state, torch.float32, dev)
-    o = q.new_empty(q.shape[:2] + (H, dv))
+    o = _outputs(v, H)
     ht = q.new_empty(state, dtype=torch.float32) if output_final_state else None
     ws = _workspace(lib.comba_decay_save_bytes if save else lib.comba_decay_fwd_workspace_bytes,
                     shp, workspace, q.device)
@@ -185,7 +205,7 @@ def comba_decay_step(q, k, v, g, state, *, slots=None, scale=None, stream=None):
         raise CombaError("comba: q must be [B,heads,dk] and state [S,H,dk,dv]")
     rows, pool = q.shape[0], state.shape[0]
     shp, ptrs, (H, dk, dv), dev = _decay_shape(1, q, k, v, g, scale, rows, 0, None)
-    o = q.new_empty((rows, H, dv))
+    o = _outputs(v, H)
     _run(load_library().comba_decay_step(
         shp, *ptrs, _dense("state", state, (pool, H, dk, dv), torch.float32, dev),
         _slots(slots, rows, dev), pool, o.data_ptr(), _on(stream, dev, o)))

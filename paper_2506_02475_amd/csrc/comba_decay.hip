@@ -1247,9 +1247,14 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
 // Four values a thread where the head's size allows (bf16, 16,384 tokens, 16 heads of 64 in
 // fp32 to 4: 22 us value by value).
 template <typename T, int C>
-__global__ __launch_bounds__(256) void k_decay_shared(const float* __restrict__ p, T* __restrict__ out, long n, int per,
+__global__ __launch_bounds__(256) void k_decay_shared(const float* __restrict__ p, T* __restrict__ out,
+                                                      const int32_t* __restrict__ cu, int S, int Ttot, int heads, int per,
                                                       int d) {
-  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
+  // (rows outside the sequences have no gradients and are left as they are)
+  const long row = (long)heads * d / C;
+  const long from_row = cu ? min(max(cu[0], 0), Ttot) : 0, to_row = cu ? min(max(cu[S], 0), Ttot) : Ttot;
+  const long n = to_row * row;
+  for (long i = from_row * row + (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
     const unsigned w = (unsigned)(d / C);
     const long head = i / w;
     const float* from = p + head * per * d + (i - head * w) * C;
@@ -1383,10 +1388,10 @@ hipError_t launch_decay_fwd(const DecayArgs& a) { return a.bf16 ? run_fwd<bf16_t
 template <typename T>
 static hipError_t run_shared(const DecayArgs& a, const float* p, void* out, int heads, int d) {
   const int c = d % 4 == 0 && (uintptr_t)out % (4 * sizeof(T)) == 0 ? 4 : 1;
-  const long n = (long)a.Ttot * heads * d / c, blocks = (n + 255) / 256;
+  const long blocks = ((long)a.Ttot * heads * d / c + 255) / 256;
   const unsigned grid = (unsigned)(blocks < 16384 ? blocks : 16384);
-  if (c == 4) k_decay_shared<T, 4><<<grid, 256, 0, a.stream>>>(p, static_cast<T*>(out), n, a.H / heads, d);
-  else k_decay_shared<T, 1><<<grid, 256, 0, a.stream>>>(p, static_cast<T*>(out), n, a.H / heads, d);
+  if (c == 4) k_decay_shared<T, 4><<<grid, 256, 0, a.stream>>>(p, static_cast<T*>(out), a.cu_seqlens, a.S, a.Ttot, heads, a.H / heads, d);
+  else k_decay_shared<T, 1><<<grid, 256, 0, a.stream>>>(p, static_cast<T*>(out), a.cu_seqlens, a.S, a.Ttot, heads, a.H / heads, d);
   return hipGetLastError();
 }
 template <typename T, int DK, bool VEC>

@@ -50,6 +50,11 @@ CASES = [
     ("segments", dict(B=1, T=1300, H=1, dk=64, dv=64, dht=True, tau=300.0)),
     ("segments_packed", dict(H=1, dk=64, dv=64, lens=[5, 700, 0, 900, 300], dht=True, tau=300.0)),
     ("segments_no_state", dict(B=2, T=600, H=1, dk=128, dv=32, h0=False, tau=300.0)),
+    ("segments_no_state_cut", dict(B=2, T=700, H=1, dk=128, dv=32, h0=False, tau=300.0)),
+    ("segments_d256", dict(B=1, T=900, H=1, dk=256, dv=200, dht=True, tau=300.0)),
+    ("segments_odd", dict(H=2, dk=33, dv=17, lens=[650, 1, 999], off=1, dht=True, tau=300.0)),
+    ("f32_d100_d200", dict(B=1, T=100, H=2, dk=100, dv=200, dtype="f32", dht=True)),
+    ("f32_wide_odd", dict(B=1, T=70, H=2, dk=201, dv=130, dtype="f32", off=1, dht=True)),
     ("f32", dict(B=2, T=150, H=2, dk=64, dv=64, dtype="f32", dht=True)),
     ("f32_d128", dict(B=1, T=90, H=2, dk=128, dv=128, dtype="f32")),
     ("f32_d256", dict(B=1, T=70, H=1, dk=256, dv=256, dtype="f32")),
