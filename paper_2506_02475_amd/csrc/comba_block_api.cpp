@@ -116,7 +116,7 @@ comba_status decay_args(const comba_decay_shape* s, comba::DecayArgs* a, bool* s
 }
 
 struct DecayLayout {
-  size_t kept, segS, segG, pq, pk, pv, total;
+  size_t kept, segS, segG, met, pq, pk, pv, total;
 };
 enum class Use { kFwd, kSave, kBwd };
 
@@ -138,6 +138,7 @@ DecayLayout decay_layout(const comba::DecayArgs& a, bool segments, Use use) {
   L.segG = take(slots * sizeof(float));
   if (use == Use::kBwd) {
     const size_t n = (size_t)a.Ttot * a.H * sizeof(float);
+    L.met = take((size_t)comba::decay_slots(a, comba::DC_CH) * a.H * comba::decay_splits(a.dv) * 8 * sizeof(float));
     L.pq = take(a.Hq < a.H ? n * a.dk : 0);
     L.pk = take(a.Hk < a.H ? n * a.dk : 0);
     L.pv = take(a.Hv < a.H ? n * a.dv : 0);
@@ -274,6 +275,7 @@ comba_status comba_decay_bwd(const comba_decay_shape* shape, const void* q, cons
   a.kept = const_cast<void*>(saved);
   a.dkept = base + L.kept;
   set_segments(&a, L, segments, base);
+  a.met = reinterpret_cast<float*>(base + L.met);
   a.pq = a.Hq < a.H ? reinterpret_cast<float*>(base + L.pq) : nullptr;
   a.pk = a.Hk < a.H ? reinterpret_cast<float*>(base + L.pk) : nullptr;
   a.pv = a.Hv < a.H ? reinterpret_cast<float*>(base + L.pv) : nullptr;

@@ -38,6 +38,7 @@ struct DecayArgs {
   void *dq, *dk_, *dv_, *dg;
   float* dh0;
   void* dkept;  // gradients of the states at every chunk's end, laid out as `kept`
+  float* met;  // [chunk slot][H][8 decay_splits] partial sums of both states' products
   float *pq, *pk, *pv;  // [tokens][H][d] gradients of shared heads before their sum, or NULL
   // sequences of more than seglen tokens run as segments of seglen (a multiple of 64)
   // side by side, each from its true state: per segment slot and head its end from
@@ -54,7 +55,7 @@ inline long decay_slots(const DecayArgs& a, long unit) {
 }
 // Padded size of the key dimension: of a scan's tiles.
 inline int decay_dkp(int dk) { return dk <= 64 ? 64 : dk <= 128 ? 128 : 256; }
-inline int decay_splits(int dv) { return (dv + DC_BV - 1) / DC_BV; }
+__host__ __device__ inline int decay_splits(int dv) { return (dv + DC_BV - 1) / DC_BV; }
 // Values of a kept state: rows (value columns) to 16, columns to a whole block.
 inline long decay_kept_values(const DecayArgs& a) {
   const int cb = !a.bf16 || a.dk <= 64 ? 16 : 32;

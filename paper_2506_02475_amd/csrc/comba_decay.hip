@@ -331,21 +331,6 @@ struct StateTile {
       *reinterpret_cast<u32x4_t*>(tile + swz<COLS>(16 * vblk + (p & 15), L::CB * cblk + L::col_of(p))) = r[i];
     }
   }
-  // sum of the products with another tile
-  __device__ __forceinline__ float dot(const StateTile& o, float s) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (is_f32<T>::value) {
-          s = fmaf(__uint_as_float(r[i][e]), __uint_as_float(o.r[i][e]), s);
-        } else {
-          s = fmaf(__uint_as_float(r[i][e] << 16), __uint_as_float(o.r[i][e] << 16), s);
-          s = fmaf(__uint_as_float(r[i][e] & 0xFFFF0000u), __uint_as_float(o.r[i][e] & 0xFFFF0000u), s);
-        }
-      }
-    return s;
-  }
 };
 template <typename T>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t state_rsrc(const void* kept, long slot_head, unsigned bytes) {
@@ -539,6 +524,50 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
       }
     }
   };
+  // REV, for dg: the products of the gradient that leaves a chunk (in fp32 here: of two states
+  // rounded to bf16 dg would have another half of a rounding's error) with the state that
+  // enters it, a partial sum for each wave.
+  struct Entering {
+    uint32_t r[MT][F32 ? 4 : 2];
+  } e0, e1;
+  auto load_state = [&](Entering& e, int it) {
+    const int c = REV ? nc - 1 - it : it;
+    const bool on = it < nc && a.dg;
+    const auto rs = state_rsrc<T>(a.kept, (long)(kslot + c) * a.H + h, layout.bytes);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      // (the lane's four key rows: as keep() left them)
+      if constexpr (F32) {
+        const auto u = __builtin_amdgcn_raw_buffer_load_b128(rs, on ? layout.at(vblk, w * MT + m, lane) : BUF_OOB, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e.r[m][i] = u[i];
+      } else {
+        const int o = MT == 1 ? g4 >> 1 : 2 * (m & 1) + (g4 >> 1), piece = MT == 1 ? o : ((o & 1) << 1) | (o >> 1);
+        const unsigned at = layout.at(vblk, MT == 1 ? w : w * (MT / 2) + m / 2, r16 + 16 * piece) + 8 * (g4 & 1);
+        const auto u = __builtin_amdgcn_raw_buffer_load_b64(rs, on ? at : BUF_OOB, 0, 0);
+        e.r[m][0] = u[0];
+        e.r[m][1] = u[1];
+      }
+    }
+  };
+  auto meet = [&](const Entering& e, int it) {
+    float s = 0.f;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t u = F32 ? e.r[m][i] : i & 1 ? e.r[m][i / 2] & 0xFFFF0000u : e.r[m][i / 2] << 16;
+        s = fmaf(S[m][i], __uint_as_float(u), s);
+      }
+    s = wave_sum(s);
+    const long at = ((long)(kslot + nc - 1 - it) * a.H + h) * NS * 8;
+    const auto rs = clip_rsrc(a.met + at, a.dg ? (unsigned)NS * 32u : 0u);
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(s), rs, lane == 0 ? (unsigned)(split * 8 + wave) * 4u : BUF_OOB, 0, 0);
+  };
+  if constexpr (REV && !LOCAL) {
+    load_state(e0, 0);
+    load_state(e1, 1);
+  }
   weigh(g0, 0);
   weigh(g1, 1);
   load_gates(g0, 2);
@@ -547,10 +576,14 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
   stage(0, in0, 0);
   load(in0, 2);
   __syncthreads();
-  auto step = [&](int b, Inputs& in, Gates& g, int it) {
+  auto step = [&](int b, Inputs& in, Gates& g, Entering& e, int it) {
     const float f = t.fades[it & 3];
     stage(b ^ 1, in, it + 1);
     if (!LOCAL) keep(it);
+    if constexpr (REV && !LOCAL) {
+      meet(e, it);
+      load_state(e, it + 2);
+    }
     load(in, it + 3);
     each([&](float x, int, int) { return x * f; });
 #pragma unroll
@@ -571,10 +604,10 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
   };
   int it = 0;
   for (; it + 1 < nc; it += 2) {
-    step(0, in1, g0, it);
-    step(1, in0, g1, it + 1);
+    step(0, in1, g0, e0, it);
+    step(1, in0, g1, e1, it + 1);
   }
-  if (it < nc) step(0, in1, g0, it);
+  if (it < nc) step(0, in1, g0, e0, it);
 
   if constexpr (LOCAL) {
     float4* e = reinterpret_cast<float4*>(end_at(slot));
@@ -721,7 +754,7 @@ struct GradTiles {
   static constexpr int VS = DV >= 128 ? DC_CH * DV : 2 * 64 * 64;
   T q[DC_CH * DK], k[DC_CH * DK], o[DC_CH * DV], vs[VS], w[DC_CH * DC_CH];
   Sums g;
-  float row[DC_CH], col[4][DC_CH], far[DC_CH], part[4];
+  float row[DC_CH], col[4][DC_CH], far[DC_CH];
 };
 
 // A tile of 64 rows, eight columns a piece: into registers, and from there into LDS.
@@ -905,7 +938,7 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
     else store4c<T, VEC>(rs, r, (unsigned)(a.H * d) * (unsigned)sizeof(T), col, d, x);
   };
   // ---- dq and dk, 64 columns at a time, and the states' part of dv
-  float xr = 0.f, yj = 0.f, carry = 0.f;
+  float xr = 0.f, yj = 0.f;
 #pragma unroll 1
   for (int n = 0; n < DK / 64; ++n) {
     floatx4 iq[4], ik[4];
@@ -913,7 +946,6 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
     for (int i = 0; i < 4; ++i) iq[i] = ik[i] = zero4();
 #pragma unroll
     for (int v = 0; v < DV / 64; ++v) {
-      carry = xs.dot(xd, carry);
       const bool last = v + 1 == DV / 64;
       if (!last || n + 1 < DK / 64) {
         xs.load(rS, layout, last ? 0 : 64 * (v + 1), last ? 64 * (n + 1) : 64 * n);
@@ -991,16 +1023,16 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
     t.row[r] = xr;
     t.far[r] = yj;
   }
-  carry = wave_sum(carry);
-  if (lane == 0) t.part[w] = carry;
   __syncthreads();
   if (w == 0) {
+    const int met = 8 * decay_splits(dv);  // partial sums of the states' products
+    float both = lane < met ? a.met[((long)slot * a.H + h) * met + lane] : 0.f;
+    both = __builtin_amdgcn_exp2f((float)Gend) * wave_sum(both);
     const int back = 63 - lane;  // lane l holds row 63 - l: suffix sums as prefix sums
     float x = wave_prefix_sum(t.row[back]);
     float y = wave_prefix_sum(t.far[lane]);
     y = __shfl_up(y, 1);
     x = __shfl(x, back);
-    const float both = __builtin_amdgcn_exp2f((float)Gend) * (((t.part[0] + t.part[1]) + t.part[2]) + t.part[3]);
     const float in = ((t.col[0][lane] + t.col[1][lane]) + t.col[2][lane]) + t.col[3][lane];
     const float dg = in + x + (lane > 0 ? y : 0.f) + both;
     if (lane < m) {
@@ -1017,7 +1049,7 @@ template <typename T>
 struct WideTiles {
   T q[DC_CH * 64], k[DC_CH * 64], s[64 * 64], d[64 * 64], w[DC_CH * DC_CH], p[DC_CH * DC_CH];
   Sums g;
-  float row[DC_CH], col[4][DC_CH], far[DC_CH], part[4];
+  float row[DC_CH], col[4][DC_CH], far[DC_CH];
 };
 
 template <typename T, bool VEC>
@@ -1079,7 +1111,7 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
   const Frag<T> fw[2] = {frag_of<T>(Bt[0], Bt[1]), frag_of<T>(Bt[2], Bt[3])};
 
   // ---- dq and dk, 64 columns at a time
-  float xr = 0.f, yj = 0.f, carry = 0.f;
+  float xr = 0.f, yj = 0.f;
   const long pq = (long)h * dk, pv = (long)h * dv;
   const auto oq = a.pq ? head_rows<float>(a.pq, tok, (long)a.H * dk, pq, m, dk)
                        : head_rows<T>(a.dq, tok, (long)a.H * dk, pq, m, dk);
@@ -1125,7 +1157,6 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
         fo[s] = load_frag<T, VEC>(rdo, 16 * w, bo, v0 + 32 * s, dv);
         fv[s] = load_frag<T, VEC>(rv, 16 * w, bv, v0 + 32 * s, dv);
       }
-      carry = xs.dot(xd, carry);
       if (v0 > 0) __syncthreads();
       xs.store(t.s);
       xd.store(t.d);
@@ -1223,16 +1254,16 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
     t.row[r] = xr;
     t.far[r] = yj;
   }
-  carry = wave_sum(carry);
-  if (lane == 0) t.part[w] = carry;
   __syncthreads();
   if (w == 0) {
+    const int met = 8 * decay_splits(dv);  // partial sums of the states' products
+    float both = lane < met ? a.met[((long)slot * a.H + h) * met + lane] : 0.f;
+    both = __builtin_amdgcn_exp2f((float)Gend) * wave_sum(both);
     const int back = 63 - lane;  // lane l holds row 63 - l: suffix sums as prefix sums
     float x = wave_prefix_sum(t.row[back]);
     float y = wave_prefix_sum(t.far[lane]);
     y = __shfl_up(y, 1);
     x = __shfl(x, back);
-    const float both = __builtin_amdgcn_exp2f((float)Gend) * (((t.part[0] + t.part[1]) + t.part[2]) + t.part[3]);
     const float in = ((t.col[0][lane] + t.col[1][lane]) + t.col[2][lane]) + t.col[3][lane];
     const float dg = in + x + (lane > 0 ? y : 0.f) + both;
     if (lane < m) {
