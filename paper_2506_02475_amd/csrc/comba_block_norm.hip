@@ -8,8 +8,10 @@
 //   dw2 = sum dn rh,  ds = sum dr' t,  dw1 = sum dp yh      (over the tokens)
 //
 // Bound by bytes: every value is read and written once.  A row lies in the registers
-// of a team (a wave, or a workgroup); a team walks rows with the next row's loads in
-// flight, and keeps the parameters and (backward) their gradients' sums in registers.
+// of a team (16 lanes, a wave, or a workgroup); a team walks rows with the next row's loads
+// in flight, and keeps the parameters and (backward) their gradients' sums in registers.
+// Gated, both norms, bf16: 16,384 rows of 4,096 channels forward 124 us (5.4 TB/s), backward
+// 247 and 5 for the sums (4.3 TB/s); of 2,048 with an fp32 stream forward 92 (5.1 TB/s).
 #include "comba_block_launch.h"
 #include "comba_layer_device.hpp"
 
@@ -24,7 +26,7 @@ constexpr int BN_WIDE = 1024;  // threads where a row does not fit registers
 template <int TEAM, int V>
 __device__ __forceinline__ void bn_sum(float (&x)[V], float (*lds)[2][16], int& turn) {
 #pragma unroll
-  for (int v = 0; v < V; ++v) x[v] = team_sum(x[v], 64);
+  for (int v = 0; v < V; ++v) x[v] = team_sum(x[v], TEAM < 64 ? TEAM : 64);
   if constexpr (TEAM > 64) {
     if (lane_id() == 0) {
 #pragma unroll
@@ -46,7 +48,7 @@ template <typename Tx, typename Ty, int KV, int C, int TEAM, bool BWD>
 __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void k_block_norm(BlockNormArgs a, int chunks) {
   __shared__ float lds[2][2][16];
   int turn = 0;
-  const int chunk = TEAM > 64 ? blockIdx.x : blockIdx.x * 4 + wave_id_s();
+  const int chunk = TEAM > 64 ? blockIdx.x : blockIdx.x * (256 / TEAM) + threadIdx.x / TEAM;
   const int l = threadIdx.x & (TEAM - 1);
   if (chunk >= chunks) return;  // whole teams
   const Tx *xt = static_cast<const Tx*>(a.x), *drt = static_cast<const Tx*>(a.dr);
@@ -190,68 +192,106 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void k_block_norm(BlockNorm
   }
 }
 
-// Rows too wide for registers: a workgroup a row, which reads it again from the caches;
-// the parameters' gradients are summed in its partial row.
-template <typename Tx, typename Ty, int C, bool BWD>
+// Rows whose values in fp32 do not fit registers: a workgroup a row, which forms them again
+// for every sum from what it loaded: KV pieces a thread, as they are, with the parameters'
+// gradients in registers (8,192 rows of 8,192 channels, forward and backward, 444 us; with
+// everything in fp32 it spilled, 861; with parameters loaded value by value 1,083); KV 0:
+// from the caches, those gradients in its partial row.
+template <typename Tx, typename Ty, int KV, int C, bool BWD>
 __global__ __launch_bounds__(BN_WIDE) void k_block_norm_wide(BlockNormArgs a, int chunks) {
   __shared__ float lds[2][2][16];
   int turn = 0;
+  constexpr int N = KV > 0 ? KV : 1;
   const int chunk = blockIdx.x;
   const Tx *xt = static_cast<const Tx*>(a.x), *drt = static_cast<const Tx*>(a.dr);
   const Ty *yt = static_cast<const Ty*>(a.y), *zt = static_cast<const Ty*>(a.z), *dnt = static_cast<const Ty*>(a.dn);
   const bool post = a.w1 != nullptr, pre = a.w2 != nullptr;
   const float inv = 1.f / a.C;
   float* part = BWD ? a.part + (long)chunk * 3 * a.C : nullptr;
-  // fn(first channel) for every piece of the thread
+  Piece<Ty, C, true> py[N], pz[N], pn[N];
+  Piece<Tx, C, true> px[N], pr[N];
+  float d1[N][C], ds[N][C], d2[N][C];
+  // fn(number, first channel) for every piece of the thread
   auto pieces = [&](auto fn) {
-    for (int c = threadIdx.x * C; c < a.C; c += BN_WIDE * C) fn(c);
+    if constexpr (KV > 0) {
+#pragma unroll
+      for (int k = 0; k < KV; ++k) {
+        const int c = (k * BN_WIDE + (int)threadIdx.x) * C;
+        if (c < a.C) fn(k, c);
+      }
+    } else {
+      for (int c = threadIdx.x * C; c < a.C; c += BN_WIDE * C) fn(0, c);
+    }
+  };
+  auto load_y = [&](long r, int k, int c) { py[k].load(yt + r * a.y_row + c, C); };
+  auto load_rest = [&](long r, int k, int c) {
+    if (zt) pz[k].load(zt + r * a.z_row + c, C);
+    if (xt) px[k].load(xt + r * a.x_row + c, C);
+    if constexpr (BWD) {
+      if (dnt) pn[k].load(dnt + r * a.C + c, C);
+      else pn[k].zero();
+      if (drt) pr[k].load(drt + r * a.C + c, C);
+    }
   };
   if constexpr (BWD) {
-    pieces([&](int c) {
-      for (int i = 0; i < C; ++i) part[c + i] = part[a.C + c + i] = part[2 * a.C + c + i] = 0.f;
+    pieces([&](int k, int c) {
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        if constexpr (KV > 0) d1[k][i] = ds[k][i] = d2[k][i] = 0.f;
+        else part[c + i] = part[a.C + c + i] = part[2 * a.C + c + i] = 0.f;
+      }
     });
   }
   for (long r = chunk; r < a.rows; r += chunks) {
     float r1 = 1.f, r2 = 0.f, m1 = 0.f, m2 = 0.f;
+    if constexpr (KV > 0) {
+      pieces([&](int k, int c) {
+        load_y(r, k, c);
+        load_rest(r, k, c);
+      });
+    }
     if (post) {
       float s[1] = {0.f};
-      pieces([&](int c) {
-        Piece<Ty, C, true> p;
-        p.load(yt + r * a.y_row + c, C);
+      pieces([&](int k, int c) {
+        if constexpr (KV == 0) load_y(r, k, c);
 #pragma unroll
-        for (int i = 0; i < C; ++i) s[0] = fmaf(p.get(i), p.get(i), s[0]);
+        for (int i = 0; i < C; ++i) s[0] = fmaf(py[k].get(i), py[k].get(i), s[0]);
       });
       bn_sum<BN_WIDE>(s, lds, turn);
       r1 = rsqrtf(s[0] * inv + a.eps);
     }
-    // fn(i, channel, yh, gate, its slope, stream) for every channel of a piece
-    auto stream = [&](int c, auto fn) {
-      Piece<Ty, C, true> p, pz;
-      Piece<Tx, C, true> px;
-      p.load(yt + r * a.y_row + c, C);
-      if (zt) pz.load(zt + r * a.z_row + c, C);
-      if (xt) px.load(xt + r * a.x_row + c, C);
+    // fn(i, channel, yh, gate, its slope, stream) for every channel of a piece, its
+    // parameters in w1, sc and w2
+    Piece<float, C, true> w1, sc, w2;
+    auto stream = [&](int k, int c, auto fn) {
+      if constexpr (KV == 0) {
+        load_y(r, k, c);
+        load_rest(r, k, c);
+      }
+      if (post) w1.load(a.w1 + c, C);
+      if (a.sc) sc.load(a.sc + c, C);
+      if (pre) w2.load(a.w2 + c, C);
+      else w2.zero();
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        if (!post) w1.r[i] = __float_as_uint(1.f);
+        if (!a.sc) sc.r[i] = __float_as_uint(1.f);
+      }
 #pragma unroll
       for (int i = 0; i < C; ++i) {
         float gate = 1.f, slope = 0.f;
-        if (zt) slope = act_slope(a.act, pz.get(i), gate);
-        const float yh = p.get(i) * r1, t = yh * (post ? a.w1[c + i] : 1.f) * gate;
-        fn(i, c + i, yh, gate, slope, fmaf(t, a.sc ? a.sc[c + i] : 1.f, xt ? px.get(i) : 0.f));
+        if (zt) slope = act_slope(a.act, pz[k].get(i), gate);
+        const float yh = py[k].get(i) * r1, t = yh * w1.get(i) * gate;
+        fn(i, c + i, yh, gate, slope, fmaf(t, sc.get(i), xt ? px[k].get(i) : 0.f));
       }
     };
-    auto dn_of = [&](int c, Piece<Ty, C, true>& p) {
-      if (dnt) p.load(dnt + r * a.C + c, C);
-      else p.zero();
-    };
     float s2[2] = {0.f, 0.f};
-    pieces([&](int c) {
-      Piece<Ty, C, true> pn;
-      if constexpr (BWD) dn_of(c, pn);
+    pieces([&](int k, int c) {
       float out[C];
-      stream(c, [&](int i, int at, float, float, float, float v) {
+      stream(k, c, [&](int i, int, float, float, float, float v) {
         out[i] = v;
         s2[0] = fmaf(v, v, s2[0]);
-        if constexpr (BWD) s2[1] = fmaf(pn.get(i) * (pre ? a.w2[at] : 0.f), v, s2[1]);
+        if constexpr (BWD) s2[1] = fmaf(pn[k].get(i) * w2.get(i), v, s2[1]);
       });
       if constexpr (!BWD) store_piece<Tx, C, true>(static_cast<Tx*>(a.r) + r * a.C + c, out, C);
     });
@@ -262,35 +302,33 @@ __global__ __launch_bounds__(BN_WIDE) void k_block_norm_wide(BlockNormArgs a, in
     }
     if constexpr (!BWD) {
       if (!pre) continue;
-      pieces([&](int c) {
+      pieces([&](int k, int c) {
         float n[C];
-        stream(c, [&](int i, int at, float, float, float, float v) { n[i] = v * r2 * a.w2[at]; });
+        stream(k, c, [&](int i, int, float, float, float, float v) { n[i] = v * r2 * w2.get(i); });
         store_piece<Ty, C, true>(static_cast<Ty*>(a.n) + r * a.C + c, n, C);
       });
     } else {
       // fn(i, channel, yh, dn rh, dr', t, dz, dp) for every channel of a piece
-      auto grad = [&](int c, auto fn) {
-        Piece<Ty, C, true> pn;
-        Piece<Tx, C, true> pr;
-        dn_of(c, pn);
-        if (drt) pr.load(drt + r * a.C + c, C);
-        stream(c, [&](int i, int at, float yh, float gate, float slope, float v) {
-          const float rh = v * r2, dn = pn.get(i);
-          const float dr = (drt ? pr.get(i) : 0.f) + r2 * (dn * (pre ? a.w2[at] : 0.f) - rh * m2);
-          const float p = yh * (post ? a.w1[at] : 1.f), dt = dr * (a.sc ? a.sc[at] : 1.f);
+      auto grad = [&](int k, int c, auto fn) {
+        stream(k, c, [&](int i, int at, float yh, float gate, float slope, float v) {
+          const float rh = v * r2, dn = pn[k].get(i);
+          const float dr = (drt ? pr[k].get(i) : 0.f) + r2 * (dn * w2.get(i) - rh * m2);
+          const float p = yh * w1.get(i), dt = dr * sc.get(i);
           fn(i, at, yh, dn * rh, dr, p * gate, dt * p * slope, dt * gate);
         });
       };
       float s1[1] = {0.f};
-      pieces([&](int c) {
+      pieces([&](int k, int c) {
         float dx[C], dz[C];
-        grad(c, [&](int i, int at, float yh, float dw2, float dr, float t, float d, float dp) {
+        grad(k, c, [&](int i, int at, float yh, float dw2, float dr, float t, float d, float dp) {
           dx[i] = dr;
           dz[i] = d;
-          s1[0] = fmaf(dp * (post ? a.w1[at] : 1.f), yh, s1[0]);
-          part[at] = fmaf(dp, yh, part[at]);
-          part[a.C + at] = fmaf(dr, t, part[a.C + at]);
-          part[2 * a.C + at] += dw2;
+          s1[0] = fmaf(dp * w1.get(i), yh, s1[0]);
+          float &g1 = KV > 0 ? d1[k][i] : part[at], &gs = KV > 0 ? ds[k][i] : part[a.C + at],
+                &g2 = KV > 0 ? d2[k][i] : part[2 * a.C + at];
+          g1 = fmaf(dp, yh, g1);
+          gs = fmaf(dr, t, gs);
+          g2 += dw2;
         });
         if (zt) store_piece<Ty, C, true>(static_cast<Ty*>(a.dz) + r * a.C + c, dz, C);
         if (a.dx) store_piece<Tx, C, true>(static_cast<Tx*>(a.dx) + r * a.C + c, dx, C);
@@ -299,14 +337,24 @@ __global__ __launch_bounds__(BN_WIDE) void k_block_norm_wide(BlockNormArgs a, in
         bn_sum<BN_WIDE>(s1, lds, turn);
         m1 = s1[0] * inv;
       }
-      pieces([&](int c) {
+      pieces([&](int k, int c) {
         float dy[C];
-        grad(c, [&](int i, int at, float yh, float, float, float, float, float dp) {
-          dy[i] = r1 * (dp * (post ? a.w1[at] : 1.f) - yh * m1);
+        grad(k, c, [&](int i, int, float yh, float, float, float, float, float dp) {
+          dy[i] = r1 * (dp * w1.get(i) - yh * m1);
         });
         store_piece<Ty, C, true>(static_cast<Ty*>(a.dy) + r * a.C + c, dy, C);
       });
     }
+  }
+  if constexpr (BWD && KV > 0) {
+    pieces([&](int k, int c) {
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        part[c + i] = d1[k][i];
+        part[a.C + c + i] = ds[k][i];
+        part[2 * a.C + c + i] = d2[k][i];
+      }
+    });
   }
 }
 
@@ -331,26 +379,30 @@ __global__ __launch_bounds__(64 * BN_WAVES) void k_block_norm_dw(BlockNormArgs a
   }
 }
 
-// The team of a row, and how many teams walk the rows.
+// The team of a row, and how many teams walk the rows: 1,024 lanes per CU, or 512 in
+// the backward where a lane has two pieces, whose registers hold no more at once (bf16,
+// gated, both norms, whole forward and backward, 512 / 1,024 / 2,048 lanes: 65,536 rows of
+// 512 channels 186 / 206 / 230 us, 16,384 of 2,048 183 / 191 / 204; one piece, 32,768 of
+// 1,024 205 / 183 / 199).
 struct BnTeam {
   int team, kv, chunks;
 };
-static BnTeam bn_team(const BlockNormArgs& a) {
+static BnTeam bn_team(const BlockNormArgs& a, bool bwd) {
   BnTeam t;
   const int pieces = (a.C + BN_C - 1) / BN_C;
-  t.team = pieces <= 128 ? 64 : pieces <= 512 ? 256 : pieces <= 1024 ? 512 : 1024;
+  t.team = pieces <= 32 ? 16 : pieces <= 128 ? 64 : pieces <= 512 ? 256 : pieces <= 1024 ? 512 : 1024;
   t.kv = pieces <= t.team ? 1 : pieces <= 2 * t.team ? 2 : 0;
-  const long chunks = 256L * 1024 / t.team;
+  const long lanes = bwd && t.kv == 2 && t.team < 1024 ? 512 : 1024, chunks = 256L * lanes / t.team;
   t.chunks = (int)(chunks > a.rows ? a.rows : chunks);
   return t;
 }
-int block_norm_bwd_blocks(const BlockNormArgs& a) { return a.rows > 0 ? bn_team(a).chunks : 0; }
+int block_norm_bwd_blocks(const BlockNormArgs& a) { return a.rows > 0 ? bn_team(a, true).chunks : 0; }
 
 template <typename Tx, typename Ty, bool BWD>
 static hipError_t run_block_norm(const BlockNormArgs& a0) {
   BlockNormArgs a = a0;
   if (a.rows > 0) {
-    const BnTeam t = bn_team(a);
+    const BnTeam t = bn_team(a, BWD);
     a.blocks = t.chunks;
     auto ok = [&](const void* p, size_t eb, long row) {
       return !p || ((uintptr_t)p % (BN_C * eb) == 0 && row % BN_C == 0);
@@ -358,20 +410,28 @@ static hipError_t run_block_norm(const BlockNormArgs& a0) {
     const bool vec = a.C % BN_C == 0 && ok(a.y, sizeof(Ty), a.y_row) && ok(a.z, sizeof(Ty), a.z_row) &&
                      ok(a.x, sizeof(Tx), a.x_row) && ok(a.r, sizeof(Tx), 0) && ok(a.n, sizeof(Ty), 0) &&
                      ok(a.dr, sizeof(Tx), 0) && ok(a.dn, sizeof(Ty), 0) && ok(a.dy, sizeof(Ty), 0) &&
-                     ok(a.dx, sizeof(Tx), 0) && ok(a.dz, sizeof(Ty), 0);
-    const unsigned grid = t.team > 64 ? t.chunks : (t.chunks + 3) / 4;
+                     ok(a.dx, sizeof(Tx), 0) && ok(a.dz, sizeof(Ty), 0) && ok(a.w1, 4, 0) && ok(a.sc, 4, 0) &&
+                     ok(a.w2, 4, 0);
+    const int each = t.team > 64 ? 1 : 256 / t.team;  // teams of a workgroup
+    const unsigned grid = (t.chunks + each - 1) / each;
 #define BN_LAUNCH(KV, TEAM)                                                                              \
   if (vec) k_block_norm<Tx, Ty, KV, BN_C, TEAM, BWD><<<grid, TEAM > 64 ? TEAM : 256, 0, a.stream>>>(a, t.chunks); \
   else k_block_norm<Tx, Ty, KV * BN_C, 1, TEAM, BWD><<<grid, TEAM > 64 ? TEAM : 256, 0, a.stream>>>(a, t.chunks);
-    if (t.team == 64 && t.kv == 1) { BN_LAUNCH(1, 64) }
+    if (t.team == 16 && t.kv == 1) { BN_LAUNCH(1, 16) }
+    else if (t.team == 16) { BN_LAUNCH(2, 16) }
+    else if (t.team == 64 && t.kv == 1) { BN_LAUNCH(1, 64) }
     else if (t.team == 64) { BN_LAUNCH(2, 64) }
     else if (t.team == 256 && t.kv == 1) { BN_LAUNCH(1, 256) }
     else if (t.team == 256) { BN_LAUNCH(2, 256) }
     else if (t.team == 512) { BN_LAUNCH(2, 512) }
-    else if (t.kv) { BN_LAUNCH(2, 1024) }
 #undef BN_LAUNCH
-    else if (vec) k_block_norm_wide<Tx, Ty, BN_C, BWD><<<grid, BN_WIDE, 0, a.stream>>>(a, t.chunks);
-    else k_block_norm_wide<Tx, Ty, 1, BWD><<<grid, BN_WIDE, 0, a.stream>>>(a, t.chunks);
+    else if (t.kv && !BWD && vec) k_block_norm<Tx, Ty, 2, BN_C, 1024, false><<<grid, 1024, 0, a.stream>>>(a, t.chunks);
+#define BN_LAUNCH(KV, C) k_block_norm_wide<Tx, Ty, KV, C, BWD><<<grid, BN_WIDE, 0, a.stream>>>(a, t.chunks)
+    else if (t.kv && vec) BN_LAUNCH(2, BN_C);
+    else if (t.kv) BN_LAUNCH(8, 1);
+    else if (vec) BN_LAUNCH(0, BN_C);
+    else BN_LAUNCH(0, 1);
+#undef BN_LAUNCH
   }
   if (BWD && (a.dw1 || a.dsc || a.dw2))
     k_block_norm_dw<<<dim3((unsigned)((a.C + 63) / 64), 3), 64 * BN_WAVES, 0, a.stream>>>(a);
