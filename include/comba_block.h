@@ -43,14 +43,19 @@ typedef struct {
  *   q [B,T,Hq,dk], k [B,T,Hk,dk], v [B,T,Hv,dv], o [B,T,H,dv] in_dtype; g [B,T,H] or
  *   [H] log-decays; h0, ht [num_seqs,H,dk,dv] fp32 or NULL.
  * g = -inf starts a state anew; log-decays below -128 count as -128, whose decay
- * is zero in fp32.  A NaN or Inf in q, k or v makes outputs of its own sequence and
- * head non-finite, up to 63 tokens before its own among them.
+ * is zero in fp32.  A NaN or Inf in an input makes outputs of its own sequence and
+ * head non-finite, up to 63 tokens before its own among them (gradients: behind it).
  * bf16: products of operands rounded to bf16, summed in fp32 (o within about two
  * roundings to bf16); the states keep fp32.
- * The workspace holds comba_decay_fwd_workspace_bytes.  The saving form's holds
- * comba_decay_save_bytes and keeps the state at every 64th token in in_dtype:
- * comba_decay_bwd takes it as `saved`, unmodified, together with the same shape and
- * inputs and a workspace of its own (comba_decay_bwd_workspace_bytes).
+ * The workspace holds comba_decay_fwd_workspace_bytes, the state at every 64th token
+ * in in_dtype among them.  The saving form's holds comba_decay_save_bytes and keeps
+ * those: comba_decay_bwd takes it as `saved`, unmodified, together with the same shape
+ * and inputs and a workspace of its own (comba_decay_bwd_workspace_bytes).
+ * Limits: H max(dk, dv) up to 2^22; pieces of 64 tokens (a sequence's last one may be
+ * partial) times H, and sequences times H times dv / 32, below 2^31 / 512.
+ * Long sequences are cut into segments that run side by side where that is faster; the
+ * choice follows from the shape, the host offsets and the device, and changes results
+ * by roundings only.  Every sum runs in an order fixed by that choice.
  */
 size_t comba_decay_fwd_workspace_bytes(const comba_decay_shape *shape);
 size_t comba_decay_save_bytes(const comba_decay_shape *shape);

@@ -379,30 +379,30 @@ __global__ __launch_bounds__(64 * BN_WAVES) void k_block_norm_dw(BlockNormArgs a
   }
 }
 
-// The team of a row, and how many teams walk the rows: 1,024 lanes per CU, or 512 in
-// the backward where a lane has two pieces, whose registers hold no more at once (bf16,
-// gated, both norms, whole forward and backward, 512 / 1,024 / 2,048 lanes: 65,536 rows of
-// 512 channels 186 / 206 / 230 us, 16,384 of 2,048 183 / 191 / 204; one piece, 32,768 of
-// 1,024 205 / 183 / 199).
+// The team of a row, and how many teams walk the rows: 1,024 lanes per CU, or 512 where a
+// lane has two pieces, whose loads in flight are enough at that (bf16, gated, both norms,
+// 512 / 1,024 / 2,048 lanes: 65,536 rows of 512 channels forward 64 / 69 / 66 us, forward and
+// backward 186 / 206 / 230; 16,384 of 2,048 65 / 71 / 69 and 183 / 191 / 204; one piece, 32,768
+// of 1,024 73 / 64 / 68 and 205 / 183 / 199).
 struct BnTeam {
   int team, kv, chunks;
 };
-static BnTeam bn_team(const BlockNormArgs& a, bool bwd) {
+static BnTeam bn_team(const BlockNormArgs& a) {
   BnTeam t;
   const int pieces = (a.C + BN_C - 1) / BN_C;
   t.team = pieces <= 32 ? 16 : pieces <= 128 ? 64 : pieces <= 512 ? 256 : pieces <= 1024 ? 512 : 1024;
   t.kv = pieces <= t.team ? 1 : pieces <= 2 * t.team ? 2 : 0;
-  const long lanes = bwd && t.kv == 2 && t.team < 1024 ? 512 : 1024, chunks = 256L * lanes / t.team;
+  const long lanes = t.kv == 2 && t.team < 1024 ? 512 : 1024, chunks = 256L * lanes / t.team;
   t.chunks = (int)(chunks > a.rows ? a.rows : chunks);
   return t;
 }
-int block_norm_bwd_blocks(const BlockNormArgs& a) { return a.rows > 0 ? bn_team(a, true).chunks : 0; }
+int block_norm_bwd_blocks(const BlockNormArgs& a) { return a.rows > 0 ? bn_team(a).chunks : 0; }
 
 template <typename Tx, typename Ty, bool BWD>
 static hipError_t run_block_norm(const BlockNormArgs& a0) {
   BlockNormArgs a = a0;
   if (a.rows > 0) {
-    const BnTeam t = bn_team(a, BWD);
+    const BnTeam t = bn_team(a);
     a.blocks = t.chunks;
     auto ok = [&](const void* p, size_t eb, long row) {
       return !p || ((uintptr_t)p % (BN_C * eb) == 0 && row % BN_C == 0);
