@@ -121,8 +121,7 @@ struct DecayLayout {
 enum class Use { kFwd, kSave, kBwd };
 
 size_t kept_bytes(const comba::DecayArgs& a) {
-  return (size_t)comba::decay_slots(a, comba::DC_CH) * a.H * comba::decay_kept_values(a) *
-         (a.bf16 ? 2 : 4);
+  return (size_t)comba::decay_slots(a, comba::DC_CH) * a.H * comba::state_bytes(a.bf16, a.dk, a.dv);
 }
 DecayLayout decay_layout(const comba::DecayArgs& a, bool segments, Use use) {
   DecayLayout L{};

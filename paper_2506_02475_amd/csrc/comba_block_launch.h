@@ -24,7 +24,7 @@ struct DecayArgs {
   const float* h0;
   void* o;
   float* ht;
-  // states at every chunk's start, [chunk slot][H][decay_kept_values] in in_dtype: written,
+  // states at every chunk's start, [chunk slot][H][state_bytes]: written,
   // read; a sequence's slots start at start / 64 + its number (fixed rows: at
   // its number times the row's chunks)
   void* kept;
@@ -56,10 +56,11 @@ inline long decay_slots(const DecayArgs& a, long unit) {
 // Padded size of the key dimension: of a scan's tiles.
 inline int decay_dkp(int dk) { return dk <= 64 ? 64 : dk <= 128 ? 128 : 256; }
 __host__ __device__ inline int decay_splits(int dv) { return (dv + DC_BV - 1) / DC_BV; }
-// Values of a kept state: rows (value columns) to 16, columns to a whole block.
-inline long decay_kept_values(const DecayArgs& a) {
-  const int cb = !a.bf16 || a.dk <= 64 ? 16 : 32;
-  return (long)((a.dv + 15) / 16 * 16) * ((a.dk + cb - 1) / cb * cb);
+// Bytes of a kept state: blocks of 16 rows (value columns), a scale for each, to 16.
+__host__ __device__ inline long state_bytes(bool bf16, int dk, int dv) {
+  const int cb = !bf16 || dk <= 64 ? 16 : 32;
+  const long blocks = (long)((dv + 15) / 16) * ((dk + cb - 1) / cb);
+  return blocks * 16 * cb * (bf16 ? 2 : 4) + (blocks * 4 + 15) / 16 * 16;
 }
 // Floats of one segment's end: every split's accumulators.
 inline long decay_end_floats(const DecayArgs& a) {

@@ -283,18 +283,43 @@ __device__ __forceinline__ void split3(float x, float y, uint32_t& hi, uint32_t&
 // a wave's lanes hold it, 16 bytes a lane: lane p has row p % 16 and the p / 16-th piece of
 // the block's columns (bf16, 32 columns: in row8_col's order).  A wave so writes whole
 // lines; rows and columns behind the heads' sizes are kept too, as the zeros they are.
+// bf16: the entering states are kept as fp16 with one power-of-two scale a block (the scales
+// behind the blocks), the gradients as bf16.  The products take both rounded to bf16, but
+// dg's part from both directions, <dS', S>, takes S as kept: a rounding of S to bf16
+// alone would put dg's error at 1.4 roundings, fp16's (an eighth, down to 2^-29 of a
+// block's largest) vanishes beside dg's own.
+// Four values by 1 / scale as fp16, and back; the scale takes a block's largest, m, to
+// [2^14, 2^15), and is NaN where m is not finite.
+__device__ __forceinline__ float half_inv_scale(float m) { return __int_as_float((142 - q_exponent(m)) << 23); }
+__device__ __forceinline__ uint2 pack_half4(const floatx4& x, float inv) {
+  typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+  const f16x4 h = {(_Float16)(x[0] * inv), (_Float16)(x[1] * inv), (_Float16)(x[2] * inv), (_Float16)(x[3] * inv)};
+  return __builtin_bit_cast(uint2, h);
+}
+__device__ __forceinline__ float4 unpack_half4(uint2 u, float s) {
+  typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+  const f16x4 h = __builtin_bit_cast(f16x4, u);
+  return make_float4((float)h[0] * s, (float)h[1] * s, (float)h[2] * s, (float)h[3] * s);
+}
 template <typename T, int DK>
 struct StateLayout {
   static constexpr int CB = is_f32<T>::value || DK == 64 ? 16 : 32;
   static constexpr int E = 16 / (int)sizeof(T);  // values of a lane
   static constexpr int PB = 16 * CB / E;         // pieces of a block
-  int blocks;                                    // side by side
-  unsigned bytes;
+  int blocks;           // side by side
+  unsigned data, bytes; // the blocks', with their scales
   __device__ __forceinline__ StateLayout(int dk, int dv)
-      : blocks((dk + CB - 1) / CB), bytes((unsigned)(((dv + 15) & ~15) * blocks * CB) * (unsigned)sizeof(T)) {}
+      : blocks((dk + CB - 1) / CB), data((unsigned)(((dv + 15) & ~15) * blocks * CB) * (unsigned)sizeof(T)),
+        bytes((unsigned)state_bytes(!is_f32<T>::value, dk, dv)) {}
+  // byte offset of a block's scale
+  __device__ __forceinline__ unsigned scale_at(int vblk, int cblk) const {
+    const unsigned b = (unsigned)(vblk * blocks + cblk);
+    return cblk < blocks && b * (PB * 16u) < data ? data + b * 4u : BUF_OOB;
+  }
   // byte offset of a block's piece p; what lies outside the state is behind its bytes
   __device__ __forceinline__ unsigned at(int vblk, int cblk, int p) const {
-    return cblk < blocks ? (unsigned)((vblk * blocks + cblk) * PB + p) * 16u : BUF_OOB;
+    const unsigned off = (unsigned)((vblk * blocks + cblk) * PB + p) * 16u;
+    return cblk < blocks && off < data ? off : BUF_OOB;
   }
   static __device__ __forceinline__ int col_of(int p) {  // first column of piece p in its block
     const int g = p >> 4;
@@ -303,12 +328,15 @@ struct StateLayout {
 };
 // A tile of 64 rows (value columns) and COLS key columns of a kept state, through registers
 // into LDS.
-template <typename T, int DK, int COLS>
+// (ENTERS: an entering state, as fp16.)
+template <typename T, int DK, int COLS, bool ENTERS>
 struct StateTile {
   typedef StateLayout<T, DK> L;
+  static constexpr bool Q = ENTERS && !is_f32<T>::value;
   static constexpr int N = 64 * COLS / L::E / 256;
   typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
   u32x4_t r[N];
+  float scale[Q ? N : 1];
   static __device__ __forceinline__ void where(int i, int& vblk, int& cblk, int& p) {
     const int idx = threadIdx.x + 256 * i, b = idx / L::PB;
     p = idx % L::PB;
@@ -320,7 +348,11 @@ struct StateTile {
     for (int i = 0; i < N; ++i) {
       int vblk, cblk, p;
       where(i, vblk, cblk, p);
-      r[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, l.at(v0 / 16 + vblk, c0 / L::CB + cblk, p), 0, 0));
+      vblk += v0 / 16;
+      cblk += c0 / L::CB;
+      r[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, l.at(vblk, cblk, p), 0, 0));
+      if constexpr (Q)
+        scale[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, l.scale_at(vblk, cblk), 0, 0));
     }
   }
   __device__ __forceinline__ void store(T* tile) const {
@@ -328,7 +360,16 @@ struct StateTile {
     for (int i = 0; i < N; ++i) {
       int vblk, cblk, p;
       where(i, vblk, cblk, p);
-      *reinterpret_cast<u32x4_t*>(tile + swz<COLS>(16 * vblk + (p & 15), L::CB * cblk + L::col_of(p))) = r[i];
+      u32x4_t x = r[i];
+      if constexpr (Q) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float4 y = unpack_half4(make_uint2(x[2 * e], x[2 * e + 1]), scale[i]);
+          x[2 * e] = bf16_pair(y.x, y.y);
+          x[2 * e + 1] = bf16_pair(y.z, y.w);
+        }
+      }
+      *reinterpret_cast<u32x4_t*>(tile + swz<COLS>(16 * vblk + (p & 15), L::CB * cblk + L::col_of(p))) = x;
     }
   }
 };
@@ -505,22 +546,31 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
     auto put = [&](int cblk, int p, uint4 y) {
       __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{y.x, y.y, y.z, y.w}, rs, layout.at(vblk, cblk, p), 0, 0);
     };
+    // four values as bf16; forward: as fp16 by the block's scale, which one lane stores
+    auto pack = [&](const floatx4& x, float inv) {
+      return REV ? make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])) : pack_half4(x, inv);
+    };
+    auto scaled = [&](float most, int cblk) {
+      most = rowgroup_max(max16(most));
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(q_scale(most)), rs,
+                                            lane == 0 ? layout.scale_at(vblk, cblk) : BUF_OOB, 0, 0);
+      return half_inv_scale(most);
+    };
     if constexpr (F32) {
 #pragma unroll
       for (int m = 0; m < MT; ++m) put(w * MT + m, lane, __builtin_bit_cast(uint4, S[m]));
     } else if constexpr (MT == 1) {
-      const uint32_t x = bf16_pair(S[0][0], S[0][1]), y = bf16_pair(S[0][2], S[0][3]);
-      const auto u = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-      const auto v = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+      const uint2 x = pack(S[0], REV ? 0.f : scaled(nmax_abs4(0.f, S[0]), w));
+      const auto u = __builtin_amdgcn_permlane16_swap(x.x, x.x, false, false);
+      const auto v = __builtin_amdgcn_permlane16_swap(x.y, x.y, false, false);
       // (both lanes of a pair have the eight: the odd ones store behind the state)
       put(g4 & 1 ? layout.blocks : w, r16 + 16 * (g4 >> 1), make_uint4(u[0], v[0], u[1], v[1]));
     } else {
 #pragma unroll
       for (int m = 0; m < MT; m += 2) {
-        const floatx4 &u = S[m], &v = S[m + 1];
-        put(w * (MT / 2) + m / 2, lane,
-            row8_from_pieces(make_uint2(bf16_pair(u[0], u[1]), bf16_pair(u[2], u[3])),
-                             make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]))));
+        const int cblk = w * (MT / 2) + m / 2;
+        const float inv = REV ? 0.f : scaled(nmax_abs4(nmax_abs4(0.f, S[m]), S[m + 1]), cblk);
+        put(cblk, lane, row8_from_pieces(pack(S[m], inv), pack(S[m + 1], inv)));
       }
     }
   };
@@ -529,6 +579,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
   // enters it, a partial sum for each wave.
   struct Entering {
     uint32_t r[MT][F32 ? 4 : 2];
+    float scale[F32 ? 1 : (MT + 1) / 2];
   } e0, e1;
   auto load_state = [&](Entering& e, int it) {
     const int c = REV ? nc - 1 - it : it;
@@ -547,18 +598,22 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_decay_scan(DecayArgs a, int un
         const auto u = __builtin_amdgcn_raw_buffer_load_b64(rs, on ? at : BUF_OOB, 0, 0);
         e.r[m][0] = u[0];
         e.r[m][1] = u[1];
+        if (m % 2 == 0) {
+          const unsigned sc = layout.scale_at(vblk, MT == 1 ? w : w * (MT / 2) + m / 2);
+          e.scale[m / 2] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, on ? sc : BUF_OOB, 0, 0));
+        }
       }
     }
   };
   auto meet = [&](const Entering& e, int it) {
     float s = 0.f;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t u = F32 ? e.r[m][i] : i & 1 ? e.r[m][i / 2] & 0xFFFF0000u : e.r[m][i / 2] << 16;
-        s = fmaf(S[m][i], __uint_as_float(u), s);
-      }
+    for (int m = 0; m < MT; ++m) {
+      float4 x;
+      if constexpr (F32) x = __builtin_bit_cast(float4, make_uint4(e.r[m][0], e.r[m][1], e.r[m][2], e.r[m][3]));
+      else x = unpack_half4(make_uint2(e.r[m][0], e.r[m][1]), e.scale[m / 2]);
+      s = fmaf(S[m][0], x.x, fmaf(S[m][1], x.y, fmaf(S[m][2], x.z, fmaf(S[m][3], x.w, s))));
+    }
     s = wave_sum(s);
     const long at = ((long)(kslot + nc - 1 - it) * a.H + h) * NS * 8;
     const auto rs = clip_rsrc(a.met + at, a.dg ? (unsigned)NS * 32u : 0u);
@@ -660,7 +715,7 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
   Gates gates;
   gates.load(a, tok, h, m);
   Piece<T, 8, VEC> pk[KI], pv[2];
-  StateTile<T, DK, DK> ps;
+  StateTile<T, DK, DK, true> ps;
 #pragma unroll
   for (int i = 0; i < KI; ++i) {
     const int idx = threadIdx.x + 256 * i;
@@ -871,7 +926,8 @@ __global__ __launch_bounds__(256, sizeof(GradTiles<T, DK, DV>) <= 80 * 1024 ? 2 
 
   Gates gates;
   gates.load(a, tok, h, m);
-  StateTile<T, DK, 64> xs, xd;  // the states' next tile
+  StateTile<T, DK, 64, true> xs;  // the states' next tiles
+  StateTile<T, DK, 64, false> xd;
   {
     Rows64<T, DK, VEC> q, k;
     Rows64<T, DV, VEC> o, v;
@@ -1125,7 +1181,8 @@ __global__ __launch_bounds__(256) void k_decay_grad_wide(DecayArgs a) {
   };
   for (int c0 = 0; c0 < dk; c0 += 64) {
     Piece<T, 8, VEC> x[2], y[2];
-    StateTile<T, 256, 64> xs, xd;
+    StateTile<T, 256, 64, true> xs;
+    StateTile<T, 256, 64, false> xd;
     auto tile = [&](__amdgpu_buffer_rsrc_t rs, unsigned rb, int r0, int c, int d, Piece<T, 8, VEC>(&p)[2]) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
