@@ -48,7 +48,7 @@ typedef struct {
  * bf16: products of operands rounded to bf16, summed in fp32 (o within about two
  * roundings to bf16); the states keep fp32.
  * The workspace holds comba_decay_fwd_workspace_bytes, the state at every 64th token
- * in in_dtype among them.  The saving form's holds comba_decay_save_bytes and keeps
+ * among them (16 bits a value for bf16: fp16 with a scale a block; else fp32).  The saving form's holds comba_decay_save_bytes and keeps
  * those: comba_decay_bwd takes it as `saved`, unmodified, together with the same shape
  * and inputs and a workspace of its own (comba_decay_bwd_workspace_bytes).
  * Limits: H max(dk, dv) up to 2^22; pieces of 64 tokens (a sequence's last one may be

@@ -57,14 +57,14 @@ comba_status check_rows(const comba_decay_shape* s, comba::DecayArgs* a, int64_t
 }
 
 // Sequences that run as segments of `seglen` tokens side by side.  A scan's workgroup takes
-// 0.9 us a chunk alone, and the CUs together 1.2 us for a chunk of one workgroup each; the
-// first pass, which finds the segments' states, adds half of that and a launch.  So a
-// sequence is cut where its own walk is longer than two shares of a CU and some, into
-// segments of which every CU gets two.  Whole / cut, us of a forward, 16 heads of 128: one
-// row of 1,000 tokens 25 / 25, of 4,096 69 / 54, of 16,384 287 / 176; two rows of 4,096
-// 83 / 94, four 154 / 196; ten packed sequences of 1 to 15,777 tokens, 36,283 in all,
-// 430 / 412; 4 heads, one row of 65,536 791 / 184.  (Packed without host offsets: as
-// if one sequence had all tokens; what is shorter than a segment stays whole.)
+// about 1 us a chunk; the first pass, which finds the segments' states, adds its own walk
+// and a launch.  So a sequence is cut where its own walk is longer than two shares of a CU
+// and some, into segments of which every CU gets two.  Whole / cut, us of a forward, 16
+// heads of 128: one row of 4,096 tokens 74 / 57, of 16,384 296 / 184; two rows of 4,096
+// 88 / 88, four 156 / 198; ten packed sequences of 1 to 15,777 tokens, 36,383 in all,
+// 436 / 422 (whole here: a lower limit won 2 to 3% on such batches and nothing elsewhere);
+// 4 heads, one row of 65,536 846 / 193.  (Packed without host offsets: as if one sequence
+// had all tokens; what is shorter than a segment stays whole.)
 void cut(comba::DecayArgs* a, int64_t longest, bool* segments) {
   int dev = 0, cus = 0;
   if (hipGetDevice(&dev) != hipSuccess ||
