@@ -42,17 +42,22 @@ typedef struct {
  *     S_t = exp(g_t) S_{t-1} + k_t v_t^T,      o_t = scale S_t^T q_t.
  *   q [B,T,Hq,dk], k [B,T,Hk,dk], v [B,T,Hv,dv], o [B,T,H,dv] in_dtype; g [B,T,H] or
  *   [H] log-decays; h0, ht [num_seqs,H,dk,dv] fp32 or NULL.
- * g = -inf starts a state anew; log-decays below -128 count as -128, whose decay
- * is zero in fp32.  A NaN or Inf in an input makes outputs of its own sequence and
+ * g = -inf starts a state anew from a finite one (zero times Inf or NaN is NaN: fill the
+ * memory of a new state); log-decays below -128 count as -128, whose decay is zero in
+ * fp32.  A NaN or Inf in an input makes outputs of its own sequence and
  * head non-finite, up to 63 tokens before its own among them (gradients: behind it).
  * bf16: products of operands rounded to bf16, summed in fp32 (o within about two
- * roundings to bf16); the states keep fp32.
+ * roundings to bf16); the states keep fp32.  The states kept for chunks have one scale for
+ * 16 value by 16 or 32 key columns: what is below 2^-29 of the largest there loses
+ * bits, below 2^-39 it counts as zero in o and the gradients (not in ht and dh0).
  * The workspace holds comba_decay_fwd_workspace_bytes, the state at every 64th token
- * among them (16 bits a value for bf16: fp16 with a scale a block; else fp32).  The saving form's holds comba_decay_save_bytes and keeps
- * those: comba_decay_bwd takes it as `saved`, unmodified, together with the same shape
- * and inputs and a workspace of its own (comba_decay_bwd_workspace_bytes).
+ * among them (bf16: 16 bits a value, fp16 and its scale; else fp32).  The saving form's
+ * holds comba_decay_save_bytes and keeps those: comba_decay_bwd takes it as `saved`,
+ * unmodified, together with the same shape and inputs and a workspace of its own
+ * (comba_decay_bwd_workspace_bytes).
  * Limits: H max(dk, dv) up to 2^22; pieces of 64 tokens (a sequence's last one may be
- * partial) times H, and sequences times H times dv / 32, below 2^31 / 512.
+ * partial) times H, and sequences times H times dv / 32, below 2^31 / 512; a step's
+ * rows below 2^24.
  * Long sequences are cut into segments that run side by side where that is faster; the
  * choice follows from the shape, the host offsets and the device, and changes results
  * by roundings only.  Every sum runs in an order fixed by that choice.

@@ -297,6 +297,7 @@ comba_status comba_decay_step(const comba_decay_shape* shape, const void* q, con
   comba_status st = decay_args(shape, &a, &segments, false);
   if (st != COMBA_OK) return st;
   if (a.cu_seqlens || shape->T != 1 || num_slots < 0) return COMBA_ERR_SHAPE;
+  if (a.S > (int)(UINT32_MAX / 256)) return COMBA_ERR_SHAPE;  // threads of a launch, 256 a row
   st = decay_inputs(&a, q, k, v, g, nullptr);
   if (st != COMBA_OK) return st;
   if (a.S > 0 && (!state || !o)) return COMBA_ERR_NULL;

@@ -150,6 +150,13 @@ def test_steps_take_one_token_and_no_offsets():
         assert call(name, decay(T=1, **{r: 1 << 60}), o=None) == ESHAPE
 
 
+def test_a_step_takes_fewer_than_2_24_rows():
+    """A launch holds fewer than 2^32 threads along a dimension, a step 256 a row."""
+    one = dict(T=1, H=1, Hq=1, Hk=1, Hv=1, dk=1, dv=1)
+    for n, code in (((1 << 24) - 1, ENULL), (1 << 24, ESHAPE)):
+        assert call("comba_decay_step", decay(B=n, num_seqs=n, **one), o=None) == code
+
+
 def test_workspaces():
     lib = comba.load_library()
     for name, size, shp in (
