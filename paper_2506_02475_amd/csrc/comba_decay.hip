@@ -327,8 +327,7 @@ struct StateLayout {
   }
 };
 // A tile of 64 rows (value columns) and COLS key columns of a kept state, through registers
-// into LDS.
-// (ENTERS: an entering state, as fp16.)
+// into LDS (ENTERS: an entering state, as fp16).
 template <typename T, int DK, int COLS, bool ENTERS>
 struct StateTile {
   typedef StateLayout<T, DK> L;
@@ -383,8 +382,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t state_rsrc(const void* kept, l
 // columns of the state in fp32 accumulators (wave w: key rows (w % 4) DK / 4 .., columns
 // 16 (w / 4) ..), and keeps what it holds before each chunk.  Forward: keys k, values v,
 // weights e^{G_end - G_j}.  REV, for the states' gradients, from the last chunk to the
-// first: keys q, values do, weights scale e^{G_r}.  LOCAL: a segment's end from a zero state, for the segments behind it.
-// The weights multiply the value columns, of which a workgroup has few, and there
+// first: keys q, values do, weights scale e^{G_r}.  LOCAL: a segment's end from a zero
+// state, for the segments behind it.  The weights multiply the value columns, of which a workgroup has few, and there
 // fp32 becomes three bf16 against the keys as they are: the state's sums keep 24 bits.
 //
 // Bound by the latency of a chunk's chain (its decays, the weighted values into LDS, their

@@ -159,6 +159,28 @@ def test_backward(name, kw):
     hold("dh0", got["dh0"], want["dh0"], None, "f32")
 
 
+@pytest.mark.parametrize("dk", [64, 128, 256])
+def test_kept_states_with_columns_of_unlike_size(dk):
+    """Values of every second column smaller by 2^12 and keys by 2^8 (queries larger by it) share
+    the scale of a block of a kept state.  Its fp16 keeps 11 bits down to 2^-29 of the largest
+    value: an eighth of a half step of bf16 more in each term, also for the smaller columns, held
+    to their own size; what is below adds 2^-39 of the largest, 2^-19 of a term here."""
+    import paper_2506_02475_amd as comba
+
+    c = _case("unlike%d" % dk, B=1, T=200, H=2, dk=dk, dv=64)
+    small_v, small_k = np.arange(64) % 2 == 1, np.arange(dk) % 2 == 1
+    c["v"] = c["v"] * np.where(small_v, np.float32(2.0 ** -12), np.float32(1))
+    c["k"] = c["k"] * np.where(small_k, np.float32(2.0 ** -8), np.float32(1))
+    c["q"] = c["q"] * np.where(small_k, np.float32(2.0 ** 8), np.float32(1))
+    c["h0"] = (c["h0"] * np.where(small_k, 2.0 ** -8, 1)[:, None]
+               * np.where(small_v, 2.0 ** -12, 1)).astype(np.float32)
+    o, _ = comba.comba_decay_fwd(*_inputs(c), scale=c["scale"])
+    want, mag = _fwd(c)[0], _fwd(_abs(c))[0]
+    o = o.reshape(want.shape)
+    for m in (small_v, ~small_v):
+        hold("o", o[..., np.flatnonzero(m)], want[..., m], 1.125 * mag[..., m], "bf16")
+
+
 STEPS = [
     ("one", dict(B=1, H=2, dk=64, dv=64)),
     ("slots", dict(B=5, H=3, dk=128, dv=128, pool=9)),
