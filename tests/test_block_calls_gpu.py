@@ -308,3 +308,67 @@ def test_steps_continue_a_prompt():
         o = comba.comba_decay_step(*(x[:, t] for x in ins[:4]), state)
         assert (o - whole[:, t]).abs().max() <= 1e-5 * whole.abs().max()
     assert (state - end).abs().max() <= 1e-5 * end.abs().max()
+
+
+def _far_rows(t, row, offset):
+    """t [1,T,..] as a column slice of rows ``row`` elements apart, at ``offset`` in each; what
+    lies between is not written."""
+    import torch
+
+    wide = torch.empty(t.shape[1] * row, device="cuda", dtype=t.dtype)
+    far = wide.view(1, t.shape[1], row)[..., offset:offset + t[0, 0].numel()]
+    far = far.unflatten(-1, t.shape[2:])
+    far.copy_(t)
+    return far
+
+
+def test_offsets_past_32_bits():
+    """Rows at the farthest distance that is taken, and a pool of states over 2^31 elements: the
+    bits of the same call on contiguous memory."""
+    import torch
+
+    import paper_2506_02475_amd as comba
+
+    q, k, v, g, _ = _inputs(T=600, H=2, Hk=2, dk=64, dv=64, B=1)
+    row = 1 << 22
+    assert q.shape[1] * row > 1 << 31
+    do = v.clone()
+
+    def run(q, g):
+        o, ht, ws = comba.comba_decay_fwd_save(q, k, v, g)
+        return [o, ht] + [x for x in comba.comba_decay_bwd(q, k, v, g, None, do, workspace=ws,
+                                                           need_dh0=False).values()
+                          if x is not None]
+
+    want = run(q, g)
+    for far_q, far_g in ((_far_rows(q, row, 64), g), (q, _far_rows(g, row, 8))):
+        for a, b in zip(run(far_q, far_g), want):
+            assert torch.equal(a, b)
+        del far_q, far_g
+    H, d = 2, 256
+    slots = (1 << 31) // (H * d * d) + 2
+    pool = torch.empty(slots, H, d, d, device="cuda")
+    q1, k1, v1, g1 = (torch.randn(2, *s, device="cuda").bfloat16()
+                      for s in ((H, d), (H, d), (H, d), (H,)))
+    g1 = -g1.abs()
+    small = torch.randn(2, H, d, d, device="cuda")
+    at = torch.tensor([slots - 1, 0], device="cuda", dtype=torch.int32)
+    pool[at.long()] = small
+    o = comba.comba_decay_step(q1, k1, v1, g1, pool, slots=at)
+    want = comba.comba_decay_step(q1, k1, v1, g1, small)
+    assert torch.equal(o, want) and torch.equal(pool[at.long()], small)
+
+
+def test_norm_rows_past_32_bits():
+    import torch
+
+    import paper_2506_02475_amd as comba
+
+    y, x, w, kw = _norm_inputs(rows=600, C=640)
+    row = 1 << 22
+    far = _far_rows(y[None], row, 64)[0]
+    want = comba.comba_block_norm_fwd(y, x, w, **kw)
+    got = comba.comba_block_norm_fwd(far, x, w, **kw)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    gr = [comba.comba_block_norm_bwd(t, x, w, x, y, **kw) for t in (y, far)]
+    assert all(torch.equal(gr[0][n], gr[1][n]) for n in gr[0])
