@@ -293,7 +293,8 @@ def _functions():
         @staticmethod
         def forward(ctx, q, k, v, g, h0, cu_seqlens, kw, grad):
             ctx.set_materialize_grads(False)
-            if g.dim() == 1 and ctx.needs_input_grad[3]:
+            # (needs_input_grad is set where gradients are off, too)
+            if grad and g.dim() == 1 and ctx.needs_input_grad[3]:
                 raise CombaError("comba: decays [H] are constants: pass g [B,T,H] to train them")
             if not (grad and any(ctx.needs_input_grad)):  # no backward: no states kept for it
                 return comba_decay_fwd(q, k, v, g, h0, cu_seqlens=cu_seqlens, **kw)

@@ -321,6 +321,18 @@ def test_trained_constants_of_the_heads_raise(fakes):
         _decay(v, torch.zeros(2, requires_grad=True))
 
 
+def test_trained_constants_of_the_heads_run_where_no_gradient_is_wanted(fakes):
+    """A model may keep them as a parameter: a call without gradients asks for none of theirs."""
+    import torch
+
+    v, g = torch.randn(1, 6, 2, 4, requires_grad=True), torch.zeros(2, requires_grad=True)
+    with torch.no_grad():
+        assert torch.equal(_decay(v, g), 2 * v)
+    with torch.inference_mode():
+        assert torch.equal(_decay(v, g), 2 * v)
+    assert [c[0] for c in fakes.calls] == ["fwd", "fwd"]
+
+
 @pytest.mark.parametrize("op", ["decay", "norm"])
 def test_second_derivatives_and_forward_mode_raise(fakes, op):
     import torch
