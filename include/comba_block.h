@@ -117,7 +117,8 @@ comba_status comba_block_norm_fwd(const comba_block_norm_shape *shape, const voi
  * From dr [rows,C] (x_dtype) and dn [rows,C] (either may be NULL: zeros): dy, dz
  * (with z), dx (with x; NULL: not wanted), and dpost_weight, dscale, dweight [C] fp32
  * where their parameter is given (each may be NULL).  Recomputes p, r and both
- * norms; sums in a fixed order.
+ * norms; sums in a fixed order.  Without weight or without dn the norm of r takes no
+ * part (dweight is zero): what x holds, Inf among it, reaches no gradient.
  */
 size_t comba_block_norm_workspace_bytes(const comba_block_norm_shape *shape);
 comba_status comba_block_norm_bwd(const comba_block_norm_shape *shape, const void *y,

@@ -53,7 +53,8 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void k_block_norm(BlockNorm
   if (chunk >= chunks) return;  // whole teams
   const Tx *xt = static_cast<const Tx*>(a.x), *drt = static_cast<const Tx*>(a.dr);
   const Ty *yt = static_cast<const Ty*>(a.y), *zt = static_cast<const Ty*>(a.z), *dnt = static_cast<const Ty*>(a.dn);
-  const bool post = a.w1 != nullptr, pre = a.w2 != nullptr;
+  // (backward: a norm of which nothing comes back takes no part)
+  const bool post = a.w1 != nullptr, pre = BWD ? a.dn != nullptr : a.w2 != nullptr;
   int c[KV], nv[KV];
   float w1[KV][C], sc[KV][C], w2[KV][C], d1[KV][C], ds[KV][C], d2[KV][C];
 #pragma unroll
@@ -132,6 +133,11 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void k_block_norm(BlockNorm
       bn_sum<TEAM>(sum, lds, turn);
       r2 = rsqrtf(sum[0] * inv + a.eps);
       m2 = sum[1] * r2 * inv;
+    } else {  // (Inf times the r2 of zero would be NaN)
+#pragma unroll
+      for (int k = 0; k < KV; ++k)
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[k][i] = 0.f;
     }
     if constexpr (!BWD) {
 #pragma unroll
@@ -205,7 +211,8 @@ __global__ __launch_bounds__(BN_WIDE) void k_block_norm_wide(BlockNormArgs a, in
   const int chunk = blockIdx.x;
   const Tx *xt = static_cast<const Tx*>(a.x), *drt = static_cast<const Tx*>(a.dr);
   const Ty *yt = static_cast<const Ty*>(a.y), *zt = static_cast<const Ty*>(a.z), *dnt = static_cast<const Ty*>(a.dn);
-  const bool post = a.w1 != nullptr, pre = a.w2 != nullptr;
+  // (backward: a norm of which nothing comes back takes no part)
+  const bool post = a.w1 != nullptr, pre = BWD ? a.dn != nullptr : a.w2 != nullptr;
   const float inv = 1.f / a.C;
   float* part = BWD ? a.part + (long)chunk * 3 * a.C : nullptr;
   Piece<Ty, C, true> py[N], pz[N], pn[N];
@@ -311,7 +318,7 @@ __global__ __launch_bounds__(BN_WIDE) void k_block_norm_wide(BlockNormArgs a, in
       // fn(i, channel, yh, dn rh, dr', t, dz, dp) for every channel of a piece
       auto grad = [&](int k, int c, auto fn) {
         stream(k, c, [&](int i, int at, float yh, float gate, float slope, float v) {
-          const float rh = v * r2, dn = pn[k].get(i);
+          const float rh = pre ? v * r2 : 0.f, dn = pn[k].get(i);  // (0 Inf is NaN)
           const float dr = (drt ? pr[k].get(i) : 0.f) + r2 * (dn * w2.get(i) - rh * m2);
           const float p = yh * w1.get(i), dt = dr * sc.get(i);
           fn(i, at, yh, dn * rh, dr, p * gate, dt * p * slope, dt * gate);
