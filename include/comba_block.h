@@ -119,6 +119,7 @@ comba_status comba_block_norm_fwd(const comba_block_norm_shape *shape, const voi
  * where their parameter is given (each may be NULL).  Recomputes p, r and both
  * norms; sums in a fixed order.  Without weight or without dn the norm of r takes no
  * part (dweight is zero): what x holds, Inf among it, reaches no gradient.
+ * Without post_weight y enters dy through the norm of r alone.
  */
 size_t comba_block_norm_workspace_bytes(const comba_block_norm_shape *shape);
 comba_status comba_block_norm_bwd(const comba_block_norm_shape *shape, const void *y,

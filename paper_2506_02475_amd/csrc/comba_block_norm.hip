@@ -174,6 +174,11 @@ __global__ __launch_bounds__(TEAM > 64 ? TEAM : 256) void k_block_norm(BlockNorm
       if (post) {
         bn_sum<TEAM>(s1, lds, turn);
         m1 = s1[0] * inv;
+      } else {  // (an Inf in y times the m1 of zero would be NaN)
+#pragma unroll
+        for (int k = 0; k < KV; ++k)
+#pragma unroll
+          for (int i = 0; i < C; ++i) y[k][i] = 0.f;
       }
 #pragma unroll
       for (int k = 0; k < KV; ++k) {
@@ -347,7 +352,7 @@ __global__ __launch_bounds__(BN_WIDE) void k_block_norm_wide(BlockNormArgs a, in
       pieces([&](int k, int c) {
         float dy[C];
         grad(k, c, [&](int i, int, float yh, float, float, float, float, float dp) {
-          dy[i] = r1 * (dp * w1.get(i) - yh * m1);
+          dy[i] = post ? r1 * (dp * w1.get(i) - yh * m1) : dp;  // (0 Inf is NaN)
         });
         store_piece<Ty, C, true>(static_cast<Ty*>(a.dy) + r * a.C + c, dy, C);
       });
