@@ -53,8 +53,8 @@ typedef struct {
  * The workspace holds comba_decay_fwd_workspace_bytes, the state at every 64th token
  * among them (bf16: 16 bits a value, fp16 and its scale; else fp32).  The saving form's
  * holds comba_decay_save_bytes and keeps those: comba_decay_bwd takes it as `saved`,
- * unmodified, together with the same shape and inputs and a workspace of its own
- * (comba_decay_bwd_workspace_bytes).
+ * unmodified, together with the same shape and inputs (either call may know the offsets on
+ * the host) and a workspace of its own (comba_decay_bwd_workspace_bytes).
  * Limits: H max(dk, dv) up to 2^22; pieces of 64 tokens (a sequence's last one may be
  * partial) times H, and sequences times H times dv / 32, below 2^31 / 512; a step's
  * rows below 2^24.

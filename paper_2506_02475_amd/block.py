@@ -165,9 +165,9 @@ def comba_decay_fwd_save(q, k, v, g, h0=None, *, scale=None, cu_seqlens=None,
 def comba_decay_bwd(q, k, v, g, h0, do, dht=None, *, workspace, scale=None, cu_seqlens=None,
                     cu_seqlens_host=None, need_dg=True, need_dh0=True, scratch=None, stream=None):
     """Backward of comba_decay_fwd_save from do [B,T,H,dv] (dtype of q) and dht [S,H,dk,dv]
-    float32, with the ``workspace`` it filled; ``scratch``: memory for the call itself, made
-    if absent.  Returns dict dq, dk, dv (dtype of q), dg (dtype of g; None for constants of
-    the heads), dh0 (float32)."""
+    float32, with the ``workspace`` it filled (either call may know the offsets on the host);
+    ``scratch``: memory for the call itself, made if absent.  Returns dict dq, dk, dv (dtype of
+    q), dg (dtype of g; None for constants of the heads), dh0 (float32)."""
     import torch
 
     lib = load_library()
@@ -183,10 +183,10 @@ def comba_decay_bwd(q, k, v, g, h0, do, dht=None, *, workspace, scale=None, cu_s
     out = {"dq": _like(q), "dk": _like(k), "dv": _like(v),
            "dg": _like(g) if need_dg and g.dim() == 3 else None,
            "dh0": q.new_empty(state, dtype=torch.float32) if need_dh0 else None}
-    if workspace is None or _memory(workspace, workspace.get_device() == dev).numel() \
-            < lib.comba_decay_save_bytes(shp):
+    if workspace is None:
         raise CombaError("comba: comba_decay_bwd needs the workspace filled by "
                          "comba_decay_fwd_save")
+    _memory(workspace, workspace.get_device() == dev)  # (the library checks that it holds the states)
     ws = _workspace(lib.comba_decay_bwd_workspace_bytes, shp, scratch, q.device)
     _run(lib.comba_decay_bwd(shp, *ptrs, *given,
                              *(_ptr(out[n]) for n in ("dq", "dk", "dv", "dg", "dh0")),
