@@ -59,8 +59,11 @@ typedef struct {
  * partial) times H, and sequences times H times dv / 32, below 2^31 / 512; a step's
  * rows below 2^24.
  * Long sequences are cut into segments that run side by side where that is faster; the
- * choice follows from the shape, the host offsets and the device, and changes results
- * by roundings only.  Every sum runs in an order fixed by that choice.
+ * choice follows from the shape, the host offsets and the device (COMBA_SCAN_SEGMENTS is
+ * not read), and changes results by roundings only.  Every sum runs in an order fixed by
+ * that choice.
+ * Log-decays above zero are taken too: a growth of more than 2^127 over a chunk of 64
+ * tokens, or over the segments of a sequence, overflows, also before a state that is zero.
  */
 size_t comba_decay_fwd_workspace_bytes(const comba_decay_shape *shape);
 size_t comba_decay_save_bytes(const comba_decay_shape *shape);

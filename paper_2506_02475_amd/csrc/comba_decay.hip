@@ -10,7 +10,14 @@
 //   dg_t  = the sum over all pairs j < t <= r of a pair's weight times its products:
 //           both tokens in the chunk, one of them, or none (e^{G_end} <dS', S>).
 //
-// All differences of G are formed from sums in 64 bits; what is masked is never formed.
+// G is summed in 64 bits.  A row's weights towards its chunk's ends are formed from those
+// sums; a pair's from two sums rounded to fp32 (bf16) or to two floats each (fp32): see Sums.
+// Masked pairs' weights are formed as well (Inf where a decay is strong) and then dropped by
+// a select, which takes nothing from what it drops.
+// bf16 operands of the matrix products are rounded: the pairs' weighted products (o, dq, dk,
+// dv), an entering state (o, dq; by way of its fp16) and a leaving one's gradient (dk, dv).  With
+// the result's own rounding that is 2.4e-3 of a tensor's 2-norm, where one rounding is 1.7e-3;
+// two terms of every operand would double the matrix instructions and the kept states.
 #include "comba_block_launch.h"
 #include "comba_layer_device.hpp"
 
@@ -59,10 +66,13 @@ __device__ __forceinline__ Frag<T> frag_of(const floatx4& a, const floatx4& b) {
   return f;
 }
 // Element offset in a tile of rows of LD bf16 (a multiple of 64; fp32: twice the bytes),
-// whose pieces of eight are exchanged inside a row so that what one access touches falls
-// on distinct ones of the 64 banks: 16 rows of one piece (operands along a row), rows r ..
-// r + 3 and r + 8 .. r + 11 of two pieces (operands down the rows), four rows of four
-// (weighted values on their way in).
+// whose pieces of eight are exchanged inside a row so that, bf16 and lanes taken in order,
+// what these accesses touch at once falls on distinct ones of the 64 banks: 16 rows of one
+// piece (ld_row, st_pairs), rows r .. r + 3 and r + 8 .. r + 11 of two pieces (ld_col), whole
+// rows (st_row8), four rows of four (weighted values on their way in).  ld_col_acc does not
+// have it: its rows r .. r + 3 and r + 4 .. r + 7 are exchanged by one bit only, so two rows
+// share their banks.  Counted, conflict cycles of LDS's busy ones: scans (ld_col) 0, outputs
+// 44% at heads of 128 and 47% at 256, gradients 34%, more than ld_col_acc alone explains.
 template <int LD>
 __device__ __forceinline__ int swz(int row, int col) {
   const int x = LD == 64 ? ((row & 2) << 1) | ((row >> 2) & 2) | ((row >> 2) & 1)
@@ -249,7 +259,11 @@ __device__ __forceinline__ double gate_sum(float g) {
   x = dpp_add<0x142, 0xA>(x);
   return dpp_add<0x143, 0xC>(x);
 }
-// Pair weights from two floats a sum: a difference keeps the accuracy of the 64 bits.
+// Pair weights from a chunk's sums.  BOTH (fp32): of two floats each, so that a difference
+// is within two roundings of itself.  Else (bf16) of one: sums are below 2^14 (64 rows of 128 log2(e) at
+// most) and there within 2^-11, a difference within 2^-10 and a weight within ln(2) 2^-10 =
+// 7e-4, a sixth of the half step (2^-8) that its product is rounded by next; of sums below
+// 2^7, the ordinary ones, 5e-6.
 struct Sums {
   float hi[DC_CH], lo[DC_CH];
   // 2^(G - G_j) of four j from j0 on
@@ -808,8 +822,9 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
 // lane holds four consecutive columns of one row.
 // The chunk's four inputs lie in LDS whole; the values' tile makes room for the states',
 // 64 x 64 at a time with the next one's loads in flight.
-// Bound by what it moves and by two workgroups a CU: 4 x 4,096 tokens, 16 heads of 128,
-// bf16, 738 MB in 215 us (194 at best), 3.4 TB/s.
+// Two workgroups a CU, eight waves, hide neither what it moves nor its LDS reads whole: 4 x
+// 4,096 tokens, 16 heads of 128, bf16, 738 MB in 215 us (194 at best), 3.4 TB/s, where the
+// outputs reach 4.9; a third of LDS's busy cycles are bank conflicts.
 template <typename T, int DK, int DV>
 struct GradTiles {
   static constexpr int VS = DV >= 128 ? DC_CH * DV : 2 * 64 * 64;
