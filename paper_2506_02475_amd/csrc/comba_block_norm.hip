@@ -323,10 +323,14 @@ __global__ __launch_bounds__(BN_WIDE) void k_block_norm_wide(BlockNormArgs a, in
       // fn(i, channel, yh, dn rh, dr', t, dz, dp) for every channel of a piece
       auto grad = [&](int k, int c, auto fn) {
         stream(k, c, [&](int i, int at, float yh, float gate, float slope, float v) {
-          const float rh = pre ? v * r2 : 0.f, dn = pn[k].get(i);  // (0 Inf is NaN)
-          const float dr = (drt ? pr[k].get(i) : 0.f) + r2 * (dn * w2.get(i) - rh * m2);
+          float dr = drt ? pr[k].get(i) : 0.f, dw2 = 0.f;
+          if (pre) {  // (as zeros the terms would be NaN where a row holds an Inf)
+            const float rh = v * r2, dn = pn[k].get(i);
+            dr += r2 * (dn * w2.get(i) - rh * m2);
+            dw2 = dn * rh;
+          }
           const float p = yh * w1.get(i), dt = dr * sc.get(i);
-          fn(i, at, yh, dn * rh, dr, p * gate, dt * p * slope, dt * gate);
+          fn(i, at, yh, dw2, dr, p * gate, dt * p * slope, dt * gate);
         });
       };
       float s1[1] = {0.f};
@@ -352,7 +356,7 @@ __global__ __launch_bounds__(BN_WIDE) void k_block_norm_wide(BlockNormArgs a, in
       pieces([&](int k, int c) {
         float dy[C];
         grad(k, c, [&](int i, int, float yh, float, float, float, float, float dp) {
-          dy[i] = post ? r1 * (dp * w1.get(i) - yh * m1) : dp;  // (0 Inf is NaN)
+          dy[i] = pre || post ? r1 * (dp * w1.get(i) - yh * m1) : dp;  // (likewise)
         });
         store_piece<Ty, C, true>(static_cast<Ty*>(a.dy) + r * a.C + c, dy, C);
       });
